@@ -49,6 +49,7 @@ extern "C" {
 
 #define RLGEN_DTYPE_F32   0  /* tensors supplied as fp32; rounded to bf16 (nearest even) on load */
 #define RLGEN_DTYPE_BF16  1  /* tensors supplied as bf16                                          */
+#define RLGEN_DTYPE_F16   2  /* tensors supplied as fp16 (the operators over pages and packed rows only) */
 
 /* Threads: calls on one context must not overlap; different contexts may be used from different
  * threads.  The library reads no environment variables. */
@@ -296,6 +297,106 @@ int rlgen_debug_set_gemm(rlgen_ctx *ctx, int32_t mode, int32_t which, int32_t va
  * infinity.  *faults (nullable, HOST) receives the bit set: 1 token id, 2 uniform, 4 score group, 8 fp16 range. */
 int rlgen_status(rlgen_ctx *ctx, void *hip_stream);
 int rlgen_status_bits(rlgen_ctx *ctx, void *hip_stream, uint32_t *faults);
+
+/* ------------------------------------------------------------------ operators over a cache in pages and packed rows
+ *
+ * The blocks around attention for a policy whose layers normalise queries and keys per head and attend to a window, and for
+ * requests that come and go: a cache in pages, the plan of a pass over it, norms and rotation with the cache write, attention over
+ * packed rows and over the cache, and the gradients of the last two.  They need no context.  Element type `dtype` is RLGEN_DTYPE_BF16
+ * or RLGEN_DTYPE_F16 for queries, keys, values, outputs and their gradients; statistics, sums and gains are fp32.
+ *
+ * Layouts
+ *  - Packed rows: the tokens of S sequences one behind the other; row_starts [S + 1] int32 holds the first row of each and the number
+ *    of rows.  A tensor [rows, heads, head_dim] has head_dim and heads contiguous and any row stride (in elements) that is a multiple of
+ *    8, so a column range of a fused projection's output can be passed as it is.  All bases 16-byte aligned.
+ *  - Cache: pages [n_pages, 2, n_kv_heads, page_size, head_dim]: of a page's tokens first the keys, then the values.  page_size is a power
+ *    of two from 8 to 1024.  Sequence s has its token t in page page_table[s * table_stride + t / page_size].  A slot is
+ *    page * page_size + t % page_size.
+ *  - head_dim is a multiple of 16, at most 256; n_kv_heads divides n_q_heads.
+ *  - Visibility: a query at position p sees key j if j <= p and (j > p - window, or j < sinks, or window == 0: no window).  A query that
+ *    sees nothing has output 0 and log-sum-exp -infinity.
+ *  - Sizes: rows, S * heads and n_pages * page_size below 2^31.  Offsets are 64-bit.
+ * Entries of row_starts, page_table and slots that lie outside their arrays are clamped or skipped, never followed. */
+#define RLGEN_PLAN_ROWS    1   /* counts[3]: more rows than max_rows (those beyond are not written)            */
+#define RLGEN_PLAN_PAGES   2   /* the free list ran out (pages and slots that lack one are -1)                 */
+#define RLGEN_PLAN_TABLE   4   /* a sequence needs more pages than a table row has (its slots beyond are -1)   */
+#define RLGEN_PLAN_LENGTH  8   /* a negative length (taken as 0)                                               */
+
+/* The plan of one pass over the cache, from the requests' lengths alone: sequence s holds ctx_lens[s] tokens and gets new_lens[s] more.
+ * Pages that it needs for them are taken from free_pages [n_free] in the order of the sequences, from entry *free_head on (DEVICE, null:
+ * 0), and entered into page_table, whose earlier entries are read for tokens that go into a page already begun.
+ *  total_lens [S], row_starts [S + 1]   out: lengths after the pass; first row of each sequence
+ *  slots, positions [max_rows]          out: where row i's key and value go, and its position; rows that no sequence has: -1 and 0
+ *  counts [4]                           out: rows; the free list's next head (min(head + pages taken, n_free)); longest length after the
+ *                                       pass; RLGEN_PLAN_* bits
+ * free_head must not be counts + 1 itself; two counts arrays in turn chain passes without the host.
+ * Errors: NULL, BAD_ARG (S < 1, max_rows < 0, n_free < 0, table_stride < 1, page_size), DEVICE. */
+int rlgen_plan_pages(const int32_t *ctx_lens, const int32_t *new_lens, int32_t S, int32_t page_size, const int32_t *free_pages,
+                     int32_t n_free, const int32_t *free_head, int32_t *page_table, int32_t table_stride, int32_t max_rows,
+                     int32_t *total_lens, int32_t *row_starts, int32_t *slots, int32_t *positions, int32_t *counts,
+                     void *hip_stream);
+
+/* cos and sin of position * theta^(-2 i / rotary_dim), evaluated in fp64: table [max_pos, rotary_dim / 2, 2] fp32.
+ * Errors: NULL, BAD_ARG, DEVICE. */
+int rlgen_rope_table(float *table, int32_t max_pos, int32_t rotary_dim, float theta, void *hip_stream);
+
+/* RMS norm of every query and key head over its head_dim, gains, then rotation of the first rotary_dim dims (pairs i, i + rotary_dim / 2,
+ * as in rlgen_generate), in one pass over the fused projection's output:
+ *  qkv [rows, (n_q_heads + 2 n_kv_heads) head_dim] of type src_dtype (any RLGEN_DTYPE_*), row stride qkv_stride
+ *  q_gain, k_gain [head_dim] fp32; rope: rlgen_rope_table's, positions [rows] int32 (clamped to [0, max_pos))
+ *  q out [rows, n_q_heads, head_dim]; k, v nullable out [rows, n_kv_heads, head_dim]; pages nullable: keys and values go to slots[row]
+ *  (a slot outside the cache is skipped).  Values are neither normalised nor rotated.
+ * At least one of pages (with slots) and k must be given; rope may be null if rotary_dim is 0.  Errors: NULL, BAD_ARG, DEVICE. */
+int rlgen_qk_norm_rope(const void *qkv, int64_t qkv_stride, int32_t src_dtype, int32_t rows, int32_t n_q_heads, int32_t n_kv_heads,
+                       int32_t head_dim, const float *q_gain, const float *k_gain, float eps, const float *rope, int32_t max_pos,
+                       int32_t rotary_dim, const int32_t *positions, int32_t dtype, void *q, int64_t q_stride, void *k,
+                       int64_t k_stride, void *v, int64_t v_stride, void *pages, int32_t n_pages, int32_t page_size,
+                       const int32_t *slots, void *hip_stream);
+
+/* Its gradients: dq, dk, dv (type dtype, of q, k and v as rlgen_qk_norm_rope returns them) to dqkv (type src_dtype, all of it written)
+ * and dq_gain, dk_gain [head_dim] fp32 (sums over rows and heads in a fixed order).  workspace: 16-byte aligned,
+ * rlgen_qk_norm_rope_backward_workspace(rows, head_dim) bytes.  Errors: NULL, BAD_ARG, WORKSPACE, DEVICE. */
+size_t rlgen_qk_norm_rope_backward_workspace(int32_t rows, int32_t head_dim);
+int rlgen_qk_norm_rope_backward(const void *qkv, int64_t qkv_stride, int32_t src_dtype, int32_t rows, int32_t n_q_heads,
+                                int32_t n_kv_heads, int32_t head_dim, const float *q_gain, const float *k_gain, float eps,
+                                const float *rope, int32_t max_pos, int32_t rotary_dim, const int32_t *positions, int32_t dtype,
+                                const void *dq, int64_t dq_stride, const void *dk, int64_t dk_stride, const void *dv,
+                                int64_t dv_stride, void *dqkv, int64_t dqkv_stride, float *dq_gain, float *dk_gain, void *workspace,
+                                size_t workspace_bytes, void *hip_stream);
+
+/* Causal attention within each packed sequence: out [rows, n_q_heads, head_dim], lse nullable [rows, n_q_heads] fp32 = log of the sum of
+ * exp(scale q k) over the visible keys.  max_len (HOST) bounds every sequence's rows; rows of a sequence beyond it are not computed.
+ * A key or value that a query does not see never reaches its output, be it infinite or NaN.
+ * Errors: NULL, BAD_ARG, DEVICE. */
+int rlgen_window_attention(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                           int32_t dtype, int32_t rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                           const int32_t *row_starts, int32_t S, int32_t max_len, int32_t window, int32_t sinks, float scale, void *out,
+                           int64_t out_stride, float *lse, void *hip_stream);
+
+/* Its gradients, from its own inputs and outputs and dout (all of dq, dk and dv is written; a query that sees nothing and a key that
+ * nobody sees have zeros).  Within a sequence infinities and NaN go where the products carry them; no other sequence is touched.
+ * workspace: 16-byte aligned, rlgen_window_attention_backward_workspace(...) bytes.  Errors: NULL, BAD_ARG, WORKSPACE, DEVICE. */
+size_t rlgen_window_attention_backward_workspace(int32_t rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t S,
+                                                 int32_t max_len, int32_t window, int32_t sinks);
+int rlgen_window_attention_backward(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                                    const void *out, int64_t out_stride, const float *lse, const void *dout, int64_t dout_stride,
+                                    int32_t dtype, int32_t rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                    const int32_t *row_starts, int32_t S, int32_t max_len, int32_t window, int32_t sinks, float scale,
+                                    void *dq, int64_t dq_stride, void *dk, int64_t dk_stride, void *dv, int64_t dv_stride,
+                                    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Attention of new tokens over the cache that already holds them: the rows of sequence s are its last row_starts[s + 1] - row_starts[s]
+ * tokens of total_lens[s] (as rlgen_plan_pages gives them).  max_new, max_total (HOST) bound rows and total_lens of every sequence;
+ * max_new == 1 is a decode step: a sequence's keys are then parted over many waves where there are few sequences.  workspace: 16-byte
+ * aligned, rlgen_window_attention_paged_workspace(...) bytes (may be 0, and workspace null then).
+ * Errors: NULL, BAD_ARG, WORKSPACE, DEVICE. */
+size_t rlgen_window_attention_paged_workspace(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t S, int32_t max_new,
+                                              int32_t max_total, int32_t window, int32_t sinks);
+int rlgen_window_attention_paged(const void *q, int64_t q_stride, int32_t dtype, int32_t rows, int32_t n_q_heads, int32_t n_kv_heads,
+                                 int32_t head_dim, const void *pages, int32_t n_pages, int32_t page_size, const int32_t *page_table,
+                                 int32_t table_stride, const int32_t *row_starts, const int32_t *total_lens, int32_t S,
+                                 int32_t max_new, int32_t max_total, int32_t window, int32_t sinks, float scale, void *out,
+                                 int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 const char *rlgen_strerror(int code);
 void rlgen_destroy(rlgen_ctx *ctx);

@@ -12,7 +12,8 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librlgen.so")
-SOURCES = ["rlgen.hip", "gemm.hip", "attention.hip", "elementwise.hip", "sampler.hip"]
+SOURCES = ["rlgen.hip", "gemm.hip", "attention.hip", "elementwise.hip", "sampler.hip", "operators.hip", "paged.hip", "window.hip",
+           "window_decode.hip", "window_backward.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed-fp32 instruction selection is switched off on the test machines

@@ -1,0 +1,470 @@
+// The paged cache's bookkeeping, and the per-head norms with rotation that write into it.
+//
+// A cache is pages [n_pages, 2, Hkv, page_size, h]: a page holds page_size keys of every kv head and then the values of the same
+// tokens, a head's rows one behind the other, so that a token's key is one run of 2 h bytes wherever its page lies.
+#include "../../include/rlgen.h"
+#include "window.h"
+
+namespace {
+
+constexpr int TPB = 256;
+
+__device__ __forceinline__ int block_sum(int v, int* red) {          // of a block of 256 threads; red: 4 ints
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, WAVE);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return red[0] + red[1] + red[2] + red[3];
+}
+__device__ __forceinline__ int block_max(int v, int* red) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, WAVE));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return max(max(red[0], red[1]), max(red[2], red[3]));
+}
+__device__ __forceinline__ int block_exclusive(int v, int* red) {    // exclusive prefix sum over the block's threads
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o, WAVE);
+    if ((threadIdx.x & 63) >= (unsigned)o) x += y;
+  }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) red[threadIdx.x >> 6] = x;
+  __syncthreads();
+  int before = 0;
+  for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) before += red[w];
+  return before + x - v;
+}
+
+constexpr int PLAN_GROUP = 4 * TPB;          // most requests to a block
+
+// How far a request's lengths go.  A negative length counts as zero.
+struct Lens { int ctx, add, had, need; };
+__device__ __forceinline__ Lens plan_lens(const PlanArgs& a, int s) {
+  Lens l;
+  l.ctx = max(a.ctx_lens[s], 0);
+  l.add = max(a.new_lens[s], 0);
+  const int round = (1 << a.page_shift) - 1;
+  l.had = (int)(((unsigned)l.ctx + round) >> a.page_shift);
+  l.need = (int)(((unsigned)l.ctx + (unsigned)l.add + round) >> a.page_shift);
+  return l;
+}
+
+// A pass's plan in one launch without scratch memory: a block owns the `group` requests from blockIdx.x * group on and adds up the
+// lengths of all requests before them itself (8 bytes a request out of L2: 1000 requests are four loads a thread), then scans its own in
+// LDS and writes their rows and pages.  Where a group has many rows, blockIdx.y parts them.  Bound by a launch and three or four
+// dependent memory latencies, not by its bytes.
+__global__ __launch_bounds__(TPB) void plan_pages_kernel(PlanArgs a) {
+  __shared__ int red[4];
+  __shared__ int row_end[PLAN_GROUP], page_end[PLAN_GROUP], lens_ctx[PLAN_GROUP], lens_had[PLAN_GROUP];
+  const int s0 = blockIdx.x * a.group, n = min(a.group, a.S - s0);
+  const bool last = s0 + n == a.S, writer = blockIdx.y == 0;
+  const int head = a.free_head ? max(*a.free_head, 0) : 0;
+  int rows = 0, pages = 0, longest = 0, faults = 0;
+  for (int s = threadIdx.x; s < s0; s += TPB) {
+    const Lens l = plan_lens(a, s);
+    rows += l.add;
+    pages += l.need - l.had;
+    if (last) {
+      longest = max(longest, l.ctx + l.add);
+      if (l.need > a.table_stride) faults |= RLGEN_PLAN_TABLE;
+      if (a.ctx_lens[s] < 0 || a.new_lens[s] < 0) faults |= RLGEN_PLAN_LENGTH;
+    }
+  }
+  const int rows0 = block_sum(rows, red), pages0 = head + block_sum(pages, red);
+  // this block's own requests: consecutive ones to a thread, so that the scan is one over threads
+  const int per = (n + TPB - 1) / TPB, own0 = threadIdx.x * per, own1 = min(own0 + per, n);
+  rows = pages = 0;
+  for (int i = own0; i < own1; ++i) {
+    const Lens l = plan_lens(a, s0 + i);
+    rows += l.add;
+    pages += l.need - l.had;
+    row_end[i] = rows;
+    page_end[i] = pages;
+    lens_ctx[i] = l.ctx;
+    lens_had[i] = l.had;
+    longest = max(longest, l.ctx + l.add);
+    if (l.need > a.table_stride) faults |= RLGEN_PLAN_TABLE;
+    if (a.ctx_lens[s0 + i] < 0 || a.new_lens[s0 + i] < 0) faults |= RLGEN_PLAN_LENGTH;
+    if (writer) a.total_lens[s0 + i] = l.ctx + l.add;
+  }
+  const int rows_before = rows0 + block_exclusive(rows, red), pages_before = pages0 + block_exclusive(pages, red);
+  for (int i = own0; i < own1; ++i) {
+    if (writer) a.row_starts[s0 + i] = i > own0 ? row_end[i - 1] : rows_before;
+    row_end[i] += rows_before;
+    page_end[i] += pages_before;
+  }
+  __syncthreads();
+  const int rows1 = row_end[n - 1], pages1 = page_end[n - 1];
+  if (last && writer) {
+    longest = block_max(longest, red);
+    if (block_sum(faults & RLGEN_PLAN_TABLE, red)) faults |= RLGEN_PLAN_TABLE;
+    if (block_sum((faults & RLGEN_PLAN_LENGTH) ? 1 : 0, red)) faults |= RLGEN_PLAN_LENGTH;
+    if (threadIdx.x == 0) {
+      if (pages1 > a.n_free) faults |= RLGEN_PLAN_PAGES;
+      if (rows1 > a.max_rows) faults |= RLGEN_PLAN_ROWS;
+      a.row_starts[a.S] = rows1;
+      a.counts[0] = rows1;
+      a.counts[1] = min(pages1, a.n_free);
+      a.counts[2] = longest;
+      a.counts[3] = faults;
+    }
+  }
+  // (a page that the free list no longer has is -1, and so are the slots in it)
+  auto fresh = [&](int at) { return at < a.n_free ? a.free_pages[at] : -1; };
+  if (writer) {
+    for (int at = pages0 + threadIdx.x; at < pages1; at += TPB) {
+      int lo = 0, hi = n - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (page_end[mid] > at) hi = mid; else lo = mid + 1;
+      }
+      const int entry = lens_had[lo] + at - (lo ? page_end[lo - 1] : pages0);
+      if (entry < a.table_stride) a.page_table[(size_t)(s0 + lo) * a.table_stride + entry] = fresh(at);
+    }
+  }
+  const int round = (1 << a.page_shift) - 1;
+  const int row_stop = last ? a.max_rows : min(rows1, a.max_rows);
+  for (int r = rows0 + blockIdx.y * TPB + threadIdx.x; r < row_stop; r += gridDim.y * TPB) {
+    if (r >= rows1) {
+      a.slots[r] = -1;
+      a.positions[r] = 0;
+      continue;
+    }
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (row_end[mid] > r) hi = mid; else lo = mid + 1;
+    }
+    const int pos = lens_ctx[lo] + r - (lo ? row_end[lo - 1] : rows0);
+    const int entry = pos >> a.page_shift;
+    int page = -1;
+    if (entry < a.table_stride)
+      page = entry < lens_had[lo] ? a.page_table[(size_t)(s0 + lo) * a.table_stride + entry]
+                                  : fresh((lo ? page_end[lo - 1] : pages0) + entry - lens_had[lo]);
+    a.slots[r] = page < 0 ? -1 : (int)((unsigned)page << a.page_shift) + (pos & round);
+    a.positions[r] = pos;
+  }
+}
+
+// ------------------------------------------------------------------ per-head norm and rotation
+// A head's vector sits in LPH lanes of a wave, eight dims to a lane; a lane keeps the same dims for all heads of a row, so the angles
+// of the row's position and the gains are loaded once.
+template <class T> struct Eight;
+template <> struct Eight<float> {
+  f32x4 a, b;
+  static __device__ __forceinline__ Eight load(const void* p, long long at) {
+    const float* x = (const float*)p + at;
+    return {*(const f32x4*)x, *(const f32x4*)(x + 4)};
+  }
+  static __device__ __forceinline__ Eight zero() { return {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}}; }
+  __device__ __forceinline__ void to(float* y) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { y[e] = a[e]; y[4 + e] = b[e]; }
+  }
+  __device__ __forceinline__ Eight from_lane(int lane) const {
+    Eight r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { r.a[e] = __shfl(a[e], lane, WAVE); r.b[e] = __shfl(b[e], lane, WAVE); }
+    return r;
+  }
+  static __device__ __forceinline__ void store(void* p, long long at, const float* y) {
+    float* x = (float*)p + at;
+    *(f32x4*)x = f32x4{y[0], y[1], y[2], y[3]};
+    *(f32x4*)(x + 4) = f32x4{y[4], y[5], y[6], y[7]};
+  }
+};
+template <class T> struct Eight {
+  u32x4 w;
+  static __device__ __forceinline__ Eight load(const void* p, long long at) { return {*(const u32x4*)((const uint16_t*)p + at)}; }
+  static __device__ __forceinline__ Eight zero() { return {u32x4{0, 0, 0, 0}}; }
+  __device__ __forceinline__ void to(float* y) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { y[2 * e] = T::low(w[e]); y[2 * e + 1] = T::high(w[e]); }
+  }
+  __device__ __forceinline__ Eight from_lane(int lane) const {
+    Eight r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r.w[e] = __shfl(w[e], lane, WAVE);
+    return r;
+  }
+  static __device__ __forceinline__ void store(void* p, long long at, const float* y) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = T::pack(y[2 * e], y[2 * e + 1]);
+    *(u32x4*)((uint16_t*)p + at) = w;
+  }
+};
+
+// A lane's angles at one position: out = y c + (the rotary partner's y) t, t with the partner's sign; c = 1, t = 0 for dims past r
+struct Angles { float c[8], t[8]; };
+__device__ __forceinline__ void load_angles(Angles& w, const float2* rope, int r, int pos, int d0, float sign) {
+  const int half = r >> 1;
+  const float2* row = rope + (size_t)pos * half;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int d = d0 + e;
+    const float2 v = d < r ? row[d < half ? d : d - half] : make_float2(1.f, 0.f);
+    w.c[e] = v.x;
+    w.t[e] = d < half ? -sign * v.y : sign * v.y;
+  }
+}
+// The rotary partners of a lane's eight values.  ALIGNED: half a rotation is whole lanes, else the vector goes through LDS.
+template <class T, bool ALIGNED>
+__device__ __forceinline__ void partners(const Eight<T>& x, float* y, float* lds, int d0, int r, int group_lane0) {
+  const int half = r >> 1;
+  if constexpr (ALIGNED) {
+    const int d = d0 < half ? d0 + half : d0 < r ? d0 - half : d0;
+    x.from_lane(group_lane0 + (d >> 3)).to(y);
+  } else {
+    float own[8];
+    x.to(own);
+    __builtin_amdgcn_wave_barrier();          // (the readers of what this overwrites are lanes of this wave)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) lds[d0 + e] = own[e];
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int d = d0 + e;
+      y[e] = lds[d < half ? d + half : d < r ? d - half : d];
+    }
+  }
+}
+template <int LPH> __device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = LPH / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, WAVE);
+  return v;
+}
+
+// Bound by HBM: every head is read and written once.  A block takes a row, its lane groups the heads of it in turn, four heads
+// requested before the first is used.
+template <class TI, class TO, int LPH, bool ALIGNED>
+__global__ __launch_bounds__(TPB) void norm_rope_kernel(NormRopeArgs a) {
+  constexpr int GPB = TPB / LPH, AHEAD = 4;
+  __shared__ float lds[ALIGNED ? 1 : GPB * LPH * 8];
+  const int li = threadIdx.x % LPH, grp = threadIdx.x / LPH, d0 = li * 8, lane0 = (threadIdx.x & 63) - li;
+  const bool on = d0 < a.h;
+  const int heads = a.Hq + 2 * a.Hkv;
+  const float inv_h = 1.0f / (float)a.h;
+  float gq[8], gk[8], pq[8], pk[8];            // gains of the lane's dims and of their partners
+  const int half = a.r >> 1;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int d = d0 + e, p = d < half ? d + half : d < a.r ? d - half : d;
+    gq[e] = on ? a.q_gain[d] : 0.f;
+    gk[e] = on ? a.k_gain[d] : 0.f;
+    pq[e] = on ? a.q_gain[p] : 0.f;
+    pk[e] = on ? a.k_gain[p] : 0.f;
+  }
+  for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    Angles w;
+    load_angles(w, a.rope, on ? a.r : 0, min(max(a.positions[row], 0), a.max_pos - 1), d0, 1.f);
+    const long long src = (long long)row * a.qkv_stride;
+    int slot = -1;
+    if (a.pages) {
+      slot = a.slots[row];
+      if ((slot >> a.page_shift) >= a.n_pages) slot = -1;
+    }
+    for (int h0 = grp; h0 < heads; h0 += GPB * AHEAD) {
+      Eight<TI> x[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int hd = h0 + u * GPB;
+        x[u] = on && hd < heads ? Eight<TI>::load(a.qkv, src + (long long)hd * a.h + d0) : Eight<TI>::zero();
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int hd = h0 + u * GPB;
+        if (hd - grp >= heads) break;            // (the block's lanes go on together)
+        float y[8], p[8], ss = 0.f;
+        x[u].to(y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
+        const float inv = rsqrtf(fmaf(group_sum<LPH>(ss), inv_h, a.eps));
+        partners<TI, ALIGNED>(x[u], p, lds + (ALIGNED ? 0 : grp * LPH * 8), d0, a.r, lane0);
+        if (!on || hd >= heads) continue;
+        const bool is_q = hd < a.Hq, is_v = hd >= a.Hq + a.Hkv;
+        if (!is_v) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = y[e] * inv * (is_q ? gq[e] : gk[e]) * w.c[e] + p[e] * inv * (is_q ? pq[e] : pk[e]) * w.t[e];
+        }
+        if (is_q) {
+          Eight<TO>::store(a.q, (long long)row * a.q_stride + (long long)hd * a.h + d0, y);
+        } else {
+          const int kvh = hd - a.Hq - (is_v ? a.Hkv : 0);
+          if (slot >= 0) {
+            const long long at = ((((long long)(slot >> a.page_shift) * 2 + (is_v ? 1 : 0)) * a.Hkv + kvh) << a.page_shift) + (slot & ((1 << a.page_shift) - 1));
+            Eight<TO>::store(a.pages, at * a.h + d0, y);
+          }
+          void* dst = is_v ? a.v : a.k;
+          if (dst) Eight<TO>::store(dst, (long long)row * (is_v ? a.v_stride : a.k_stride) + (long long)kvh * a.h + d0, y);
+        }
+      }
+    }
+  }
+}
+
+// Gradients: the vectors of a head as above.  The gains' gradients are sums over all rows and heads: every lane keeps those of its dims
+// in registers over all rows of its block, the lane groups of the block meet in LDS in their order, and a second launch adds up the
+// blocks, so that a result does not depend on which block came first.
+template <class TI, class TO, int LPH, bool ALIGNED>
+__global__ __launch_bounds__(TPB) void norm_rope_backward_kernel(NormRopeArgs a) {
+  constexpr int GPB = TPB / LPH, AHEAD = 2;
+  __shared__ float lds[GPB * LPH * 8];
+  const int li = threadIdx.x % LPH, grp = threadIdx.x / LPH, d0 = li * 8, lane0 = (threadIdx.x & 63) - li;
+  const bool on = d0 < a.h;
+  const int heads = a.Hq + 2 * a.Hkv;
+  const float inv_h = 1.0f / (float)a.h;
+  float gq[8], gk[8], sum_q[8], sum_k[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    gq[e] = on ? a.q_gain[d0 + e] : 0.f;
+    gk[e] = on ? a.k_gain[d0 + e] : 0.f;
+    sum_q[e] = sum_k[e] = 0.f;
+  }
+  for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    Angles w;
+    load_angles(w, a.rope, on ? a.r : 0, min(max(a.positions[row], 0), a.max_pos - 1), d0, -1.f);
+    for (int h0 = grp; h0 < heads; h0 += GPB * AHEAD) {
+      Eight<TI> x[AHEAD];
+      Eight<TO> g[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int hd = h0 + u * GPB;
+        const bool is_q = hd < a.Hq, is_v = hd >= a.Hq + a.Hkv;
+        x[u] = on && hd < heads && !is_v ? Eight<TI>::load(a.qkv, (long long)row * a.qkv_stride + (long long)hd * a.h + d0) : Eight<TI>::zero();
+        const void* src = is_q ? a.dq : is_v ? a.dv : a.dk;
+        const long long at = (long long)row * (is_q ? a.dq_stride : is_v ? a.dv_stride : a.dk_stride) + (long long)(is_q ? hd : is_v ? hd - a.Hq - a.Hkv : hd - a.Hq) * a.h + d0;
+        g[u] = on && hd < heads ? Eight<TO>::load(src, at) : Eight<TO>::zero();
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int hd = h0 + u * GPB;
+        if (hd - grp >= heads) break;
+        const bool is_q = hd < a.Hq, is_v = hd >= a.Hq + a.Hkv;
+        float y[8], d[8], p[8], ss = 0.f, tx = 0.f;
+        x[u].to(y);
+        g[u].to(d);
+        partners<TO, ALIGNED>(g[u], p, lds + grp * LPH * 8, d0, a.r, lane0);
+        float out[8];
+        if (!is_v) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            d[e] = fmaf(d[e], w.c[e], p[e] * w.t[e]);
+            out[e] = d[e] * (is_q ? gq[e] : gk[e]);
+            ss = fmaf(y[e], y[e], ss);
+            tx = fmaf(out[e], y[e], tx);
+          }
+        }
+        ss = group_sum<LPH>(ss);
+        tx = group_sum<LPH>(tx);
+        if (!on || hd >= heads) continue;
+        if (is_v) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) out[e] = d[e];
+        } else {
+          const float inv = rsqrtf(fmaf(ss, inv_h, a.eps)), back = inv * inv * tx * inv_h;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float dg = d[e] * (y[e] * inv);
+            if (is_q) sum_q[e] += dg; else sum_k[e] += dg;
+            out[e] = inv * (out[e] - y[e] * back);
+          }
+        }
+        Eight<TI>::store(a.dqkv, (long long)row * a.dqkv_stride + (long long)hd * a.h + d0, out);
+      }
+    }
+  }
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) lds[grp * LPH * 8 + d0 + e] = which ? sum_k[e] : sum_q[e];
+    __syncthreads();
+    for (int d = threadIdx.x; d < a.h; d += TPB) {
+      float v = 0.f;
+      for (int g = 0; g < GPB; ++g) v += lds[g * LPH * 8 + d];
+      a.partial[((size_t)blockIdx.x * 2 + which) * a.h + d] = v;
+    }
+  }
+}
+
+// sums[which][d] over the blocks of norm_rope_backward_kernel: sixteen lanes to a sum, each a run of blocks in order
+__global__ __launch_bounds__(TPB) void gain_grad_kernel(const float* partial, int blocks, int h, float* dq_gain, float* dk_gain) {
+  __shared__ float red[16][16];
+  const int col = threadIdx.x & 15, part = threadIdx.x >> 4, d = blockIdx.x * 16 + col;
+  float v = 0.f;
+  if (d < 2 * h)
+    for (int b = part; b < blocks; b += 16) v += partial[(size_t)b * 2 * h + d];
+  red[part][col] = v;
+  __syncthreads();
+  if (part == 0 && d < 2 * h) {
+    for (int p = 1; p < 16; ++p) v += red[p][col];
+    if (d < h) dq_gain[d] = v; else dk_gain[d - h] = v;
+  }
+}
+
+template <class TI, class TO, int LPH>
+hipError_t launch_norm_rope(const NormRopeArgs& a, bool backward, int blocks, hipStream_t s) {
+  const bool aligned = (a.r >> 1) % 8 == 0;
+  if (backward) {
+    if (aligned) hipLaunchKernelGGL((norm_rope_backward_kernel<TI, TO, LPH, true>), dim3(blocks), dim3(TPB), 0, s, a);
+    else hipLaunchKernelGGL((norm_rope_backward_kernel<TI, TO, LPH, false>), dim3(blocks), dim3(TPB), 0, s, a);
+  } else {
+    if (aligned) hipLaunchKernelGGL((norm_rope_kernel<TI, TO, LPH, true>), dim3(blocks), dim3(TPB), 0, s, a);
+    else hipLaunchKernelGGL((norm_rope_kernel<TI, TO, LPH, false>), dim3(blocks), dim3(TPB), 0, s, a);
+  }
+  return hipGetLastError();
+}
+template <class TI, class TO>
+hipError_t by_head(const NormRopeArgs& a, bool backward, int blocks, hipStream_t s) {
+  if (a.h <= 64) return launch_norm_rope<TI, TO, 8>(a, backward, blocks, s);
+  if (a.h <= 128) return launch_norm_rope<TI, TO, 16>(a, backward, blocks, s);
+  return launch_norm_rope<TI, TO, 32>(a, backward, blocks, s);
+}
+hipError_t by_type(const NormRopeArgs& a, bool backward, int blocks, hipStream_t s) {
+  const bool f16 = a.dtype == RLGEN_DTYPE_F16;
+  switch (a.src_dtype) {
+    case RLGEN_DTYPE_F32: return f16 ? by_head<float, TypeF16>(a, backward, blocks, s) : by_head<float, TypeBf16>(a, backward, blocks, s);
+    case RLGEN_DTYPE_BF16: return f16 ? by_head<TypeBf16, TypeF16>(a, backward, blocks, s) : by_head<TypeBf16, TypeBf16>(a, backward, blocks, s);
+    case RLGEN_DTYPE_F16: return f16 ? by_head<TypeF16, TypeF16>(a, backward, blocks, s) : by_head<TypeF16, TypeBf16>(a, backward, blocks, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+// blocks of the backward pass: enough for every CU to hold four, few enough for the sums of their partial gains
+int backward_blocks(int rows) { return rows < 1024 ? rows : 1024; }
+
+}  // namespace
+
+hipError_t rl_plan_pages(PlanArgs a, hipStream_t s) {
+  // 256 blocks of requests at most while a block's requests fit its LDS; rows of a group are parted until a part has 1024 of them or
+  // the launch 1024 blocks
+  a.group = (a.S + 255) / 256;
+  if (a.group > PLAN_GROUP) a.group = PLAN_GROUP;
+  const int groups = (a.S + a.group - 1) / a.group;
+  const long long per = ((long long)a.max_rows + groups - 1) / groups;
+  long long chunks = (per + 1023) / 1024, most = 1024 / groups > 1 ? 1024 / groups : 1;
+  a.chunks = (int)(chunks < 1 ? 1 : chunks < most ? chunks : most);
+  hipLaunchKernelGGL(plan_pages_kernel, dim3(groups, a.chunks), dim3(TPB), 0, s, a);
+  return hipGetLastError();
+}
+hipError_t rl_norm_rope(const NormRopeArgs& a, hipStream_t s) {
+  if (a.rows <= 0) return hipSuccess;
+  return by_type(a, false, a.rows < 65536 ? a.rows : 65536, s);
+}
+size_t rl_norm_rope_backward_bytes(int rows, int h) { return (size_t)backward_blocks(rows < 1 ? 1 : rows) * 2 * h * sizeof(float); }
+hipError_t rl_norm_rope_backward(const NormRopeArgs& a, hipStream_t s) {
+  const int blocks = backward_blocks(a.rows);
+  if (blocks > 0) {
+    const hipError_t e = by_type(a, true, blocks, s);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(gain_grad_kernel, dim3((2 * a.h + 15) / 16), dim3(TPB), 0, s, a.partial, blocks, a.h, a.dq_gain, a.dk_gain);
+  return hipGetLastError();
+}

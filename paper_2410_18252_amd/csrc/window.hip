@@ -1,0 +1,279 @@
+// Attention with a sliding window and first tokens that stay visible, over packed sequences: keys and values as rows (training, fresh
+// prompts) or out of the cache's pages (a chunk of new tokens behind a context).
+//
+// A query at position p sees key j if j <= p and (j > p - window, or j < sinks, or there is no window).  The keys that a tile of
+// queries sees are two runs, the sinks and the window; tiles of keys walk the one and then the other, so the work follows the window
+// and not the context.  Softmax in one pass over the keys with a running maximum and sum in 32 bits.
+//
+// The query heads of a kv head and the tokens make one axis (row m: token m / G, head m % G of the group), so a tile of 128 rows spans
+// 128 / G tokens: grouped heads read a key once, and the diagonal and the window's edge waste less.
+//   S^T[key, m] = K q^T             32x32x16 matrix instructions, K fragments from LDS, q in registers
+//   O^T[d, m]  += V^T[d, key] P^T   the probabilities leave the first product in the layout the second wants; V is read transposed
+// The probabilities are rounded to the inputs' type for the second product (the sum that they are divided by is of the unrounded ones):
+// an error of the order of the output's own rounding.
+#include "../../include/rlgen.h"
+#include "window_tiles.h"
+
+namespace {
+
+constexpr int TPB = 256, BM = 128;
+
+// Rows m_first .. m_first + 31 of a group's queries by one wave, key by key: what the matrix products cannot give where a value is infinite
+// or NaN, since a probability of zero times it is NaN for every query of the tile, not only for those that see it.  Reached only by
+// waves that found such a result.  64 keys at a time, one to a lane for the scores; for the sums a lane owns every 64th dim.
+template <class T, bool PAGED>
+__device__ void rows_key_by_key(const WindowArgs& a, const Seq& q, int s, int kvh, int m_first, int M, int lane) {
+  const int G = a.Hq / a.Hkv;
+  auto key_row = [&](int key, bool value) {
+    if constexpr (PAGED) {
+      const unsigned entry = a.page_table[(size_t)s * a.table_stride + (key >> a.page_shift)], page = entry < (unsigned)a.n_pages ? entry : 0;
+      const long long row = ((((long long)page * 2 + (value ? 1 : 0)) * a.Hkv + kvh) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
+      return (const uint16_t*)a.pages + row * a.h;
+    } else {
+      return (const uint16_t*)(value ? a.v : a.k) + (long long)(q.row0 + key) * (value ? a.v_stride : a.k_stride) + (long long)kvh * a.h;
+    }
+  };
+  for (int m = m_first; m < min(m_first + 32, M); ++m) {
+    const int tok = m / G, head = kvh * G + m - tok * G, pos = q.ctx + tok, end = min(pos + 1, q.total);
+    const int w_lo = a.window ? max(pos - a.window + 1, 0) : 0, sinks = max(min(min(a.sinks, w_lo), end), 0);
+    const uint16_t* qp = (const uint16_t*)a.q + (long long)(q.row0 + tok) * a.q_stride + (long long)head * a.h;
+    float mx = -INFINITY, sum = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+    const int seen = sinks + max(end - w_lo, 0);
+    for (int i0 = 0; i0 < seen; i0 += 64) {
+      const int i = i0 + lane;
+      float sc = -INFINITY;
+      if (i < seen) {
+        const uint16_t* kp = key_row(i < sinks ? i : w_lo + i - sinks, false);
+        sc = 0.f;
+        for (int d = 0; d < a.h; d += 2) {
+          const uint32_t kw = *(const uint32_t*)(kp + d), qw = *(const uint32_t*)(qp + d);
+          sc = fmaf(T::low(kw), T::low(qw), sc);
+          sc = fmaf(T::high(kw), T::high(qw), sc);
+        }
+        sc *= a.scale * 1.4426950408889634f;
+      }
+      const float now = fmaxf(mx, wave_max(sc)), base = now == -INFINITY ? 0.f : now;
+      const float shrink = __builtin_amdgcn_exp2f(mx - base), p = __builtin_amdgcn_exp2f(sc - base);
+      mx = now;
+      sum = sum * shrink + wave_sum(p);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] *= shrink;
+      for (int j = 0; j < min(64, seen - i0); ++j) {
+        const float pj = __shfl(p, j, WAVE);
+        const uint16_t* vp = key_row(i0 + j < sinks ? i0 + j : w_lo + i0 + j - sinks, true);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (lane + 64 * e < a.h) y[e] = fmaf(pj, T::low(vp[lane + 64 * e]), y[e]);
+      }
+    }
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    const long long row = q.row0 + tok;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (lane + 64 * e < a.h) ((uint16_t*)a.out)[row * a.out_stride + (long long)head * a.h + lane + 64 * e] = (uint16_t)T::pack(y[e] * inv, 0.f);
+    if (a.lse && lane == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  }
+}
+
+// Bound by the exp and the instructions around it as much as by the matrix cores.
+template <class T, int HD, bool PAGED>
+__global__ __launch_bounds__(TPB) void window_rows_kernel(WindowArgs a, int tiles) {
+  typedef typename T::vec8 vec8;
+  constexpr int BN = HD > 128 ? 32 : 64, SUB = BN / 32, KS = HD / 16, DT = (HD + 31) / 32, CPR = HD / 8;
+  constexpr int TILE = BN * HD, PIECES = BN * CPR / 64, PER = (PIECES + 3) / 4;      // pieces: requests of a kilobyte, dealt to the four waves
+  __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][TILE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, g = lane >> 5;
+  const int G = a.Hq / a.Hkv;
+  int unit, mt;
+  if (!map_block(blockIdx.x, a.S * a.Hkv, tiles, unit, mt)) return;
+  const int s = unit / a.Hkv, kvh = unit - s * a.Hkv;
+  const Seq q = load_seq(a, s, PAGED);
+  const int m0 = mt * BM, M = q.n * G;
+  if (m0 >= M) return;
+  const int p_lo = q.ctx + m0 / G, p_hi = q.ctx + min(m0 + BM - 1, M - 1) / G;
+  const int key_end = min(p_hi + 1, q.total);                      // keys from here on are seen by nobody
+  const int w_lo = a.window ? max(p_lo - a.window + 1, 0) : 0;
+  const int sink_tiles = (min(min(a.sinks, w_lo), key_end) + BN - 1) / BN;
+  const int w_base = max(w_lo, sink_tiles * BN);
+  const int n_tiles = sink_tiles + (key_end > w_base ? (key_end - w_base + BN - 1) / BN : 0);
+  auto tile_key = [&](int t) { return t < sink_tiles ? t * BN : w_base + (t - sink_tiles) * BN; };
+
+  // this lane's row
+  const int m = m0 + wave * 32 + c;
+  const bool live = m < M;
+  const int tok = min(m, M - 1) / G, head = kvh * G + min(m, M - 1) % G, pos = q.ctx + tok;
+  const int wp_lo = q.ctx + min(m0 + wave * 32, M - 1) / G, wp_hi = q.ctx + min(m0 + wave * 32 + 31, M - 1) / G;
+  vec8 qf[KS];
+  {
+    const uint16_t* qp = (const uint16_t*)a.q + (long long)(q.row0 + tok) * a.q_stride + (long long)head * a.h;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const int d = 16 * i + 8 * g;
+      qf[i] = d < a.h ? *(const vec8*)(qp + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
+    }
+  }
+
+  // requests: piece n of a tile is 64 chunks, lane l the chunk 64 n + l of the tile as it lies in LDS
+  const uint16_t *kp = (const uint16_t*)a.k, *vp = (const uint16_t*)a.v;
+  int row_of[PER], chunk_of[PER];
+#pragma unroll
+  for (int n = 0; n < PER; ++n) {
+    const int at = (n * 4 + wave) * 64 + lane;
+    row_of[n] = at / CPR;
+    chunk_of[n] = ((at % CPR) ^ chunk_swap<HD>(row_of[n])) * 8;
+  }
+  const int key_max = q.total - 1;
+  [[maybe_unused]] int page_of[PER];
+  auto fetch_pages = [&](int t) {
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int n = 0; n < PER; ++n) page_of[n] = a.page_table[(size_t)s * a.table_stride + (min(tile_key(t) + row_of[n], key_max) >> a.page_shift)];
+    }
+  };
+  auto request = [&](int t, int buf) {
+    const int base = tile_key(t);
+#pragma unroll
+    for (int n = 0; n < PER; ++n) {
+      if (PIECES % 4 != 0 && n * 4 + wave >= PIECES) break;
+      const int key = min(base + row_of[n], key_max);
+      const uint16_t *ks, *vs;
+      if constexpr (PAGED) {
+        const unsigned page = (unsigned)page_of[n] < (unsigned)a.n_pages ? page_of[n] : 0;      // (an entry outside is not followed)
+        const long long row = (((long long)page * 2 * a.Hkv + kvh) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
+        ks = (const uint16_t*)a.pages + row * a.h + chunk_of[n];
+        vs = ks + ((long long)a.Hkv << a.page_shift) * a.h;
+      } else {
+        ks = kp + (long long)(q.row0 + key) * a.k_stride + (long long)kvh * a.h + chunk_of[n];
+        vs = vp + (long long)(q.row0 + key) * a.v_stride + (long long)kvh * a.h + chunk_of[n];
+      }
+      if (chunk_of[n] >= a.h) ks = vs = (const uint16_t*)&zero_chunk;
+      const int to = (n * 4 + wave) * 512;
+      __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(lds[buf][0] + to), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(lds[buf][1] + to), 16, 0, 0);
+    }
+  };
+
+  f32x16 o[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+  float mx = -INFINITY, sum = 0.f;             // of the scores times scale log2 e
+  const float scale2 = a.scale * 1.4426950408889634f;
+  if (n_tiles > 0) {
+    fetch_pages(0);
+    request(0, 0);
+    if (n_tiles > 1) fetch_pages(1);
+  }
+  for (int t = 0; t < n_tiles; ++t) {
+    // this tile has landed, and nobody reads the other buffer any more
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
+    if (t + 2 < n_tiles) fetch_pages(t + 2);
+    const int kb = tile_key(t);
+    if (kb > wp_hi || (a.window && kb + BN - 1 <= wp_lo - a.window && kb >= a.sinks)) continue;
+    const uint16_t *kt = lds[t & 1][0], *vt = lds[t & 1][1];
+    f32x16 sc[SUB];
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) sc[u] = T::mfma32(row_frag<HD, vec8>(kt, 32 * u + c, i, g), qf[i], sc[u]);
+    }
+    const bool whole = kb + BN - 1 <= wp_lo && (a.window == 0 || kb > wp_hi - a.window || kb + BN - 1 < a.sinks);
+    float top = -INFINITY;
+    if (!whole) {
+#pragma unroll
+      for (int u = 0; u < SUB; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[u][i] = visible(pos, kb + 32 * u + acc_row(i, g), a.window, a.sinks) ? sc[u][i] : -INFINITY;
+    }
+#pragma unroll
+    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[u][i]);
+    top = fmaxf(top, other_half(top)) * scale2;
+    const float now = fmaxf(mx, top);
+    const float base = now == -INFINITY ? 0.f : now;          // a row that has seen no key yet keeps zeros
+    if (__any(now > mx)) {
+      const float shrink = __builtin_amdgcn_exp2f(mx - base);
+      sum *= shrink;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= shrink;
+    }
+    mx = now;
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      float part = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        sc[u][i] = __builtin_amdgcn_exp2f(fmaf(sc[u][i], scale2, -base));
+        part += sc[u][i];
+      }
+      sum += part;
+    }
+#pragma unroll
+    for (int u = 0; u < 2 * SUB; ++u) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = T::pack(sc[u >> 1][8 * (u & 1) + 2 * e], sc[u >> 1][8 * (u & 1) + 2 * e + 1]);
+      const vec8 pf = __builtin_bit_cast(vec8, w);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] = T::mfma32(column_frag<HD, vec8>(vt, 16 * u, d, lane), pf, o[d]);
+    }
+  }
+  sum += other_half(sum);
+  const float inv = sum > 0.f ? 1.0f / sum : (sum == 0.f ? 0.f : sum);      // (NaN stays)
+  bool finite = fabsf(sum) < INFINITY;
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) finite &= fabsf(o[t][i]) < INFINITY;
+  if (__any(live && !finite)) {
+    rows_key_by_key<T, PAGED>(a, q, s, kvh, m0 + wave * 32, M, lane);
+    return;
+  }
+  if (!live) return;
+  const long long row = q.row0 + tok;
+  if (a.lse && g == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  uint16_t* op = (uint16_t*)a.out + row * a.out_stride + (long long)head * a.h;
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int d = 32 * t + 8 * j + 4 * g;
+      if (d >= a.h) continue;
+      u32x2 w;
+      w[0] = T::pack(o[t][4 * j] * inv, o[t][4 * j + 1] * inv);
+      w[1] = T::pack(o[t][4 * j + 2] * inv, o[t][4 * j + 3] * inv);
+      *(u32x2*)(op + d) = w;
+    }
+}
+
+template <class T, int HD>
+hipError_t launch_rows(const WindowArgs& a, hipStream_t s) {
+  const int tiles = (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
+  const dim3 grid(mapped_blocks((long long)a.S * a.Hkv, tiles));
+  if (a.pages) hipLaunchKernelGGL((window_rows_kernel<T, HD, true>), grid, dim3(TPB), 0, s, a, tiles);
+  else hipLaunchKernelGGL((window_rows_kernel<T, HD, false>), grid, dim3(TPB), 0, s, a, tiles);
+  return hipGetLastError();
+}
+template <class T>
+hipError_t by_head(const WindowArgs& a, hipStream_t s) {
+  // the smallest of the compiled sizes that holds the head; dims past it are zeros in LDS
+  if (a.h <= 32) return launch_rows<T, 32>(a, s);
+  if (a.h <= 64) return launch_rows<T, 64>(a, s);
+  if (a.h <= 80) return launch_rows<T, 80>(a, s);
+  if (a.h <= 96) return launch_rows<T, 96>(a, s);
+  if (a.h <= 128) return launch_rows<T, 128>(a, s);
+  return launch_rows<T, 256>(a, s);
+}
+
+}  // namespace
+
+hipError_t rl_window_rows(const WindowArgs& a, hipStream_t s) {
+  if (a.rows <= 0) return hipSuccess;
+  return a.dtype == RLGEN_DTYPE_F16 ? by_head<TypeF16>(a, s) : by_head<TypeBf16>(a, s);
+}

@@ -1,0 +1,423 @@
+// Gradients of the windowed attention over packed rows.
+//
+// With P = exp(scale q k - lse), dP = dout v, delta = sum over dims of dout out and dS = P (dP - delta):
+//   dv = sum over queries of P dout,   dk = scale sum over queries of dS q,   dq = scale sum over keys of dS k
+// P is computed again from the saved log-sum-exp, once in a kernel whose blocks own keys and once in one whose blocks own queries:
+// seven matrix products instead of the five that one kernel with atomic sums would need, but every sum has one order, so that results do
+// not change from run to run.  P and dS are rounded to the inputs' type for their second products, errors of the order of the
+// gradients' own rounding; fp16, whose smallest normal number a dS easily falls below, multiplies dS by a power of two taken from the
+// largest |dout|.
+#include "../../include/rlgen.h"
+#include "window_tiles.h"
+
+namespace {
+
+constexpr int TPB = 256, BM = 128;
+constexpr int DELTA_BLOCKS = 512;
+constexpr float LOG2E = 1.4426950408889634f;
+
+// Everything below in the caller's workspace, and how the queries that see the sinks from beyond the window are parted.
+struct Backward {
+  WindowArgs a;
+  float *delta, *peak, *part;
+  int sinks, chunk, chunks;             // sinks that are parted (0: none); tokens to a part; parts of the longest sequence
+};
+
+// delta [rows, Hq] and, for each block, the largest |dout|
+template <class T>
+__global__ __launch_bounds__(TPB) void delta_kernel(Backward b) {
+  __shared__ float red[4];
+  const WindowArgs& a = b.a;
+  const int li = threadIdx.x & 15;
+  const long long items = (long long)a.rows * a.Hq;
+  float peak = 0.f;
+  for (long long it = (long long)blockIdx.x * 16 + (threadIdx.x >> 4); it < items; it += (long long)gridDim.x * 16) {
+    const long long row = it / a.Hq;
+    const int head = (int)(it - row * a.Hq);
+    float v = 0.f;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int d = 128 * x + 8 * li;
+      if (d >= a.h) continue;
+      const u32x4 o = *(const u32x4*)((const uint16_t*)a.o + row * a.o_stride + (long long)head * a.h + d);
+      const u32x4 g = *(const u32x4*)((const uint16_t*)a.dout + row * a.dout_stride + (long long)head * a.h + d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v = fmaf(T::low(o[e]), T::low(g[e]), v);
+        v = fmaf(T::high(o[e]), T::high(g[e]), v);
+        peak = fmaxf(peak, fmaxf(fabsf(T::low(g[e])), fabsf(T::high(g[e]))));
+      }
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor(v, o, WAVE);
+    if (li == 0) b.delta[it] = v;
+  }
+  peak = wave_max(peak);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = peak;
+  __syncthreads();
+  if (threadIdx.x == 0) b.peak[blockIdx.x] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+}
+
+// What fp16 multiplies dS by: 2^-3 over the power of two below the largest |dout|, so that neither a probability of 1e-5 vanishes nor a
+// sum over 256 dims against values up to some hundreds leaves the type's range.
+template <class T>
+__device__ __forceinline__ float ds_factor(const Backward& b) {
+  if constexpr (__is_same(T, TypeBf16)) return 1.f;
+  float peak = 0.f;
+  for (int i = threadIdx.x & 63; i < DELTA_BLOCKS; i += 64) peak = fmaxf(peak, b.peak[i]);
+  peak = wave_max(peak);
+  if (!(peak > 0.f) || peak > 3e38f) return 1.f;
+  return __uint_as_float((uint32_t)(254 - (int)(__float_as_uint(peak) >> 23)) << 23) * 0.125f;      // (127 - e) - 3 with e = exponent of peak
+}
+
+// ------------------------------------------------------------------ keys' side
+// A block owns 128 keys of a kv head, a wave 32 of them with K and V in registers; the rows of the group's queries that see them pass
+// through LDS (q and dout, each read by rows for S = q K^T and dP = dout V^T, and transposed for dv^T = dout^T P and dk^T = q^T dS).
+// Sinks are seen by every query behind them: what lies beyond the window is parted over blocks of its own, whose sums meet in
+// sink_sum_kernel; else the block of the first keys would run for as long as all others together.
+template <class T, int HD>
+__global__ __launch_bounds__(TPB, 1) void keys_backward_kernel(Backward b, int key_tiles, int jobs) {
+  typedef typename T::vec8 vec8;
+  const WindowArgs& a = b.a;
+  constexpr int BQ = HD > 128 ? 32 : 64, SUB = BQ / 32, KS = HD / 16, DT = (HD + 31) / 32, CPR = HD / 8;
+  constexpr int TILE = BQ * HD, PIECES = BQ * CPR / 64, PER = (PIECES + 3) / 4;
+  __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][TILE];
+  __shared__ __attribute__((aligned(16))) float stat[2][3][64];            // of a tile's rows: lse, delta, position (bits)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, g = lane >> 5;
+  const int G = a.Hq / a.Hkv;
+  int unit, job;
+  if (!map_block(blockIdx.x, a.S * a.Hkv, jobs, unit, job)) return;
+  job = jobs - 1 - job;
+  const int s = unit / a.Hkv, kvh = unit - s * a.Hkv;
+  const Seq q = load_seq(a, s, false);
+  // which keys, and the tokens that the job adds up
+  int kt = job, tok0, tok1, slot = -1;
+  if (job >= key_tiles) {
+    kt = (job - key_tiles) / b.chunks;
+    slot = 1 + (job - key_tiles) % b.chunks;
+    tok0 = kt * BM + BM - 1 + a.window + (slot - 1) * b.chunk;
+    tok1 = min(tok0 + b.chunk, q.n);
+    if (tok0 >= q.n) return;
+  } else {
+    if (kt * BM >= q.n) return;
+    tok0 = kt * BM;
+    tok1 = q.n;
+    if (a.window && (b.sinks > 0 || kt * BM >= a.sinks)) tok1 = (int)min((long long)q.n, (long long)kt * BM + BM - 1 + a.window);
+    if (kt * BM < b.sinks) slot = 0;
+  }
+  const int kw = kt * BM + wave * 32, key = kw + c;
+  const int M = q.n * G, m0 = tok0 * G, m1 = tok1 * G, n_tiles = (m1 - m0 + BQ - 1) / BQ;
+  // parts beyond the window concern the sinks alone
+  const bool idle = kw >= q.n || (slot > 0 && kw >= b.sinks);
+
+  vec8 kf[KS], vf[KS];
+  {
+    const long long row = q.row0 + min(key, q.n - 1);
+    const uint16_t* kp = (const uint16_t*)a.k + row * a.k_stride + (long long)kvh * a.h;
+    const uint16_t* vp = (const uint16_t*)a.v + row * a.v_stride + (long long)kvh * a.h;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const int d = 16 * i + 8 * g;
+      kf[i] = d < a.h ? *(const vec8*)(kp + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
+      vf[i] = d < a.h ? *(const vec8*)(vp + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
+    }
+  }
+  const float factor = ds_factor<T>(b);
+  auto request = [&](int t, int buf) {
+    const int base = m0 + t * BQ;
+#pragma unroll
+    for (int n = 0; n < PER; ++n) {
+      if (PIECES % 4 != 0 && n * 4 + wave >= PIECES) break;
+      const int at = (n * 4 + wave) * 64 + lane, r = at / CPR, chunk = ((at % CPR) ^ chunk_swap<HD>(r)) * 8;
+      const int m = min(base + r, M - 1), tok = m / G, head = kvh * G + m - tok * G;
+      const uint16_t* qs = (const uint16_t*)a.q + (long long)(q.row0 + tok) * a.q_stride + (long long)head * a.h + chunk;
+      const uint16_t* os = (const uint16_t*)a.dout + (long long)(q.row0 + tok) * a.dout_stride + (long long)head * a.h + chunk;
+      if (chunk >= a.h) qs = os = (const uint16_t*)&zero_chunk;
+      const int to = (n * 4 + wave) * 512;
+      __builtin_amdgcn_global_load_lds((gptr_t)qs, (lptr_t)(lds[buf][0] + to), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((gptr_t)os, (lptr_t)(lds[buf][1] + to), 16, 0, 0);
+    }
+    if (wave < 3) {
+      const int m = min(base + lane, M - 1), tok = m / G, head = kvh * G + m - tok * G;
+      const long long at = (long long)(q.row0 + tok) * a.Hq + head;
+      if (wave == 2) stat[buf][2][lane] = __int_as_float(base + lane < m1 ? tok : -1);      // (a row past the job's sees nothing)
+      else __builtin_amdgcn_global_load_lds((gptr_t)((wave ? b.delta : a.lse) + at), (lptr_t)stat[buf][wave], 4, 0, 0);
+    }
+  };
+
+  f32x16 dk[DT], dv[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dk[t][i] = dv[t][i] = 0.f;
+  const float scale2 = a.scale * LOG2E;
+  if (n_tiles > 0) request(0, 0);
+  for (int t = 0; t < n_tiles; ++t) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
+    if (idle) continue;
+    const uint16_t *qt = lds[t & 1][0], *ot = lds[t & 1][1];
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      const int base = m0 + t * BQ + 32 * u;
+      if (base >= m1) break;
+      const int p_lo = base / G, p_hi = min(base + 31, M - 1) / G;
+      if (p_hi < kw || (a.window && kw + 31 <= p_lo - a.window && kw >= a.sinks)) continue;
+      const bool whole = base + 31 < m1 && kw + 31 <= p_lo && (a.window == 0 || kw > p_hi - a.window || kw + 31 < a.sinks);
+      f32x16 sc, dp;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) sc = T::mfma32(row_frag<HD, vec8>(qt, 32 * u + c, i, g), kf[i], sc);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) dp = T::mfma32(row_frag<HD, vec8>(ot, 32 * u + c, i, g), vf[i], dp);
+      u32x4 pw[2], sw[2];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int r = 32 * u + 8 * j + 4 * g;
+        const f32x4 lse = *(const f32x4*)&stat[t & 1][0][r], delta = *(const f32x4*)&stat[t & 1][1][r], where = *(const f32x4*)&stat[t & 1][2][r];
+        float p[4], ds[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(fmaf(sc[4 * j + e], scale2, -lse[e] * LOG2E));
+          ds[e] = p[e] * (dp[4 * j + e] - delta[e]) * factor;
+          const bool seen = (bool)(whole | visible(__float_as_int(where[e]), key, a.window, a.sinks));
+          p[e] = seen ? p[e] : 0.f;
+          ds[e] = seen ? ds[e] : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          pw[j >> 1][2 * (j & 1) + e] = T::pack(p[2 * e], p[2 * e + 1]);
+          sw[j >> 1][2 * (j & 1) + e] = T::pack(ds[2 * e], ds[2 * e + 1]);
+        }
+      }
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) dv[d] = T::mfma32(column_frag<HD, vec8>(ot, 32 * u + 16 * v, d, lane), __builtin_bit_cast(vec8, pw[v]), dv[d]);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) dk[d] = T::mfma32(column_frag<HD, vec8>(qt, 32 * u + 16 * v, d, lane), __builtin_bit_cast(vec8, sw[v]), dk[d]);
+      }
+    }
+  }
+  if (key >= q.n || (slot > 0 && key >= b.sinks)) return;
+  const float back = a.scale / factor;
+  const bool parted = slot >= 0 && key < b.sinks;
+  const long long row = q.row0 + key;
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int d = 32 * t + 8 * j + 4 * g;
+      if (d >= a.h) continue;
+      const f32x4 yk = f32x4{dk[t][4 * j], dk[t][4 * j + 1], dk[t][4 * j + 2], dk[t][4 * j + 3]} * back;
+      const f32x4 yv = {dv[t][4 * j], dv[t][4 * j + 1], dv[t][4 * j + 2], dv[t][4 * j + 3]};
+      if (parted) {
+        float* to = b.part + ((((long long)unit * (b.chunks + 1) + slot) * 2) * b.sinks + key) * a.h + d;
+        *(f32x4*)to = yk;
+        *(f32x4*)(to + (long long)b.sinks * a.h) = yv;
+      } else {
+        *(u32x2*)((uint16_t*)a.dk + row * a.dk_stride + (long long)kvh * a.h + d) = u32x2{T::pack(yk[0], yk[1]), T::pack(yk[2], yk[3])};
+        *(u32x2*)((uint16_t*)a.dv + row * a.dv_stride + (long long)kvh * a.h + d) = u32x2{T::pack(yv[0], yv[1]), T::pack(yv[2], yv[3])};
+      }
+    }
+}
+
+// The parts of the sinks' gradients, in order.
+template <class T>
+__global__ __launch_bounds__(TPB) void sink_sum_kernel(Backward b) {
+  const WindowArgs& a = b.a;
+  const int unit = blockIdx.x, s = unit / a.Hkv, kvh = unit - s * a.Hkv;
+  const Seq q = load_seq(a, s, false);
+  const int quads = a.h / 4, n = min(b.sinks, q.n);
+  for (int at = blockIdx.y * TPB + threadIdx.x; at < 2 * n * quads; at += gridDim.y * TPB) {
+    const int which = at / (n * quads), rest = at - which * n * quads, key = rest / quads, d = (rest - key * quads) * 4;
+    const long long beyond = (long long)q.n - ((key / BM) * BM + BM - 1 + (long long)a.window);
+    const int parts = 1 + (beyond > 0 ? (int)((beyond + b.chunk - 1) / b.chunk) : 0);
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < parts; ++p) y += *(const f32x4*)(b.part + ((((long long)unit * (b.chunks + 1) + p) * 2 + which) * b.sinks + key) * a.h + d);
+    uint16_t* to = (uint16_t*)(which ? a.dv : a.dk) + (long long)(q.row0 + key) * (which ? a.dv_stride : a.dk_stride) + (long long)kvh * a.h + d;
+    *(u32x2*)to = u32x2{T::pack(y[0], y[1]), T::pack(y[2], y[3])};
+  }
+}
+
+// ------------------------------------------------------------------ queries' side
+// The forward pass's walk: a block owns 128 rows of a group's queries, a wave 32 of them with q and dout in registers; keys and values pass
+// through LDS (K by rows and transposed, V by rows).
+template <class T, int HD>
+__global__ __launch_bounds__(TPB) void queries_backward_kernel(Backward b, int tiles) {
+  typedef typename T::vec8 vec8;
+  const WindowArgs& a = b.a;
+  constexpr int BN = HD > 128 ? 32 : 64, SUB = BN / 32, KS = HD / 16, DT = (HD + 31) / 32, CPR = HD / 8;
+  constexpr int TILE = BN * HD, PIECES = BN * CPR / 64, PER = (PIECES + 3) / 4;
+  __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][TILE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, g = lane >> 5;
+  const int G = a.Hq / a.Hkv;
+  int unit, mt;
+  if (!map_block(blockIdx.x, a.S * a.Hkv, tiles, unit, mt)) return;
+  const int s = unit / a.Hkv, kvh = unit - s * a.Hkv;
+  const Seq q = load_seq(a, s, false);
+  const int m0 = mt * BM, M = q.n * G;
+  if (m0 >= M) return;
+  const int p_lo = m0 / G, p_hi = min(m0 + BM - 1, M - 1) / G, key_end = p_hi + 1;
+  const int w_lo = a.window ? max(p_lo - a.window + 1, 0) : 0;
+  const int sink_tiles = (min(min(a.sinks, w_lo), key_end) + BN - 1) / BN;
+  const int w_base = max(w_lo, sink_tiles * BN);
+  const int n_tiles = sink_tiles + (key_end > w_base ? (key_end - w_base + BN - 1) / BN : 0);
+  auto tile_key = [&](int t) { return t < sink_tiles ? t * BN : w_base + (t - sink_tiles) * BN; };
+  const int m = m0 + wave * 32 + c;
+  const bool live = m < M;
+  const int tok = min(m, M - 1) / G, head = kvh * G + min(m, M - 1) % G, pos = tok;
+  const int wp_lo = min(m0 + wave * 32, M - 1) / G, wp_hi = min(m0 + wave * 32 + 31, M - 1) / G;
+  const long long row = q.row0 + tok;
+  vec8 qf[KS], of[KS];
+#pragma unroll
+  for (int i = 0; i < KS; ++i) {
+    const int d = 16 * i + 8 * g;
+    qf[i] = d < a.h ? *(const vec8*)((const uint16_t*)a.q + row * a.q_stride + (long long)head * a.h + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
+    of[i] = d < a.h ? *(const vec8*)((const uint16_t*)a.dout + row * a.dout_stride + (long long)head * a.h + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
+  }
+  const float lse2 = a.lse[row * a.Hq + head] * LOG2E, delta = b.delta[row * a.Hq + head], factor = ds_factor<T>(b);
+  const int key_max = q.n - 1;
+  auto request = [&](int t, int buf) {
+    const int base = tile_key(t);
+#pragma unroll
+    for (int n = 0; n < PER; ++n) {
+      if (PIECES % 4 != 0 && n * 4 + wave >= PIECES) break;
+      const int at = (n * 4 + wave) * 64 + lane, r = at / CPR, chunk = ((at % CPR) ^ chunk_swap<HD>(r)) * 8;
+      const long long from = q.row0 + min(base + r, key_max);
+      const uint16_t* ks = (const uint16_t*)a.k + from * a.k_stride + (long long)kvh * a.h + chunk;
+      const uint16_t* vs = (const uint16_t*)a.v + from * a.v_stride + (long long)kvh * a.h + chunk;
+      if (chunk >= a.h) ks = vs = (const uint16_t*)&zero_chunk;
+      const int to = (n * 4 + wave) * 512;
+      __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(lds[buf][0] + to), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(lds[buf][1] + to), 16, 0, 0);
+    }
+  };
+  f32x16 dq[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dq[t][i] = 0.f;
+  const float scale2 = a.scale * LOG2E;
+  if (n_tiles > 0) request(0, 0);
+  for (int t = 0; t < n_tiles; ++t) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
+    const uint16_t *kt = lds[t & 1][0], *vt = lds[t & 1][1];
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      const int kb = tile_key(t) + 32 * u;
+      if (kb > wp_hi || (a.window && kb + 31 <= wp_lo - a.window && kb >= a.sinks)) continue;
+      const bool whole = kb + 31 <= wp_lo && (a.window == 0 || kb > wp_hi - a.window || kb + 31 < a.sinks);
+      f32x16 sc, dp;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) sc = T::mfma32(row_frag<HD, vec8>(kt, 32 * u + c, i, g), qf[i], sc);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) dp = T::mfma32(row_frag<HD, vec8>(vt, 32 * u + c, i, g), of[i], dp);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float ds = __builtin_amdgcn_exp2f(fmaf(sc[i], scale2, -lse2)) * (dp[i] - delta) * factor;
+        dp[i] = (whole | visible(pos, kb + acc_row(i, g), a.window, a.sinks)) ? ds : 0.f;
+      }
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = T::pack(dp[8 * v + 2 * e], dp[8 * v + 2 * e + 1]);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) dq[d] = T::mfma32(column_frag<HD, vec8>(kt, 32 * u + 16 * v, d, lane), __builtin_bit_cast(vec8, w), dq[d]);
+      }
+    }
+  }
+  if (!live) return;
+  const float back = a.scale / factor;
+  uint16_t* to = (uint16_t*)a.dq + row * a.dq_stride + (long long)head * a.h;
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int d = 32 * t + 8 * j + 4 * g;
+      if (d >= a.h) continue;
+      *(u32x2*)(to + d) = u32x2{T::pack(dq[t][4 * j] * back, dq[t][4 * j + 1] * back), T::pack(dq[t][4 * j + 2] * back, dq[t][4 * j + 3] * back)};
+    }
+}
+
+// Sinks are parted while their partial sums (two fp32 vectors a sink, kv head and part) stay below 64 MB; parts of four windows at least
+// 1024 tokens cost a block about what a tile of keys costs.
+void part_sinks(Backward& b) {
+  const WindowArgs& a = b.a;
+  b.sinks = b.chunks = 0;
+  b.chunk = 1;
+  const int sinks = a.sinks < a.max_new ? a.sinks : a.max_new;
+  const long long beyond = (long long)a.max_new - (BM - 1 + (long long)a.window);
+  if (!a.window || sinks < 1 || beyond < 1) return;
+  long long chunk = a.window > 1024 ? a.window : 1024, chunks = (beyond + chunk - 1) / chunk;
+  const long long slot = (long long)a.S * a.Hkv * sinks * a.h * 2 * 4;
+  if (chunks > 63) chunks = 63;
+  if (slot * (chunks + 1) > (64ll << 20)) chunks = (64ll << 20) / slot - 1;
+  if (chunks < 1) return;
+  b.sinks = sinks;
+  b.chunks = (int)chunks;
+  b.chunk = (int)((beyond + chunks - 1) / chunks);
+}
+size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
+// places the buffers and returns their size
+size_t place(Backward& b, char* ws) {
+  const WindowArgs& a = b.a;
+  size_t at = 0;
+  b.delta = (float*)(ws + at);
+  at += round_up((size_t)a.rows * a.Hq * sizeof(float));
+  b.peak = (float*)(ws + at);
+  at += round_up(DELTA_BLOCKS * sizeof(float));
+  b.part = (float*)(ws + at);
+  at += (size_t)a.S * a.Hkv * (b.chunks + 1) * 2 * b.sinks * a.h * sizeof(float);
+  return at;
+}
+
+template <class T, int HD>
+hipError_t launch(const Backward& b, hipStream_t s) {
+  const WindowArgs& a = b.a;
+  const long long units = (long long)a.S * a.Hkv;
+  const int key_tiles = (a.max_new + BM - 1) / BM, jobs = key_tiles + (b.sinks + BM - 1) / BM * b.chunks;
+  hipLaunchKernelGGL((delta_kernel<T>), dim3(DELTA_BLOCKS), dim3(TPB), 0, s, b);
+  hipLaunchKernelGGL((keys_backward_kernel<T, HD>), dim3(mapped_blocks(units, jobs)), dim3(TPB), 0, s, b, key_tiles, jobs);
+  if (b.sinks > 0) {
+    const int per = (2 * b.sinks * (a.h / 4) + TPB - 1) / TPB;
+    hipLaunchKernelGGL((sink_sum_kernel<T>), dim3((unsigned)units, per < 64 ? per : 64), dim3(TPB), 0, s, b);
+  }
+  const int tiles = (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
+  hipLaunchKernelGGL((queries_backward_kernel<T, HD>), dim3(mapped_blocks(units, tiles)), dim3(TPB), 0, s, b, tiles);
+  return hipGetLastError();
+}
+template <class T>
+hipError_t by_head(const Backward& b, hipStream_t s) {
+  const int h = b.a.h;
+  if (h <= 32) return launch<T, 32>(b, s);
+  if (h <= 64) return launch<T, 64>(b, s);
+  if (h <= 80) return launch<T, 80>(b, s);
+  if (h <= 96) return launch<T, 96>(b, s);
+  if (h <= 128) return launch<T, 128>(b, s);
+  return launch<T, 256>(b, s);
+}
+
+}  // namespace
+
+size_t rl_window_backward_bytes(const WindowArgs& a) {
+  Backward b;
+  b.a = a;
+  part_sinks(b);
+  return place(b, nullptr);
+}
+hipError_t rl_window_backward(const WindowArgs& a, hipStream_t s) {
+  if (a.rows <= 0) return hipSuccess;
+  Backward b;
+  b.a = a;
+  part_sinks(b);
+  place(b, (char*)a.ws);
+  return a.dtype == RLGEN_DTYPE_F16 ? by_head<TypeF16>(b, s) : by_head<TypeBf16>(b, s);
+}

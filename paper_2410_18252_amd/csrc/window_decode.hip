@@ -1,0 +1,335 @@
+// Windowed attention of single tokens over the paged cache: the bandwidth-bound step of serving.
+//
+// One wave takes 32 keys of one kv head at a time, the query heads of its group in the columns of 16x16x32 matrix instructions:
+//   S^T[key, col] = K q^T          a lane reads 16 bytes of a key: the fragment as it lies in the page
+//   O^T[dim, col] += V^T P^T       a lane reads the same eight (four) dims of eight keys; their words change places in registers, which
+//                                  gives the fragments of V^T without a pass through LDS
+// The scores leave the first product where the second wants its probabilities (key 8 g + 4 t + j in lane group g).  Visible keys are two
+// runs, sinks and window, so a step's cost follows the window.  Eight keys in a row share a page, so a lane looks up two pages for
+// 32 keys, one iteration before it needs them; the next 32 keys are requested before the present ones are used.
+// Values that are not seen are zeroed, not multiplied by zero.
+#include "../../include/rlgen.h"
+#include "window_tiles.h"
+
+namespace {
+
+constexpr int TPB = 256;
+
+struct Part { float m, l; };
+
+// JW waves share a job (a sequence's kv head and up to CB of its query heads), each taking every JW-th group of 32 keys; the
+// maxima, sums and outputs meet in LDS.  PARTS: several blocks share it as well and leave their share for window_join_kernel.
+template <class T, int HD, int JW>
+__global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void window_decode_kernel(WindowArgs a, int parts, int col_blocks) {
+  typedef typename T::vec8 vec8;
+  constexpr int KS = (HD + 31) / 32, VW = HD > 64 ? 8 : 4, CH = HD > 128 ? 2 : 1, CB = HD > 128 ? 8 : 16;
+  extern __shared__ float joined[];            // JW > 1: [JW][columns][h]
+  __shared__ Part part_of[4][16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  const int G = a.Hq / a.Hkv;
+  long long job = JW > 1 ? blockIdx.x : (long long)blockIdx.x * 4 + wave;
+  const int part = (int)(job % parts);
+  job /= parts;
+  if (job >= (long long)a.S * a.Hkv * col_blocks) return;
+  const int cb = (int)(job % col_blocks), kvh = (int)(job / col_blocks % a.Hkv), s = (int)(job / col_blocks / a.Hkv);
+  const Seq q = load_seq(a, s, true);
+  if (q.n < 1) return;
+  const int cols = min(G - cb * CB, CB), head0 = kvh * G + cb * CB;
+  const int pos = q.ctx, key_end = min(pos + 1, q.total);
+  const int w_lo = a.window ? max(pos - a.window + 1, 0) : 0;
+  const int sink_groups = (max(min(min(a.sinks, w_lo), key_end), 0) + 31) >> 5;
+  const int w_base = max(w_lo & ~7, sink_groups * 32);
+  const int groups = sink_groups + (key_end > w_base ? (key_end - w_base + 31) >> 5 : 0);
+  auto group_key = [&](int i) { return i < sink_groups ? i * 32 : w_base + (i - sink_groups) * 32; };
+  const int i0 = (int)((long long)groups * part / parts) + (JW > 1 ? wave : 0), i1 = (int)((long long)groups * (part + 1) / parts);
+
+  vec8 qf[KS];
+  {
+    const uint16_t* qp = (const uint16_t*)a.q + (long long)q.row0 * a.q_stride + (long long)(head0 + min(c, cols - 1)) * a.h;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const int d = 32 * i + 8 * g;
+      qf[i] = d < a.h ? *(const vec8*)(qp + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
+    }
+  }
+  const int last8 = (key_end - 1) & ~7, in_page = (1 << a.page_shift) - 1;
+  const int* table = a.page_table + (size_t)s * a.table_stride;
+  const long long plane = ((long long)a.Hkv << a.page_shift) * a.h;      // from a page's keys to its values
+  auto key8 = [&](int i, int quad) { return min(group_key(i) + 8 * quad, last8); };
+  auto lookup = [&](int i, int& pk, int& pv) {
+    pk = table[key8(i, c >> 2) >> a.page_shift];
+    pv = table[key8(i, g) >> a.page_shift];
+  };
+  auto page_row = [&](int page, int key) {            // (an entry outside the cache is not followed)
+    const unsigned p = (unsigned)page < (unsigned)a.n_pages ? page : 0;
+    return (const uint16_t*)a.pages + ((((long long)p * 2 * a.Hkv + kvh) << a.page_shift) + (key & in_page)) * a.h;
+  };
+  typedef uint32_t vraw_t __attribute__((ext_vector_type(VW / 2)));
+  auto load = [&](int i, int pk, int pv, u32x4 (&k)[2][KS], vraw_t (&v)[CH][8]) {
+    const uint16_t* kp = page_row(pk, key8(i, c >> 2)) + (c & 3) * a.h + 8 * g;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < KS; ++j) {
+        if (32 * j + 8 * g < a.h) k[t][j] = __builtin_nontemporal_load((const u32x4*)(kp + 4 * t * a.h + 32 * j));
+        else k[t][j] = u32x4{0, 0, 0, 0};
+      }
+    const uint16_t* vp = page_row(pv, key8(i, g)) + plane + VW * c;
+#pragma unroll
+    for (int x = 0; x < CH; ++x)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (128 * x + VW * c < a.h) v[x][e] = __builtin_nontemporal_load((const vraw_t*)(vp + e * a.h + 128 * x));
+        else
+#pragma unroll
+          for (int w = 0; w < VW / 2; ++w) v[x][e][w] = 0;
+  };
+
+  f32x4 o[CH][VW];
+#pragma unroll
+  for (int x = 0; x < CH; ++x)
+#pragma unroll
+    for (int e = 0; e < VW; ++e) o[x][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float mx = -INFINITY, sum = 0.f;
+  const float scale2 = a.scale * 1.4426950408889634f;
+  u32x4 k[2][KS], k_next[2][KS];
+  vraw_t v[CH][8], v_next[CH][8];
+  int pk, pv;
+  if (i0 < i1) {
+    lookup(i0, pk, pv);
+    load(i0, pk, pv, k, v);
+    lookup(min(i0 + JW, i1 - 1), pk, pv);
+  }
+  for (int i = i0; i < i1; i += JW) {
+    if (i + JW < i1) {
+      load(i + JW, pk, pv, k_next, v_next);
+      lookup(min(i + 2 * JW, i1 - 1), pk, pv);
+    }
+    const int kb = group_key(i);
+    f32x4 sc[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      sc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < KS; ++j) sc[t] = T::mfma16(__builtin_bit_cast(vec8, k[t][j]), qf[j], sc[t]);
+    }
+    const int key0 = kb + 8 * g;
+    if (kb + 31 >= key_end || (kb < w_lo && kb + 31 >= a.sinks)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int key = key0 + e;
+        // (selections, not a branch: of a branch that writes single elements of these vectors the compiler lost one)
+        const bool seen = (key < key_end) & ((key >= w_lo) | (key < a.sinks));
+        const uint32_t keep = seen ? 0xffffffffu : 0u;
+        sc[e >> 2][e & 3] = seen ? sc[e >> 2][e & 3] : -INFINITY;
+#pragma unroll
+        for (int x = 0; x < CH; ++x)
+#pragma unroll
+          for (int w = 0; w < VW / 2; ++w) v[x][e][w] &= keep;
+      }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, sc[e >> 2][e & 3]);
+    top = fmaxf(top, __shfl_xor(top, 16, WAVE));
+    top = fmaxf(top, __shfl_xor(top, 32, WAVE)) * scale2;
+    const float now = fmaxf(mx, top), base = now == -INFINITY ? 0.f : now;
+    if (__any(now > mx)) {
+      const float shrink = __builtin_amdgcn_exp2f(mx - base);
+      sum *= shrink;
+#pragma unroll
+      for (int x = 0; x < CH; ++x)
+#pragma unroll
+        for (int e = 0; e < VW; ++e) o[x][e] *= shrink;
+    }
+    mx = now;
+    float p[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(fmaf(sc[e >> 2][e & 3], scale2, -base));
+      sum += p[e];
+    }
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = T::pack(p[2 * e], p[2 * e + 1]);
+    const vec8 pf = __builtin_bit_cast(vec8, w);
+#pragma unroll
+    for (int x = 0; x < CH; ++x)
+#pragma unroll
+      for (int e = 0; e < VW; ++e) {
+        u32x4 f;                                   // dim VW c + e of the eight keys
+#pragma unroll
+        for (int y = 0; y < 4; ++y) f[y] = __builtin_amdgcn_perm(v[x][2 * y + 1][e >> 1], v[x][2 * y][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+        o[x][e] = T::mfma16(__builtin_bit_cast(vec8, f), pf, o[x][e]);
+      }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < KS; ++j) k[t][j] = k_next[t][j];
+#pragma unroll
+    for (int x = 0; x < CH; ++x)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[x][e] = v_next[x][e];
+  }
+  sum += __shfl_xor(sum, 16, WAVE);
+  sum += __shfl_xor(sum, 32, WAVE);
+  // lane (c, g) holds of column c the dims VW (4 g + j) + e, j = 0..3
+  const long long row = q.row0;
+  if constexpr (JW == 1) {
+    if (c >= cols) return;
+    const float inv = sum > 0.f ? 1.0f / sum : (sum == 0.f ? 0.f : sum);
+    const int head = head0 + c;
+    if (a.lse && g == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+    uint16_t* op = (uint16_t*)a.out + row * a.out_stride + (long long)head * a.h;
+#pragma unroll
+    for (int x = 0; x < CH; ++x)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int d = 128 * x + VW * (4 * g + j);
+        if (d >= a.h) continue;
+        vraw_t y;
+#pragma unroll
+        for (int e = 0; e < VW / 2; ++e) y[e] = T::pack(o[x][2 * e][j] * inv, o[x][2 * e + 1][j] * inv);
+        *(vraw_t*)(op + d) = y;
+      }
+    return;
+  } else {
+    if (g == 0) part_of[wave][c] = Part{mx, sum};
+    if (c < cols) {
+      float* mine = joined + ((size_t)wave * cols + c) * a.h;
+#pragma unroll
+      for (int x = 0; x < CH; ++x)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int d = 128 * x + VW * (4 * g + j);
+          if (d >= a.h) continue;
+#pragma unroll
+          for (int e = 0; e < VW; ++e) mine[d + e] = o[x][e][j];
+        }
+    }
+    __syncthreads();
+    float* po = (float*)a.ws;                                            // partial outputs, then their maxima and sums
+    Part* pm = (Part*)(po + (long long)a.S * a.Hq * parts * a.h);
+    for (int at = threadIdx.x * 2; at < cols * a.h; at += TPB * 2) {
+      const int col = at / a.h, d = at - col * a.h;
+      float m = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < JW; ++w) m = fmaxf(m, part_of[w][col].m);
+      const float base = m == -INFINITY ? 0.f : m;
+      float l = 0.f, y0 = 0.f, y1 = 0.f;
+#pragma unroll
+      for (int w = 0; w < JW; ++w) {
+        const float f = __builtin_amdgcn_exp2f(part_of[w][col].m - base);
+        l = fmaf(part_of[w][col].l, f, l);
+        y0 = fmaf(joined[((size_t)w * cols + col) * a.h + d], f, y0);
+        y1 = fmaf(joined[((size_t)w * cols + col) * a.h + d + 1], f, y1);
+      }
+      const int head = head0 + col;
+      if (parts > 1) {
+        const long long slot = ((long long)s * a.Hq + head) * parts + part;
+        *(float2*)(po + slot * a.h + d) = make_float2(y0, y1);
+        if (d == 0) pm[slot] = Part{m, l};
+      } else {
+        const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
+        *(uint32_t*)((uint16_t*)a.out + row * a.out_stride + (long long)head * a.h + d) = T::pack(y0 * inv, y1 * inv);
+        if (d == 0 && a.lse) a.lse[row * a.Hq + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+      }
+    }
+  }
+}
+
+// Adds up the parts of a query head, in their order: 64 lanes along the dims, the four waves a part each in turn.
+template <class T>
+__global__ __launch_bounds__(TPB) void window_join_kernel(WindowArgs a, int parts) {
+  __shared__ float part_sum[4][256];
+  __shared__ float weight_sum[4];
+  const int s = blockIdx.x / a.Hq, head = blockIdx.x - s * a.Hq;
+  const Seq q = load_seq(a, s, true);
+  if (q.n < 1) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float* po = (const float*)a.ws;
+  const Part* pm = (const Part*)(po + (long long)a.S * a.Hq * parts * a.h);
+  const long long slot = ((long long)s * a.Hq + head) * parts;
+  float m = -INFINITY;
+  for (int p = lane; p < parts; p += 64) m = fmaxf(m, pm[slot + p].m);
+  m = wave_max(m);
+  const float base = m == -INFINITY ? 0.f : m;
+  float y[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
+  for (int p = wave; p < parts; p += 4) {
+    const float f = __builtin_amdgcn_exp2f(pm[slot + p].m - base);
+    l = fmaf(pm[slot + p].l, f, l);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (lane + 64 * e < a.h) y[e] = fmaf(po[(slot + p) * a.h + lane + 64 * e], f, y[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) part_sum[wave][lane + 64 * e] = y[e];
+  if (lane == 0) weight_sum[wave] = l;
+  __syncthreads();
+  l = weight_sum[0] + weight_sum[1] + weight_sum[2] + weight_sum[3];
+  const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
+  const int d = threadIdx.x * 2;
+  if (d < a.h) {
+    float v[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) v[e] = (part_sum[0][d + e] + part_sum[1][d + e] + part_sum[2][d + e] + part_sum[3][d + e]) * inv;
+    *(uint32_t*)((uint16_t*)a.out + (long long)q.row0 * a.out_stride + (long long)head * a.h + d) = T::pack(v[0], v[1]);
+  }
+  if (threadIdx.x == 0 && a.lse) a.lse[(long long)q.row0 * a.Hq + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+// Waves to a job and blocks to a job
+struct Split { int waves, parts, col_blocks; };
+Split decode_split(const WindowArgs& a) {
+  const int G = a.Hq / a.Hkv, cb = a.h > 128 ? 8 : 16;
+  Split r{1, 1, (G + cb - 1) / cb};
+  const long long jobs = (long long)a.S * a.Hkv * r.col_blocks;
+  long long seen = a.max_total;
+  if (a.window && (long long)a.window + a.sinks < seen) seen = (long long)a.window + a.sinks;
+  const long long groups = (seen + 31) / 32;
+  if (jobs >= 2048 || groups < 2) return r;
+  r.waves = 4;
+  long long parts = (512 + jobs - 1) / jobs, most = (groups + 7) / 8;
+  if (parts > most) parts = most;
+  if (parts > 64) parts = 64;
+  r.parts = parts < 1 ? 1 : (int)parts;
+  return r;
+}
+
+template <class T, int HD>
+hipError_t launch(const WindowArgs& a, hipStream_t s) {
+  const Split r = decode_split(a);
+  const long long jobs = (long long)a.S * a.Hkv * r.col_blocks * r.parts;
+  const int G = a.Hq / a.Hkv, cb = HD > 128 ? 8 : 16;
+  if (r.waves == 1) {
+    hipLaunchKernelGGL((window_decode_kernel<T, HD, 1>), dim3((unsigned)((jobs + 3) / 4)), dim3(TPB), 0, s, a, r.parts, r.col_blocks);
+  } else {
+    const size_t lds = (size_t)4 * (G < cb ? G : cb) * a.h * sizeof(float);
+    hipLaunchKernelGGL((window_decode_kernel<T, HD, 4>), dim3((unsigned)jobs), dim3(TPB), lds, s, a, r.parts, r.col_blocks);
+    if (r.parts > 1) {
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL((window_join_kernel<T>), dim3((unsigned)(a.S * a.Hq)), dim3(TPB), 0, s, a, r.parts);
+    }
+  }
+  return hipGetLastError();
+}
+template <class T>
+hipError_t by_head(const WindowArgs& a, hipStream_t s) {
+  if (a.h <= 64) return launch<T, 64>(a, s);
+  if (a.h <= 96) return launch<T, 96>(a, s);
+  if (a.h <= 128) return launch<T, 128>(a, s);
+  return launch<T, 256>(a, s);
+}
+
+}  // namespace
+
+size_t rl_window_decode_bytes(const WindowArgs& a) {
+  const Split r = decode_split(a);
+  return r.parts > 1 ? (size_t)a.S * a.Hq * r.parts * ((size_t)a.h * sizeof(float) + sizeof(Part)) : 0;
+}
+hipError_t rl_window_decode(const WindowArgs& a, hipStream_t s) {
+  if (a.rows <= 0) return hipSuccess;
+  return a.dtype == RLGEN_DTYPE_F16 ? by_head<TypeF16>(a, s) : by_head<TypeBf16>(a, s);
+}

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Dict, Optional
+from typing import Dict, NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -22,14 +22,18 @@ lib = C.CDLL(LIB_PATH)
 OK = 0
 ERR_NULL, ERR_BAD_CFG, ERR_BAD_ARG, ERR_CAPACITY, ERR_WORKSPACE, ERR_UNIMPLEMENTED, ERR_DEVICE = -1, -2, -3, -4, -5, -6, -7
 ARCH_NEOX, ARCH_LLAMA = 0, 1
-DTYPE_F32, DTYPE_BF16 = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
 
 EXPORTS = ["rlgen_workspace_bytes", "rlgen_create", "rlgen_update_weights", "rlgen_generate", "rlgen_score",
            "rlgen_debug_logits", "rlgen_debug_sample", "rlgen_sample_static", "rlgen_sequence_logprob", "rlgen_dpo_loss", "rlgen_select_pairs", "rlgen_proximal_rloo",
            "rlgen_get_timings", "rlgen_set_profiling", "rlgen_set_decode_split", "rlgen_set_decode_split_min", "rlgen_set_eos",
            "rlgen_set_eos_compaction", "rlgen_set_score_groups", "rlgen_debug_get_gemm", "rlgen_debug_set_gemm", "rlgen_status",
-           "rlgen_status_bits", "rlgen_strerror", "rlgen_destroy"]
+           "rlgen_status_bits", "rlgen_strerror", "rlgen_destroy", "rlgen_plan_pages", "rlgen_rope_table", "rlgen_qk_norm_rope",
+           "rlgen_qk_norm_rope_backward", "rlgen_qk_norm_rope_backward_workspace", "rlgen_window_attention",
+           "rlgen_window_attention_backward", "rlgen_window_attention_backward_workspace", "rlgen_window_attention_paged",
+           "rlgen_window_attention_paged_workspace"]
 FAULT_TOKEN, FAULT_UNIFORM, FAULT_GROUP, FAULT_RANGE = 1, 2, 4, 8
+PLAN_ROWS, PLAN_PAGES, PLAN_TABLE, PLAN_LENGTH = 1, 2, 4, 8
 
 
 class ModelCfg(C.Structure):
@@ -54,7 +58,7 @@ class Weights(C.Structure):
                 ("lm_head", C.c_void_p), ("layers", C.POINTER(LayerWeights))]
 
 
-_vp, _i32, _f32 = C.c_void_p, C.c_int32, C.c_float
+_vp, _i32, _f32, _i64, _size = C.c_void_p, C.c_int32, C.c_float, C.c_int64, C.c_size_t
 lib.rlgen_workspace_bytes.restype = C.c_size_t
 lib.rlgen_workspace_bytes.argtypes = [C.POINTER(ModelCfg)]
 lib.rlgen_create.restype = C.c_int
@@ -103,6 +107,20 @@ lib.rlgen_debug_set_gemm.restype = C.c_int
 lib.rlgen_debug_set_gemm.argtypes = [_vp, _i32, _i32, _i32]
 lib.rlgen_strerror.restype = C.c_char_p
 lib.rlgen_strerror.argtypes = [C.c_int]
+_NORM_ROPE = [_vp, _i64, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _f32, _vp, _i32, _i32, _vp, _i32]
+_ROWS = [_vp, _i64]
+for _name, _types in {
+        "rlgen_plan_pages": [_vp, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp],
+        "rlgen_rope_table": [_vp, _i32, _i32, _f32, _vp],
+        "rlgen_qk_norm_rope": _NORM_ROPE + 3 * _ROWS + [_vp, _i32, _i32, _vp, _vp],
+        "rlgen_qk_norm_rope_backward": _NORM_ROPE + 4 * _ROWS + [_vp, _vp, _vp, _size, _vp],
+        "rlgen_window_attention": 3 * _ROWS + [_i32] * 5 + [_vp] + [_i32] * 4 + [_f32] + _ROWS + [_vp, _vp],
+        "rlgen_window_attention_backward": 4 * _ROWS + [_vp] + _ROWS + [_i32] * 5 + [_vp] + [_i32] * 4 + [_f32] + 3 * _ROWS + [_vp, _size, _vp],
+        "rlgen_window_attention_paged": _ROWS + [_i32] * 5 + [_vp, _i32, _i32, _vp, _i32, _vp, _vp] + [_i32] * 5 + [_f32] + _ROWS + [_vp, _vp, _size, _vp]}.items():
+    getattr(lib, _name).restype, getattr(lib, _name).argtypes = C.c_int, _types
+for _name, _count in {"rlgen_qk_norm_rope_backward_workspace": 2, "rlgen_window_attention_backward_workspace": 8,
+                      "rlgen_window_attention_paged_workspace": 8}.items():
+    getattr(lib, _name).restype, getattr(lib, _name).argtypes = _size, [_i32] * _count
 lib.rlgen_destroy.restype = None
 lib.rlgen_destroy.argtypes = [_vp]
 
@@ -372,3 +390,176 @@ def rlgen_debug_get_gemm(p: Policy, mode: int, which: int):
 
 def rlgen_debug_set_gemm(p: Policy, mode: int, which: int, variant: int):
     _check(lib.rlgen_debug_set_gemm(p.ctx, mode, which, int(variant)), "rlgen_debug_set_gemm")
+
+
+# ------------------------------------------------------------------ operators over a cache in pages and packed rows
+_DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
+
+
+def _heads(t: torch.Tensor, dtype: torch.dtype):
+    """[rows, heads, head_dim] with heads and head_dim contiguous: (address, row stride)."""
+    assert t.dim() == 3 and t.dtype == dtype and t.is_cuda and t.stride(2) == 1 and (t.stride(1) == t.shape[2] or t.shape[1] == 1)
+    # (the row stride of a tensor of one row or none means nothing)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _ints(t: torch.Tensor, *shape):
+    assert t.dtype == torch.int32 and t.is_cuda and t.is_contiguous() and tuple(t.shape) == shape
+    return t.data_ptr()
+
+
+class PagePlan(NamedTuple):
+    """What rlgen_plan_pages fills, all int32 on the device: total_lens [S], row_starts [S + 1], slots and positions [max_rows],
+    counts [4] (rows, the free list's next head, longest length, PLAN_* bits)."""
+    total_lens: torch.Tensor
+    row_starts: torch.Tensor
+    slots: torch.Tensor
+    positions: torch.Tensor
+    counts: torch.Tensor
+
+
+def rlgen_plan_pages(ctx_lens: torch.Tensor, new_lens: torch.Tensor, page_size: int, free_pages: torch.Tensor, page_table: torch.Tensor,
+                     max_rows: int, free_head: Optional[torch.Tensor] = None, out=None) -> PagePlan:
+    """ctx_lens, new_lens [S], free_pages [n], page_table [S, pages of a sequence] (in and out), free_head [1] or None: int32 on the
+    device.  `out`: a PagePlan (or tuple) of tensors to fill."""
+    S, stride = page_table.shape
+    if out is None:
+        buf = ctx_lens.new_empty(2 * S + 5 + 2 * max_rows)
+        out = torch.split(buf, [S, S + 1, max_rows, max_rows, 4])
+    plan = PagePlan(*out)
+    _check(lib.rlgen_plan_pages(_ints(ctx_lens, S), _ints(new_lens, S), S, page_size, _ints(free_pages, free_pages.numel()), free_pages.numel(),
+                                None if free_head is None else _ints(free_head, 1), _ints(page_table, S, stride), stride, max_rows,
+                                _ints(plan.total_lens, S), _ints(plan.row_starts, S + 1), _ints(plan.slots, max_rows),
+                                _ints(plan.positions, max_rows), _ints(plan.counts, 4), _stream()), "rlgen_plan_pages")
+    return plan
+
+
+def rlgen_rope_table(max_pos: int, rotary_dim: int, theta: float, device="cuda") -> torch.Tensor:
+    """[max_pos, rotary_dim / 2, 2] fp32: cos and sin."""
+    table = torch.empty((max_pos, rotary_dim // 2, 2), dtype=torch.float32, device=device)
+    _check(lib.rlgen_rope_table(_ptr(table), max_pos, rotary_dim, theta, _stream()), "rlgen_rope_table")
+    return table
+
+
+def _norm_rope_args(qkv, q_gain, k_gain, eps, rope, positions, n_q, n_kv, dtype):
+    h, rows = q_gain.numel(), qkv.shape[0]
+    assert qkv.dim() == 2 and qkv.is_cuda and qkv.stride(1) == 1 and qkv.shape[1] == (n_q + 2 * n_kv) * h
+    for t in (q_gain, k_gain):
+        assert t.dtype == torch.float32 and t.is_contiguous() and t.numel() == h
+    max_pos, r = 1, 0
+    if rope is not None:
+        assert rope.dtype == torch.float32 and rope.is_contiguous() and rope.dim() == 3 and rope.shape[2] == 2
+        max_pos, r = rope.shape[0], 2 * rope.shape[1]
+    stride = qkv.stride(0) if rows > 1 else qkv.shape[1]
+    return (qkv.data_ptr(), stride, _DTYPES[qkv.dtype], rows, n_q, n_kv, h, q_gain.data_ptr(), k_gain.data_ptr(), eps, _ptr(rope), max_pos, r,
+            _ints(positions, rows), _DTYPES[dtype])
+
+
+def _pages(pages: torch.Tensor, n_kv: int, h: int):
+    assert pages.is_cuda and pages.is_contiguous() and pages.dim() == 5 and pages.shape[1:3] == (2, n_kv) and pages.shape[4] == h
+    return pages.data_ptr(), pages.shape[0], pages.shape[3]
+
+
+def rlgen_qk_norm_rope(qkv: torch.Tensor, q_gain: torch.Tensor, k_gain: torch.Tensor, eps: float, rope: Optional[torch.Tensor],
+                       positions: torch.Tensor, pages: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
+                       n_kv_heads: Optional[int] = None, dtype: Optional[torch.dtype] = None, out=None):
+    """qkv [rows, (n_q + 2 n_kv) h] (fp32, bf16 or fp16; any row stride) -> q [rows, n_q, h].  With `pages` [n, 2, n_kv, page_size, h] keys and
+    values go to slots [rows] of them and q is returned; without, n_kv_heads says how many there are and (q, k, v) of `dtype` (default
+    qkv's) are returned.  `out`: q, or (q, k, v), to write into."""
+    h = q_gain.numel()
+    n_kv = pages.shape[2] if pages is not None else n_kv_heads
+    n_q = qkv.shape[1] // h - 2 * n_kv
+    rows = qkv.shape[0]
+    if pages is not None:
+        dtype = pages.dtype
+        q, k, v = (torch.empty((rows, n_q, h), dtype=dtype, device=qkv.device) if out is None else out), None, None
+        where = (*_pages(pages, n_kv, h), _ints(slots, rows))
+        rest = (None, 0, None, 0)
+    else:
+        dtype = qkv.dtype if dtype is None else dtype
+        q, k, v = out if out is not None else (torch.empty((rows, n, h), dtype=dtype, device=qkv.device) for n in (n_q, n_kv, n_kv))
+        assert k.shape == v.shape == (rows, n_kv, h)
+        where = (None, 0, 0, None)
+        rest = (*_heads(k, dtype), *_heads(v, dtype))
+    assert q.shape == (rows, n_q, h)
+    _check(lib.rlgen_qk_norm_rope(*_norm_rope_args(qkv, q_gain, k_gain, eps, rope, positions, n_q, n_kv, dtype), *_heads(q, dtype), *rest, *where,
+                                  _stream()), "rlgen_qk_norm_rope")
+    return q if pages is not None else (q, k, v)
+
+
+def rlgen_qk_norm_rope_backward(qkv, q_gain, k_gain, eps: float, rope, positions, dq, dk, dv, out=None, workspace=None):
+    """dq [rows, n_q, h], dk and dv [rows, n_kv, h] -> (dqkv like qkv, dq_gain [h], dk_gain [h])."""
+    rows, n_q, h = dq.shape
+    n_kv = dk.shape[1]
+    assert dk.shape == dv.shape == (rows, n_kv, h)
+    if out is None:
+        out = (torch.empty((rows, qkv.shape[1]), dtype=qkv.dtype, device=qkv.device), torch.empty_like(q_gain), torch.empty_like(k_gain))
+    dqkv, dqg, dkg = out
+    assert dqkv.dtype == qkv.dtype and dqkv.shape == qkv.shape and dqkv.stride(1) == 1
+    for t in (dqg, dkg):
+        assert t.dtype == torch.float32 and t.is_contiguous() and t.numel() == h
+    need = lib.rlgen_qk_norm_rope_backward_workspace(rows, h)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=qkv.device)
+    _check(lib.rlgen_qk_norm_rope_backward(*_norm_rope_args(qkv, q_gain, k_gain, eps, rope, positions, n_q, n_kv, dq.dtype), *_heads(dq, dq.dtype),
+                                           *_heads(dk, dq.dtype), *_heads(dv, dq.dtype), dqkv.data_ptr(), dqkv.stride(0) if rows > 1 else dqkv.shape[1],
+                                           dqg.data_ptr(), dkg.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()),
+           "rlgen_qk_norm_rope_backward")
+    return dqkv, dqg, dkg
+
+
+def rlgen_window_attention(q, k, v, row_starts, max_len: int, window: int, sinks: int, scale: float, out=None):
+    """Packed rows: q [rows, n_q, h], k and v [rows, n_kv, h] (any row stride), row_starts [S + 1] int32.  Returns (out [rows, n_q, h],
+    lse [rows, n_q] fp32); `out`: the two to write into."""
+    rows, n_q, h = q.shape
+    n_kv, dt = k.shape[1], q.dtype
+    assert k.shape == v.shape == (rows, n_kv, h)
+    o, lse = out if out is not None else (torch.empty((rows, n_q, h), dtype=dt, device=q.device),
+                                          torch.empty((rows, n_q), dtype=torch.float32, device=q.device))
+    assert o.shape == q.shape and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (rows, n_q)
+    S = row_starts.numel() - 1
+    _check(lib.rlgen_window_attention(*_heads(q, dt), *_heads(k, dt), *_heads(v, dt), _DTYPES[dt], rows, n_q, n_kv, h, _ints(row_starts, S + 1), S,
+                                      max_len, window, sinks, scale, *_heads(o, dt), lse.data_ptr(), _stream()), "rlgen_window_attention")
+    return o, lse
+
+
+def rlgen_window_attention_backward(q, k, v, out, lse, dout, row_starts, max_len: int, window: int, sinks: int, scale: float, grads=None,
+                                    workspace=None):
+    """From rlgen_window_attention's inputs, its (out, lse) and dout: (dq, dk, dv).  `grads`: the three to write into."""
+    rows, n_q, h = q.shape
+    n_kv, dt = k.shape[1], q.dtype
+    assert k.shape == v.shape == (rows, n_kv, h) and out.shape == dout.shape == q.shape
+    assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (rows, n_q)
+    dq, dk, dv = grads if grads is not None else (torch.empty((rows, n, h), dtype=dt, device=q.device) for n in (n_q, n_kv, n_kv))
+    assert dq.shape == q.shape and dk.shape == dv.shape == k.shape
+    S = row_starts.numel() - 1
+    need = lib.rlgen_window_attention_backward_workspace(rows, n_q, n_kv, h, S, max_len, window, sinks)
+    if workspace is None:
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+    _check(lib.rlgen_window_attention_backward(*_heads(q, dt), *_heads(k, dt), *_heads(v, dt), *_heads(out, dt), lse.data_ptr(), *_heads(dout, dt),
+                                               _DTYPES[dt], rows, n_q, n_kv, h, _ints(row_starts, S + 1), S, max_len, window, sinks, scale,
+                                               *_heads(dq, dt), *_heads(dk, dt), *_heads(dv, dt), workspace.data_ptr(),
+                                               workspace.numel() * workspace.element_size(), _stream()), "rlgen_window_attention_backward")
+    return dq, dk, dv
+
+
+def rlgen_window_attention_paged(q, pages, page_table, row_starts, total_lens, max_new: int, max_total: int, window: int, sinks: int,
+                                 scale: float, out=None, workspace=None):
+    """q [rows, n_q, h]: the last row_starts[s + 1] - row_starts[s] of the total_lens[s] tokens that the cache holds of each sequence.
+    Returns (out [rows, n_q, h], lse [rows, n_q] fp32); max_new == 1 is a decode step."""
+    rows, n_q, h = q.shape
+    n_kv, dt = pages.shape[2], q.dtype
+    assert pages.dtype == dt
+    S, stride = page_table.shape
+    o, lse = out if out is not None else (torch.empty((rows, n_q, h), dtype=dt, device=q.device),
+                                          torch.empty((rows, n_q), dtype=torch.float32, device=q.device))
+    assert o.shape == q.shape and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (rows, n_q)
+    need = lib.rlgen_window_attention_paged_workspace(n_q, n_kv, h, S, max_new, max_total, window, sinks)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(lib.rlgen_window_attention_paged(*_heads(q, dt), _DTYPES[dt], rows, n_q, n_kv, h, *_pages(pages, n_kv, h), _ints(page_table, S, stride), stride,
+                                            _ints(row_starts, S + 1), _ints(total_lens, S), S, max_new, max_total, window, sinks, scale,
+                                            *_heads(o, dt), lse.data_ptr(), _ptr(workspace),
+                                            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()),
+           "rlgen_window_attention_paged")
+    return o, lse
