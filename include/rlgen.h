@@ -307,8 +307,8 @@ int rlgen_status_bits(rlgen_ctx *ctx, void *hip_stream, uint32_t *faults);
  *
  * Layouts
  *  - Packed rows: the tokens of S sequences one behind the other; row_starts [S + 1] int32 holds the first row of each and the number
- *    of rows.  A tensor [rows, heads, head_dim] has head_dim and heads contiguous and any row stride (in elements) that is a multiple of
- *    8, so a column range of a fused projection's output can be passed as it is.  All bases 16-byte aligned.
+ *    of rows.  A tensor [rows, heads, head_dim] has head_dim and heads contiguous and any row stride (in elements) up to 2^23 that is a
+ *    multiple of 8, so a column range of a fused projection's output can be passed as it is.  All bases 16-byte aligned.
  *  - Cache: pages [n_pages, 2, n_kv_heads, page_size, head_dim]: of a page's tokens first the keys, then the values.  page_size is a power
  *    of two from 8 to 1024.  Sequence s has its token t in page page_table[s * table_stride + t / page_size].  A slot is
  *    page * page_size + t % page_size.

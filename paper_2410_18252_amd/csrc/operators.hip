@@ -21,7 +21,10 @@ bool heads_ok(int rows, int Hq, int Hkv, int h) {
          (int64_t)(Hq + 2ll * Hkv) * h <= INT32_MAX;
 }
 // rows of `heads` heads one behind the other, 16-byte loads
-bool rows_ok(const void* p, int64_t stride, int64_t heads, int h, int step = 8) { return aligned16(p) && stride >= heads * h && stride % step == 0; }
+constexpr int64_t MAX_STRIDE = 1 << 23;      // (64 rows of a tile lie within 32-bit offsets)
+bool rows_ok(const void* p, int64_t stride, int64_t heads, int h, int step = 8) {
+  return aligned16(p) && stride >= heads * h && stride % step == 0 && stride <= MAX_STRIDE;
+}
 bool pages_ok(const void* pages, int n_pages, int shift, int Hkv, int h) {
   return aligned16(pages) && n_pages >= 1 && shift >= 0 && ((int64_t)n_pages << shift) <= INT32_MAX && ((int64_t)Hkv << shift) * h <= INT32_MAX;
 }

@@ -75,13 +75,12 @@ __device__ void rows_key_by_key(const WindowArgs& a, const Seq& q, int s, int kv
   }
 }
 
-// Bound by the exp and the instructions around it as much as by the matrix cores.
 template <class T, int HD, bool PAGED>
-__global__ __launch_bounds__(TPB) void window_rows_kernel(WindowArgs a, int tiles) {
+__global__ __launch_bounds__(TPB, HD > 128 && PAGED ? 1 : 2) void window_rows_kernel(WindowArgs a, int tiles) {
   typedef typename T::vec8 vec8;
-  constexpr int BN = HD > 128 ? 32 : 64, SUB = BN / 32, KS = HD / 16, DT = (HD + 31) / 32, CPR = HD / 8;
-  constexpr int TILE = BN * HD, PIECES = BN * CPR / 64, PER = (PIECES + 3) / 4;      // pieces: requests of a kilobyte, dealt to the four waves
-  __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][TILE];
+  constexpr int BN = HD > 128 ? 32 : 64, SUB = BN / 32, KS = HD / 16, DT = (HD + 31) / 32, TILE = BN * HD;
+  typedef Pieces<HD, BN> P;
+  __shared__ __attribute__((aligned(256))) uint16_t lds[2][2][TILE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, g = lane >> 5;
   const int G = a.Hq / a.Hkv;
@@ -110,47 +109,48 @@ __global__ __launch_bounds__(TPB) void window_rows_kernel(WindowArgs a, int tile
 #pragma unroll
     for (int i = 0; i < KS; ++i) {
       const int d = 16 * i + 8 * g;
-      qf[i] = d < a.h ? *(const vec8*)(qp + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
+      qf[i] = signed_query(d < a.h ? *(const vec8*)(qp + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0}), a.scale);
     }
   }
 
-  // requests: piece n of a tile is 64 chunks, lane l the chunk 64 n + l of the tile as it lies in LDS
-  const uint16_t *kp = (const uint16_t*)a.k, *vp = (const uint16_t*)a.v;
-  int row_of[PER], chunk_of[PER];
-#pragma unroll
-  for (int n = 0; n < PER; ++n) {
-    const int at = (n * 4 + wave) * 64 + lane;
-    row_of[n] = at / CPR;
-    chunk_of[n] = ((at % CPR) ^ chunk_swap<HD>(row_of[n])) * 8;
-  }
   const int key_max = q.total - 1;
-  [[maybe_unused]] int page_of[PER];
+  [[maybe_unused]] P k_off, v_off;                                 // rows: a lane's offsets behind the tile's first row
+  [[maybe_unused]] int page_of[P::PER];                            // pages: of the tile that is requested next
+  if constexpr (!PAGED) {
+    k_off = piece_offsets<HD, BN>(wave, lane, a.k_stride, a.h);
+    v_off = piece_offsets<HD, BN>(wave, lane, a.v_stride, a.h);
+  }
   auto fetch_pages = [&](int t) {
     if constexpr (PAGED) {
 #pragma unroll
-      for (int n = 0; n < PER; ++n) page_of[n] = a.page_table[(size_t)s * a.table_stride + (min(tile_key(t) + row_of[n], key_max) >> a.page_shift)];
+      for (int n = 0; n < P::PER; ++n) {
+        int row, dim;
+        P::place(n, wave, lane, row, dim);
+        page_of[n] = a.page_table[(size_t)s * a.table_stride + (min(tile_key(t) + row, key_max) >> a.page_shift)];
+      }
     }
   };
   auto request = [&](int t, int buf) {
     const int base = tile_key(t);
+    if constexpr (PAGED) {
 #pragma unroll
-    for (int n = 0; n < PER; ++n) {
-      if (PIECES % 4 != 0 && n * 4 + wave >= PIECES) break;
-      const int key = min(base + row_of[n], key_max);
-      const uint16_t *ks, *vs;
-      if constexpr (PAGED) {
+      for (int n = 0; n < P::PER; ++n) {
+        if (P::ALL % 4 != 0 && n * 4 + wave >= P::ALL) break;
+        int row, dim;
+        P::place(n, wave, lane, row, dim);
+        const int key = min(base + row, key_max);                  // (rows past the last are masked)
         const unsigned page = (unsigned)page_of[n] < (unsigned)a.n_pages ? page_of[n] : 0;      // (an entry outside is not followed)
-        const long long row = (((long long)page * 2 * a.Hkv + kvh) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
-        ks = (const uint16_t*)a.pages + row * a.h + chunk_of[n];
-        vs = ks + ((long long)a.Hkv << a.page_shift) * a.h;
-      } else {
-        ks = kp + (long long)(q.row0 + key) * a.k_stride + (long long)kvh * a.h + chunk_of[n];
-        vs = vp + (long long)(q.row0 + key) * a.v_stride + (long long)kvh * a.h + chunk_of[n];
+        const long long at = (((long long)page * 2 * a.Hkv + kvh) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
+        const uint16_t* ks = (const uint16_t*)a.pages + at * a.h + dim;
+        const uint16_t* vs = ks + ((long long)a.Hkv << a.page_shift) * a.h;
+        if (dim >= a.h) ks = vs = (const uint16_t*)&zero_chunk;
+        const int to = (n * 4 + wave) * 512;
+        __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(lds[buf][0] + to), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(lds[buf][1] + to), 16, 0, 0);
       }
-      if (chunk_of[n] >= a.h) ks = vs = (const uint16_t*)&zero_chunk;
-      const int to = (n * 4 + wave) * 512;
-      __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(lds[buf][0] + to), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(lds[buf][1] + to), 16, 0, 0);
+    } else {
+      request_pieces<HD, BN>(rows_buffer(a.k, (long long)q.row0 + base, q.n - base, a.k_stride, kvh, a.h), k_off, lds[buf][0], wave);
+      request_pieces<HD, BN>(rows_buffer(a.v, (long long)q.row0 + base, q.n - base, a.v_stride, kvh, a.h), v_off, lds[buf][1], wave);
     }
   };
 
@@ -159,8 +159,15 @@ __global__ __launch_bounds__(TPB) void window_rows_kernel(WindowArgs a, int tile
   for (int t = 0; t < DT; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-  float mx = -INFINITY, sum = 0.f;             // of the scores times scale log2 e
-  const float scale2 = a.scale * 1.4426950408889634f;
+  // Of the scores times scale log2 e.  The maximum that the sums refer to follows the true one only when that is more than RISE ahead:
+  // probabilities up to 2^RISE keep the type's relative precision, and most tiles then rescale nothing.
+  constexpr float RISE = 8.f;
+  float mx = -INFINITY, sum = 0.f;
+  const float scale2 = score_factor(a.scale);
+  const lds_t k_base = lds_address(lds[0][0]) + row_base<HD>(lane);
+  ColumnBase<HD> v_base = column_base<HD>(lane);
+  v_base.all += lds_address(lds[0][1]);
+  v_base.last += lds_address(lds[0][1]);
   if (n_tiles > 0) {
     fetch_pages(0);
     request(0, 0);
@@ -173,37 +180,38 @@ __global__ __launch_bounds__(TPB) void window_rows_kernel(WindowArgs a, int tile
     if (t + 2 < n_tiles) fetch_pages(t + 2);
     const int kb = tile_key(t);
     if (kb > wp_hi || (a.window && kb + BN - 1 <= wp_lo - a.window && kb >= a.sinks)) continue;
-    const uint16_t *kt = lds[t & 1][0], *vt = lds[t & 1][1];
+    const lds_t buffer = (t & 1) * 4 * TILE;
+    const ColumnBase<HD> vb = {v_base.all + buffer, v_base.last + buffer};
     f32x16 sc[SUB];
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) {
+    for (int u = 0; u < SUB; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < KS; ++i) sc[u] = T::mfma32(row_frag<HD, vec8>(kt, 32 * u + c, i, g), qf[i], sc[u]);
-    }
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) sc[u] = T::mfma32(row_frag<HD, vec8>(k_base + buffer, 32 * u, i), qf[i], sc[u]);
     const bool whole = kb + BN - 1 <= wp_lo && (a.window == 0 || kb > wp_hi - a.window || kb + BN - 1 < a.sinks);
-    float top = -INFINITY;
     if (!whole) {
 #pragma unroll
       for (int u = 0; u < SUB; ++u)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[u][i] = visible(pos, kb + 32 * u + acc_row(i, g), a.window, a.sinks) ? sc[u][i] : -INFINITY;
     }
+    float top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < SUB; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[u][i]);
     top = fmaxf(top, other_half(top)) * scale2;
-    const float now = fmaxf(mx, top);
-    const float base = now == -INFINITY ? 0.f : now;          // a row that has seen no key yet keeps zeros
-    if (__any(now > mx)) {
-      const float shrink = __builtin_amdgcn_exp2f(mx - base);
+    if (__any(top > mx + RISE)) {
+      const float now = fmaxf(mx, top), shrink = __builtin_amdgcn_exp2f(mx - (now == -INFINITY ? 0.f : now));
+      mx = now;
       sum *= shrink;
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] *= shrink;
     }
-    mx = now;
+    const float base = mx == -INFINITY ? 0.f : mx;            // a row that has seen no key yet keeps zeros
 #pragma unroll
     for (int u = 0; u < SUB; ++u) {
       float part = 0.f;
@@ -221,7 +229,7 @@ __global__ __launch_bounds__(TPB) void window_rows_kernel(WindowArgs a, int tile
       for (int e = 0; e < 4; ++e) w[e] = T::pack(sc[u >> 1][8 * (u & 1) + 2 * e], sc[u >> 1][8 * (u & 1) + 2 * e + 1]);
       const vec8 pf = __builtin_bit_cast(vec8, w);
 #pragma unroll
-      for (int d = 0; d < DT; ++d) o[d] = T::mfma32(column_frag<HD, vec8>(vt, 16 * u, d, lane), pf, o[d]);
+      for (int d = 0; d < DT; ++d) o[d] = T::mfma32(column_frag<HD, vec8>(vb, 16 * u, d), pf, o[d]);
     }
   }
   sum += other_half(sum);

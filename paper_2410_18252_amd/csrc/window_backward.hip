@@ -19,11 +19,11 @@ constexpr float LOG2E = 1.4426950408889634f;
 // Everything below in the caller's workspace, and how the queries that see the sinks from beyond the window are parted.
 struct Backward {
   WindowArgs a;
-  float *delta, *peak, *part;
+  float *lse2, *delta, *peak, *part;    // [rows, Hq]: lse log2 e, delta; the largest |dout| of each block; the sinks' parts
   int sinks, chunk, chunks;             // sinks that are parted (0: none); tokens to a part; parts of the longest sequence
 };
 
-// delta [rows, Hq] and, for each block, the largest |dout|
+// delta and lse log2 e, and for each block the largest |dout|
 template <class T>
 __global__ __launch_bounds__(TPB) void delta_kernel(Backward b) {
   __shared__ float red[4];
@@ -50,7 +50,10 @@ __global__ __launch_bounds__(TPB) void delta_kernel(Backward b) {
     }
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) v += __shfl_xor(v, o, WAVE);
-    if (li == 0) b.delta[it] = v;
+    if (li == 0) {
+      b.delta[it] = v;
+      b.lse2[it] = a.lse[it] * LOG2E;
+    }
   }
   peak = wave_max(peak);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = peak;
@@ -76,13 +79,17 @@ __device__ __forceinline__ float ds_factor(const Backward& b) {
 // Sinks are seen by every query behind them: what lies beyond the window is parted over blocks of its own, whose sums meet in
 // sink_sum_kernel; else the block of the first keys would run for as long as all others together.
 template <class T, int HD>
-__global__ __launch_bounds__(TPB, 1) void keys_backward_kernel(Backward b, int key_tiles, int jobs) {
+__global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void keys_backward_kernel(Backward b, int key_tiles, int jobs) {
   typedef typename T::vec8 vec8;
   const WindowArgs& a = b.a;
-  constexpr int BQ = HD > 128 ? 32 : 64, SUB = BQ / 32, KS = HD / 16, DT = (HD + 31) / 32, CPR = HD / 8;
-  constexpr int TILE = BQ * HD, PIECES = BQ * CPR / 64, PER = (PIECES + 3) / 4;
-  __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][TILE];
-  __shared__ __attribute__((aligned(16))) float stat[2][3][64];            // of a tile's rows: lse, delta, position (bits)
+  // Two waves to a SIMD hide each other's latencies, so a wave has 256 registers: from 128 dims on V waits in LDS instead, for which
+  // the tiles of queries are halved.
+  constexpr bool V_IN_LDS = HD >= 128;
+  constexpr int BQ = V_IN_LDS ? 32 : 64, SUB = BQ / 32, KS = HD / 16, DT = (HD + 31) / 32, TILE = BQ * HD;
+  typedef Pieces<HD, BQ> P;
+  __shared__ __attribute__((aligned(256))) uint16_t lds[2][2][TILE];
+  __shared__ __attribute__((aligned(256))) uint16_t v_tile[V_IN_LDS ? BM * HD : 128];
+  __shared__ __attribute__((aligned(16))) float stat[2][3][64];            // of a tile's rows: lse log2 e, delta, position (bits)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, g = lane >> 5;
   const int G = a.Hq / a.Hkv;
@@ -111,7 +118,7 @@ __global__ __launch_bounds__(TPB, 1) void keys_backward_kernel(Backward b, int k
   // parts beyond the window concern the sinks alone
   const bool idle = kw >= q.n || (slot > 0 && kw >= b.sinks);
 
-  vec8 kf[KS], vf[KS];
+  vec8 kf[KS], vf[V_IN_LDS ? 1 : KS];
   {
     const long long row = q.row0 + min(key, q.n - 1);
     const uint16_t* kp = (const uint16_t*)a.k + row * a.k_stride + (long long)kvh * a.h;
@@ -120,29 +127,32 @@ __global__ __launch_bounds__(TPB, 1) void keys_backward_kernel(Backward b, int k
     for (int i = 0; i < KS; ++i) {
       const int d = 16 * i + 8 * g;
       kf[i] = d < a.h ? *(const vec8*)(kp + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
-      vf[i] = d < a.h ? *(const vec8*)(vp + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
+      if constexpr (!V_IN_LDS) vf[i] = d < a.h ? *(const vec8*)(vp + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
     }
+    if constexpr (V_IN_LDS)
+      request_pieces<HD, BM>(rows_buffer(a.v, (long long)q.row0 + kt * BM, q.n - kt * BM, a.v_stride, kvh, a.h), piece_offsets<HD, BM>(wave, lane, a.v_stride, a.h),
+                             v_tile, wave);
   }
   const float factor = ds_factor<T>(b);
+  // where tiles begin with a group's first head they all have the same offsets
+  const bool even = BQ % G == 0;
+  P q_off = flat_offsets<HD, BQ>(wave, lane, a.q_stride, a.h, G, 0), o_off = flat_offsets<HD, BQ>(wave, lane, a.dout_stride, a.h, G, 0);
   auto request = [&](int t, int buf) {
-    const int base = m0 + t * BQ;
-#pragma unroll
-    for (int n = 0; n < PER; ++n) {
-      if (PIECES % 4 != 0 && n * 4 + wave >= PIECES) break;
-      const int at = (n * 4 + wave) * 64 + lane, r = at / CPR, chunk = ((at % CPR) ^ chunk_swap<HD>(r)) * 8;
-      const int m = min(base + r, M - 1), tok = m / G, head = kvh * G + m - tok * G;
-      const uint16_t* qs = (const uint16_t*)a.q + (long long)(q.row0 + tok) * a.q_stride + (long long)head * a.h + chunk;
-      const uint16_t* os = (const uint16_t*)a.dout + (long long)(q.row0 + tok) * a.dout_stride + (long long)head * a.h + chunk;
-      if (chunk >= a.h) qs = os = (const uint16_t*)&zero_chunk;
-      const int to = (n * 4 + wave) * 512;
-      __builtin_amdgcn_global_load_lds((gptr_t)qs, (lptr_t)(lds[buf][0] + to), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((gptr_t)os, (lptr_t)(lds[buf][1] + to), 16, 0, 0);
+    const int base = m0 + t * BQ, tok_base = base / G;
+    if (!even) {
+      q_off = flat_offsets<HD, BQ>(wave, lane, a.q_stride, a.h, G, base - tok_base * G);
+      o_off = flat_offsets<HD, BQ>(wave, lane, a.dout_stride, a.h, G, base - tok_base * G);
     }
+    const long long left = q.n - tok_base, group = (long long)kvh * G * a.h;
+    request_pieces<HD, BQ>(buffer_of((const uint16_t*)a.q + ((long long)q.row0 + tok_base) * a.q_stride + group, ((left - 1) * a.q_stride + G * a.h) * 2),
+                           q_off, lds[buf][0], wave);
+    request_pieces<HD, BQ>(buffer_of((const uint16_t*)a.dout + ((long long)q.row0 + tok_base) * a.dout_stride + group, ((left - 1) * a.dout_stride + G * a.h) * 2),
+                           o_off, lds[buf][1], wave);
     if (wave < 3) {
       const int m = min(base + lane, M - 1), tok = m / G, head = kvh * G + m - tok * G;
       const long long at = (long long)(q.row0 + tok) * a.Hq + head;
       if (wave == 2) stat[buf][2][lane] = __int_as_float(base + lane < m1 ? tok : -1);      // (a row past the job's sees nothing)
-      else __builtin_amdgcn_global_load_lds((gptr_t)((wave ? b.delta : a.lse) + at), (lptr_t)stat[buf][wave], 4, 0, 0);
+      else __builtin_amdgcn_global_load_lds((gptr_t)((wave ? b.delta : b.lse2) + at), (lptr_t)stat[buf][wave], 4, 0, 0);
     }
   };
 
@@ -152,12 +162,14 @@ __global__ __launch_bounds__(TPB, 1) void keys_backward_kernel(Backward b, int k
 #pragma unroll
     for (int i = 0; i < 16; ++i) dk[t][i] = dv[t][i] = 0.f;
   const float scale2 = a.scale * LOG2E;
+  const lds_t tiles = lds_address(lds[0][0]), by_row = row_base<HD>(lane), v_row = lds_address(v_tile) + wave * 32 * HD * 2 + by_row;
+  const ColumnBase<HD> by_column = column_base<HD>(lane);
   if (n_tiles > 0) request(0, 0);
   for (int t = 0; t < n_tiles; ++t) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
     if (idle) continue;
-    const uint16_t *qt = lds[t & 1][0], *ot = lds[t & 1][1];
+    const lds_t qt = tiles + (t & 1) * 4 * TILE, ot = qt + 2 * TILE;
 #pragma unroll
     for (int u = 0; u < SUB; ++u) {
       const int base = m0 + t * BQ + 32 * u;
@@ -169,22 +181,31 @@ __global__ __launch_bounds__(TPB, 1) void keys_backward_kernel(Backward b, int k
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < KS; ++i) sc = T::mfma32(row_frag<HD, vec8>(qt, 32 * u + c, i, g), kf[i], sc);
+      for (int i = 0; i < KS; ++i) sc = T::mfma32(row_frag<HD, vec8>(qt + by_row, 32 * u, i), kf[i], sc);
 #pragma unroll
-      for (int i = 0; i < KS; ++i) dp = T::mfma32(row_frag<HD, vec8>(ot, 32 * u + c, i, g), vf[i], dp);
+      for (int i = 0; i < KS; ++i) {
+        if constexpr (V_IN_LDS) dp = T::mfma32(row_frag<HD, vec8>(ot + by_row, 32 * u, i), row_frag<HD, vec8>(v_row, 0, i), dp);
+        else dp = T::mfma32(row_frag<HD, vec8>(ot + by_row, 32 * u, i), vf[i], dp);
+      }
       u32x4 pw[2], sw[2];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int r = 32 * u + 8 * j + 4 * g;
-        const f32x4 lse = *(const f32x4*)&stat[t & 1][0][r], delta = *(const f32x4*)&stat[t & 1][1][r], where = *(const f32x4*)&stat[t & 1][2][r];
+        const f32x4 lse2 = *(const f32x4*)&stat[t & 1][0][r], delta = *(const f32x4*)&stat[t & 1][1][r];
         float p[4], ds[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(fmaf(sc[4 * j + e], scale2, -lse[e] * LOG2E));
+          p[e] = __builtin_amdgcn_exp2f(fmaf(sc[4 * j + e], scale2, -lse2[e]));
           ds[e] = p[e] * (dp[4 * j + e] - delta[e]) * factor;
-          const bool seen = (bool)(whole | visible(__float_as_int(where[e]), key, a.window, a.sinks));
-          p[e] = seen ? p[e] : 0.f;
-          ds[e] = seen ? ds[e] : 0.f;
+        }
+        if (!whole) {
+          const f32x4 where = *(const f32x4*)&stat[t & 1][2][r];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool seen = visible(__float_as_int(where[e]), key, a.window, a.sinks);
+            p[e] = seen ? p[e] : 0.f;
+            ds[e] = seen ? ds[e] : 0.f;
+          }
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -192,12 +213,13 @@ __global__ __launch_bounds__(TPB, 1) void keys_backward_kernel(Backward b, int k
           sw[j >> 1][2 * (j & 1) + e] = T::pack(ds[2 * e], ds[2 * e + 1]);
         }
       }
+      const ColumnBase<HD> oc = {ot + by_column.all, ot + by_column.last}, qc = {qt + by_column.all, qt + by_column.last};
 #pragma unroll
       for (int v = 0; v < 2; ++v) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) dv[d] = T::mfma32(column_frag<HD, vec8>(ot, 32 * u + 16 * v, d, lane), __builtin_bit_cast(vec8, pw[v]), dv[d]);
+        for (int d = 0; d < DT; ++d) dv[d] = T::mfma32(column_frag<HD, vec8>(oc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, pw[v]), dv[d]);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) dk[d] = T::mfma32(column_frag<HD, vec8>(qt, 32 * u + 16 * v, d, lane), __builtin_bit_cast(vec8, sw[v]), dk[d]);
+        for (int d = 0; d < DT; ++d) dk[d] = T::mfma32(column_frag<HD, vec8>(qc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, sw[v]), dk[d]);
       }
     }
   }
@@ -246,12 +268,11 @@ __global__ __launch_bounds__(TPB) void sink_sum_kernel(Backward b) {
 // The forward pass's walk: a block owns 128 rows of a group's queries, a wave 32 of them with q and dout in registers; keys and values pass
 // through LDS (K by rows and transposed, V by rows).
 template <class T, int HD>
-__global__ __launch_bounds__(TPB) void queries_backward_kernel(Backward b, int tiles) {
+__global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void queries_backward_kernel(Backward b, int tiles) {
   typedef typename T::vec8 vec8;
   const WindowArgs& a = b.a;
-  constexpr int BN = HD > 128 ? 32 : 64, SUB = BN / 32, KS = HD / 16, DT = (HD + 31) / 32, CPR = HD / 8;
-  constexpr int TILE = BN * HD, PIECES = BN * CPR / 64, PER = (PIECES + 3) / 4;
-  __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][TILE];
+  constexpr int BN = HD > 128 ? 32 : 64, SUB = BN / 32, KS = HD / 16, DT = (HD + 31) / 32, TILE = BN * HD;
+  __shared__ __attribute__((aligned(256))) uint16_t lds[2][2][TILE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, g = lane >> 5;
   const int G = a.Hq / a.Hkv;
@@ -279,22 +300,12 @@ __global__ __launch_bounds__(TPB) void queries_backward_kernel(Backward b, int t
     qf[i] = d < a.h ? *(const vec8*)((const uint16_t*)a.q + row * a.q_stride + (long long)head * a.h + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
     of[i] = d < a.h ? *(const vec8*)((const uint16_t*)a.dout + row * a.dout_stride + (long long)head * a.h + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
   }
-  const float lse2 = a.lse[row * a.Hq + head] * LOG2E, delta = b.delta[row * a.Hq + head], factor = ds_factor<T>(b);
-  const int key_max = q.n - 1;
+  const float lse2 = b.lse2[row * a.Hq + head], delta = b.delta[row * a.Hq + head], factor = ds_factor<T>(b);
+  const Pieces<HD, BN> k_off = piece_offsets<HD, BN>(wave, lane, a.k_stride, a.h), v_off = piece_offsets<HD, BN>(wave, lane, a.v_stride, a.h);
   auto request = [&](int t, int buf) {
     const int base = tile_key(t);
-#pragma unroll
-    for (int n = 0; n < PER; ++n) {
-      if (PIECES % 4 != 0 && n * 4 + wave >= PIECES) break;
-      const int at = (n * 4 + wave) * 64 + lane, r = at / CPR, chunk = ((at % CPR) ^ chunk_swap<HD>(r)) * 8;
-      const long long from = q.row0 + min(base + r, key_max);
-      const uint16_t* ks = (const uint16_t*)a.k + from * a.k_stride + (long long)kvh * a.h + chunk;
-      const uint16_t* vs = (const uint16_t*)a.v + from * a.v_stride + (long long)kvh * a.h + chunk;
-      if (chunk >= a.h) ks = vs = (const uint16_t*)&zero_chunk;
-      const int to = (n * 4 + wave) * 512;
-      __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(lds[buf][0] + to), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(lds[buf][1] + to), 16, 0, 0);
-    }
+    request_pieces<HD, BN>(rows_buffer(a.k, (long long)q.row0 + base, q.n - base, a.k_stride, kvh, a.h), k_off, lds[buf][0], wave);
+    request_pieces<HD, BN>(rows_buffer(a.v, (long long)q.row0 + base, q.n - base, a.v_stride, kvh, a.h), v_off, lds[buf][1], wave);
   };
   f32x16 dq[DT];
 #pragma unroll
@@ -302,11 +313,14 @@ __global__ __launch_bounds__(TPB) void queries_backward_kernel(Backward b, int t
 #pragma unroll
     for (int i = 0; i < 16; ++i) dq[t][i] = 0.f;
   const float scale2 = a.scale * LOG2E;
+  const lds_t tiles0 = lds_address(lds[0][0]), by_row = row_base<HD>(lane);
+  const ColumnBase<HD> by_column = column_base<HD>(lane);
   if (n_tiles > 0) request(0, 0);
   for (int t = 0; t < n_tiles; ++t) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
-    const uint16_t *kt = lds[t & 1][0], *vt = lds[t & 1][1];
+    const lds_t kt = tiles0 + (t & 1) * 4 * TILE, vt = kt + 2 * TILE;
+    const ColumnBase<HD> kc = {kt + by_column.all, kt + by_column.last};
 #pragma unroll
     for (int u = 0; u < SUB; ++u) {
       const int kb = tile_key(t) + 32 * u;
@@ -316,9 +330,9 @@ __global__ __launch_bounds__(TPB) void queries_backward_kernel(Backward b, int t
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < KS; ++i) sc = T::mfma32(row_frag<HD, vec8>(kt, 32 * u + c, i, g), qf[i], sc);
+      for (int i = 0; i < KS; ++i) sc = T::mfma32(row_frag<HD, vec8>(kt + by_row, 32 * u, i), qf[i], sc);
 #pragma unroll
-      for (int i = 0; i < KS; ++i) dp = T::mfma32(row_frag<HD, vec8>(vt, 32 * u + c, i, g), of[i], dp);
+      for (int i = 0; i < KS; ++i) dp = T::mfma32(row_frag<HD, vec8>(vt + by_row, 32 * u, i), of[i], dp);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float ds = __builtin_amdgcn_exp2f(fmaf(sc[i], scale2, -lse2)) * (dp[i] - delta) * factor;
@@ -330,7 +344,7 @@ __global__ __launch_bounds__(TPB) void queries_backward_kernel(Backward b, int t
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = T::pack(dp[8 * v + 2 * e], dp[8 * v + 2 * e + 1]);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) dq[d] = T::mfma32(column_frag<HD, vec8>(kt, 32 * u + 16 * v, d, lane), __builtin_bit_cast(vec8, w), dq[d]);
+        for (int d = 0; d < DT; ++d) dq[d] = T::mfma32(column_frag<HD, vec8>(kc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, w), dq[d]);
       }
     }
   }
@@ -370,6 +384,8 @@ size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 size_t place(Backward& b, char* ws) {
   const WindowArgs& a = b.a;
   size_t at = 0;
+  b.lse2 = (float*)(ws + at);
+  at += round_up((size_t)a.rows * a.Hq * sizeof(float));
   b.delta = (float*)(ws + at);
   at += round_up((size_t)a.rows * a.Hq * sizeof(float));
   b.peak = (float*)(ws + at);

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void window_decode_kernel(Wi
 #pragma unroll
     for (int i = 0; i < KS; ++i) {
       const int d = 32 * i + 8 * g;
-      qf[i] = d < a.h ? *(const vec8*)(qp + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
+      qf[i] = signed_query(d < a.h ? *(const vec8*)(qp + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0}), a.scale);
     }
   }
   const int last8 = (key_end - 1) & ~7, in_page = (1 << a.page_shift) - 1;
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void window_decode_kernel(Wi
 #pragma unroll
     for (int e = 0; e < VW; ++e) o[x][e] = f32x4{0.f, 0.f, 0.f, 0.f};
   float mx = -INFINITY, sum = 0.f;
-  const float scale2 = a.scale * 1.4426950408889634f;
+  const float scale2 = score_factor(a.scale);
   u32x4 k[2][KS], k_next[2][KS];
   vraw_t v[CH][8], v_next[CH][8];
   int pk, pv;

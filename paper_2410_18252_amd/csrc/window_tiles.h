@@ -17,27 +17,105 @@ template <int HD> __host__ __device__ constexpr int chunk_swap(int row) {
   else return (row >> 3) & 1;
 }
 
+// Bits of a chunk's number that chunk_swap changes, and what it changes between a row and the one eight below
+template <int HD> constexpr int SWAP_MASK = HD % 128 == 0 ? 15 : HD % 64 == 0 ? 7 : HD % 32 == 0 ? 3 : 1;
+template <int HD> constexpr int SWAP_EIGHT = HD % 32 == 0 ? 2 : 1;
+
 // sixteen zeros for the chunks of a tile row past the head's dims
 static __device__ const u32x4 zero_chunk = {0, 0, 0, 0};
 
-// Fragment of 32 rows x 16 dims with the row in the lane: lane (c = lane % 32, g = lane / 32) holds row row0 + c, dims 16 step + 8 g .. + 7
-template <int HD, class V8> __device__ __forceinline__ V8 row_frag(const uint16_t* tile, int row, int step, int g) {
-  return *(const V8*)(tile + row * HD + (((2 * step + g) ^ chunk_swap<HD>(row)) << 3));
+typedef uint32_t lds_t;                  // byte address in LDS
+__device__ __forceinline__ lds_t lds_address(const void* p) { return (lds_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
+
+// Fragment of 32 rows x 16 dims with the row in the lane: lane (c = lane % 32, g = lane / 32) holds row row0 + c, dims 16 step + 8 g .. + 7.
+// A lane's address differs from step to step in the swapped bits (an exclusive or: the tile's rows are multiples of what they span)
+// and in a constant; row0 is a multiple of 16.
+template <int HD> __device__ __forceinline__ lds_t row_base(int lane) {
+  const int c = lane & 31, g = lane >> 5;
+  return c * HD * 2 + ((g ^ chunk_swap<HD>(c)) << 4);
+}
+template <int HD, class V8> __device__ __forceinline__ V8 row_frag(lds_t base, int row0, int step) {
+  constexpr int M = SWAP_MASK<HD>;
+  return *(__attribute__((address_space(3))) const V8*)(uintptr_t)((base ^ (((2 * step) & M) << 4)) + (((2 * step) & ~M) << 4) + row0 * HD * 2);
 }
 // The transposed one, 32 dims x 16 rows: lane (c, g) holds dim 32 t + c and the rows row0 + 4 g .. + 3 and row0 + 8 + 4 g .. + 3, which
 // are the rows whose products a 32x32 result leaves in that lane group's registers 8 u .. 8 u + 7 (u = row0 / 16).
 // The instruction gives lane i of 16 column i of the 4 x 16 values whose 8-byte pieces lanes 4 r + q (row r, columns 4 q .. + 3) point at.
-template <int HD, class V8> __device__ __forceinline__ V8 column_frag(const uint16_t* tile, int row0, int t, int lane) {
-  const int i = lane & 15, b = (lane >> 4) & 1, g = lane >> 5;
-  const int dim = 32 * t + (32 * t + 16 < HD ? 16 * b : 0) + 4 * (i & 3);      // (dims past an odd last 16 repeat it: their results are not kept)
+// A last 16 dims alone (odd HD / 16) are read twice: the results of the second are not kept.
+template <int HD> struct ColumnBase { lds_t all, last; };
+template <int HD> __device__ __forceinline__ ColumnBase<HD> column_base(int lane) {
+  constexpr int M = SWAP_MASK<HD>;
+  const int i = lane & 15, b = (lane >> 4) & 1, row = 4 * (lane >> 5) + (i >> 2), sw = chunk_swap<HD>(row);
+  ColumnBase<HD> r;
+  const int chunk = 2 * b + ((i & 3) >> 1), chunk0 = (i & 3) >> 1;
+  r.all = row * HD * 2 + ((chunk & ~M) << 4) + (((chunk & M) ^ sw) << 4) + 8 * (i & 1);
+  r.last = HD % 32 ? row * HD * 2 + ((chunk0 & ~M) << 4) + (((chunk0 & M) ^ sw) << 4) + 8 * (i & 1) : r.all;
+  return r;
+}
+template <int HD, class V8> __device__ __forceinline__ V8 column_frag(ColumnBase<HD> base, int row0, int t) {
+  constexpr int M = SWAP_MASK<HD>;
+  const lds_t b = HD % 32 && 32 * t + 16 >= HD ? base.last : base.all;
   union { s16x4 half[2]; V8 whole; } r;
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int row = row0 + 8 * j + 4 * g + (i >> 2);
-    const uint16_t* p = tile + row * HD + (((dim >> 3) ^ chunk_swap<HD>(row)) << 3) + (dim & 7);
-    r.half[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
-  }
+  for (int j = 0; j < 2; ++j)
+    r.half[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)(
+        (b ^ ((((4 * t) & M) ^ (j * SWAP_EIGHT<HD>)) << 4)) + (((4 * t) & ~M) << 4) + (row0 + 8 * j) * HD * 2));
   return r.whole;
+}
+
+// Requests of a tile straight into LDS, a kilobyte of it at a time dealt to the four waves: piece n of a wave is the 64 chunks from
+// (4 n + wave) 64 on, as they lie in the tile.  Rows lie `stride` elements apart behind a base common to the block, so a lane keeps one
+// 32-bit offset a piece for the whole loop; the buffer's range check turns what lies past the last row into zeros, and
+// so it does with chunks past the head's dims, which are given an offset beyond any range.
+constexpr uint32_t OUT_OF_RANGE = 0x80000000u;
+template <int HD, int ROWS> struct Pieces {
+  static constexpr int CPR = HD / 8, ALL = ROWS * CPR / 64, PER = (ALL + 3) / 4;
+  uint32_t off[PER];
+  static __device__ __forceinline__ void place(int n, int wave, int lane, int& row, int& dim) {
+    const int at = (n * 4 + wave) * 64 + lane;
+    row = at / CPR;
+    dim = ((at % CPR) ^ chunk_swap<HD>(row)) * 8;
+  }
+};
+struct Buffer { const void* base; int bytes; };
+__device__ __forceinline__ Buffer buffer_of(const void* base, long long bytes) { return {base, (int)min(max(bytes, 0ll), 0x7fffffffll)}; }
+// the same for rows of one kv head from `row` on, `rows` of them left
+__device__ __forceinline__ Buffer rows_buffer(const void* base, long long row, long long rows, long long stride, int head, int h) {
+  return buffer_of((const uint16_t*)base + row * stride + (long long)head * h, ((rows - 1) * stride + h) * 2);
+}
+template <int HD, int ROWS> __device__ __forceinline__ Pieces<HD, ROWS> piece_offsets(int wave, int lane, long long stride, int h) {
+  Pieces<HD, ROWS> p;
+#pragma unroll
+  for (int n = 0; n < p.PER; ++n) {
+    int row, dim;
+    p.place(n, wave, lane, row, dim);
+    p.off[n] = dim < h ? (uint32_t)(row * (int)stride + dim) * 2 : OUT_OF_RANGE;
+  }
+  return p;
+}
+// Rows of the axis that queries and heads make: row rem + r of the tile is token (rem + r) / G, head (rem + r) % G behind the base's
+template <int HD, int ROWS> __device__ __forceinline__ Pieces<HD, ROWS> flat_offsets(int wave, int lane, long long stride, int h, int G, int rem) {
+  Pieces<HD, ROWS> p;
+#pragma unroll
+  for (int n = 0; n < p.PER; ++n) {
+    int row, dim;
+    p.place(n, wave, lane, row, dim);
+    const int tok = (rem + row) / G, head = rem + row - tok * G;
+    p.off[n] = dim < h ? (uint32_t)(tok * (int)stride + head * h + dim) * 2 : OUT_OF_RANGE;
+  }
+  return p;
+}
+// (lane i's 16 bytes go to LDS 16 i behind `to`; the host's compiler does not know the descriptor's type)
+__device__ __forceinline__ void request(Buffer from, uint32_t offset, const uint16_t* to) {
+#ifdef __HIP_DEVICE_COMPILE__
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)from.base, 0, from.bytes, 0x00027000), (lptr_t)to, 16, offset, 0, 0, 0);
+#endif
+}
+template <int HD, int ROWS>
+__device__ __forceinline__ void request_pieces(Buffer from, const Pieces<HD, ROWS>& p, const uint16_t* tile, int wave) {
+#pragma unroll
+  for (int n = 0; n < p.PER; ++n)
+    if (p.ALL % 4 == 0 || n * 4 + wave < p.ALL) request(from, p.off[n], tile + (n * 4 + wave) * 512);
 }
 
 // Row of register i of a 32x32 result in lane group g (its column is lane % 32)
@@ -70,3 +148,12 @@ __device__ __forceinline__ bool map_block(int id, int units, int tiles, int& uni
   return unit < units;
 }
 inline unsigned mapped_blocks(long long units, long long tiles) { return (unsigned)((units + 7) / 8 * 8 * tiles); }
+
+// The sign of a scale goes to the queries (their sign bits, exactly), so that the largest product has the largest score; a scale of zero
+// becomes one that every score vanishes under, since -infinity stands for masked scores.
+template <class V8> __device__ __forceinline__ V8 signed_query(V8 q, float scale) {
+  u32x4 w = __builtin_bit_cast(u32x4, q);
+  w ^= (__float_as_uint(scale) >> 31) * 0x80008000u;
+  return __builtin_bit_cast(V8, w);
+}
+__device__ __forceinline__ float score_factor(float scale) { return fmaxf(fabsf(scale) * 1.4426950408889634f, 1e-37f); }
