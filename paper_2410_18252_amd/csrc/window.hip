@@ -79,6 +79,7 @@ template <class T, int HD, bool PAGED>
 __global__ __launch_bounds__(TPB, HD > 128 && PAGED ? 1 : 2) void window_rows_kernel(WindowArgs a, int tiles) {
   typedef typename T::vec8 vec8;
   constexpr int BN = HD > 128 ? 32 : 64, SUB = BN / 32, KS = HD / 16, DT = (HD + 31) / 32, TILE = BN * HD;
+  constexpr int AHEAD = 6;
   typedef Pieces<HD, BN> P;
   __shared__ __attribute__((aligned(256))) uint16_t lds[2][2][TILE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -120,6 +121,7 @@ __global__ __launch_bounds__(TPB, HD > 128 && PAGED ? 1 : 2) void window_rows_ke
     k_off = piece_offsets<HD, BN>(wave, lane, a.k_stride, a.h);
     v_off = piece_offsets<HD, BN>(wave, lane, a.v_stride, a.h);
   }
+  const RowSource k_rows = row_source(a.k, q.row0, a.k_stride, kvh, 1, a.h), v_rows = row_source(a.v, q.row0, a.v_stride, kvh, 1, a.h);
   auto fetch_pages = [&](int t) {
     if constexpr (PAGED) {
 #pragma unroll
@@ -145,12 +147,13 @@ __global__ __launch_bounds__(TPB, HD > 128 && PAGED ? 1 : 2) void window_rows_ke
         const uint16_t* vs = ks + ((long long)a.Hkv << a.page_shift) * a.h;
         if (dim >= a.h) ks = vs = (const uint16_t*)&zero_chunk;
         const int to = (n * 4 + wave) * 512;
-        __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(lds[buf][0] + to), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(lds[buf][1] + to), 16, 0, 0);
+        ::request(ks, lds[buf][0] + to);
+        ::request(vs, lds[buf][1] + to);
       }
     } else {
-      request_pieces<HD, BN>(rows_buffer(a.k, (long long)q.row0 + base, q.n - base, a.k_stride, kvh, a.h), k_off, lds[buf][0], wave);
-      request_pieces<HD, BN>(rows_buffer(a.v, (long long)q.row0 + base, q.n - base, a.v_stride, kvh, a.h), v_off, lds[buf][1], wave);
+      const int rows = min(q.n - base, BN);
+      request_pieces<HD, BN>(k_rows.tile(base, rows), k_off, lds[buf][0], wave);
+      request_pieces<HD, BN>(v_rows.tile(base, rows), v_off, lds[buf][1], wave);
     }
   };
 
@@ -191,6 +194,7 @@ __global__ __launch_bounds__(TPB, HD > 128 && PAGED ? 1 : 2) void window_rows_ke
     for (int i = 0; i < KS; ++i)
 #pragma unroll
       for (int u = 0; u < SUB; ++u) sc[u] = T::mfma32(row_frag<HD, vec8>(k_base + buffer, 32 * u, i), qf[i], sc[u]);
+    order_products<1, AHEAD, KS * SUB>();
     const bool whole = kb + BN - 1 <= wp_lo && (a.window == 0 || kb > wp_hi - a.window || kb + BN - 1 < a.sinks);
     if (!whole) {
 #pragma unroll
@@ -203,7 +207,7 @@ __global__ __launch_bounds__(TPB, HD > 128 && PAGED ? 1 : 2) void window_rows_ke
     for (int u = 0; u < SUB; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[u][i]);
-    top = fmaxf(top, other_half(top)) * scale2;
+    top = max_halves(top) * scale2;
     if (__any(top > mx + RISE)) {
       const float now = fmaxf(mx, top), shrink = __builtin_amdgcn_exp2f(mx - (now == -INFINITY ? 0.f : now));
       mx = now;
@@ -232,7 +236,7 @@ __global__ __launch_bounds__(TPB, HD > 128 && PAGED ? 1 : 2) void window_rows_ke
       for (int d = 0; d < DT; ++d) o[d] = T::mfma32(column_frag<HD, vec8>(vb, 16 * u, d), pf, o[d]);
     }
   }
-  sum += other_half(sum);
+  sum = sum_halves(sum);
   const float inv = sum > 0.f ? 1.0f / sum : (sum == 0.f ? 0.f : sum);      // (NaN stays)
   bool finite = fabsf(sum) < INFINITY;
 #pragma unroll

@@ -130,29 +130,28 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void keys_backward_kernel(Ba
       if constexpr (!V_IN_LDS) vf[i] = d < a.h ? *(const vec8*)(vp + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
     }
     if constexpr (V_IN_LDS)
-      request_pieces<HD, BM>(rows_buffer(a.v, (long long)q.row0 + kt * BM, q.n - kt * BM, a.v_stride, kvh, a.h), piece_offsets<HD, BM>(wave, lane, a.v_stride, a.h),
-                             v_tile, wave);
+      request_pieces<HD, BM>(row_source(a.v, q.row0, a.v_stride, kvh, 1, a.h).tile(kt * BM, min(q.n - kt * BM, BM)),
+                             piece_offsets<HD, BM>(wave, lane, a.v_stride, a.h), v_tile, wave);
   }
   const float factor = ds_factor<T>(b);
   // where tiles begin with a group's first head they all have the same offsets
   const bool even = BQ % G == 0;
   P q_off = flat_offsets<HD, BQ>(wave, lane, a.q_stride, a.h, G, 0), o_off = flat_offsets<HD, BQ>(wave, lane, a.dout_stride, a.h, G, 0);
+  const RowSource q_rows = row_source(a.q, q.row0, a.q_stride, kvh * G, G, a.h), o_rows = row_source(a.dout, q.row0, a.dout_stride, kvh * G, G, a.h);
   auto request = [&](int t, int buf) {
-    const int base = m0 + t * BQ, tok_base = base / G;
+    const int base = m0 + t * BQ, tok_base = even ? tok0 + t * (BQ / G) : base / G;
     if (!even) {
       q_off = flat_offsets<HD, BQ>(wave, lane, a.q_stride, a.h, G, base - tok_base * G);
       o_off = flat_offsets<HD, BQ>(wave, lane, a.dout_stride, a.h, G, base - tok_base * G);
     }
-    const long long left = q.n - tok_base, group = (long long)kvh * G * a.h;
-    request_pieces<HD, BQ>(buffer_of((const uint16_t*)a.q + ((long long)q.row0 + tok_base) * a.q_stride + group, ((left - 1) * a.q_stride + G * a.h) * 2),
-                           q_off, lds[buf][0], wave);
-    request_pieces<HD, BQ>(buffer_of((const uint16_t*)a.dout + ((long long)q.row0 + tok_base) * a.dout_stride + group, ((left - 1) * a.dout_stride + G * a.h) * 2),
-                           o_off, lds[buf][1], wave);
+    const int rows = min(q.n - tok_base, BQ);
+    request_pieces<HD, BQ>(q_rows.tile(tok_base, rows), q_off, lds[buf][0], wave);
+    request_pieces<HD, BQ>(o_rows.tile(tok_base, rows), o_off, lds[buf][1], wave);
     if (wave < 3) {
       const int m = min(base + lane, M - 1), tok = m / G, head = kvh * G + m - tok * G;
       const long long at = (long long)(q.row0 + tok) * a.Hq + head;
       if (wave == 2) stat[buf][2][lane] = __int_as_float(base + lane < m1 ? tok : -1);      // (a row past the job's sees nothing)
-      else __builtin_amdgcn_global_load_lds((gptr_t)((wave ? b.delta : b.lse2) + at), (lptr_t)stat[buf][wave], 4, 0, 0);
+      else request_word((wave ? b.delta : b.lse2) + at, stat[buf][wave]);
     }
   };
 
@@ -187,6 +186,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void keys_backward_kernel(Ba
         if constexpr (V_IN_LDS) dp = T::mfma32(row_frag<HD, vec8>(ot + by_row, 32 * u, i), row_frag<HD, vec8>(v_row, 0, i), dp);
         else dp = T::mfma32(row_frag<HD, vec8>(ot + by_row, 32 * u, i), vf[i], dp);
       }
+      if constexpr (!V_IN_LDS) order_products<1, 6, 2 * KS>();
       u32x4 pw[2], sw[2];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -302,10 +302,12 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void queries_backward_kernel
   }
   const float lse2 = b.lse2[row * a.Hq + head], delta = b.delta[row * a.Hq + head], factor = ds_factor<T>(b);
   const Pieces<HD, BN> k_off = piece_offsets<HD, BN>(wave, lane, a.k_stride, a.h), v_off = piece_offsets<HD, BN>(wave, lane, a.v_stride, a.h);
+  const RowSource k_rows = row_source(a.k, q.row0, a.k_stride, kvh, 1, a.h), v_rows = row_source(a.v, q.row0, a.v_stride, kvh, 1, a.h);
   auto request = [&](int t, int buf) {
     const int base = tile_key(t);
-    request_pieces<HD, BN>(rows_buffer(a.k, (long long)q.row0 + base, q.n - base, a.k_stride, kvh, a.h), k_off, lds[buf][0], wave);
-    request_pieces<HD, BN>(rows_buffer(a.v, (long long)q.row0 + base, q.n - base, a.v_stride, kvh, a.h), v_off, lds[buf][1], wave);
+    const int rows = min(q.n - base, BN);
+    request_pieces<HD, BN>(k_rows.tile(base, rows), k_off, lds[buf][0], wave);
+    request_pieces<HD, BN>(v_rows.tile(base, rows), v_off, lds[buf][1], wave);
   };
   f32x16 dq[DT];
 #pragma unroll
@@ -333,6 +335,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void queries_backward_kernel
       for (int i = 0; i < KS; ++i) sc = T::mfma32(row_frag<HD, vec8>(kt + by_row, 32 * u, i), qf[i], sc);
 #pragma unroll
       for (int i = 0; i < KS; ++i) dp = T::mfma32(row_frag<HD, vec8>(vt + by_row, 32 * u, i), of[i], dp);
+      order_products<1, 6, 2 * KS>();
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float ds = __builtin_amdgcn_exp2f(fmaf(sc[i], scale2, -lse2)) * (dp[i] - delta) * factor;

@@ -2,8 +2,6 @@
 #pragma once
 #include "window.h"
 
-typedef const __attribute__((address_space(1))) void* gptr_t;
-typedef __attribute__((address_space(3))) void* lptr_t;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // A tile keeps rows of HD 16-bit values one behind the other; what varies is where a row's 16-byte chunk c sits: at c ^ chunk_swap(row).
@@ -78,10 +76,17 @@ template <int HD, int ROWS> struct Pieces {
   }
 };
 struct Buffer { const void* base; int bytes; };
-__device__ __forceinline__ Buffer buffer_of(const void* base, long long bytes) { return {base, (int)min(max(bytes, 0ll), 0x7fffffffll)}; }
-// the same for rows of one kv head from `row` on, `rows` of them left
-__device__ __forceinline__ Buffer rows_buffer(const void* base, long long row, long long rows, long long stride, int head, int h) {
-  return buffer_of((const uint16_t*)base + row * stride + (long long)head * h, ((rows - 1) * stride + h) * 2);
+// `rows` rows of one kv head (of `width` elements in all) `step` rows behind `first`, the latter at most what is left
+struct RowSource {
+  const uint16_t* first;
+  uint32_t row_bytes;                      // (strides are at most 2^23 elements, tiles at most 128 rows)
+  int width_bytes;
+  __device__ __forceinline__ Buffer tile(int step, int rows) const {
+    return {(const char*)first + (uint64_t)(uint32_t)step * row_bytes, (rows - 1) * (int)row_bytes + width_bytes};
+  }
+};
+__device__ __forceinline__ RowSource row_source(const void* base, int row0, long long stride, int head, int heads, int h) {
+  return {(const uint16_t*)base + (long long)row0 * stride + (long long)head * h, (uint32_t)stride * 2, heads * h * 2};
 }
 template <int HD, int ROWS> __device__ __forceinline__ Pieces<HD, ROWS> piece_offsets(int wave, int lane, long long stride, int h) {
   Pieces<HD, ROWS> p;
@@ -105,11 +110,23 @@ template <int HD, int ROWS> __device__ __forceinline__ Pieces<HD, ROWS> flat_off
   }
   return p;
 }
-// (lane i's 16 bytes go to LDS 16 i behind `to`; the host's compiler does not know the descriptor's type)
-__device__ __forceinline__ void request(Buffer from, uint32_t offset, const uint16_t* to) {
-#ifdef __HIP_DEVICE_COMPILE__
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)from.base, 0, from.bytes, 0x00027000), (lptr_t)to, 16, offset, 0, 0, 0);
-#endif
+// Requests into LDS: lane i's 16 (4) bytes go 16 (4) i behind `to`, which the wave has in common.  Written as instructions because in front
+// of every LDS read the compiler waits for all requests that it knows to write LDS, those of the next tile among them; the barrier
+// that a tile begins with waits for them instead.  They have no output register, so none can be overwritten by a late answer, and m0 is
+// used by nothing else in these kernels.
+__device__ __forceinline__ void request(Buffer from, uint32_t offset, const void* to) {
+  u32x4 d;
+  d[0] = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)from.base);
+  d[1] = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)from.base >> 32) & 0xffffu);
+  d[2] = __builtin_amdgcn_readfirstlane(from.bytes);
+  d[3] = 0x00027000;
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(d), "s"(__builtin_amdgcn_readfirstlane(lds_address(to))) : "memory");
+}
+__device__ __forceinline__ void request(const void* from, const void* to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(__builtin_amdgcn_readfirstlane(lds_address(to))) : "memory");
+}
+__device__ __forceinline__ void request_word(const float* from, const float* to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(__builtin_amdgcn_readfirstlane(lds_address(to))) : "memory");
 }
 template <int HD, int ROWS>
 __device__ __forceinline__ void request_pieces(Buffer from, const Pieces<HD, ROWS>& p, const uint16_t* tile, int wave) {
@@ -121,8 +138,28 @@ __device__ __forceinline__ void request_pieces(Buffer from, const Pieces<HD, ROW
 // Row of register i of a 32x32 result in lane group g (its column is lane % 32)
 __device__ __forceinline__ constexpr int acc_row(int i, int g) { return (i >> 2) * 8 + 4 * g + (i & 3); }
 
-// lane exchange across the two halves of a wave
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, WAVE); }
+// The larger (the sum) of a lane's value and that of its partner in the other half of the wave: the instruction exchanges the upper
+// half of one register with the lower half of another, no pass through LDS.
+__device__ __forceinline__ float max_halves(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_halves(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Orders the scheduler's work on a run of products whose operands come from LDS: READS reads ahead, then for every AT_ONCE products
+// as many further reads (a product's own reads are then as far ahead; left to itself the scheduler asks for each pair and waits).
+template <int READS_EACH, int AHEAD, int PRODUCTS> __device__ __forceinline__ void order_products() {
+  constexpr int READS = READS_EACH * PRODUCTS, FIRST = AHEAD * READS_EACH < READS ? AHEAD * READS_EACH : READS;
+  __builtin_amdgcn_sched_group_barrier(0x100, FIRST, 0);
+#pragma unroll
+  for (int i = 0; i < PRODUCTS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if ((i + AHEAD + 1) * READS_EACH <= READS) __builtin_amdgcn_sched_group_barrier(0x100, READS_EACH, 0);
+  }
+}
 
 __device__ __forceinline__ bool visible(int pos, int key, int window, int sinks) {
   return (key <= pos) & ((window == 0) | (key > pos - window) | (key < sinks));
