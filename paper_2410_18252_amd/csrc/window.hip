@@ -76,9 +76,9 @@ __device__ void rows_key_by_key(const WindowArgs& a, const Seq& q, int s, int kv
 }
 
 template <class T, int HD, bool PAGED>
-__global__ __launch_bounds__(TPB, HD > 128 && PAGED ? 1 : 2) void window_rows_kernel(WindowArgs a, int tiles) {
+__global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 2) void window_rows_kernel(WindowArgs a, int tiles) {
   typedef typename T::vec8 vec8;
-  constexpr int BN = HD > 128 ? 32 : 64, SUB = BN / 32, KS = HD / 16, DT = (HD + 31) / 32, TILE = BN * HD;
+  constexpr int BN = HD > 96 ? 32 : 64, SUB = BN / 32, KS = HD / 16, DT = (HD + 31) / 32, TILE = BN * HD;
   constexpr int AHEAD = 6;
   typedef Pieces<HD, BN> P;
   __shared__ __attribute__((aligned(256))) uint16_t lds[2][2][TILE];
@@ -198,9 +198,11 @@ __global__ __launch_bounds__(TPB, HD > 128 && PAGED ? 1 : 2) void window_rows_ke
     const bool whole = kb + BN - 1 <= wp_lo && (a.window == 0 || kb > wp_hi - a.window || kb + BN - 1 < a.sinks);
     if (!whole) {
 #pragma unroll
-      for (int u = 0; u < SUB; ++u)
+      for (int u = 0; u < SUB; ++u) {
+        const uint32_t bits = group_bits(seen_keys(pos, kb + 32 * u, a.window, a.sinks), g);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[u][i] = visible(pos, kb + 32 * u + acc_row(i, g), a.window, a.sinks) ? sc[u][i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) sc[u][i] = or_else(sc[u][i], element_mask(bits, i), 0xff800000u);      // -infinity
+      }
     }
     float top = -INFINITY;
 #pragma unroll

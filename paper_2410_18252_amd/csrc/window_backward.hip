@@ -115,6 +115,8 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void keys_backward_kernel(Ba
   }
   const int kw = kt * BM + wave * 32, key = kw + c;
   const int M = q.n * G, m0 = tok0 * G, m1 = tok1 * G, n_tiles = (m1 - m0 + BQ - 1) / BQ;
+  // the last position that sees this lane's key, from the key on (a position of -1 is beyond any)
+  const uint32_t seen_by = a.window && key >= a.sinks ? a.window - 1 : 0x7fffffff - key;
   // parts beyond the window concern the sinks alone
   const bool idle = kw >= q.n || (slot > 0 && kw >= b.sinks);
 
@@ -196,17 +198,14 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void keys_backward_kernel(Ba
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           p[e] = __builtin_amdgcn_exp2f(fmaf(sc[4 * j + e], scale2, -lse2[e]));
-          ds[e] = p[e] * (dp[4 * j + e] - delta[e]) * factor;
         }
         if (!whole) {
           const f32x4 where = *(const f32x4*)&stat[t & 1][2][r];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const bool seen = visible(__float_as_int(where[e]), key, a.window, a.sinks);
-            p[e] = seen ? p[e] : 0.f;
-            ds[e] = seen ? ds[e] : 0.f;
-          }
+          for (int e = 0; e < 4; ++e) p[e] = (uint32_t)(__float_as_int(where[e]) - key) <= seen_by ? p[e] : 0.f;
         }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ds[e] = p[e] * (dp[4 * j + e] - delta[e]) * factor;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           pw[j >> 1][2 * (j & 1) + e] = T::pack(p[2 * e], p[2 * e + 1]);
@@ -328,6 +327,8 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void queries_backward_kernel
       const int kb = tile_key(t) + 32 * u;
       if (kb > wp_hi || (a.window && kb + 31 <= wp_lo - a.window && kb >= a.sinks)) continue;
       const bool whole = kb + 31 <= wp_lo && (a.window == 0 || kb > wp_hi - a.window || kb + 31 < a.sinks);
+      uint32_t bits = ~0u;
+      if (!whole) bits = group_bits(seen_keys(pos, kb, a.window, a.sinks), g);
       f32x16 sc, dp;
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
@@ -339,7 +340,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void queries_backward_kernel
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float ds = __builtin_amdgcn_exp2f(fmaf(sc[i], scale2, -lse2)) * (dp[i] - delta) * factor;
-        dp[i] = (whole | visible(pos, kb + acc_row(i, g), a.window, a.sinks)) ? ds : 0.f;
+        dp[i] = or_else(ds, element_mask(bits, i), 0u);
       }
 #pragma unroll
       for (int v = 0; v < 2; ++v) {

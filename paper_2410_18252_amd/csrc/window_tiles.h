@@ -161,9 +161,17 @@ template <int READS_EACH, int AHEAD, int PRODUCTS> __device__ __forceinline__ vo
   }
 }
 
-__device__ __forceinline__ bool visible(int pos, int key, int window, int sinks) {
-  return (key <= pos) & ((window == 0) | (key > pos - window) | (key < sinks));
+// Who is seen, as bits: of the 32 keys from first_key on, those that a query at pos sees (first_key is common to the wave).  A lane group's
+// share of them, for the registers of a 32x32 result, is what group_bits leaves; element i's bit is then acc_row(i, 0).
+__device__ __forceinline__ uint32_t seen_keys(int pos, int first_key, int window, int sinks) {
+  const int hi = pos - first_key, lo = hi - window + 1, n = sinks - first_key;
+  const uint32_t up = hi < 0 ? 0u : hi >= 31 ? ~0u : (2u << hi) - 1u;
+  const uint32_t down = window == 0 || lo <= 0 ? ~0u : lo > 31 ? 0u : ~0u << lo;
+  return up & (down | (n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u));
 }
+__device__ __forceinline__ uint32_t group_bits(uint32_t seen, int g) { return seen >> (4 * g); }
+__device__ __forceinline__ uint32_t element_mask(uint32_t bits, int i) { return (uint32_t)__builtin_amdgcn_sbfe((int)bits, acc_row(i, 0), 1); }
+__device__ __forceinline__ float or_else(float v, uint32_t mask, uint32_t other) { return __uint_as_float((__float_as_uint(v) & mask) | (~mask & other)); }
 
 // One sequence of a call: its rows, its keys and the position of its first row.
 struct Seq { int row0, n, total, ctx; };
