@@ -45,10 +45,10 @@ bool window_ok(const WindowArgs& a) {
   return heads_ok(a.rows, a.Hq, a.Hkv, a.h) && type16(a.dtype) && a.S >= 1 && (int64_t)a.S * a.Hq <= INT32_MAX && a.max_new >= 1 &&
          a.window >= 0 && a.sinks >= 0 && std::isfinite(a.scale) && (int64_t)a.max_new * (a.Hq / a.Hkv) <= INT32_MAX - 256;
 }
-// every tile of the longest sequence for every sequence and kv head: a launch's blocks
+// every tile of the longest sequence for every sequence and kv head, and what the order of blocks adds: a launch's blocks
 bool grid_ok(const WindowArgs& a) {
-  const int64_t tiles = ((int64_t)a.max_new * (a.Hq / a.Hkv) + 127) / 128;
-  return tiles * (((int64_t)a.S * a.Hkv + 7) / 8 * 8) <= INT32_MAX / 64;          // (a launch has at most 2^32 threads)
+  const int64_t tiles = ((int64_t)a.max_new * (a.Hq / a.Hkv) + 127) / 128 + 128;
+  return tiles * ((int64_t)a.S * a.Hkv + 1024) <= INT32_MAX / 128;                // (a launch has at most 2^32 threads)
 }
 WindowArgs window_shape(int dtype, int rows, int Hq, int Hkv, int h, int S, int max_new, int window, int sinks, float scale) {
   WindowArgs a{};

@@ -395,18 +395,22 @@ __global__ __launch_bounds__(TPB) void norm_rope_backward_kernel(NormRopeArgs a)
   }
 }
 
-// sums[which][d] over the blocks of norm_rope_backward_kernel: sixteen lanes to a sum, each a run of blocks in order
-__global__ __launch_bounds__(TPB) void gain_grad_kernel(const float* partial, int blocks, int h, float* dq_gain, float* dk_gain) {
-  __shared__ float red[16][16];
-  const int col = threadIdx.x & 15, part = threadIdx.x >> 4, d = blockIdx.x * 16 + col;
+// The gains' gradients over the blocks of norm_rope_backward_kernel: a block adds up eight dims, 128 runs of blocks at once and then the
+// runs, always in the same order.
+__global__ __launch_bounds__(1024) void gain_grad_kernel(const float* partial, int blocks, int h, float* dq_gain, float* dk_gain) {
+  __shared__ float red[128][8];
+  const int col = threadIdx.x & 7, part = threadIdx.x >> 3, d = blockIdx.x * 8 + col;       // 2 h is a multiple of 8
   float v = 0.f;
-  if (d < 2 * h)
-    for (int b = part; b < blocks; b += 16) v += partial[(size_t)b * 2 * h + d];
+#pragma unroll 8
+  for (int b = part; b < blocks; b += 128) v += partial[(size_t)b * 2 * h + d];
   red[part][col] = v;
   __syncthreads();
-  if (part == 0 && d < 2 * h) {
-    for (int p = 1; p < 16; ++p) v += red[p][col];
-    if (d < h) dq_gain[d] = v; else dk_gain[d - h] = v;
+  if (part < 8) {
+    for (int p = part + 8; p < 128; p += 8) v += red[p][col];
+    // the eight runs left sit in lanes 8 apart
+#pragma unroll
+    for (int o = 8; o < 64; o <<= 1) v += __shfl_xor(v, o, WAVE);
+    if (part == 0) (d < h ? dq_gain : dk_gain - h)[d] = v;
   }
 }
 
@@ -465,6 +469,6 @@ hipError_t rl_norm_rope_backward(const NormRopeArgs& a, hipStream_t s) {
     const hipError_t e = by_type(a, true, blocks, s);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(gain_grad_kernel, dim3((2 * a.h + 15) / 16), dim3(TPB), 0, s, a.partial, blocks, a.h, a.dq_gain, a.dk_gain);
+  hipLaunchKernelGGL(gain_grad_kernel, dim3(a.h / 4), dim3(1024), 0, s, a.partial, blocks, a.h, a.dq_gain, a.dk_gain);
   return hipGetLastError();
 }

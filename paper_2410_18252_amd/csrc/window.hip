@@ -87,6 +87,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 2) 
   const int G = a.Hq / a.Hkv;
   int unit, mt;
   if (!map_block(blockIdx.x, a.S * a.Hkv, tiles, unit, mt)) return;
+  mt = tiles - 1 - mt;                                             // (late rows see most)
   const int s = unit / a.Hkv, kvh = unit - s * a.Hkv;
   const Seq q = load_seq(a, s, PAGED);
   const int m0 = mt * BM, M = q.n * G;
@@ -152,8 +153,8 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 2) 
       }
     } else {
       const int rows = min(q.n - base, BN);
-      request_pieces<HD, BN>(k_rows.tile(base, rows), k_off, lds[buf][0], wave);
-      request_pieces<HD, BN>(v_rows.tile(base, rows), v_off, lds[buf][1], wave);
+      request_pieces(k_rows.tile(base, rows), k_off, lds[buf][0], wave);
+      request_pieces(v_rows.tile(base, rows), v_off, lds[buf][1], wave);
     }
   };
 
@@ -171,6 +172,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 2) 
   ColumnBase<HD> v_base = column_base<HD>(lane);
   v_base.all += lds_address(lds[0][1]);
   v_base.last += lds_address(lds[0][1]);
+  settle(qf);
   if (n_tiles > 0) {
     fetch_pages(0);
     request(0, 0);
@@ -179,6 +181,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 2) 
   for (int t = 0; t < n_tiles; ++t) {
     // this tile has landed, and nobody reads the other buffer any more
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if constexpr (PAGED) settle_words(page_of);
     if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
     if (t + 2 < n_tiles) fetch_pages(t + 2);
     const int kb = tile_key(t);
@@ -269,7 +272,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 2) 
 template <class T, int HD>
 hipError_t launch_rows(const WindowArgs& a, hipStream_t s) {
   const int tiles = (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
-  const dim3 grid(mapped_blocks((long long)a.S * a.Hkv, tiles));
+  const dim3 grid(mapped_blocks(a.S * a.Hkv, tiles));
   if (a.pages) hipLaunchKernelGGL((window_rows_kernel<T, HD, true>), grid, dim3(TPB), 0, s, a, tiles);
   else hipLaunchKernelGGL((window_rows_kernel<T, HD, false>), grid, dim3(TPB), 0, s, a, tiles);
   return hipGetLastError();

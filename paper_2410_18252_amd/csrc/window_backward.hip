@@ -13,7 +13,7 @@
 namespace {
 
 constexpr int TPB = 256, BM = 128;
-constexpr int DELTA_BLOCKS = 512;
+constexpr int DELTA_BLOCKS = 1024;
 constexpr float LOG2E = 1.4426950408889634f;
 
 // Everything below in the caller's workspace, and how the queries that see the sinks from beyond the window are parted.
@@ -23,42 +23,57 @@ struct Backward {
   int sinks, chunk, chunks;             // sinks that are parted (0: none); tokens to a part; parts of the longest sequence
 };
 
-// delta and lse log2 e, and for each block the largest |dout|
-template <class T>
+// delta and lse log2 e, and in fp16 for each block the largest |dout|.  Bound by HBM: out and dout once.
+template <class T, int CH>
 __global__ __launch_bounds__(TPB) void delta_kernel(Backward b) {
   __shared__ float red[4];
   const WindowArgs& a = b.a;
+  constexpr int AHEAD = 4 / CH;                // (row, head) pairs requested before the first is used
   const int li = threadIdx.x & 15;
-  const long long items = (long long)a.rows * a.Hq;
+  const long long items = (long long)a.rows * a.Hq, step = (long long)gridDim.x * 16;
   float peak = 0.f;
-  for (long long it = (long long)blockIdx.x * 16 + (threadIdx.x >> 4); it < items; it += (long long)gridDim.x * 16) {
-    const long long row = it / a.Hq;
-    const int head = (int)(it - row * a.Hq);
-    float v = 0.f;
+  for (long long it0 = (long long)blockIdx.x * 16 + (threadIdx.x >> 4); it0 < items; it0 += step * AHEAD) {
+    u32x4 o[AHEAD][CH], g[AHEAD][CH];
+    float lse[AHEAD];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int d = 128 * x + 8 * li;
-      if (d >= a.h) continue;
-      const u32x4 o = *(const u32x4*)((const uint16_t*)a.o + row * a.o_stride + (long long)head * a.h + d);
-      const u32x4 g = *(const u32x4*)((const uint16_t*)a.dout + row * a.dout_stride + (long long)head * a.h + d);
+    for (int u = 0; u < AHEAD; ++u) {
+      const long long it = it0 + u * step < items ? it0 + u * step : it0;
+      const long long row = it / a.Hq;
+      const long long head = (it - row * a.Hq) * a.h;
+      lse[u] = a.lse[it];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v = fmaf(T::low(o[e]), T::low(g[e]), v);
-        v = fmaf(T::high(o[e]), T::high(g[e]), v);
-        peak = fmaxf(peak, fmaxf(fabsf(T::low(g[e])), fabsf(T::high(g[e]))));
+      for (int x = 0; x < CH; ++x) {
+        const int d = 128 * x + 8 * li;
+        o[u][x] = d < a.h ? *(const u32x4*)((const uint16_t*)a.o + row * a.o_stride + head + d) : u32x4{0, 0, 0, 0};
+        g[u][x] = d < a.h ? *(const u32x4*)((const uint16_t*)a.dout + row * a.dout_stride + head + d) : u32x4{0, 0, 0, 0};
       }
     }
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor(v, o, WAVE);
-    if (li == 0) {
-      b.delta[it] = v;
-      b.lse2[it] = a.lse[it] * LOG2E;
+    for (int u = 0; u < AHEAD; ++u) {
+      float v = 0.f;
+#pragma unroll
+      for (int x = 0; x < CH; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v = fmaf(T::low(o[u][x][e]), T::low(g[u][x][e]), v);
+          v = fmaf(T::high(o[u][x][e]), T::high(g[u][x][e]), v);
+          if constexpr (__is_same(T, TypeF16)) peak = fmaxf(peak, fmaxf(fabsf(T::low(g[u][x][e])), fabsf(T::high(g[u][x][e]))));
+        }
+#pragma unroll
+      for (int s = 8; s > 0; s >>= 1) v += __shfl_xor(v, s, WAVE);
+      const long long it = it0 + u * step;
+      if (li == 0 && it < items) {
+        b.delta[it] = v;
+        b.lse2[it] = lse[u] * LOG2E;
+      }
     }
   }
-  peak = wave_max(peak);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = peak;
-  __syncthreads();
-  if (threadIdx.x == 0) b.peak[blockIdx.x] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  if constexpr (__is_same(T, TypeF16)) {
+    peak = wave_max(peak);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = peak;
+    __syncthreads();
+    if (threadIdx.x == 0) b.peak[blockIdx.x] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  }
 }
 
 // What fp16 multiplies dS by: 2^-3 over the power of two below the largest |dout|, so that neither a probability of 1e-5 vanishes nor a
@@ -78,31 +93,35 @@ __device__ __forceinline__ float ds_factor(const Backward& b) {
 // through LDS (q and dout, each read by rows for S = q K^T and dP = dout V^T, and transposed for dv^T = dout^T P and dk^T = q^T dS).
 // Sinks are seen by every query behind them: what lies beyond the window is parted over blocks of its own, whose sums meet in
 // sink_sum_kernel; else the block of the first keys would run for as long as all others together.
+// At 128 dims eight waves share a block's keys, the second four taking the second half of every tile of queries, and add up in LDS at the
+// end: a block's keys, whose queries are a long serial walk, then take half as long.
+template <int HD> constexpr int KEYS_HALVES = HD == 128 ? 2 : 1;
+
 template <class T, int HD>
-__global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void keys_backward_kernel(Backward b, int key_tiles, int jobs) {
+__global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, HD > 128 ? 1 : 2) void keys_backward_kernel(Backward b, int key_tiles, int jobs) {
   typedef typename T::vec8 vec8;
   const WindowArgs& a = b.a;
-  // Two waves to a SIMD hide each other's latencies, so a wave has 256 registers: from 128 dims on V waits in LDS instead, for which
-  // the tiles of queries are halved.
+  // Two waves to a SIMD hide each other's latencies, so a wave has 256 registers: from 128 dims on V waits in LDS instead.
   constexpr bool V_IN_LDS = HD >= 128;
-  constexpr int BQ = V_IN_LDS ? 32 : 64, SUB = BQ / 32, KS = HD / 16, DT = (HD + 31) / 32, TILE = BQ * HD;
-  typedef Pieces<HD, BQ> P;
+  constexpr int HALVES = KEYS_HALVES<HD>, WAVES = 4 * HALVES;
+  constexpr int BQ = HD > 128 ? 32 : 64, SUB = BQ / 32 / HALVES, KS = HD / 16, DT = (HD + 31) / 32, TILE = BQ * HD;
+  typedef Pieces<HD, BQ, WAVES> P;
   __shared__ __attribute__((aligned(256))) uint16_t lds[2][2][TILE];
   __shared__ __attribute__((aligned(256))) uint16_t v_tile[V_IN_LDS ? BM * HD : 128];
   __shared__ __attribute__((aligned(16))) float stat[2][3][64];            // of a tile's rows: lse log2 e, delta, position (bits)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int key_wave = HALVES > 1 ? wave & 3 : wave, half = HALVES > 1 ? wave >> 2 : 0;
   const int c = lane & 31, g = lane >> 5;
   const int G = a.Hq / a.Hkv;
   int unit, job;
   if (!map_block(blockIdx.x, a.S * a.Hkv, jobs, unit, job)) return;
-  job = jobs - 1 - job;
   const int s = unit / a.Hkv, kvh = unit - s * a.Hkv;
   const Seq q = load_seq(a, s, false);
   // which keys, and the tokens that the job adds up
-  int kt = job, tok0, tok1, slot = -1;
-  if (job >= key_tiles) {
-    kt = (job - key_tiles) / b.chunks;
-    slot = 1 + (job - key_tiles) % b.chunks;
+  int kt = job - (jobs - key_tiles), tok0, tok1, slot = -1;
+  if (kt < 0) {
+    kt = job / b.chunks;
+    slot = 1 + job % b.chunks;
     tok0 = kt * BM + BM - 1 + a.window + (slot - 1) * b.chunk;
     tok1 = min(tok0 + b.chunk, q.n);
     if (tok0 >= q.n) return;
@@ -113,7 +132,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void keys_backward_kernel(Ba
     if (a.window && (b.sinks > 0 || kt * BM >= a.sinks)) tok1 = (int)min((long long)q.n, (long long)kt * BM + BM - 1 + a.window);
     if (kt * BM < b.sinks) slot = 0;
   }
-  const int kw = kt * BM + wave * 32, key = kw + c;
+  const int kw = kt * BM + key_wave * 32, key = kw + c;
   const int M = q.n * G, m0 = tok0 * G, m1 = tok1 * G, n_tiles = (m1 - m0 + BQ - 1) / BQ;
   // the last position that sees this lane's key, from the key on (a position of -1 is beyond any)
   const uint32_t seen_by = a.window && key >= a.sinks ? a.window - 1 : 0x7fffffff - key;
@@ -132,23 +151,23 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void keys_backward_kernel(Ba
       if constexpr (!V_IN_LDS) vf[i] = d < a.h ? *(const vec8*)(vp + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
     }
     if constexpr (V_IN_LDS)
-      request_pieces<HD, BM>(row_source(a.v, q.row0, a.v_stride, kvh, 1, a.h).tile(kt * BM, min(q.n - kt * BM, BM)),
-                             piece_offsets<HD, BM>(wave, lane, a.v_stride, a.h), v_tile, wave);
+      request_pieces(row_source(a.v, q.row0, a.v_stride, kvh, 1, a.h).tile(kt * BM, min(q.n - kt * BM, BM)),
+                             piece_offsets<HD, BM, WAVES>(wave, lane, a.v_stride, a.h), v_tile, wave);
   }
   const float factor = ds_factor<T>(b);
   // where tiles begin with a group's first head they all have the same offsets
   const bool even = BQ % G == 0;
-  P q_off = flat_offsets<HD, BQ>(wave, lane, a.q_stride, a.h, G, 0), o_off = flat_offsets<HD, BQ>(wave, lane, a.dout_stride, a.h, G, 0);
+  P q_off = flat_offsets<HD, BQ, WAVES>(wave, lane, a.q_stride, a.h, G, 0), o_off = flat_offsets<HD, BQ, WAVES>(wave, lane, a.dout_stride, a.h, G, 0);
   const RowSource q_rows = row_source(a.q, q.row0, a.q_stride, kvh * G, G, a.h), o_rows = row_source(a.dout, q.row0, a.dout_stride, kvh * G, G, a.h);
   auto request = [&](int t, int buf) {
     const int base = m0 + t * BQ, tok_base = even ? tok0 + t * (BQ / G) : base / G;
     if (!even) {
-      q_off = flat_offsets<HD, BQ>(wave, lane, a.q_stride, a.h, G, base - tok_base * G);
-      o_off = flat_offsets<HD, BQ>(wave, lane, a.dout_stride, a.h, G, base - tok_base * G);
+      q_off = flat_offsets<HD, BQ, WAVES>(wave, lane, a.q_stride, a.h, G, base - tok_base * G);
+      o_off = flat_offsets<HD, BQ, WAVES>(wave, lane, a.dout_stride, a.h, G, base - tok_base * G);
     }
     const int rows = min(q.n - tok_base, BQ);
-    request_pieces<HD, BQ>(q_rows.tile(tok_base, rows), q_off, lds[buf][0], wave);
-    request_pieces<HD, BQ>(o_rows.tile(tok_base, rows), o_off, lds[buf][1], wave);
+    request_pieces(q_rows.tile(tok_base, rows), q_off, lds[buf][0], wave);
+    request_pieces(o_rows.tile(tok_base, rows), o_off, lds[buf][1], wave);
     if (wave < 3) {
       const int m = min(base + lane, M - 1), tok = m / G, head = kvh * G + m - tok * G;
       const long long at = (long long)(q.row0 + tok) * a.Hq + head;
@@ -163,8 +182,10 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void keys_backward_kernel(Ba
 #pragma unroll
     for (int i = 0; i < 16; ++i) dk[t][i] = dv[t][i] = 0.f;
   const float scale2 = a.scale * LOG2E;
-  const lds_t tiles = lds_address(lds[0][0]), by_row = row_base<HD>(lane), v_row = lds_address(v_tile) + wave * 32 * HD * 2 + by_row;
+  const lds_t tiles = lds_address(lds[0][0]) + half * SUB * 32 * HD * 2, by_row = row_base<HD>(lane), v_row = lds_address(v_tile) + key_wave * 32 * HD * 2 + by_row;
   const ColumnBase<HD> by_column = column_base<HD>(lane);
+  settle(kf);
+  if constexpr (!V_IN_LDS) settle(vf);
   if (n_tiles > 0) request(0, 0);
   for (int t = 0; t < n_tiles; ++t) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -173,7 +194,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void keys_backward_kernel(Ba
     const lds_t qt = tiles + (t & 1) * 4 * TILE, ot = qt + 2 * TILE;
 #pragma unroll
     for (int u = 0; u < SUB; ++u) {
-      const int base = m0 + t * BQ + 32 * u;
+      const int base = m0 + t * BQ + 32 * (half * SUB + u);
       if (base >= m1) break;
       const int p_lo = base / G, p_hi = min(base + 31, M - 1) / G;
       if (p_hi < kw || (a.window && kw + 31 <= p_lo - a.window && kw >= a.sinks)) continue;
@@ -192,7 +213,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void keys_backward_kernel(Ba
       u32x4 pw[2], sw[2];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int r = 32 * u + 8 * j + 4 * g;
+        const int r = 32 * (half * SUB + u) + 8 * j + 4 * g;
         const f32x4 lse2 = *(const f32x4*)&stat[t & 1][0][r], delta = *(const f32x4*)&stat[t & 1][1][r];
         float p[4], ds[4];
 #pragma unroll
@@ -221,6 +242,30 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void keys_backward_kernel(Ba
         for (int d = 0; d < DT; ++d) dk[d] = T::mfma32(column_frag<HD, vec8>(qc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, sw[v]), dk[d]);
       }
     }
+  }
+  if constexpr (HALVES > 1) {
+    // the second half's sums through LDS, first those of dv, then those of dk: a register of 64 lanes a 256-byte row
+    static_assert(sizeof(lds) >= 4 * DT * 16 * 64 * sizeof(float), "the tiles' place holds one gradient of four waves");
+    float* meet = (float*)lds + key_wave * DT * 16 * 64 + lane;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      f32x16(&x)[DT] = which ? dk : dv;
+      __syncthreads();
+      if (half == 1) {
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) meet[(t * 16 + i) * 64] = x[t][i];
+      }
+      __syncthreads();
+      if (half == 0) {
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[t][i] += meet[(t * 16 + i) * 64];
+      }
+    }
+    if (half == 1) return;
   }
   if (key >= q.n || (slot > 0 && key >= b.sinks)) return;
   const float back = a.scale / factor;
@@ -277,6 +322,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void queries_backward_kernel
   const int G = a.Hq / a.Hkv;
   int unit, mt;
   if (!map_block(blockIdx.x, a.S * a.Hkv, tiles, unit, mt)) return;
+  mt = tiles - 1 - mt;
   const int s = unit / a.Hkv, kvh = unit - s * a.Hkv;
   const Seq q = load_seq(a, s, false);
   const int m0 = mt * BM, M = q.n * G;
@@ -299,14 +345,15 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void queries_backward_kernel
     qf[i] = d < a.h ? *(const vec8*)((const uint16_t*)a.q + row * a.q_stride + (long long)head * a.h + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
     of[i] = d < a.h ? *(const vec8*)((const uint16_t*)a.dout + row * a.dout_stride + (long long)head * a.h + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
   }
-  const float lse2 = b.lse2[row * a.Hq + head], delta = b.delta[row * a.Hq + head], factor = ds_factor<T>(b);
+  float of_row[2] = {b.lse2[row * a.Hq + head], b.delta[row * a.Hq + head]};
+  const float factor = ds_factor<T>(b);
   const Pieces<HD, BN> k_off = piece_offsets<HD, BN>(wave, lane, a.k_stride, a.h), v_off = piece_offsets<HD, BN>(wave, lane, a.v_stride, a.h);
   const RowSource k_rows = row_source(a.k, q.row0, a.k_stride, kvh, 1, a.h), v_rows = row_source(a.v, q.row0, a.v_stride, kvh, 1, a.h);
   auto request = [&](int t, int buf) {
     const int base = tile_key(t);
     const int rows = min(q.n - base, BN);
-    request_pieces<HD, BN>(k_rows.tile(base, rows), k_off, lds[buf][0], wave);
-    request_pieces<HD, BN>(v_rows.tile(base, rows), v_off, lds[buf][1], wave);
+    request_pieces(k_rows.tile(base, rows), k_off, lds[buf][0], wave);
+    request_pieces(v_rows.tile(base, rows), v_off, lds[buf][1], wave);
   };
   f32x16 dq[DT];
 #pragma unroll
@@ -316,6 +363,10 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void queries_backward_kernel
   const float scale2 = a.scale * LOG2E;
   const lds_t tiles0 = lds_address(lds[0][0]), by_row = row_base<HD>(lane);
   const ColumnBase<HD> by_column = column_base<HD>(lane);
+  settle(qf);
+  settle(of);
+  settle_words(of_row);
+  const float lse2 = of_row[0], delta = of_row[1];
   if (n_tiles > 0) request(0, 0);
   for (int t = 0; t < n_tiles; ++t) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -402,10 +453,10 @@ size_t place(Backward& b, char* ws) {
 template <class T, int HD>
 hipError_t launch(const Backward& b, hipStream_t s) {
   const WindowArgs& a = b.a;
-  const long long units = (long long)a.S * a.Hkv;
+  const int units = a.S * a.Hkv;
   const int key_tiles = (a.max_new + BM - 1) / BM, jobs = key_tiles + (b.sinks + BM - 1) / BM * b.chunks;
-  hipLaunchKernelGGL((delta_kernel<T>), dim3(DELTA_BLOCKS), dim3(TPB), 0, s, b);
-  hipLaunchKernelGGL((keys_backward_kernel<T, HD>), dim3(mapped_blocks(units, jobs)), dim3(TPB), 0, s, b, key_tiles, jobs);
+  hipLaunchKernelGGL((delta_kernel<T, (HD > 128 ? 2 : 1)>), dim3(DELTA_BLOCKS), dim3(TPB), 0, s, b);
+  hipLaunchKernelGGL((keys_backward_kernel<T, HD>), dim3(mapped_blocks(units, jobs)), dim3(TPB * KEYS_HALVES<HD>), 0, s, b, key_tiles, jobs);
   if (b.sinks > 0) {
     const int per = (2 * b.sinks * (a.h / 4) + TPB - 1) / TPB;
     hipLaunchKernelGGL((sink_sum_kernel<T>), dim3((unsigned)units, per < 64 ? per : 64), dim3(TPB), 0, s, b);

@@ -61,16 +61,16 @@ template <int HD, class V8> __device__ __forceinline__ V8 column_frag(ColumnBase
   return r.whole;
 }
 
-// Requests of a tile straight into LDS, a kilobyte of it at a time dealt to the four waves: piece n of a wave is the 64 chunks from
-// (4 n + wave) 64 on, as they lie in the tile.  Rows lie `stride` elements apart behind a base common to the block, so a lane keeps one
+// Requests of a tile straight into LDS, a kilobyte of it at a time dealt to the WAVES waves of the block: piece n of a wave is the 64 chunks from
+// (WAVES n + wave) 64 on, as they lie in the tile.  Rows lie `stride` elements apart behind a base common to the block, so a lane keeps one
 // 32-bit offset a piece for the whole loop; the buffer's range check turns what lies past the last row into zeros, and
 // so it does with chunks past the head's dims, which are given an offset beyond any range.
 constexpr uint32_t OUT_OF_RANGE = 0x80000000u;
-template <int HD, int ROWS> struct Pieces {
-  static constexpr int CPR = HD / 8, ALL = ROWS * CPR / 64, PER = (ALL + 3) / 4;
+template <int HD, int ROWS, int WAVES = 4> struct Pieces {
+  static constexpr int CPR = HD / 8, ALL = ROWS * CPR / 64, PER = (ALL + WAVES - 1) / WAVES;
   uint32_t off[PER];
   static __device__ __forceinline__ void place(int n, int wave, int lane, int& row, int& dim) {
-    const int at = (n * 4 + wave) * 64 + lane;
+    const int at = (n * WAVES + wave) * 64 + lane;
     row = at / CPR;
     dim = ((at % CPR) ^ chunk_swap<HD>(row)) * 8;
   }
@@ -88,8 +88,8 @@ struct RowSource {
 __device__ __forceinline__ RowSource row_source(const void* base, int row0, long long stride, int head, int heads, int h) {
   return {(const uint16_t*)base + (long long)row0 * stride + (long long)head * h, (uint32_t)stride * 2, heads * h * 2};
 }
-template <int HD, int ROWS> __device__ __forceinline__ Pieces<HD, ROWS> piece_offsets(int wave, int lane, long long stride, int h) {
-  Pieces<HD, ROWS> p;
+template <int HD, int ROWS, int WAVES = 4> __device__ __forceinline__ Pieces<HD, ROWS, WAVES> piece_offsets(int wave, int lane, long long stride, int h) {
+  Pieces<HD, ROWS, WAVES> p;
 #pragma unroll
   for (int n = 0; n < p.PER; ++n) {
     int row, dim;
@@ -99,8 +99,9 @@ template <int HD, int ROWS> __device__ __forceinline__ Pieces<HD, ROWS> piece_of
   return p;
 }
 // Rows of the axis that queries and heads make: row rem + r of the tile is token (rem + r) / G, head (rem + r) % G behind the base's
-template <int HD, int ROWS> __device__ __forceinline__ Pieces<HD, ROWS> flat_offsets(int wave, int lane, long long stride, int h, int G, int rem) {
-  Pieces<HD, ROWS> p;
+template <int HD, int ROWS, int WAVES = 4>
+__device__ __forceinline__ Pieces<HD, ROWS, WAVES> flat_offsets(int wave, int lane, long long stride, int h, int G, int rem) {
+  Pieces<HD, ROWS, WAVES> p;
 #pragma unroll
   for (int n = 0; n < p.PER; ++n) {
     int row, dim;
@@ -128,11 +129,27 @@ __device__ __forceinline__ void request(const void* from, const void* to) {
 __device__ __forceinline__ void request_word(const float* from, const float* to) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(__builtin_amdgcn_readfirstlane(lds_address(to))) : "memory");
 }
-template <int HD, int ROWS>
-__device__ __forceinline__ void request_pieces(Buffer from, const Pieces<HD, ROWS>& p, const uint16_t* tile, int wave) {
+template <int HD, int ROWS, int WAVES>
+__device__ __forceinline__ void request_pieces(Buffer from, const Pieces<HD, ROWS, WAVES>& p, const uint16_t* tile, int wave) {
 #pragma unroll
   for (int n = 0; n < p.PER; ++n)
-    if (p.ALL % 4 == 0 || n * 4 + wave < p.ALL) request(from, p.off[n], tile + (n * 4 + wave) * 512);
+    if (p.ALL % WAVES == 0 || n * WAVES + wave < p.ALL) request(from, p.off[n], tile + (n * WAVES + wave) * 512);
+}
+
+// Has the wave wait for fragments that it loaded itself: in front of a loop, or the compiler waits inside it, where requests of the next
+// tile are on their way too.
+template <class V8, int N> __device__ __forceinline__ void settle(V8 (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    u32x4 w = __builtin_bit_cast(u32x4, f[i]);
+    asm volatile("" : "+v"(w));
+    f[i] = __builtin_bit_cast(V8, w);
+  }
+}
+
+template <class W, int N> __device__ __forceinline__ void settle_words(W (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
 }
 
 // Row of register i of a 32x32 result in lane group g (its column is lane % 32)
@@ -184,15 +201,22 @@ __device__ __forceinline__ Seq load_seq(const WindowArgs& a, int s, bool paged) 
   q.ctx = q.total - q.n;
   return q;
 }
-// Block -> (sequence, kv head) and tile.  Blocks go round the eight XCDs, each with an L2 of its own: the tiles of one unit, which read the
-// same keys, stay on one XCD.  Late tiles first where they see more.
-__device__ __forceinline__ bool map_block(int id, int units, int tiles, int& unit, int& tile) {
-  const int x = id & 7, y = id >> 3;
-  unit = y / tiles * 8 + x;
-  tile = tiles - 1 - y % tiles;
+// Block -> unit (sequence and kv head) and its job.  Blocks go round the eight XCDs, each with an L2 of its own: the jobs of one unit, which
+// read the same rows, stay on one XCD.  Jobs are numbered from the longest on.  Where an XCD has up to eight of them for each of its 32 CUs its
+// units go job by job, job 0 of each first, so that the launch ends with short ones (keys' side of three sequences of 1500 to 4000 tokens
+// on 8 kv heads 362 -> 329 us); with more of them one unit goes behind the other, which L2 is glad of (24 sequences of 257 to 576 tokens, 32
+// heads of size 80: forward 82 us, 89 job by job).
+__host__ __device__ inline int units_at_once(int units, int jobs) {
+  const int on_xcd = (units + 7) / 8;
+  return (long long)on_xcd * jobs <= 256 ? on_xcd : 1;
+}
+__device__ __forceinline__ bool map_block(int id, int units, int jobs, int& unit, int& job) {
+  const int at_once = units_at_once(units, jobs), x = id & 7, y = id >> 3, group = y / (at_once * jobs), r = y - group * at_once * jobs;
+  job = r / at_once;
+  unit = (group * at_once + r - job * at_once) * 8 + x;
   return unit < units;
 }
-inline unsigned mapped_blocks(long long units, long long tiles) { return (unsigned)((units + 7) / 8 * 8 * tiles); }
+inline unsigned mapped_blocks(int units, int jobs) { return (unsigned)((units + 7) / 8 * 8) * jobs; }      // (at_once is all or one)
 
 // The sign of a scale goes to the queries (their sign bits, exactly), so that the largest product has the largest score; a scale of zero
 // becomes one that every score vanishes under, since -infinity stands for masked scores.
