@@ -152,10 +152,13 @@ __global__ __launch_bounds__(TPB) void plan_pages_kernel(PlanArgs a) {
 }
 
 // ------------------------------------------------------------------ per-head norm and rotation
-// A head's vector sits in LPH lanes of a wave, eight dims to a lane; a lane keeps the same dims for all heads of a row, so the angles
-// of the row's position and the gains are loaded once.
+// A head's vector sits in LPH lanes of a wave, eight dims to a lane.  One or four waves take a row; their lane groups go through the
+// heads of it, first the queries', then the keys', then the values', AHEAD heads of a kind to a step, and the next step is requested before
+// the present one is used.  A lane keeps the same dims throughout, so a row's angles are loaded once and met with the gains (which wait in
+// LDS, each with its rotary partner's) once for each kind.
 template <class T> struct Eight;
 template <> struct Eight<float> {
+  typedef float word;
   f32x4 a, b;
   static __device__ __forceinline__ Eight load(const void* p, long long at) {
     const float* x = (const float*)p + at;
@@ -172,6 +175,9 @@ template <> struct Eight<float> {
     for (int e = 0; e < 4; ++e) { r.a[e] = __shfl(a[e], lane, WAVE); r.b[e] = __shfl(b[e], lane, WAVE); }
     return r;
   }
+  __device__ __forceinline__ void leave(float* lds) const { *(f32x4*)lds = a; *(f32x4*)(lds + 4) = b; }
+  static __device__ __forceinline__ float2 pair(const float* lds, int at) { return *(const float2*)(lds + at); }
+  static __device__ __forceinline__ float one(const float* lds, int at) { return lds[at]; }
   static __device__ __forceinline__ void store(void* p, long long at, const float* y) {
     float* x = (float*)p + at;
     *(f32x4*)x = f32x4{y[0], y[1], y[2], y[3]};
@@ -179,6 +185,7 @@ template <> struct Eight<float> {
   }
 };
 template <class T> struct Eight {
+  typedef uint16_t word;
   u32x4 w;
   static __device__ __forceinline__ Eight load(const void* p, long long at) { return {*(const u32x4*)((const uint16_t*)p + at)}; }
   static __device__ __forceinline__ Eight zero() { return {u32x4{0, 0, 0, 0}}; }
@@ -192,6 +199,12 @@ template <class T> struct Eight {
     for (int e = 0; e < 4; ++e) r.w[e] = __shfl(w[e], lane, WAVE);
     return r;
   }
+  __device__ __forceinline__ void leave(uint16_t* lds) const { *(u32x4*)lds = w; }
+  static __device__ __forceinline__ float2 pair(const uint16_t* lds, int at) {
+    const uint32_t v = *(const uint32_t*)(lds + at);
+    return make_float2(T::low(v), T::high(v));
+  }
+  static __device__ __forceinline__ float one(const uint16_t* lds, int at) { return T::low(lds[at]); }
   static __device__ __forceinline__ void store(void* p, long long at, const float* y) {
     u32x4 w;
 #pragma unroll
@@ -200,7 +213,8 @@ template <class T> struct Eight {
   }
 };
 
-// A lane's angles at one position: out = y c + (the rotary partner's y) t, t with the partner's sign; c = 1, t = 0 for dims past r
+__device__ __forceinline__ int rotary_partner(int d, int r) { return d < (r >> 1) ? d + (r >> 1) : d < r ? d - (r >> 1) : d; }
+// A lane's angles at one position: out = y c + (the partner's y) t, t with the partner's sign; c = 1, t = 0 for dims past r
 struct Angles { float c[8], t[8]; };
 __device__ __forceinline__ void load_angles(Angles& w, const float2* rope, int r, int pos, int d0, float sign) {
   const int half = r >> 1;
@@ -213,26 +227,43 @@ __device__ __forceinline__ void load_angles(Angles& w, const float2* rope, int r
     w.t[e] = d < half ? -sign * v.y : sign * v.y;
   }
 }
-// The rotary partners of a lane's eight values.  ALIGNED: half a rotation is whole lanes, else the vector goes through LDS.
-template <class T, bool ALIGNED>
-__device__ __forceinline__ void partners(const Eight<T>& x, float* y, float* lds, int d0, int r, int group_lane0) {
+// The rotary partners of AHEAD heads' values.  ALIGNED: half a rotation is whole lanes, which exchange their registers; else the rotated
+// lanes leave them in LDS and read them shifted, in pairs where half a rotation is even.
+template <class T, bool ALIGNED, int AHEAD, int LPH>
+__device__ __forceinline__ void partners(const Eight<T> (&x)[AHEAD], float (&y)[AHEAD][8], typename Eight<T>::word* lds, int d0, int r, int lane0) {
   const int half = r >> 1;
   if constexpr (ALIGNED) {
-    const int d = d0 < half ? d0 + half : d0 < r ? d0 - half : d0;
-    x.from_lane(group_lane0 + (d >> 3)).to(y);
-  } else {
-    float own[8];
-    x.to(own);
-    __builtin_amdgcn_wave_barrier();          // (the readers of what this overwrites are lanes of this wave)
+    const int from = lane0 + (rotary_partner(d0, r) >> 3);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) lds[d0 + e] = own[e];
+    for (int u = 0; u < AHEAD; ++u) x[u].from_lane(from).to(y[u]);
+  } else {
+    const bool turned = d0 < r;
+    __builtin_amdgcn_wave_barrier();          // (the readers of what this overwrites are lanes of this wave)
+    if (turned) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) x[u].leave(lds + u * LPH * 8 + d0);
+    }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int d = d0 + e;
-      y[e] = lds[d < half ? d + half : d < r ? d - half : d];
+    for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[u][e] = 0.f;
+    if (turned) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+        if (half & 1) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[u][e] = d0 + e < r ? Eight<T>::one(lds + u * LPH * 8, rotary_partner(d0 + e, r)) : 0.f;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const float2 v = d0 + e < r ? Eight<T>::pair(lds + u * LPH * 8, rotary_partner(d0 + e, r)) : make_float2(0.f, 0.f);
+            y[u][e] = v.x;
+            y[u][e + 1] = v.y;
+          }
+        }
     }
   }
 }
@@ -241,143 +272,203 @@ template <int LPH> __device__ __forceinline__ float group_sum(float v) {
   for (int o = LPH / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, WAVE);
   return v;
 }
+// One step of a row: AHEAD heads of one kind to a lane group
+enum { QUERIES, KEYS, VALUES };
+struct Step { int kind, first; };
+template <int AHEAD> __device__ __forceinline__ Step step_of(int j, int groups, int Hq, int Hkv) {
+  const int per = groups * AHEAD, nq = (Hq + per - 1) / per, nk = (Hkv + per - 1) / per;
+  return j < nq ? Step{QUERIES, j * per} : j < nq + nk ? Step{KEYS, (j - nq) * per} : Step{VALUES, (j - nq - nk) * per};
+}
+template <int AHEAD> __device__ __forceinline__ int steps_of(int groups, int Hq, int Hkv) {
+  const int per = groups * AHEAD;
+  return (Hq + per - 1) / per + 2 * ((Hkv + per - 1) / per);
+}
 
-// Bound by HBM: every head is read and written once.  A block takes a row, its lane groups the heads of it in turn, four heads
-// requested before the first is used.
+// Bound by HBM: every head is read and written once.
 template <class TI, class TO, int LPH, bool ALIGNED>
-__global__ __launch_bounds__(TPB) void norm_rope_kernel(NormRopeArgs a) {
-  constexpr int GPB = TPB / LPH, AHEAD = 4;
-  __shared__ float lds[ALIGNED ? 1 : GPB * LPH * 8];
-  const int li = threadIdx.x % LPH, grp = threadIdx.x / LPH, d0 = li * 8, lane0 = (threadIdx.x & 63) - li;
-  const bool on = d0 < a.h;
-  const int heads = a.Hq + 2 * a.Hkv;
-  const float inv_h = 1.0f / (float)a.h;
-  float gq[8], gk[8], pq[8], pk[8];            // gains of the lane's dims and of their partners
-  const int half = a.r >> 1;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int d = d0 + e, p = d < half ? d + half : d < a.r ? d - half : d;
-    gq[e] = on ? a.q_gain[d] : 0.f;
-    gk[e] = on ? a.k_gain[d] : 0.f;
-    pq[e] = on ? a.q_gain[p] : 0.f;
-    pk[e] = on ? a.k_gain[p] : 0.f;
+__global__ __launch_bounds__(TPB) void norm_rope_kernel(NormRopeArgs a, int row_waves) {
+  constexpr int AHEAD = 4;
+  typedef typename Eight<TI>::word word;
+  __shared__ __attribute__((aligned(16))) float gains[2][2][LPH * 8];            // of queries, keys: a dim's own, its partner's
+  __shared__ __attribute__((aligned(16))) word shift[ALIGNED ? 1 : TPB / LPH][ALIGNED ? 1 : AHEAD * LPH * 8];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int li = lane % LPH, d0 = li * 8, lane0 = lane - li;
+  for (int d = threadIdx.x; d < LPH * 8; d += TPB) {
+    const int p = rotary_partner(d, a.r);
+    gains[0][0][d] = d < a.h ? a.q_gain[d] : 0.f;
+    gains[0][1][d] = d < a.h ? a.q_gain[p] : 0.f;
+    gains[1][0][d] = d < a.h ? a.k_gain[d] : 0.f;
+    gains[1][1][d] = d < a.h ? a.k_gain[p] : 0.f;
   }
-  for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    Angles w;
-    load_angles(w, a.rope, on ? a.r : 0, min(max(a.positions[row], 0), a.max_pos - 1), d0, 1.f);
-    const long long src = (long long)row * a.qkv_stride;
-    int slot = -1;
-    if (a.pages) {
-      slot = a.slots[row];
-      if ((slot >> a.page_shift) >= a.n_pages) slot = -1;
+  __syncthreads();
+  const bool on = d0 < a.h;
+  const float inv_h = 1.0f / (float)a.h;
+  const int groups = row_waves * (64 / LPH), group = (wave & (row_waves - 1)) * (64 / LPH) + lane / LPH;
+  const int n_steps = steps_of<AHEAD>(groups, a.Hq, a.Hkv);
+  const int per_block = 4 / row_waves, row_step = gridDim.x * per_block;
+  auto load = [&](int row, int j, Eight<TI> (&x)[AHEAD]) {
+    const Step s = step_of<AHEAD>(j, groups, a.Hq, a.Hkv);
+    const int heads = s.kind == QUERIES ? a.Hq : a.Hkv, head0 = s.kind == QUERIES ? 0 : s.kind == KEYS ? a.Hq : a.Hq + a.Hkv;
+    const long long src = (long long)row * a.qkv_stride + (long long)head0 * a.h + d0;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int hd = s.first + u * groups + group;
+      x[u] = on && hd < heads ? Eight<TI>::load(a.qkv, src + (long long)hd * a.h) : Eight<TI>::zero();
     }
-    for (int h0 = grp; h0 < heads; h0 += GPB * AHEAD) {
-      Eight<TI> x[AHEAD];
+  };
+  int row = blockIdx.x * per_block + wave / row_waves;
+  if (row >= a.rows) return;
+  Eight<TI> x[AHEAD], x_next[AHEAD];
+  load(row, 0, x);
+  int pos = a.positions[row], slot = a.pages ? a.slots[row] : -1;
+  for (; row < a.rows; row += row_step) {
+    Angles w;
+    load_angles(w, a.rope, on ? a.r : 0, min(max(pos, 0), a.max_pos - 1), d0, 1.f);
+    const int page = slot >> a.page_shift, to_slot = slot >= 0 && page < a.n_pages ? slot : -1;
+    const int row_next = row + row_step;
+    if (row_next < a.rows) {
+      pos = a.positions[row_next];
+      if (a.pages) slot = a.slots[row_next];
+    }
+    float own[8], other[8];
+    int kind = -1;
+    for (int j = 0; j < n_steps; ++j) {
+      if (j + 1 < n_steps) load(row, j + 1, x_next);
+      else if (row_next < a.rows) load(row_next, 0, x_next);
+      const Step s = step_of<AHEAD>(j, groups, a.Hq, a.Hkv);
+      const int heads = s.kind == QUERIES ? a.Hq : a.Hkv;
+      if (s.kind != kind && s.kind != VALUES) {
+        kind = s.kind;
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        const int hd = h0 + u * GPB;
-        x[u] = on && hd < heads ? Eight<TI>::load(a.qkv, src + (long long)hd * a.h + d0) : Eight<TI>::zero();
+        for (int e = 0; e < 8; ++e) {
+          own[e] = gains[kind][0][d0 + e] * w.c[e];
+          other[e] = gains[kind][1][d0 + e] * w.t[e];
+        }
       }
+      float p[AHEAD][8];
+      if (s.kind != VALUES) partners<TI, ALIGNED, AHEAD, LPH>(x, p, shift[ALIGNED ? 0 : threadIdx.x / LPH], d0, a.r, lane0);
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
-        const int hd = h0 + u * GPB;
-        if (hd - grp >= heads) break;            // (the block's lanes go on together)
-        float y[8], p[8], ss = 0.f;
+        const int hd = s.first + u * groups + group;
+        float y[8];
         x[u].to(y);
+        if (s.kind != VALUES) {
+          float ss = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
-        const float inv = rsqrtf(fmaf(group_sum<LPH>(ss), inv_h, a.eps));
-        partners<TI, ALIGNED>(x[u], p, lds + (ALIGNED ? 0 : grp * LPH * 8), d0, a.r, lane0);
+          for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
+          const float inv = rsqrtf(fmaf(group_sum<LPH>(ss), inv_h, a.eps));
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = inv * fmaf(y[e], own[e], p[u][e] * other[e]);
+        }
         if (!on || hd >= heads) continue;
-        const bool is_q = hd < a.Hq, is_v = hd >= a.Hq + a.Hkv;
-        if (!is_v) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = y[e] * inv * (is_q ? gq[e] : gk[e]) * w.c[e] + p[e] * inv * (is_q ? pq[e] : pk[e]) * w.t[e];
-        }
-        if (is_q) {
+        if (s.kind == QUERIES) {
           Eight<TO>::store(a.q, (long long)row * a.q_stride + (long long)hd * a.h + d0, y);
-        } else {
-          const int kvh = hd - a.Hq - (is_v ? a.Hkv : 0);
-          if (slot >= 0) {
-            const long long at = ((((long long)(slot >> a.page_shift) * 2 + (is_v ? 1 : 0)) * a.Hkv + kvh) << a.page_shift) + (slot & ((1 << a.page_shift) - 1));
-            Eight<TO>::store(a.pages, at * a.h + d0, y);
-          }
-          void* dst = is_v ? a.v : a.k;
-          if (dst) Eight<TO>::store(dst, (long long)row * (is_v ? a.v_stride : a.k_stride) + (long long)kvh * a.h + d0, y);
+          continue;
         }
+        const int which = s.kind == VALUES;
+        if (to_slot >= 0) {
+          const long long at = ((((long long)page * 2 + which) * a.Hkv + hd) << a.page_shift) + (to_slot & ((1 << a.page_shift) - 1));
+          Eight<TO>::store(a.pages, at * a.h + d0, y);
+        }
+        void* dst = which ? a.v : a.k;
+        if (dst) Eight<TO>::store(dst, (long long)row * (which ? a.v_stride : a.k_stride) + (long long)hd * a.h + d0, y);
       }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) x[u] = x_next[u];
     }
   }
 }
 
-// Gradients: the vectors of a head as above.  The gains' gradients are sums over all rows and heads: every lane keeps those of its dims
-// in registers over all rows of its block, the lane groups of the block meet in LDS in their order, and a second launch adds up the
-// blocks, so that a result does not depend on which block came first.
+// Gradients: the same walk over x and the incoming gradients.  The gains' gradients are sums over all rows and heads: every lane keeps
+// those of its dims in registers over all its rows, the lane groups of the block meet in LDS in their order, and a second launch adds up
+// the blocks, so that a result does not depend on which block came first.
 template <class TI, class TO, int LPH, bool ALIGNED>
-__global__ __launch_bounds__(TPB) void norm_rope_backward_kernel(NormRopeArgs a) {
-  constexpr int GPB = TPB / LPH, AHEAD = 2;
-  __shared__ float lds[GPB * LPH * 8];
-  const int li = threadIdx.x % LPH, grp = threadIdx.x / LPH, d0 = li * 8, lane0 = (threadIdx.x & 63) - li;
-  const bool on = d0 < a.h;
-  const int heads = a.Hq + 2 * a.Hkv;
-  const float inv_h = 1.0f / (float)a.h;
-  float gq[8], gk[8], sum_q[8], sum_k[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    gq[e] = on ? a.q_gain[d0 + e] : 0.f;
-    gk[e] = on ? a.k_gain[d0 + e] : 0.f;
-    sum_q[e] = sum_k[e] = 0.f;
+__global__ __launch_bounds__(TPB) void norm_rope_backward_kernel(NormRopeArgs a, int row_waves) {
+  constexpr int AHEAD = 2;
+  typedef typename Eight<TO>::word word;
+  __shared__ __attribute__((aligned(16))) float gains[2][LPH * 8];
+  __shared__ __attribute__((aligned(16))) float sums[TPB / LPH][LPH * 8];
+  __shared__ __attribute__((aligned(16))) word shift[ALIGNED ? 1 : TPB / LPH][ALIGNED ? 1 : AHEAD * LPH * 8];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int li = lane % LPH, d0 = li * 8, lane0 = lane - li;
+  for (int d = threadIdx.x; d < LPH * 8; d += TPB) {
+    gains[0][d] = d < a.h ? a.q_gain[d] : 0.f;
+    gains[1][d] = d < a.h ? a.k_gain[d] : 0.f;
   }
-  for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
+  __syncthreads();
+  const bool on = d0 < a.h;
+  const float inv_h = 1.0f / (float)a.h;
+  const int groups = row_waves * (64 / LPH), group = (wave & (row_waves - 1)) * (64 / LPH) + lane / LPH;
+  const int n_steps = steps_of<AHEAD>(groups, a.Hq, a.Hkv);
+  const int per_block = 4 / row_waves, row_step = gridDim.x * per_block;
+  auto load = [&](int row, int j, Eight<TI> (&x)[AHEAD], Eight<TO> (&g)[AHEAD]) {
+    const Step s = step_of<AHEAD>(j, groups, a.Hq, a.Hkv);
+    const int heads = s.kind == QUERIES ? a.Hq : a.Hkv;
+    const void* from = s.kind == QUERIES ? a.dq : s.kind == KEYS ? a.dk : a.dv;
+    const long long at = (long long)row * (s.kind == QUERIES ? a.dq_stride : s.kind == KEYS ? a.dk_stride : a.dv_stride) + d0;
+    const long long src = (long long)row * a.qkv_stride + (s.kind == QUERIES ? 0ll : (long long)a.Hq * a.h) + d0;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int hd = s.first + u * groups + group;
+      const bool live = on && hd < heads;
+      x[u] = live && s.kind != VALUES ? Eight<TI>::load(a.qkv, src + (long long)hd * a.h) : Eight<TI>::zero();
+      g[u] = live ? Eight<TO>::load(from, at + (long long)hd * a.h) : Eight<TO>::zero();
+    }
+  };
+  float sum_q[8], sum_k[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum_q[e] = sum_k[e] = 0.f;
+  int row = blockIdx.x * per_block + wave / row_waves;
+  Eight<TI> x[AHEAD], x_next[AHEAD];
+  Eight<TO> g[AHEAD], g_next[AHEAD];
+  int pos = 0;
+  if (row < a.rows) {
+    load(row, 0, x, g);
+    pos = a.positions[row];
+  }
+  for (; row < a.rows; row += row_step) {
     Angles w;
-    load_angles(w, a.rope, on ? a.r : 0, min(max(a.positions[row], 0), a.max_pos - 1), d0, -1.f);
-    for (int h0 = grp; h0 < heads; h0 += GPB * AHEAD) {
-      Eight<TI> x[AHEAD];
-      Eight<TO> g[AHEAD];
+    load_angles(w, a.rope, on ? a.r : 0, min(max(pos, 0), a.max_pos - 1), d0, -1.f);
+    const int row_next = row + row_step;
+    if (row_next < a.rows) pos = a.positions[row_next];
+    for (int j = 0; j < n_steps; ++j) {
+      if (j + 1 < n_steps) load(row, j + 1, x_next, g_next);
+      else if (row_next < a.rows) load(row_next, 0, x_next, g_next);
+      const Step s = step_of<AHEAD>(j, groups, a.Hq, a.Hkv);
+      const int heads = s.kind == QUERIES ? a.Hq : a.Hkv, head0 = s.kind == QUERIES ? 0 : s.kind == KEYS ? a.Hq : a.Hq + a.Hkv;
+      float p[AHEAD][8];
+      if (s.kind != VALUES) partners<TO, ALIGNED, AHEAD, LPH>(g, p, shift[ALIGNED ? 0 : threadIdx.x / LPH], d0, a.r, lane0);
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
-        const int hd = h0 + u * GPB;
-        const bool is_q = hd < a.Hq, is_v = hd >= a.Hq + a.Hkv;
-        x[u] = on && hd < heads && !is_v ? Eight<TI>::load(a.qkv, (long long)row * a.qkv_stride + (long long)hd * a.h + d0) : Eight<TI>::zero();
-        const void* src = is_q ? a.dq : is_v ? a.dv : a.dk;
-        const long long at = (long long)row * (is_q ? a.dq_stride : is_v ? a.dv_stride : a.dk_stride) + (long long)(is_q ? hd : is_v ? hd - a.Hq - a.Hkv : hd - a.Hq) * a.h + d0;
-        g[u] = on && hd < heads ? Eight<TO>::load(src, at) : Eight<TO>::zero();
-      }
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        const int hd = h0 + u * GPB;
-        if (hd - grp >= heads) break;
-        const bool is_q = hd < a.Hq, is_v = hd >= a.Hq + a.Hkv;
-        float y[8], d[8], p[8], ss = 0.f, tx = 0.f;
-        x[u].to(y);
+        const int hd = s.first + u * groups + group;
+        float d[8];
         g[u].to(d);
-        partners<TO, ALIGNED>(g[u], p, lds + grp * LPH * 8, d0, a.r, lane0);
-        float out[8];
-        if (!is_v) {
+        if (s.kind != VALUES) {
+          float y[8], t[8], ss = 0.f, tx = 0.f;
+          x[u].to(y);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            d[e] = fmaf(d[e], w.c[e], p[e] * w.t[e]);
-            out[e] = d[e] * (is_q ? gq[e] : gk[e]);
+            d[e] = fmaf(d[e], w.c[e], p[u][e] * w.t[e]);
+            t[e] = d[e] * gains[s.kind][d0 + e];
             ss = fmaf(y[e], y[e], ss);
-            tx = fmaf(out[e], y[e], tx);
+            tx = fmaf(t[e], y[e], tx);
           }
-        }
-        ss = group_sum<LPH>(ss);
-        tx = group_sum<LPH>(tx);
-        if (!on || hd >= heads) continue;
-        if (is_v) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) out[e] = d[e];
-        } else {
+          ss = group_sum<LPH>(ss);
+          tx = group_sum<LPH>(tx);
           const float inv = rsqrtf(fmaf(ss, inv_h, a.eps)), back = inv * inv * tx * inv_h;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const float dg = d[e] * (y[e] * inv);
-            if (is_q) sum_q[e] += dg; else sum_k[e] += dg;
-            out[e] = inv * (out[e] - y[e] * back);
+            if (s.kind == QUERIES) sum_q[e] += dg; else sum_k[e] += dg;
+            d[e] = inv * (t[e] - y[e] * back);
           }
         }
-        Eight<TI>::store(a.dqkv, (long long)row * a.dqkv_stride + (long long)hd * a.h + d0, out);
+        if (on && hd < heads) Eight<TI>::store(a.dqkv, (long long)row * a.dqkv_stride + (long long)(head0 + hd) * a.h + d0, d);
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        x[u] = x_next[u];
+        g[u] = g_next[u];
       }
     }
   }
@@ -385,11 +476,11 @@ __global__ __launch_bounds__(TPB) void norm_rope_backward_kernel(NormRopeArgs a)
   for (int which = 0; which < 2; ++which) {
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < 8; ++e) lds[grp * LPH * 8 + d0 + e] = which ? sum_k[e] : sum_q[e];
+    for (int e = 0; e < 8; ++e) sums[threadIdx.x / LPH][d0 + e] = which ? sum_k[e] : sum_q[e];
     __syncthreads();
     for (int d = threadIdx.x; d < a.h; d += TPB) {
       float v = 0.f;
-      for (int g = 0; g < GPB; ++g) v += lds[g * LPH * 8 + d];
+      for (int i = 0; i < TPB / LPH; ++i) v += sums[i][d];
       a.partial[((size_t)blockIdx.x * 2 + which) * a.h + d] = v;
     }
   }
@@ -414,35 +505,40 @@ __global__ __launch_bounds__(1024) void gain_grad_kernel(const float* partial, i
   }
 }
 
+// Blocks, and waves to a row.  Four waves share a row while rows are fewer than waves that the CUs hold.
+struct Launch { int blocks, row_waves; };
+Launch norm_rope_launch(int rows, bool backward) {
+  const int row_waves = rows < 4096 ? 4 : 1, blocks = (int)(((long long)rows * row_waves + 3) / 4), most = backward ? 1024 : 2048;
+  return {blocks < most ? blocks : most, row_waves};
+}
 template <class TI, class TO, int LPH>
-hipError_t launch_norm_rope(const NormRopeArgs& a, bool backward, int blocks, hipStream_t s) {
+hipError_t launch_norm_rope(const NormRopeArgs& a, bool backward, Launch l, hipStream_t s) {
   const bool aligned = (a.r >> 1) % 8 == 0;
+  const dim3 grid(l.blocks), block(TPB);
   if (backward) {
-    if (aligned) hipLaunchKernelGGL((norm_rope_backward_kernel<TI, TO, LPH, true>), dim3(blocks), dim3(TPB), 0, s, a);
-    else hipLaunchKernelGGL((norm_rope_backward_kernel<TI, TO, LPH, false>), dim3(blocks), dim3(TPB), 0, s, a);
+    if (aligned) hipLaunchKernelGGL((norm_rope_backward_kernel<TI, TO, LPH, true>), grid, block, 0, s, a, l.row_waves);
+    else hipLaunchKernelGGL((norm_rope_backward_kernel<TI, TO, LPH, false>), grid, block, 0, s, a, l.row_waves);
   } else {
-    if (aligned) hipLaunchKernelGGL((norm_rope_kernel<TI, TO, LPH, true>), dim3(blocks), dim3(TPB), 0, s, a);
-    else hipLaunchKernelGGL((norm_rope_kernel<TI, TO, LPH, false>), dim3(blocks), dim3(TPB), 0, s, a);
+    if (aligned) hipLaunchKernelGGL((norm_rope_kernel<TI, TO, LPH, true>), grid, block, 0, s, a, l.row_waves);
+    else hipLaunchKernelGGL((norm_rope_kernel<TI, TO, LPH, false>), grid, block, 0, s, a, l.row_waves);
   }
   return hipGetLastError();
 }
 template <class TI, class TO>
-hipError_t by_head(const NormRopeArgs& a, bool backward, int blocks, hipStream_t s) {
-  if (a.h <= 64) return launch_norm_rope<TI, TO, 8>(a, backward, blocks, s);
-  if (a.h <= 128) return launch_norm_rope<TI, TO, 16>(a, backward, blocks, s);
-  return launch_norm_rope<TI, TO, 32>(a, backward, blocks, s);
+hipError_t by_head(const NormRopeArgs& a, bool backward, Launch l, hipStream_t s) {
+  if (a.h <= 64) return launch_norm_rope<TI, TO, 8>(a, backward, l, s);
+  if (a.h <= 128) return launch_norm_rope<TI, TO, 16>(a, backward, l, s);
+  return launch_norm_rope<TI, TO, 32>(a, backward, l, s);
 }
-hipError_t by_type(const NormRopeArgs& a, bool backward, int blocks, hipStream_t s) {
+hipError_t by_type(const NormRopeArgs& a, bool backward, Launch l, hipStream_t s) {
   const bool f16 = a.dtype == RLGEN_DTYPE_F16;
   switch (a.src_dtype) {
-    case RLGEN_DTYPE_F32: return f16 ? by_head<float, TypeF16>(a, backward, blocks, s) : by_head<float, TypeBf16>(a, backward, blocks, s);
-    case RLGEN_DTYPE_BF16: return f16 ? by_head<TypeBf16, TypeF16>(a, backward, blocks, s) : by_head<TypeBf16, TypeBf16>(a, backward, blocks, s);
-    case RLGEN_DTYPE_F16: return f16 ? by_head<TypeF16, TypeF16>(a, backward, blocks, s) : by_head<TypeF16, TypeBf16>(a, backward, blocks, s);
+    case RLGEN_DTYPE_F32: return f16 ? by_head<float, TypeF16>(a, backward, l, s) : by_head<float, TypeBf16>(a, backward, l, s);
+    case RLGEN_DTYPE_BF16: return f16 ? by_head<TypeBf16, TypeF16>(a, backward, l, s) : by_head<TypeBf16, TypeBf16>(a, backward, l, s);
+    case RLGEN_DTYPE_F16: return f16 ? by_head<TypeF16, TypeF16>(a, backward, l, s) : by_head<TypeF16, TypeBf16>(a, backward, l, s);
     default: return hipErrorInvalidValue;
   }
 }
-// blocks of the backward pass: enough for every CU to hold four, few enough for the sums of their partial gains
-int backward_blocks(int rows) { return rows < 1024 ? rows : 1024; }
 
 }  // namespace
 
@@ -460,15 +556,15 @@ hipError_t rl_plan_pages(PlanArgs a, hipStream_t s) {
 }
 hipError_t rl_norm_rope(const NormRopeArgs& a, hipStream_t s) {
   if (a.rows <= 0) return hipSuccess;
-  return by_type(a, false, a.rows < 65536 ? a.rows : 65536, s);
+  return by_type(a, false, norm_rope_launch(a.rows, false), s);
 }
-size_t rl_norm_rope_backward_bytes(int rows, int h) { return (size_t)backward_blocks(rows < 1 ? 1 : rows) * 2 * h * sizeof(float); }
+size_t rl_norm_rope_backward_bytes(int rows, int h) { return (size_t)norm_rope_launch(rows < 1 ? 1 : rows, true).blocks * 2 * h * sizeof(float); }
 hipError_t rl_norm_rope_backward(const NormRopeArgs& a, hipStream_t s) {
-  const int blocks = backward_blocks(a.rows);
-  if (blocks > 0) {
-    const hipError_t e = by_type(a, true, blocks, s);
+  const Launch l = norm_rope_launch(a.rows, true);
+  if (l.blocks > 0) {
+    const hipError_t e = by_type(a, true, l, s);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(gain_grad_kernel, dim3(a.h / 4), dim3(1024), 0, s, a.partial, blocks, a.h, a.dq_gain, a.dk_gain);
+  hipLaunchKernelGGL(gain_grad_kernel, dim3(a.h / 4), dim3(1024), 0, s, a.partial, l.blocks, a.h, a.dq_gain, a.dk_gain);
   return hipGetLastError();
 }
