@@ -286,8 +286,8 @@ template <int AHEAD> __device__ __forceinline__ int steps_of(int groups, int Hq,
 
 // Bound by HBM: every head is read and written once.
 template <class TI, class TO, int LPH, bool ALIGNED>
-__global__ __launch_bounds__(TPB) void norm_rope_kernel(NormRopeArgs a, int row_waves) {
-  constexpr int AHEAD = 4;
+__global__ __launch_bounds__(TPB, sizeof(typename Eight<TI>::word) == 2 ? 4 : 3) void norm_rope_kernel(NormRopeArgs a, int row_waves) {
+  constexpr int AHEAD = 2;
   typedef typename Eight<TI>::word word;
   __shared__ __attribute__((aligned(16))) float gains[2][2][LPH * 8];            // of queries, keys: a dim's own, its partner's
   __shared__ __attribute__((aligned(16))) word shift[ALIGNED ? 1 : TPB / LPH][ALIGNED ? 1 : AHEAD * LPH * 8];
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(TPB) void norm_rope_kernel(NormRopeArgs a, int row_
 // the blocks, so that a result does not depend on which block came first.
 template <class TI, class TO, int LPH, bool ALIGNED>
 __global__ __launch_bounds__(TPB) void norm_rope_backward_kernel(NormRopeArgs a, int row_waves) {
-  constexpr int AHEAD = 2;
+  constexpr int AHEAD = 1;
   typedef typename Eight<TO>::word word;
   __shared__ __attribute__((aligned(16))) float gains[2][LPH * 8];
   __shared__ __attribute__((aligned(16))) float sums[TPB / LPH][LPH * 8];
@@ -507,9 +507,10 @@ __global__ __launch_bounds__(1024) void gain_grad_kernel(const float* partial, i
 
 // Blocks, and waves to a row.  Four waves share a row while rows are fewer than waves that the CUs hold.
 struct Launch { int blocks, row_waves; };
-Launch norm_rope_launch(int rows, bool backward) {
-  const int row_waves = rows < 4096 ? 4 : 1, blocks = (int)(((long long)rows * row_waves + 3) / 4), most = backward ? 1024 : 2048;
-  return {blocks < most ? blocks : most, row_waves};
+Launch norm_rope_launch(int rows) {
+  const int row_waves = rows < 4096 ? 4 : 1;
+  const long long blocks = ((long long)rows * row_waves + 3) / 4;
+  return {(int)(blocks < 1024 ? blocks : 1024), row_waves};
 }
 template <class TI, class TO, int LPH>
 hipError_t launch_norm_rope(const NormRopeArgs& a, bool backward, Launch l, hipStream_t s) {
@@ -556,11 +557,11 @@ hipError_t rl_plan_pages(PlanArgs a, hipStream_t s) {
 }
 hipError_t rl_norm_rope(const NormRopeArgs& a, hipStream_t s) {
   if (a.rows <= 0) return hipSuccess;
-  return by_type(a, false, norm_rope_launch(a.rows, false), s);
+  return by_type(a, false, norm_rope_launch(a.rows), s);
 }
-size_t rl_norm_rope_backward_bytes(int rows, int h) { return (size_t)norm_rope_launch(rows < 1 ? 1 : rows, true).blocks * 2 * h * sizeof(float); }
+size_t rl_norm_rope_backward_bytes(int rows, int h) { return (size_t)norm_rope_launch(rows < 1 ? 1 : rows).blocks * 2 * h * sizeof(float); }
 hipError_t rl_norm_rope_backward(const NormRopeArgs& a, hipStream_t s) {
-  const Launch l = norm_rope_launch(a.rows, true);
+  const Launch l = norm_rope_launch(a.rows);
   if (l.blocks > 0) {
     const hipError_t e = by_type(a, true, l, s);
     if (e != hipSuccess) return e;

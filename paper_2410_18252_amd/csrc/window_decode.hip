@@ -239,47 +239,48 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void window_decode_kernel(Wi
   }
 }
 
-// Adds up the parts of a query head, in their order: 64 lanes along the dims, the four waves a part each in turn.
+// Adds up the parts of a query head, in their order: a block takes 64 dims, lane d one of them, the waves a part each in turn.  A part's
+// share of the sum depends on its maximum alone, so all loads of eight parts are on their way at once.
 template <class T>
 __global__ __launch_bounds__(TPB) void window_join_kernel(WindowArgs a, int parts) {
-  __shared__ float part_sum[4][256];
-  __shared__ float weight_sum[4];
+  __shared__ float part_sum[4][64];
   const int s = blockIdx.x / a.Hq, head = blockIdx.x - s * a.Hq;
   const Seq q = load_seq(a, s, true);
   if (q.n < 1) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.y * 64 + lane;
   const float* po = (const float*)a.ws;
   const Part* pm = (const Part*)(po + (long long)a.S * a.Hq * parts * a.h);
   const long long slot = ((long long)s * a.Hq + head) * parts;
-  float m = -INFINITY;
-  for (int p = lane; p < parts; p += 64) m = fmaxf(m, pm[slot + p].m);
-  m = wave_max(m);
-  const float base = m == -INFINITY ? 0.f : m;
-  float y[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
-  for (int p = wave; p < parts; p += 4) {
-    const float f = __builtin_amdgcn_exp2f(pm[slot + p].m - base);
-    l = fmaf(pm[slot + p].l, f, l);
+  // (at most 64 parts)
+  const Part mine = lane < parts ? pm[slot + lane] : Part{-INFINITY, 0.f};
+  float y = 0.f;
+  constexpr int AHEAD = 8;
+  float v[2][AHEAD];
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (lane + 64 * e < a.h) y[e] = fmaf(po[(slot + p) * a.h + lane + 64 * e], f, y[e]);
-  }
+  for (int half = 0; half < 2; ++half)
 #pragma unroll
-  for (int e = 0; e < 4; ++e) part_sum[wave][lane + 64 * e] = y[e];
-  if (lane == 0) weight_sum[wave] = l;
+    for (int i = 0; i < AHEAD; ++i) {
+      const int p = wave + 4 * (half * AHEAD + i);
+      v[half][i] = p < parts && d < a.h ? po[(slot + p) * a.h + d] : 0.f;
+    }
+  const float m = wave_max(mine.m), base = m == -INFINITY ? 0.f : m, f = __builtin_amdgcn_exp2f(mine.m - base);
+#pragma unroll
+  for (int half = 0; half < 2; ++half)
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) y = fmaf(v[half][i], __shfl(f, min(wave + 4 * (half * AHEAD + i), 63), WAVE), y);
+  part_sum[wave][lane] = y;
+  const float l = wave_sum(mine.l * f);
   __syncthreads();
-  l = weight_sum[0] + weight_sum[1] + weight_sum[2] + weight_sum[3];
-  const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
-  const int d = threadIdx.x * 2;
-  if (d < a.h) {
-    float v[2];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) v[e] = (part_sum[0][d + e] + part_sum[1][d + e] + part_sum[2][d + e] + part_sum[3][d + e]) * inv;
-    *(uint32_t*)((uint16_t*)a.out + (long long)q.row0 * a.out_stride + (long long)head * a.h + d) = T::pack(v[0], v[1]);
+  if (wave == 0 && d < a.h) {
+    const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
+    const float sum = (part_sum[0][lane] + part_sum[1][lane] + part_sum[2][lane] + part_sum[3][lane]) * inv;
+    ((uint16_t*)a.out)[(long long)q.row0 * a.out_stride + (long long)head * a.h + d] = (uint16_t)T::pack(sum, 0.f);
+    if (d == 0 && a.lse) a.lse[(long long)q.row0 * a.Hq + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
   }
-  if (threadIdx.x == 0 && a.lse) a.lse[(long long)q.row0 * a.Hq + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 // Waves to a job and blocks to a job
+constexpr int MAX_PARTS = 64;                 // (window_join_kernel's lanes)
 struct Split { int waves, parts, col_blocks; };
 Split decode_split(const WindowArgs& a) {
   const int G = a.Hq / a.Hkv, cb = a.h > 128 ? 8 : 16;
@@ -292,7 +293,7 @@ Split decode_split(const WindowArgs& a) {
   r.waves = 4;
   long long parts = (512 + jobs - 1) / jobs, most = (groups + 7) / 8;
   if (parts > most) parts = most;
-  if (parts > 64) parts = 64;
+  if (parts > MAX_PARTS) parts = MAX_PARTS;
   r.parts = parts < 1 ? 1 : (int)parts;
   return r;
 }
@@ -310,7 +311,7 @@ hipError_t launch(const WindowArgs& a, hipStream_t s) {
     if (r.parts > 1) {
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
-      hipLaunchKernelGGL((window_join_kernel<T>), dim3((unsigned)(a.S * a.Hq)), dim3(TPB), 0, s, a, r.parts);
+      hipLaunchKernelGGL((window_join_kernel<T>), dim3((unsigned)(a.S * a.Hq), (a.h + 63) / 64), dim3(TPB), 0, s, a, r.parts);
     }
   }
   return hipGetLastError();
