@@ -6,7 +6,7 @@
 // seven matrix products instead of the five that one kernel with atomic sums would need, but every sum has one order, so that results do
 // not change from run to run.  P and dS are rounded to the inputs' type for their second products, errors of the order of the
 // gradients' own rounding; fp16, whose smallest normal number a dS easily falls below, multiplies dS by a power of two taken from the
-// largest |dout|.
+// largest |dout| and |v|.
 #include "../../include/rlgen.h"
 #include "window_tiles.h"
 
@@ -15,23 +15,25 @@ namespace {
 constexpr int TPB = 256, BM = 128;
 constexpr int DELTA_BLOCKS = 1024;
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr int FEW_KEYS = 16;
 
 // Everything below in the caller's workspace, and how the queries that see the sinks from beyond the window are parted.
 struct Backward {
   WindowArgs a;
-  float *lse2, *delta, *peak, *part;    // [rows, Hq]: lse log2 e, delta; the largest |dout| of each block; the sinks' parts
+  float *lse2, *delta, *peak, *part;    // [rows, Hq]: lse log2 e, delta; the largest |dout| and |v| of each block; the sinks' parts
   int sinks, chunk, chunks;             // sinks that are parted (0: none); tokens to a part; parts of the longest sequence
 };
 
-// delta and lse log2 e, and in fp16 for each block the largest |dout|.  Bound by HBM: out and dout once.
+// delta and lse log2 e, and in fp16 for each block the largest |dout| and |v|.  Bound by HBM: out and dout (and
+// v) once.
 template <class T, int CH>
 __global__ __launch_bounds__(TPB) void delta_kernel(Backward b) {
-  __shared__ float red[4];
+  __shared__ float red[2][4];
   const WindowArgs& a = b.a;
   constexpr int AHEAD = 4 / CH;                // (row, head) pairs requested before the first is used
   const int li = threadIdx.x & 15;
   const long long items = (long long)a.rows * a.Hq, step = (long long)gridDim.x * 16;
-  float peak = 0.f;
+  float peak[2] = {0.f, 0.f};
   for (long long it0 = (long long)blockIdx.x * 16 + (threadIdx.x >> 4); it0 < items; it0 += step * AHEAD) {
     u32x4 o[AHEAD][CH], g[AHEAD][CH];
     float lse[AHEAD];
@@ -55,9 +57,10 @@ __global__ __launch_bounds__(TPB) void delta_kernel(Backward b) {
       for (int x = 0; x < CH; ++x)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          v = fmaf(T::low(o[u][x][e]), T::low(g[u][x][e]), v);
-          v = fmaf(T::high(o[u][x][e]), T::high(g[u][x][e]), v);
-          if constexpr (__is_same(T, TypeF16)) peak = fmaxf(peak, fmaxf(fabsf(T::low(g[u][x][e])), fabsf(T::high(g[u][x][e]))));
+          const float lo = T::low(g[u][x][e]), hi = T::high(g[u][x][e]);
+          v = fmaf(T::low(o[u][x][e]), lo, v);
+          v = fmaf(T::high(o[u][x][e]), hi, v);
+          if constexpr (__is_same(T, TypeF16)) peak[0] = fmaxf(peak[0], fmaxf(fabsf(lo), fabsf(hi)));
         }
 #pragma unroll
       for (int s = 8; s > 0; s >>= 1) v += __shfl_xor(v, s, WAVE);
@@ -69,23 +72,54 @@ __global__ __launch_bounds__(TPB) void delta_kernel(Backward b) {
     }
   }
   if constexpr (__is_same(T, TypeF16)) {
-    peak = wave_max(peak);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = peak;
+    const long long values = (long long)a.rows * a.Hkv;
+    for (long long it0 = (long long)blockIdx.x * 16 + (threadIdx.x >> 4); it0 < values; it0 += step * AHEAD) {
+      u32x4 w[AHEAD][CH];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const long long it = it0 + u * step < values ? it0 + u * step : it0, row = it / a.Hkv;
+        const uint16_t* p = (const uint16_t*)a.v + row * a.v_stride + (it - row * a.Hkv) * a.h;
+#pragma unroll
+        for (int x = 0; x < CH; ++x) {
+          const int d = 128 * x + 8 * li;
+          w[u][x] = d < a.h ? *(const u32x4*)(p + d) : u32x4{0, 0, 0, 0};
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+        for (int x = 0; x < CH; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) peak[1] = fmaxf(peak[1], fmaxf(fabsf(T::low(w[u][x][e])), fabsf(T::high(w[u][x][e]))));
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      peak[i] = wave_max(peak[i]);
+      if ((threadIdx.x & 63) == 0) red[i][threadIdx.x >> 6] = peak[i];
+    }
     __syncthreads();
-    if (threadIdx.x == 0) b.peak[blockIdx.x] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    if (threadIdx.x < 2) {
+      const float* r = red[threadIdx.x];
+      b.peak[threadIdx.x * DELTA_BLOCKS + blockIdx.x] = fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3]));
+    }
   }
 }
 
-// What fp16 multiplies dS by: 2^-3 over the power of two below the largest |dout|, so that neither a probability of 1e-5 vanishes nor a
-// sum over 256 dims against values up to some hundreds leaves the type's range.
+// What fp16 multiplies dS by: a power of two with which none leaves the type's range.  |dP| is at most h max|dout| max|v| and so is
+// |delta|, and P is at most 1.  (Infinite or NaN inputs: 1.)
 template <class T>
 __device__ __forceinline__ float ds_factor(const Backward& b) {
   if constexpr (__is_same(T, TypeBf16)) return 1.f;
-  float peak = 0.f;
-  for (int i = threadIdx.x & 63; i < DELTA_BLOCKS; i += 64) peak = fmaxf(peak, b.peak[i]);
-  peak = wave_max(peak);
-  if (!(peak > 0.f) || peak > 3e38f) return 1.f;
-  return __uint_as_float((uint32_t)(254 - (int)(__float_as_uint(peak) >> 23)) << 23) * 0.125f;      // (127 - e) - 3 with e = exponent of peak
+  float peak[2] = {0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    for (int i = threadIdx.x & 63; i < DELTA_BLOCKS; i += 64) peak[k] = fmaxf(peak[k], b.peak[k * DELTA_BLOCKS + i]);
+    peak[k] = wave_max(peak[k]);
+  }
+  const float most = 2.f * (float)b.a.h * peak[0] * peak[1];
+  if (!(most > 1e-30f) || most > 1e30f) return 1.f;
+  // 2^14 over the power of two at or below `most`: dS is below 2^15
+  return __uint_as_float((uint32_t)(254 + 14 - (int)(__float_as_uint(most) >> 23)) << 23);
 }
 
 // ------------------------------------------------------------------ keys' side
@@ -311,8 +345,8 @@ __global__ __launch_bounds__(TPB) void sink_sum_kernel(Backward b) {
 // ------------------------------------------------------------------ queries' side
 // The forward pass's walk: a block owns 128 rows of a group's queries, a wave 32 of them with q and dout in registers; keys and values pass
 // through LDS (K by rows and transposed, V by rows).
-template <class T, int HD>
-__global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void queries_backward_kernel(Backward b, int tiles) {
+template <class T, int HD, bool FEW>
+__global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void queries_backward_kernel(Backward b, int tiles) {
   typedef typename T::vec8 vec8;
   const WindowArgs& a = b.a;
   constexpr int BN = HD > 128 ? 32 : 64, SUB = BN / 32, KS = HD / 16, DT = (HD + 31) / 32, TILE = BN * HD;
@@ -366,12 +400,55 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void queries_backward_kernel
   settle(qf);
   settle(of);
   settle_words(of_row);
-  const float lse2 = of_row[0], delta = of_row[1];
+  const float lse2 = of_row[0];
+  float delta = of_row[1];
+  // This lane's row against 32 keys of the tile in buffer `buf`: scores (of the products' scale) and dP
+  auto products = [&](int buf, int u, f32x16& sc, f32x16& dp) {
+    const lds_t kt = tiles0 + buf * 4 * TILE, vt = kt + 2 * TILE;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) sc = T::mfma32(row_frag<HD, vec8>(kt + by_row, 32 * u, i), qf[i], sc);
+#pragma unroll
+    for (int i = 0; i < KS; ++i) dp = T::mfma32(row_frag<HD, vec8>(vt + by_row, 32 * u, i), of[i], dp);
+    order_products<1, 6, 2 * KS>();
+  };
+  // out was rounded, and where a row sees few keys its delta is nearly as large as its dP: there the rounding shows in dS.  Such rows
+  // take delta from the sum over their keys of P dP and leave it for the keys' side: a sequence's first 32 rows from the 32 keys that they
+  // see at most, which begin the first tile; with a window of up to FEW_KEYS (FEW) all rows, in a pass of its own.
+  auto own_delta = [&](int buf, int u, int kb) {
+    f32x16 sc, dp;
+    products(buf, u, sc, dp);
+    const uint32_t bits = group_bits(seen_keys(pos, kb, a.window, a.sinks), g);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += or_else(__builtin_amdgcn_exp2f(fmaf(sc[i], scale2, -lse2)) * dp[i], element_mask(bits, i), 0u);
+    return sum;
+  };
   if (n_tiles > 0) request(0, 0);
+  if constexpr (FEW) {
+    float sum = 0.f;
+    for (int t = 0; t < n_tiles; ++t) {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
+      for (int u = 0; u < SUB; ++u) sum += own_delta(t & 1, u, tile_key(t) + 32 * u);
+    }
+    delta = sum_halves(sum);
+    if (live && g == 0) b.delta[row * a.Hq + head] = delta;
+    __syncthreads();                           // (the tiles are filled again)
+    if (n_tiles > 0) request(0, 0);
+  } else if (p_lo < 32) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (wp_lo < 32) {
+      const float sum = sum_halves(own_delta(0, 0, tile_key(0)));
+      delta = pos < 32 ? sum : delta;
+      if (live && g == 0 && pos < 32) b.delta[row * a.Hq + head] = sum;
+    }
+  }
   for (int t = 0; t < n_tiles; ++t) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
-    const lds_t kt = tiles0 + (t & 1) * 4 * TILE, vt = kt + 2 * TILE;
+    const lds_t kt = tiles0 + (t & 1) * 4 * TILE;
     const ColumnBase<HD> kc = {kt + by_column.all, kt + by_column.last};
 #pragma unroll
     for (int u = 0; u < SUB; ++u) {
@@ -381,13 +458,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void queries_backward_kernel
       uint32_t bits = ~0u;
       if (!whole) bits = group_bits(seen_keys(pos, kb, a.window, a.sinks), g);
       f32x16 sc, dp;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
-#pragma unroll
-      for (int i = 0; i < KS; ++i) sc = T::mfma32(row_frag<HD, vec8>(kt + by_row, 32 * u, i), qf[i], sc);
-#pragma unroll
-      for (int i = 0; i < KS; ++i) dp = T::mfma32(row_frag<HD, vec8>(vt + by_row, 32 * u, i), of[i], dp);
-      order_products<1, 6, 2 * KS>();
+      products(t & 1, u, sc, dp);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float ds = __builtin_amdgcn_exp2f(fmaf(sc[i], scale2, -lse2)) * (dp[i] - delta) * factor;
@@ -444,7 +515,7 @@ size_t place(Backward& b, char* ws) {
   b.delta = (float*)(ws + at);
   at += round_up((size_t)a.rows * a.Hq * sizeof(float));
   b.peak = (float*)(ws + at);
-  at += round_up(DELTA_BLOCKS * sizeof(float));
+  at += round_up(2 * DELTA_BLOCKS * sizeof(float));
   b.part = (float*)(ws + at);
   at += (size_t)a.S * a.Hkv * (b.chunks + 1) * 2 * b.sinks * a.h * sizeof(float);
   return at;
@@ -456,13 +527,16 @@ hipError_t launch(const Backward& b, hipStream_t s) {
   const int units = a.S * a.Hkv;
   const int key_tiles = (a.max_new + BM - 1) / BM, jobs = key_tiles + (b.sinks + BM - 1) / BM * b.chunks;
   hipLaunchKernelGGL((delta_kernel<T, (HD > 128 ? 2 : 1)>), dim3(DELTA_BLOCKS), dim3(TPB), 0, s, b);
+  const int tiles = (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
+  if (a.window > 0 && a.window <= FEW_KEYS)
+    hipLaunchKernelGGL((queries_backward_kernel<T, HD, true>), dim3(mapped_blocks(units, tiles)), dim3(TPB), 0, s, b, tiles);
+  else
+    hipLaunchKernelGGL((queries_backward_kernel<T, HD, false>), dim3(mapped_blocks(units, tiles)), dim3(TPB), 0, s, b, tiles);
   hipLaunchKernelGGL((keys_backward_kernel<T, HD>), dim3(mapped_blocks(units, jobs)), dim3(TPB * KEYS_HALVES<HD>), 0, s, b, key_tiles, jobs);
   if (b.sinks > 0) {
     const int per = (2 * b.sinks * (a.h / 4) + TPB - 1) / TPB;
     hipLaunchKernelGGL((sink_sum_kernel<T>), dim3((unsigned)units, per < 64 ? per : 64), dim3(TPB), 0, s, b);
   }
-  const int tiles = (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
-  hipLaunchKernelGGL((queries_backward_kernel<T, HD>), dim3(mapped_blocks(units, tiles)), dim3(TPB), 0, s, b, tiles);
   return hipGetLastError();
 }
 template <class T>
