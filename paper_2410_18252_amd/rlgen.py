@@ -396,15 +396,20 @@ def rlgen_debug_set_gemm(p: Policy, mode: int, which: int, variant: int):
 _DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
 
 
+_I32 = torch.int32
+
+
 def _heads(t: torch.Tensor, dtype: torch.dtype):
     """[rows, heads, head_dim] with heads and head_dim contiguous: (address, row stride)."""
-    assert t.dim() == 3 and t.dtype == dtype and t.is_cuda and t.stride(2) == 1 and (t.stride(1) == t.shape[2] or t.shape[1] == 1)
+    rows, heads, h = t.shape
+    row, head, dim = t.stride()
+    assert t.dtype is dtype and t.is_cuda and dim == 1 and (head == h or heads == 1)
     # (the row stride of a tensor of one row or none means nothing)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return t.data_ptr(), row if rows > 1 else heads * h
 
 
 def _ints(t: torch.Tensor, *shape):
-    assert t.dtype == torch.int32 and t.is_cuda and t.is_contiguous() and tuple(t.shape) == shape
+    assert t.dtype is _I32 and t.is_cuda and t.shape == shape and t.is_contiguous()
     return t.data_ptr()
 
 
@@ -426,12 +431,13 @@ def rlgen_plan_pages(ctx_lens: torch.Tensor, new_lens: torch.Tensor, page_size: 
     if out is None:
         buf = ctx_lens.new_empty(2 * S + 5 + 2 * max_rows)
         out = torch.split(buf, [S, S + 1, max_rows, max_rows, 4])
-    plan = PagePlan(*out)
-    _check(lib.rlgen_plan_pages(_ints(ctx_lens, S), _ints(new_lens, S), S, page_size, _ints(free_pages, free_pages.numel()), free_pages.numel(),
+    total_lens, row_starts, slots, positions, counts = out
+    n_free = free_pages.numel()
+    _check(lib.rlgen_plan_pages(_ints(ctx_lens, S), _ints(new_lens, S), S, page_size, _ints(free_pages, n_free), n_free,
                                 None if free_head is None else _ints(free_head, 1), _ints(page_table, S, stride), stride, max_rows,
-                                _ints(plan.total_lens, S), _ints(plan.row_starts, S + 1), _ints(plan.slots, max_rows),
-                                _ints(plan.positions, max_rows), _ints(plan.counts, 4), _stream()), "rlgen_plan_pages")
-    return plan
+                                _ints(total_lens, S), _ints(row_starts, S + 1), _ints(slots, max_rows), _ints(positions, max_rows),
+                                _ints(counts, 4), _stream()), "rlgen_plan_pages")
+    return out if type(out) is PagePlan else PagePlan(total_lens, row_starts, slots, positions, counts)
 
 
 def rlgen_rope_table(max_pos: int, rotary_dim: int, theta: float, device="cuda") -> torch.Tensor:
@@ -442,22 +448,23 @@ def rlgen_rope_table(max_pos: int, rotary_dim: int, theta: float, device="cuda")
 
 
 def _norm_rope_args(qkv, q_gain, k_gain, eps, rope, positions, n_q, n_kv, dtype):
-    h, rows = q_gain.numel(), qkv.shape[0]
-    assert qkv.dim() == 2 and qkv.is_cuda and qkv.stride(1) == 1 and qkv.shape[1] == (n_q + 2 * n_kv) * h
-    for t in (q_gain, k_gain):
-        assert t.dtype == torch.float32 and t.is_contiguous() and t.numel() == h
-    max_pos, r = 1, 0
+    rows, width = qkv.shape
+    row, dim = qkv.stride()
+    h = q_gain.numel()
+    assert qkv.is_cuda and dim == 1 and width == (n_q + 2 * n_kv) * h
+    assert q_gain.dtype is torch.float32 and q_gain.is_contiguous() and k_gain.dtype is torch.float32 and k_gain.is_contiguous() and k_gain.numel() == h
+    max_pos, half = 1, 0
     if rope is not None:
-        assert rope.dtype == torch.float32 and rope.is_contiguous() and rope.dim() == 3 and rope.shape[2] == 2
-        max_pos, r = rope.shape[0], 2 * rope.shape[1]
-    stride = qkv.stride(0) if rows > 1 else qkv.shape[1]
-    return (qkv.data_ptr(), stride, _DTYPES[qkv.dtype], rows, n_q, n_kv, h, q_gain.data_ptr(), k_gain.data_ptr(), eps, _ptr(rope), max_pos, r,
-            _ints(positions, rows), _DTYPES[dtype])
+        max_pos, half, two = rope.shape
+        assert rope.dtype is torch.float32 and rope.is_contiguous() and two == 2
+    return (qkv.data_ptr(), row if rows > 1 else width, _DTYPES[qkv.dtype], rows, n_q, n_kv, h, q_gain.data_ptr(), k_gain.data_ptr(), eps,
+            None if rope is None else rope.data_ptr(), max_pos, 2 * half, _ints(positions, rows), _DTYPES[dtype])
 
 
 def _pages(pages: torch.Tensor, n_kv: int, h: int):
-    assert pages.is_cuda and pages.is_contiguous() and pages.dim() == 5 and pages.shape[1:3] == (2, n_kv) and pages.shape[4] == h
-    return pages.data_ptr(), pages.shape[0], pages.shape[3]
+    n_pages, two, heads, page_size, dims = pages.shape
+    assert pages.is_cuda and pages.is_contiguous() and two == 2 and heads == n_kv and dims == h
+    return pages.data_ptr(), n_pages, page_size
 
 
 def rlgen_qk_norm_rope(qkv: torch.Tensor, q_gain: torch.Tensor, k_gain: torch.Tensor, eps: float, rope: Optional[torch.Tensor],
