@@ -76,9 +76,9 @@ __device__ void rows_key_by_key(const WindowArgs& a, const Seq& q, int s, int kv
 }
 
 template <class T, int HD, bool PAGED>
-__global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 2) void window_rows_kernel(WindowArgs a, int tiles) {
+__global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) void window_rows_kernel(WindowArgs a, int tiles) {
   typedef typename T::vec8 vec8;
-  constexpr int BN = HD > 96 ? 32 : 64, SUB = BN / 32, KS = HD / 16, DT = (HD + 31) / 32, TILE = BN * HD;
+  constexpr int BN = 32, KS = HD / 16, DT = (HD + 31) / 32, TILE = BN * HD;
   constexpr int AHEAD = 6;
   typedef Pieces<HD, BN> P;
   __shared__ __attribute__((aligned(256))) uint16_t lds[2][2][TILE];
@@ -172,12 +172,12 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 2) 
   ColumnBase<HD> v_base = column_base<HD>(lane);
   v_base.all += lds_address(lds[0][1]);
   v_base.last += lds_address(lds[0][1]);
-  settle(qf);
   if (n_tiles > 0) {
     fetch_pages(0);
     request(0, 0);
     if (n_tiles > 1) fetch_pages(1);
   }
+  settle(qf);                                  // (behind the first request: one wait for both)
   for (int t = 0; t < n_tiles; ++t) {
     // this tile has landed, and nobody reads the other buffer any more
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -188,30 +188,21 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 2) 
     if (kb > wp_hi || (a.window && kb + BN - 1 <= wp_lo - a.window && kb >= a.sinks)) continue;
     const lds_t buffer = (t & 1) * 4 * TILE;
     const ColumnBase<HD> vb = {v_base.all + buffer, v_base.last + buffer};
-    f32x16 sc[SUB];
+    f32x16 sc;
 #pragma unroll
-    for (int u = 0; u < SUB; ++u)
+    for (int i = 0; i < 16; ++i) sc[i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
-#pragma unroll
-    for (int i = 0; i < KS; ++i)
-#pragma unroll
-      for (int u = 0; u < SUB; ++u) sc[u] = T::mfma32(row_frag<HD, vec8>(k_base + buffer, 32 * u, i), qf[i], sc[u]);
-    order_products<1, AHEAD, KS * SUB>();
+    for (int i = 0; i < KS; ++i) sc = T::mfma32(row_frag<HD, vec8>(k_base + buffer, 0, i), qf[i], sc);
+    order_products<1, AHEAD, KS>();
     const bool whole = kb + BN - 1 <= wp_lo && (a.window == 0 || kb > wp_hi - a.window || kb + BN - 1 < a.sinks);
-    if (!whole) {
-#pragma unroll
-      for (int u = 0; u < SUB; ++u) {
-        const uint32_t bits = group_bits(seen_keys(pos, kb + 32 * u, a.window, a.sinks), g);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[u][i] = or_else(sc[u][i], element_mask(bits, i), 0xff800000u);      // -infinity
-      }
-    }
     float top = -INFINITY;
+    if (!whole) {
+      const uint32_t bits = group_bits(seen_keys(pos, kb, a.window, a.sinks), g);
 #pragma unroll
-    for (int u = 0; u < SUB; ++u)
+      for (int i = 0; i < 16; ++i) sc[i] = or_else(sc[i], element_mask(bits, i), 0xff800000u);      // -infinity
+    }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[u][i]);
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[i]);
     top = max_halves(top) * scale2;
     if (__any(top > mx + RISE)) {
       const float now = fmaxf(mx, top), shrink = __builtin_amdgcn_exp2f(mx - (now == -INFINITY ? 0.f : now));
@@ -221,21 +212,18 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 2) 
       for (int d = 0; d < DT; ++d) o[d] *= shrink;
     }
     const float base = mx == -INFINITY ? 0.f : mx;            // a row that has seen no key yet keeps zeros
+    float part = 0.f;
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) {
-      float part = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sc[u][i] = __builtin_amdgcn_exp2f(fmaf(sc[u][i], scale2, -base));
-        part += sc[u][i];
-      }
-      sum += part;
+    for (int i = 0; i < 16; ++i) {
+      sc[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], scale2, -base));
+      part += sc[i];
     }
+    sum += part;
 #pragma unroll
-    for (int u = 0; u < 2 * SUB; ++u) {
+    for (int u = 0; u < 2; ++u) {
       u32x4 w;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = T::pack(sc[u >> 1][8 * (u & 1) + 2 * e], sc[u >> 1][8 * (u & 1) + 2 * e + 1]);
+      for (int e = 0; e < 4; ++e) w[e] = T::pack(sc[8 * u + 2 * e], sc[8 * u + 2 * e + 1]);
       const vec8 pf = __builtin_bit_cast(vec8, w);
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] = T::mfma32(column_frag<HD, vec8>(vb, 16 * u, d), pf, o[d]);
@@ -252,21 +240,9 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 2) 
     rows_key_by_key<T, PAGED>(a, q, s, kvh, m0 + wave * 32, M, lane);
     return;
   }
-  if (!live) return;
   const long long row = q.row0 + tok;
-  if (a.lse && g == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
-  uint16_t* op = (uint16_t*)a.out + row * a.out_stride + (long long)head * a.h;
-#pragma unroll
-  for (int t = 0; t < DT; ++t)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int d = 32 * t + 8 * j + 4 * g;
-      if (d >= a.h) continue;
-      u32x2 w;
-      w[0] = T::pack(o[t][4 * j] * inv, o[t][4 * j + 1] * inv);
-      w[1] = T::pack(o[t][4 * j + 2] * inv, o[t][4 * j + 3] * inv);
-      *(u32x2*)(op + d) = w;
-    }
+  if (live && a.lse && g == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  store_row<T, DT>((uint16_t*)a.out + row * a.out_stride + (long long)head * a.h, o, inv, a.h, g, live);
 }
 
 template <class T, int HD>

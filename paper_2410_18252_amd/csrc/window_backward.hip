@@ -218,9 +218,9 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, HD > 128 ? 1 : 2) void keys_
   const float scale2 = a.scale * LOG2E;
   const lds_t tiles = lds_address(lds[0][0]) + half * SUB * 32 * HD * 2, by_row = row_base<HD>(lane), v_row = lds_address(v_tile) + key_wave * 32 * HD * 2 + by_row;
   const ColumnBase<HD> by_column = column_base<HD>(lane);
-  settle(kf);
-  if constexpr (!V_IN_LDS) settle(vf);
   if (n_tiles > 0) request(0, 0);
+  settle(kf);                                  // (behind the first request: one wait for both)
+  if constexpr (!V_IN_LDS) settle(vf);
   for (int t = 0; t < n_tiles; ++t) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
@@ -301,27 +301,24 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, HD > 128 ? 1 : 2) void keys_
     }
     if (half == 1) return;
   }
-  if (key >= q.n || (slot > 0 && key >= b.sinks)) return;
   const float back = a.scale / factor;
   const bool parted = slot >= 0 && key < b.sinks;
   const long long row = q.row0 + key;
+  if (parted && key < q.n) {
+    float* to = b.part + ((((long long)unit * (b.chunks + 1) + slot) * 2) * b.sinks + key) * a.h;
 #pragma unroll
-  for (int t = 0; t < DT; ++t)
+    for (int t = 0; t < DT; ++t)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int d = 32 * t + 8 * j + 4 * g;
-      if (d >= a.h) continue;
-      const f32x4 yk = f32x4{dk[t][4 * j], dk[t][4 * j + 1], dk[t][4 * j + 2], dk[t][4 * j + 3]} * back;
-      const f32x4 yv = {dv[t][4 * j], dv[t][4 * j + 1], dv[t][4 * j + 2], dv[t][4 * j + 3]};
-      if (parted) {
-        float* to = b.part + ((((long long)unit * (b.chunks + 1) + slot) * 2) * b.sinks + key) * a.h + d;
-        *(f32x4*)to = yk;
-        *(f32x4*)(to + (long long)b.sinks * a.h) = yv;
-      } else {
-        *(u32x2*)((uint16_t*)a.dk + row * a.dk_stride + (long long)kvh * a.h + d) = u32x2{T::pack(yk[0], yk[1]), T::pack(yk[2], yk[3])};
-        *(u32x2*)((uint16_t*)a.dv + row * a.dv_stride + (long long)kvh * a.h + d) = u32x2{T::pack(yv[0], yv[1]), T::pack(yv[2], yv[3])};
+      for (int j = 0; j < 4; ++j) {
+        const int d = 32 * t + 8 * j + 4 * g;
+        if (d >= a.h) continue;
+        *(f32x4*)(to + d) = f32x4{dk[t][4 * j], dk[t][4 * j + 1], dk[t][4 * j + 2], dk[t][4 * j + 3]} * back;
+        *(f32x4*)(to + (long long)b.sinks * a.h + d) = f32x4{dv[t][4 * j], dv[t][4 * j + 1], dv[t][4 * j + 2], dv[t][4 * j + 3]};
       }
-    }
+  }
+  const bool whole_sum = key < q.n && slot <= 0 && !parted;
+  store_row<T, DT>((uint16_t*)a.dk + row * a.dk_stride + (long long)kvh * a.h, dk, back, a.h, g, whole_sum);
+  store_row<T, DT>((uint16_t*)a.dv + row * a.dv_stride + (long long)kvh * a.h, dv, 1.f, a.h, g, whole_sum);
 }
 
 // The parts of the sinks' gradients, in order.
@@ -397,6 +394,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
   const float scale2 = a.scale * LOG2E;
   const lds_t tiles0 = lds_address(lds[0][0]), by_row = row_base<HD>(lane);
   const ColumnBase<HD> by_column = column_base<HD>(lane);
+  if (n_tiles > 0) request(0, 0);
   settle(qf);
   settle(of);
   settle_words(of_row);
@@ -425,7 +423,6 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
     for (int i = 0; i < 16; ++i) sum += or_else(__builtin_amdgcn_exp2f(fmaf(sc[i], scale2, -lse2)) * dp[i], element_mask(bits, i), 0u);
     return sum;
   };
-  if (n_tiles > 0) request(0, 0);
   if constexpr (FEW) {
     float sum = 0.f;
     for (int t = 0; t < n_tiles; ++t) {
@@ -474,17 +471,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
       }
     }
   }
-  if (!live) return;
-  const float back = a.scale / factor;
-  uint16_t* to = (uint16_t*)a.dq + row * a.dq_stride + (long long)head * a.h;
-#pragma unroll
-  for (int t = 0; t < DT; ++t)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int d = 32 * t + 8 * j + 4 * g;
-      if (d >= a.h) continue;
-      *(u32x2*)(to + d) = u32x2{T::pack(dq[t][4 * j] * back, dq[t][4 * j + 1] * back), T::pack(dq[t][4 * j + 2] * back, dq[t][4 * j + 3] * back)};
-    }
+  store_row<T, DT>((uint16_t*)a.dq + row * a.dq_stride + (long long)head * a.h, dq, a.scale / factor, a.h, g, live);
 }
 
 // Sinks are parted while their partial sums (two fp32 vectors a sink, kv head and part) stay below 64 MB; parts of four windows at least

@@ -190,6 +190,25 @@ __device__ __forceinline__ uint32_t group_bits(uint32_t seen, int g) { return se
 __device__ __forceinline__ uint32_t element_mask(uint32_t bits, int i) { return (uint32_t)__builtin_amdgcn_sbfe((int)bits, acc_row(i, 0), 1); }
 __device__ __forceinline__ float or_else(float v, uint32_t mask, uint32_t other) { return __uint_as_float((__float_as_uint(v) & mask) | (~mask & other)); }
 
+// Writes the transposed result of a wave, x[t] dims 32 t .. of the row in each lane's column, times f, as the row's 16-bit values: a lane
+// has four dims of every eight and its partner in the other half of the wave the other four, so they exchange and store 16 bytes each.
+template <class T, int DT> __device__ __forceinline__ void store_row(uint16_t* row, const f32x16 (&x)[DT], float f, int h, int g, bool live) {
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int i = 8 * j + 2 * e;
+        const auto r = __builtin_amdgcn_permlane32_swap(T::pack(x[t][i] * f, x[t][i + 1] * f), T::pack(x[t][i + 4] * f, x[t][i + 5] * f), false, false);
+        w[e] = r[0];
+        w[2 + e] = r[1];
+      }
+      if (live && 32 * t + 16 * j < h) *(u32x4*)(row + 32 * t + 16 * j + 8 * g) = w;
+    }
+}
+
 // One sequence of a call: its rows, its keys and the position of its first row.
 struct Seq { int row0, n, total, ctx; };
 __device__ __forceinline__ Seq load_seq(const WindowArgs& a, int s, bool paged) {
