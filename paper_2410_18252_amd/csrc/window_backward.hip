@@ -22,6 +22,8 @@ struct Backward {
   WindowArgs a;
   float *lse2, *delta, *peak, *part;    // [rows, Hq]: lse log2 e, delta; the largest |dout| and |v| of each block; the sinks' parts
   int sinks, chunk, chunks;             // sinks that are parted (0: none); tokens to a part; parts of the longest sequence
+  float* run_part;                      // [runs, rows, Hkv, 2, h]
+  int run, runs;                        // tokens to a part of what a tile of keys is seen by, most parts (1: not parted)
 };
 
 // delta and lse log2 e, and in fp16 for each block the largest |dout| and |v|.  Bound by HBM: out and dout (and
@@ -126,10 +128,17 @@ __device__ __forceinline__ float ds_factor(const Backward& b) {
 // A block owns 128 keys of a kv head, a wave 32 of them with K and V in registers; the rows of the group's queries that see them pass
 // through LDS (q and dout, each read by rows for S = q K^T and dP = dout V^T, and transposed for dv^T = dout^T P and dk^T = q^T dS).
 // Sinks are seen by every query behind them: what lies beyond the window is parted over blocks of its own, whose sums meet in
-// sink_sum_kernel; else the block of the first keys would run for as long as all others together.
+// parts_sum_kernel; else the block of the first keys would run for as long as all others together.  The same where few kv heads with many
+// query heads, or a long sequence, would leave a few blocks the longest walks.
 // At 128 dims eight waves share a block's keys, the second four taking the second half of every tile of queries, and add up in LDS at the
 // end: a block's keys, whose queries are a long serial walk, then take half as long.
 template <int HD> constexpr int KEYS_HALVES = HD == 128 ? 2 : 1;
+
+// The token behind the last that a tile of keys is seen by, its parted sinks apart
+__device__ __forceinline__ int last_seer(const Backward& b, int kt, int n) {
+  const WindowArgs& a = b.a;
+  return a.window && (b.sinks > 0 || kt * BM >= a.sinks) ? (int)min((long long)n, (long long)kt * BM + BM - 1 + a.window) : n;
+}
 
 template <class T, int HD>
 __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, HD > 128 ? 1 : 2) void keys_backward_kernel(Backward b, int key_tiles, int jobs) {
@@ -152,20 +161,26 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, HD > 128 ? 1 : 2) void keys_
   const int s = unit / a.Hkv, kvh = unit - s * a.Hkv;
   const Seq q = load_seq(a, s, false);
   // which keys, and the tokens that the job adds up
-  int kt = job - (jobs - key_tiles), tok0, tok1, slot = -1;
-  if (kt < 0) {
+  const int sink_jobs = jobs - key_tiles * b.runs;
+  int kt, tok0, tok1, slot = -1, run = 0;
+  if (job < sink_jobs) {
     kt = job / b.chunks;
     slot = 1 + job % b.chunks;
     tok0 = kt * BM + BM - 1 + a.window + (slot - 1) * b.chunk;
     tok1 = min(tok0 + b.chunk, q.n);
-    if (tok0 >= q.n) return;
   } else {
-    if (kt * BM >= q.n) return;
+    kt = (job - sink_jobs) / b.runs;
+    run = job - sink_jobs - kt * b.runs;
     tok0 = kt * BM;
-    tok1 = q.n;
-    if (a.window && (b.sinks > 0 || kt * BM >= a.sinks)) tok1 = (int)min((long long)q.n, (long long)kt * BM + BM - 1 + a.window);
-    if (kt * BM < b.sinks) slot = 0;
+    tok1 = last_seer(b, kt, q.n);
+    if (b.runs > 1) {
+      tok0 += run * b.run;
+      tok1 = min(tok0 + b.run, tok1);
+    } else if (kt * BM < b.sinks) {
+      slot = 0;
+    }
   }
+  if (kt * BM >= q.n || tok0 >= tok1) return;
   const int kw = kt * BM + key_wave * 32, key = kw + c;
   const int M = q.n * G, m0 = tok0 * G, m1 = tok1 * G, n_tiles = (m1 - m0 + BQ - 1) / BQ;
   // the last position that sees this lane's key, from the key on (a position of -1 is beyond any)
@@ -302,10 +317,12 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, HD > 128 ? 1 : 2) void keys_
     if (half == 1) return;
   }
   const float back = a.scale / factor;
-  const bool parted = slot >= 0 && key < b.sinks;
+  const bool parted = slot >= 0 && key < b.sinks, in_runs = slot < 0 && b.runs > 1;
   const long long row = q.row0 + key;
-  if (parted && key < q.n) {
-    float* to = b.part + ((((long long)unit * (b.chunks + 1) + slot) * 2) * b.sinks + key) * a.h;
+  if ((parted || in_runs) && key < q.n) {
+    float* to = in_runs ? b.run_part + (((long long)run * a.rows + row) * a.Hkv + kvh) * 2 * a.h
+                        : b.part + ((((long long)unit * (b.chunks + 1) + slot) * 2) * b.sinks + key) * a.h;
+    const long long to_values = in_runs ? a.h : (long long)b.sinks * a.h;
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -313,28 +330,35 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, HD > 128 ? 1 : 2) void keys_
         const int d = 32 * t + 8 * j + 4 * g;
         if (d >= a.h) continue;
         *(f32x4*)(to + d) = f32x4{dk[t][4 * j], dk[t][4 * j + 1], dk[t][4 * j + 2], dk[t][4 * j + 3]} * back;
-        *(f32x4*)(to + (long long)b.sinks * a.h + d) = f32x4{dv[t][4 * j], dv[t][4 * j + 1], dv[t][4 * j + 2], dv[t][4 * j + 3]};
+        *(f32x4*)(to + to_values + d) = f32x4{dv[t][4 * j], dv[t][4 * j + 1], dv[t][4 * j + 2], dv[t][4 * j + 3]};
       }
   }
-  const bool whole_sum = key < q.n && slot <= 0 && !parted;
+  const bool whole_sum = key < q.n && slot <= 0 && !parted && !in_runs;
   store_row<T, DT>((uint16_t*)a.dk + row * a.dk_stride + (long long)kvh * a.h, dk, back, a.h, g, whole_sum);
   store_row<T, DT>((uint16_t*)a.dv + row * a.dv_stride + (long long)kvh * a.h, dv, 1.f, a.h, g, whole_sum);
 }
 
-// The parts of the sinks' gradients, in order.
+// Adds up the parts of SUM_KEYS of a tile's keys (tile blockIdx.y), always in the same order.
+constexpr int SUM_KEYS = 16;
 template <class T>
-__global__ __launch_bounds__(TPB) void sink_sum_kernel(Backward b) {
+__global__ __launch_bounds__(TPB) void parts_sum_kernel(Backward b) {
   const WindowArgs& a = b.a;
-  const int unit = blockIdx.x, s = unit / a.Hkv, kvh = unit - s * a.Hkv;
+  const int unit = blockIdx.x, kt = blockIdx.y, s = unit / a.Hkv, kvh = unit - s * a.Hkv;
   const Seq q = load_seq(a, s, false);
-  const int quads = a.h / 4, n = min(b.sinks, q.n);
-  for (int at = blockIdx.y * TPB + threadIdx.x; at < 2 * n * quads; at += gridDim.y * TPB) {
-    const int which = at / (n * quads), rest = at - which * n * quads, key = rest / quads, d = (rest - key * quads) * 4;
-    const long long beyond = (long long)q.n - ((key / BM) * BM + BM - 1 + (long long)a.window);
-    const int parts = 1 + (beyond > 0 ? (int)((beyond + b.chunk - 1) / b.chunk) : 0);
+  const int quads = a.h / 4, key0 = kt * BM + blockIdx.z * SUM_KEYS, n = min(min(b.runs > 1 ? key0 + SUM_KEYS : b.sinks, key0 + SUM_KEYS), q.n) - key0;
+  if (n <= 0) return;
+  const int runs = b.runs > 1 ? (last_seer(b, kt, q.n) - kt * BM + b.run - 1) / b.run : 0;
+  const long long beyond = (long long)q.n - (kt * BM + BM - 1 + (long long)a.window);
+  const int slots = 1 + (beyond > 0 ? (int)((beyond + b.chunk - 1) / b.chunk) : 0);
+  for (int at = threadIdx.x; at < 2 * n * quads; at += TPB) {
+    const int which = at / (n * quads), rest = at - which * n * quads, key = key0 + rest / quads, d = rest % quads * 4;
+    const long long row = q.row0 + key;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < parts; ++p) y += *(const f32x4*)(b.part + ((((long long)unit * (b.chunks + 1) + p) * 2 + which) * b.sinks + key) * a.h + d);
-    uint16_t* to = (uint16_t*)(which ? a.dv : a.dk) + (long long)(q.row0 + key) * (which ? a.dv_stride : a.dk_stride) + (long long)kvh * a.h + d;
+#pragma unroll 4
+    for (int r = 0; r < runs; ++r) y += *(const f32x4*)(b.run_part + ((((long long)r * a.rows + row) * a.Hkv + kvh) * 2 + which) * a.h + d);
+    if (key < b.sinks)
+      for (int p = runs > 0 ? 1 : 0; p < slots; ++p) y += *(const f32x4*)(b.part + ((((long long)unit * (b.chunks + 1) + p) * 2 + which) * b.sinks + key) * a.h + d);
+    uint16_t* to = (uint16_t*)(which ? a.dv : a.dk) + row * (which ? a.dv_stride : a.dk_stride) + (long long)kvh * a.h + d;
     *(u32x2*)to = u32x2{T::pack(y[0], y[1]), T::pack(y[2], y[3])};
   }
 }
@@ -474,8 +498,8 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
   store_row<T, DT>((uint16_t*)a.dq + row * a.dq_stride + (long long)head * a.h, dq, a.scale / factor, a.h, g, live);
 }
 
-// Sinks are parted while their partial sums (two fp32 vectors a sink, kv head and part) stay below 64 MB; parts of four windows at least
-// 1024 tokens cost a block about what a tile of keys costs.
+// Sinks are parted while their partial sums (two fp32 vectors a sink, kv head and part) stay below 64 MB, into parts of a window but at
+// least 1024 tokens, which cost a block about what a tile of keys costs.
 void part_sinks(Backward& b) {
   const WindowArgs& a = b.a;
   b.sinks = b.chunks = 0;
@@ -492,6 +516,32 @@ void part_sinks(Backward& b) {
   b.chunks = (int)chunks;
   b.chunk = (int)((beyond + chunks - 1) / chunks);
 }
+// The queries that see a tile of keys are parted where the longest such walk would take well over an even share of all (512 blocks, two to
+// a CU; one where h > 128): few kv heads with many query heads each, a long sequence.  A part has at least 512 rows; partial sums stay below 256 MB.
+// Measured on six sequences of 500 to 2000 tokens, 12 heads over 2 of 96: 476 us in one walk, 224 parted with 10 for the sums; 16 over 4 of
+// 64: 222 us, 97 with 6.  Where walks are even already a part only adds its sums: 8 over 4 of 256 in half tiles of 512 blocks' share: 547
+// us, 642 with 87.
+void part_runs(Backward& b) {
+  const WindowArgs& a = b.a;
+  b.runs = 1;
+  b.run = a.max_new;
+  const int G = a.Hq / a.Hkv;
+  long long longest = a.max_new;
+  const bool bounded = a.window > 0 && (b.sinks > 0 || a.sinks == 0) && (long long)a.window + BM - 1 < longest;
+  if (bounded) longest = (long long)a.window + BM - 1;
+  const long long tiles = (long long)a.rows * a.Hkv / BM + (long long)a.S * a.Hkv / 2 + 1;
+  const int even = a.h > 128 ? 256 : 512;
+  long long run = (tiles * (bounded ? longest : longest / 2) + even - 1) / even;
+  if (run < (512 + G - 1) / G) run = (512 + G - 1) / G;
+  if (2 * longest <= 3 * run) return;
+  long long runs = (longest + run - 1) / run;
+  if (runs > 8) runs = 8;
+  const long long part = (long long)a.rows * a.Hkv * 2 * a.h * 4;
+  if (part * runs > (256ll << 20)) runs = (256ll << 20) / part;
+  if (runs < 2) return;
+  b.runs = (int)runs;
+  b.run = (int)((longest + runs - 1) / runs);
+}
 size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 // places the buffers and returns their size
 size_t place(Backward& b, char* ws) {
@@ -504,7 +554,9 @@ size_t place(Backward& b, char* ws) {
   b.peak = (float*)(ws + at);
   at += round_up(2 * DELTA_BLOCKS * sizeof(float));
   b.part = (float*)(ws + at);
-  at += (size_t)a.S * a.Hkv * (b.chunks + 1) * 2 * b.sinks * a.h * sizeof(float);
+  at += round_up((size_t)a.S * a.Hkv * (b.chunks + 1) * 2 * b.sinks * a.h * sizeof(float));
+  b.run_part = (float*)(ws + at);
+  if (b.runs > 1) at += (size_t)b.runs * a.rows * a.Hkv * 2 * a.h * sizeof(float);
   return at;
 }
 
@@ -512,7 +564,7 @@ template <class T, int HD>
 hipError_t launch(const Backward& b, hipStream_t s) {
   const WindowArgs& a = b.a;
   const int units = a.S * a.Hkv;
-  const int key_tiles = (a.max_new + BM - 1) / BM, jobs = key_tiles + (b.sinks + BM - 1) / BM * b.chunks;
+  const int key_tiles = (a.max_new + BM - 1) / BM, sink_tiles = (b.sinks + BM - 1) / BM, jobs = key_tiles * b.runs + sink_tiles * b.chunks;
   hipLaunchKernelGGL((delta_kernel<T, (HD > 128 ? 2 : 1)>), dim3(DELTA_BLOCKS), dim3(TPB), 0, s, b);
   const int tiles = (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
   if (a.window > 0 && a.window <= FEW_KEYS)
@@ -520,10 +572,7 @@ hipError_t launch(const Backward& b, hipStream_t s) {
   else
     hipLaunchKernelGGL((queries_backward_kernel<T, HD, false>), dim3(mapped_blocks(units, tiles)), dim3(TPB), 0, s, b, tiles);
   hipLaunchKernelGGL((keys_backward_kernel<T, HD>), dim3(mapped_blocks(units, jobs)), dim3(TPB * KEYS_HALVES<HD>), 0, s, b, key_tiles, jobs);
-  if (b.sinks > 0) {
-    const int per = (2 * b.sinks * (a.h / 4) + TPB - 1) / TPB;
-    hipLaunchKernelGGL((sink_sum_kernel<T>), dim3((unsigned)units, per < 64 ? per : 64), dim3(TPB), 0, s, b);
-  }
+  if (b.sinks > 0 || b.runs > 1) hipLaunchKernelGGL((parts_sum_kernel<T>), dim3((unsigned)units, b.runs > 1 ? key_tiles : sink_tiles, BM / SUM_KEYS), dim3(TPB), 0, s, b);
   return hipGetLastError();
 }
 template <class T>
@@ -543,6 +592,7 @@ size_t rl_window_backward_bytes(const WindowArgs& a) {
   Backward b;
   b.a = a;
   part_sinks(b);
+  part_runs(b);
   return place(b, nullptr);
 }
 hipError_t rl_window_backward(const WindowArgs& a, hipStream_t s) {
@@ -550,6 +600,7 @@ hipError_t rl_window_backward(const WindowArgs& a, hipStream_t s) {
   Backward b;
   b.a = a;
   part_sinks(b);
+  part_runs(b);
   place(b, (char*)a.ws);
   return a.dtype == RLGEN_DTYPE_F16 ? by_head<TypeF16>(b, s) : by_head<TypeBf16>(b, s);
 }
