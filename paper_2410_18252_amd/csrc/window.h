@@ -47,7 +47,7 @@ struct WindowArgs {
   void *dq, *dk, *dv; long long dq_stride, dk_stride, dv_stride;
   void* ws; size_t ws_bytes;
 };
-hipError_t rl_window_rows(const WindowArgs& a, hipStream_t s);
+hipError_t rl_window_rows(WindowArgs a, hipStream_t s);
 size_t rl_window_decode_bytes(const WindowArgs& a);
 hipError_t rl_window_decode(const WindowArgs& a, hipStream_t s);
 size_t rl_window_backward_bytes(const WindowArgs& a);

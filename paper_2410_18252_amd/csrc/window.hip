@@ -266,7 +266,8 @@ hipError_t by_head(const WindowArgs& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t rl_window_rows(const WindowArgs& a, hipStream_t s) {
+hipError_t rl_window_rows(WindowArgs a, hipStream_t s) {
   if (a.rows <= 0) return hipSuccess;
+  if (a.max_new > a.rows) a.max_new = a.rows;
   return a.dtype == RLGEN_DTYPE_F16 ? by_head<TypeF16>(a, s) : by_head<TypeBf16>(a, s);
 }

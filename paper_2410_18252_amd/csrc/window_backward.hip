@@ -131,8 +131,11 @@ __device__ __forceinline__ float ds_factor(const Backward& b) {
 // parts_sum_kernel; else the block of the first keys would run for as long as all others together.  The same where few kv heads with many
 // query heads, or a long sequence, would leave a few blocks the longest walks.
 // At 128 dims eight waves share a block's keys, the second four taking the second half of every tile of queries, and add up in LDS at the
-// end: a block's keys, whose queries are a long serial walk, then take half as long.
-template <int HD> constexpr int KEYS_HALVES = HD == 128 ? 2 : 1;
+// end: a block's keys, whose queries are a long serial walk, then take half as long (three sequences of
+// 1500 to 4000, window 1024, 32 heads over 8: 357 us, 480 with four waves).
+template <int HD> constexpr int KEYS_HALVES = HD >= 128 ? 2 : 1;
+// At 256 dims both gradients of a wave's keys would need all 512 registers and more: the first four waves take dv, the second dk, and both
+// take S: five products for four, but two waves to a SIMD (six sequences of 500 to 2000, eight heads: 547 us as one wave to a SIMD, 247).
 
 // The token behind the last that a tile of keys is seen by, its parted sinks apart
 __device__ __forceinline__ int last_seer(const Backward& b, int kt, int n) {
@@ -141,13 +144,14 @@ __device__ __forceinline__ int last_seer(const Backward& b, int kt, int n) {
 }
 
 template <class T, int HD>
-__global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, HD > 128 ? 1 : 2) void keys_backward_kernel(Backward b, int key_tiles, int jobs) {
+__global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel(Backward b, int key_tiles, int jobs) {
   typedef typename T::vec8 vec8;
   const WindowArgs& a = b.a;
   // Two waves to a SIMD hide each other's latencies, so a wave has 256 registers: from 128 dims on V waits in LDS instead.
   constexpr bool V_IN_LDS = HD >= 128;
+  constexpr bool BY_GRADIENT = HD > 128;
   constexpr int HALVES = KEYS_HALVES<HD>, WAVES = 4 * HALVES;
-  constexpr int BQ = HD > 128 ? 32 : 64, SUB = BQ / 32 / HALVES, KS = HD / 16, DT = (HD + 31) / 32, TILE = BQ * HD;
+  constexpr int BQ = HD > 128 ? 32 : 64, SUB = BY_GRADIENT ? 1 : BQ / 32 / HALVES, KS = HD / 16, DT = (HD + 31) / 32, TILE = BQ * HD;
   typedef Pieces<HD, BQ, WAVES> P;
   __shared__ __attribute__((aligned(256))) uint16_t lds[2][2][TILE];
   __shared__ __attribute__((aligned(256))) uint16_t v_tile[V_IN_LDS ? BM * HD : 128];
@@ -225,13 +229,14 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, HD > 128 ? 1 : 2) void keys_
     }
   };
 
-  f32x16 dk[DT], dv[DT];
+  f32x16 dk[DT], dv[BY_GRADIENT ? 1 : DT];     // (by gradient: a wave's own one in dk)
 #pragma unroll
   for (int t = 0; t < DT; ++t)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) dk[t][i] = dv[t][i] = 0.f;
+    for (int i = 0; i < 16; ++i) dk[t][i] = dv[BY_GRADIENT ? 0 : t][i] = 0.f;
   const float scale2 = a.scale * LOG2E;
-  const lds_t tiles = lds_address(lds[0][0]) + half * SUB * 32 * HD * 2, by_row = row_base<HD>(lane), v_row = lds_address(v_tile) + key_wave * 32 * HD * 2 + by_row;
+  const int sub0 = BY_GRADIENT ? 0 : half * SUB;
+  const lds_t tiles = lds_address(lds[0][0]) + sub0 * 32 * HD * 2, by_row = row_base<HD>(lane), v_row = lds_address(v_tile) + key_wave * 32 * HD * 2 + by_row;
   const ColumnBase<HD> by_column = column_base<HD>(lane);
   if (n_tiles > 0) request(0, 0);
   settle(kf);                                  // (behind the first request: one wait for both)
@@ -243,7 +248,7 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, HD > 128 ? 1 : 2) void keys_
     const lds_t qt = tiles + (t & 1) * 4 * TILE, ot = qt + 2 * TILE;
 #pragma unroll
     for (int u = 0; u < SUB; ++u) {
-      const int base = m0 + t * BQ + 32 * (half * SUB + u);
+      const int base = m0 + t * BQ + 32 * (sub0 + u);
       if (base >= m1) break;
       const int p_lo = base / G, p_hi = min(base + 31, M - 1) / G;
       if (p_hi < kw || (a.window && kw + 31 <= p_lo - a.window && kw >= a.sinks)) continue;
@@ -253,6 +258,7 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, HD > 128 ? 1 : 2) void keys_
       for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
 #pragma unroll
       for (int i = 0; i < KS; ++i) sc = T::mfma32(row_frag<HD, vec8>(qt + by_row, 32 * u, i), kf[i], sc);
+      if (!BY_GRADIENT || half)
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
         if constexpr (V_IN_LDS) dp = T::mfma32(row_frag<HD, vec8>(ot + by_row, 32 * u, i), row_frag<HD, vec8>(v_row, 0, i), dp);
@@ -262,7 +268,7 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, HD > 128 ? 1 : 2) void keys_
       u32x4 pw[2], sw[2];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int r = 32 * (half * SUB + u) + 8 * j + 4 * g;
+        const int r = 32 * (sub0 + u) + 8 * j + 4 * g;
         const f32x4 lse2 = *(const f32x4*)&stat[t & 1][0][r], delta = *(const f32x4*)&stat[t & 1][1][r];
         float p[4], ds[4];
 #pragma unroll
@@ -285,14 +291,21 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, HD > 128 ? 1 : 2) void keys_
       const ColumnBase<HD> oc = {ot + by_column.all, ot + by_column.last}, qc = {qt + by_column.all, qt + by_column.last};
 #pragma unroll
       for (int v = 0; v < 2; ++v) {
+        if constexpr (BY_GRADIENT) {
+          const ColumnBase<HD> mine = {half ? qc.all : oc.all, half ? qc.last : oc.last};
+          const u32x4 w = half ? sw[v] : pw[v];
 #pragma unroll
-        for (int d = 0; d < DT; ++d) dv[d] = T::mfma32(column_frag<HD, vec8>(oc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, pw[v]), dv[d]);
+          for (int d = 0; d < DT; ++d) dk[d] = T::mfma32(column_frag<HD, vec8>(mine, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, w), dk[d]);
+        } else {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) dk[d] = T::mfma32(column_frag<HD, vec8>(qc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, sw[v]), dk[d]);
+          for (int d = 0; d < DT; ++d) dv[d] = T::mfma32(column_frag<HD, vec8>(oc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, pw[v]), dv[d]);
+#pragma unroll
+          for (int d = 0; d < DT; ++d) dk[d] = T::mfma32(column_frag<HD, vec8>(qc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, sw[v]), dk[d]);
+        }
       }
     }
   }
-  if constexpr (HALVES > 1) {
+  if constexpr (HALVES > 1 && !BY_GRADIENT) {
     // the second half's sums through LDS, first those of dv, then those of dk: a register of 64 lanes a 256-byte row
     static_assert(sizeof(lds) >= 4 * DT * 16 * 64 * sizeof(float), "the tiles' place holds one gradient of four waves");
     float* meet = (float*)lds + key_wave * DT * 16 * 64 + lane;
@@ -329,13 +342,21 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, HD > 128 ? 1 : 2) void keys_
       for (int j = 0; j < 4; ++j) {
         const int d = 32 * t + 8 * j + 4 * g;
         if (d >= a.h) continue;
-        *(f32x4*)(to + d) = f32x4{dk[t][4 * j], dk[t][4 * j + 1], dk[t][4 * j + 2], dk[t][4 * j + 3]} * back;
-        *(f32x4*)(to + to_values + d) = f32x4{dv[t][4 * j], dv[t][4 * j + 1], dv[t][4 * j + 2], dv[t][4 * j + 3]};
+        if constexpr (BY_GRADIENT) {
+          *(f32x4*)(to + (half ? 0 : to_values) + d) = f32x4{dk[t][4 * j], dk[t][4 * j + 1], dk[t][4 * j + 2], dk[t][4 * j + 3]} * (half ? back : 1.f);
+        } else {
+          *(f32x4*)(to + d) = f32x4{dk[t][4 * j], dk[t][4 * j + 1], dk[t][4 * j + 2], dk[t][4 * j + 3]} * back;
+          *(f32x4*)(to + to_values + d) = f32x4{dv[t][4 * j], dv[t][4 * j + 1], dv[t][4 * j + 2], dv[t][4 * j + 3]};
+        }
       }
   }
   const bool whole_sum = key < q.n && slot <= 0 && !parted && !in_runs;
-  store_row<T, DT>((uint16_t*)a.dk + row * a.dk_stride + (long long)kvh * a.h, dk, back, a.h, g, whole_sum);
-  store_row<T, DT>((uint16_t*)a.dv + row * a.dv_stride + (long long)kvh * a.h, dv, 1.f, a.h, g, whole_sum);
+  if constexpr (BY_GRADIENT) {
+    store_row<T, DT>((uint16_t*)(half ? a.dk : a.dv) + row * (half ? a.dk_stride : a.dv_stride) + (long long)kvh * a.h, dk, half ? back : 1.f, a.h, g, whole_sum);
+  } else {
+    store_row<T, DT>((uint16_t*)a.dk + row * a.dk_stride + (long long)kvh * a.h, dk, back, a.h, g, whole_sum);
+    store_row<T, DT>((uint16_t*)a.dv + row * a.dv_stride + (long long)kvh * a.h, dv, 1.f, a.h, g, whole_sum);
+  }
 }
 
 // Adds up the parts of SUM_KEYS of a tile's keys (tile blockIdx.y), always in the same order.
@@ -519,8 +540,7 @@ void part_sinks(Backward& b) {
 // The queries that see a tile of keys are parted where the longest such walk would take well over an even share of all (512 blocks, two to
 // a CU; one where h > 128): few kv heads with many query heads each, a long sequence.  A part has at least 512 rows; partial sums stay below 256 MB.
 // Measured on six sequences of 500 to 2000 tokens, 12 heads over 2 of 96: 476 us in one walk, 224 parted with 10 for the sums; 16 over 4 of
-// 64: 222 us, 97 with 6.  Where walks are even already a part only adds its sums: 8 over 4 of 256 in half tiles of 512 blocks' share: 547
-// us, 642 with 87.
+// 64: 222 us, 97 with 6.
 void part_runs(Backward& b) {
   const WindowArgs& a = b.a;
   b.runs = 1;
@@ -541,6 +561,14 @@ void part_runs(Backward& b) {
   if (runs < 2) return;
   b.runs = (int)runs;
   b.run = (int)((longest + runs - 1) / runs);
+}
+Backward parted(const WindowArgs& a) {
+  Backward b;
+  b.a = a;
+  if (b.a.max_new > a.rows) b.a.max_new = a.rows < 1 ? 1 : a.rows;
+  part_sinks(b);
+  part_runs(b);
+  return b;
 }
 size_t round_up(size_t n) { return (n + 255) / 256 * 256; }
 // places the buffers and returns their size
@@ -565,6 +593,7 @@ hipError_t launch(const Backward& b, hipStream_t s) {
   const WindowArgs& a = b.a;
   const int units = a.S * a.Hkv;
   const int key_tiles = (a.max_new + BM - 1) / BM, sink_tiles = (b.sinks + BM - 1) / BM, jobs = key_tiles * b.runs + sink_tiles * b.chunks;
+  if ((long long)(units + 7) * jobs * TPB * KEYS_HALVES<HD> > 0xffffffffll) return hipErrorInvalidConfiguration;      // (before the first launch)
   hipLaunchKernelGGL((delta_kernel<T, (HD > 128 ? 2 : 1)>), dim3(DELTA_BLOCKS), dim3(TPB), 0, s, b);
   const int tiles = (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
   if (a.window > 0 && a.window <= FEW_KEYS)
@@ -589,18 +618,12 @@ hipError_t by_head(const Backward& b, hipStream_t s) {
 }  // namespace
 
 size_t rl_window_backward_bytes(const WindowArgs& a) {
-  Backward b;
-  b.a = a;
-  part_sinks(b);
-  part_runs(b);
+  Backward b = parted(a);
   return place(b, nullptr);
 }
 hipError_t rl_window_backward(const WindowArgs& a, hipStream_t s) {
   if (a.rows <= 0) return hipSuccess;
-  Backward b;
-  b.a = a;
-  part_sinks(b);
-  part_runs(b);
+  Backward b = parted(a);
   place(b, (char*)a.ws);
   return a.dtype == RLGEN_DTYPE_F16 ? by_head<TypeF16>(b, s) : by_head<TypeBf16>(b, s);
 }

@@ -218,6 +218,7 @@ __device__ __forceinline__ Seq load_seq(const WindowArgs& a, int s, bool paged) 
   q.total = q.n;
   if (paged) q.total = (int)min((long long)max(a.total_lens[s], 0), (long long)a.table_stride << a.page_shift);
   q.ctx = q.total - q.n;
+  q.n = min(q.n, a.max_new);           // (grids and workspaces are sized by the caller's bound)
   return q;
 }
 // Block -> unit (sequence and kv head) and its job.  Blocks go round the eight XCDs, each with an L2 of its own: the jobs of one unit, which
