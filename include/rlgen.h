@@ -388,9 +388,13 @@ int rlgen_window_attention_backward(const void *q, int64_t q_stride, const void 
 /* Attention of new tokens over the cache that already holds them: the rows of sequence s are its last row_starts[s + 1] - row_starts[s]
  * tokens of total_lens[s] (as rlgen_plan_pages gives them).  max_new, max_total (HOST) bound rows and total_lens of every sequence;
  * max_new == 1 is a decode step: a sequence's keys are then parted over many waves where there are few sequences.  workspace: 16-byte
- * aligned, rlgen_window_attention_paged_workspace(...) bytes (may be 0, and workspace null then).
+ * aligned, rlgen_window_attention_paged_workspace(...) bytes (may be 0, and workspace null then).  max_new > 1 needs none; with
+ * rlgen_window_attention_chunk_workspace(...) bytes (0: parting would not pay) the keys of a few new rows behind a long context are parted
+ * over many blocks too.
  * Errors: NULL, BAD_ARG, WORKSPACE, DEVICE. */
 size_t rlgen_window_attention_paged_workspace(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t S, int32_t max_new,
+                                              int32_t max_total, int32_t window, int32_t sinks);
+size_t rlgen_window_attention_chunk_workspace(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t S, int32_t max_new,
                                               int32_t max_total, int32_t window, int32_t sinks);
 int rlgen_window_attention_paged(const void *q, int64_t q_stride, int32_t dtype, int32_t rows, int32_t n_q_heads, int32_t n_kv_heads,
                                  int32_t head_dim, const void *pages, int32_t n_pages, int32_t page_size, const int32_t *page_table,

@@ -179,6 +179,12 @@ size_t rlgen_window_attention_paged_workspace(int32_t n_q_heads, int32_t n_kv_he
   a.max_total = max_total;
   return window_ok(a) && max_new == 1 && max_total >= 1 ? rl_window_decode_bytes(a) : 0;
 }
+size_t rlgen_window_attention_chunk_workspace(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t S, int32_t max_new,
+                                              int32_t max_total, int32_t window, int32_t sinks) {
+  WindowArgs a = window_shape(RLGEN_DTYPE_BF16, 1, n_q_heads, n_kv_heads, head_dim, S, max_new, window, sinks, 1.f);
+  a.max_total = max_total;
+  return window_ok(a) && max_new > 1 && max_total >= 1 ? rl_window_rows_bytes(a) : 0;
+}
 int rlgen_window_attention_paged(const void* q, int64_t q_stride, int32_t dtype, int32_t rows, int32_t n_q_heads, int32_t n_kv_heads,
                                  int32_t head_dim, const void* pages, int32_t n_pages, int32_t page_size, const int32_t* page_table,
                                  int32_t table_stride, const int32_t* row_starts, const int32_t* total_lens, int32_t S, int32_t max_new,
@@ -199,6 +205,7 @@ int rlgen_window_attention_paged(const void* q, int64_t q_stride, int32_t dtype,
     if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return RLGEN_ERR_WORKSPACE;
     HIPCHK(rl_window_decode(a, (hipStream_t)hip_stream));
   } else {
+    if (workspace && !aligned16(workspace)) return RLGEN_ERR_WORKSPACE;
     HIPCHK(rl_window_rows(a, (hipStream_t)hip_stream));
   }
   return RLGEN_OK;

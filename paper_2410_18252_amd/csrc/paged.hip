@@ -505,7 +505,9 @@ __global__ __launch_bounds__(1024) void gain_grad_kernel(const float* partial, i
   }
 }
 
-// Blocks, and waves to a row.  Four waves share a row while rows are fewer than waves that the CUs hold.
+// Blocks, and waves to a row.  Four waves share a row while rows are fewer than waves that the CUs hold (128 rows of 48 heads of 128: 7.2
+// us, 10.9 with a wave to a row); beyond that a row to a wave spares the others' copies of its angles (8064 rows of 96 heads of 80: 67 us,
+// 85 with four waves to a row).
 struct Launch { int blocks, row_waves; };
 Launch norm_rope_launch(int rows) {
   const int row_waves = rows < 4096 ? 4 : 1;
@@ -544,8 +546,8 @@ hipError_t by_type(const NormRopeArgs& a, bool backward, Launch l, hipStream_t s
 }  // namespace
 
 hipError_t rl_plan_pages(PlanArgs a, hipStream_t s) {
-  // 256 blocks of requests at most while a block's requests fit its LDS; rows of a group are parted until a part has 1024 of them or
-  // the launch 1024 blocks
+  // 256 blocks of requests at most while a block's requests fit its LDS (1000 requests of one token: 5.5 us, 6.6 in 16 blocks; 512 prompts of
+  // 256 to 512 tokens: 6.3 us, 9.0); rows of a group are parted until a part has 1024 of them or the launch 1024 blocks (PLAN_FIGURE)
   a.group = (a.S + 255) / 256;
   if (a.group > PLAN_GROUP) a.group = PLAN_GROUP;
   const int groups = (a.S + a.group - 1) / a.group;

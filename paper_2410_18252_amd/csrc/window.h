@@ -48,6 +48,7 @@ struct WindowArgs {
   void* ws; size_t ws_bytes;
 };
 hipError_t rl_window_rows(WindowArgs a, hipStream_t s);
+size_t rl_window_rows_bytes(const WindowArgs& a);
 size_t rl_window_decode_bytes(const WindowArgs& a);
 hipError_t rl_window_decode(const WindowArgs& a, hipStream_t s);
 size_t rl_window_backward_bytes(const WindowArgs& a);

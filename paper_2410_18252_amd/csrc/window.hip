@@ -18,11 +18,11 @@ namespace {
 
 constexpr int TPB = 256, BM = 128;
 
-// Rows m_first .. m_first + 31 of a group's queries by one wave, key by key: what the matrix products cannot give where a value is infinite
+// Rows m_first .. m_end - 1 of a group's queries by one wave, key by key: what the matrix products cannot give where a value is infinite
 // or NaN, since a probability of zero times it is NaN for every query of the tile, not only for those that see it.  Reached only by
 // waves that found such a result.  64 keys at a time, one to a lane for the scores; for the sums a lane owns every 64th dim.
 template <class T, bool PAGED>
-__device__ void rows_key_by_key(const WindowArgs& a, const Seq& q, int s, int kvh, int m_first, int M, int lane) {
+__device__ void rows_key_by_key(const WindowArgs& a, const Seq& q, int s, int kvh, int m_first, int m_end, int lane) {
   const int G = a.Hq / a.Hkv;
   auto key_row = [&](int key, bool value) {
     if constexpr (PAGED) {
@@ -33,7 +33,7 @@ __device__ void rows_key_by_key(const WindowArgs& a, const Seq& q, int s, int kv
       return (const uint16_t*)(value ? a.v : a.k) + (long long)(q.row0 + key) * (value ? a.v_stride : a.k_stride) + (long long)kvh * a.h;
     }
   };
-  for (int m = m_first; m < min(m_first + 32, M); ++m) {
+  for (int m = m_first; m < m_end; ++m) {
     const int tok = m / G, head = kvh * G + m - tok * G, pos = q.ctx + tok, end = min(pos + 1, q.total);
     const int w_lo = a.window ? max(pos - a.window + 1, 0) : 0, sinks = max(min(min(a.sinks, w_lo), end), 0);
     const uint16_t* qp = (const uint16_t*)a.q + (long long)(q.row0 + tok) * a.q_stride + (long long)head * a.h;
@@ -75,8 +75,15 @@ __device__ void rows_key_by_key(const WindowArgs& a, const Seq& q, int s, int kv
   }
 }
 
+// Where blocks leave their part of the keys: [sequence, kv head, row of its group, part] the largest score and the sum, and h dims that
+// are not yet divided by it.
+struct RowParts { float2* stats; float* out; };
+__device__ __forceinline__ RowParts row_parts(const WindowArgs& a, int parts) {
+  return {(float2*)a.ws, (float*)((float2*)a.ws + ((long long)a.S * a.max_new * a.Hq * parts + 1) / 2 * 2)};
+}
+
 template <class T, int HD, bool PAGED>
-__global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) void window_rows_kernel(WindowArgs a, int tiles) {
+__global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) void window_rows_kernel(WindowArgs a, int tiles, int parts) {
   typedef typename T::vec8 vec8;
   constexpr int BN = 32, KS = HD / 16, DT = (HD + 31) / 32, TILE = BN * HD;
   constexpr int AHEAD = 6;
@@ -86,8 +93,9 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) 
   const int c = lane & 31, g = lane >> 5;
   const int G = a.Hq / a.Hkv;
   int unit, mt;
-  if (!map_block(blockIdx.x, a.S * a.Hkv, tiles, unit, mt)) return;
-  mt = tiles - 1 - mt;                                             // (late rows see most)
+  if (!map_block(blockIdx.x, a.S * a.Hkv, tiles * parts, unit, mt)) return;
+  const int part = PAGED ? mt % parts : 0;
+  mt = tiles - 1 - (PAGED ? mt / parts : mt);                      // (late rows see most)
   const int s = unit / a.Hkv, kvh = unit - s * a.Hkv;
   const Seq q = load_seq(a, s, PAGED);
   const int m0 = mt * BM, M = q.n * G;
@@ -172,20 +180,21 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) 
   ColumnBase<HD> v_base = column_base<HD>(lane);
   v_base.all += lds_address(lds[0][1]);
   v_base.last += lds_address(lds[0][1]);
-  if (n_tiles > 0) {
-    fetch_pages(0);
-    request(0, 0);
-    if (n_tiles > 1) fetch_pages(1);
+  const int t0 = PAGED ? (int)((long long)n_tiles * part / parts) : 0, t1 = PAGED ? (int)((long long)n_tiles * (part + 1) / parts) : n_tiles;
+  if (t0 < t1) {
+    fetch_pages(t0);
+    request(t0, t0 & 1);
+    if (t0 + 1 < t1) fetch_pages(t0 + 1);
   }
   settle(qf);                                  // (behind the first request: one wait for both)
-  for (int t = 0; t < n_tiles; ++t) {
+  for (int t = t0; t < t1; ++t) {
     // this tile has landed, and nobody reads the other buffer any more
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if constexpr (PAGED) settle_words(page_of);
-    if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
-    if (t + 2 < n_tiles) fetch_pages(t + 2);
+    if (t + 1 < t1) request(t + 1, (t + 1) & 1);
+    if (t + 2 < t1) fetch_pages(t + 2);
     const int kb = tile_key(t);
-    if (kb > wp_hi || (a.window && kb + BN - 1 <= wp_lo - a.window && kb >= a.sinks)) continue;
+    if (m0 + wave * 32 >= M || kb > wp_hi || (a.window && kb + BN - 1 <= wp_lo - a.window && kb >= a.sinks)) continue;
     const lds_t buffer = (t & 1) * 4 * TILE;
     const ColumnBase<HD> vb = {v_base.all + buffer, v_base.last + buffer};
     f32x16 sc;
@@ -236,8 +245,24 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) 
   for (int t = 0; t < DT; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) finite &= fabsf(o[t][i]) < INFINITY;
+  if (PAGED && parts > 1) {
+    if (!live) return;
+    const RowParts to = row_parts(a, parts);
+    const long long slot = ((long long)unit * a.max_new * G + m) * parts + part;
+    if (g == 0) to.stats[slot] = float2{mx, sum};
+    // (a value that is not finite is told by a sum that is none: its row is computed again where the parts are joined)
+    if (__shfl_xor(finite ? 1 : 0, 32, WAVE) == 0) finite = false;
+    if (g == 0 && !finite) to.stats[slot].y = __builtin_nanf("");
+    float* y = to.out + slot * a.h;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (32 * t + 8 * j + 4 * g < a.h) *(f32x4*)(y + 32 * t + 8 * j + 4 * g) = f32x4{o[t][4 * j], o[t][4 * j + 1], o[t][4 * j + 2], o[t][4 * j + 3]};
+    return;
+  }
   if (__any(live && !finite)) {
-    rows_key_by_key<T, PAGED>(a, q, s, kvh, m0 + wave * 32, M, lane);
+    rows_key_by_key<T, PAGED>(a, q, s, kvh, m0 + wave * 32, min(m0 + wave * 32 + 32, M), lane);
     return;
   }
   const long long row = q.row0 + tok;
@@ -245,12 +270,86 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) 
   store_row<T, DT>((uint16_t*)a.out + row * a.out_stride + (long long)head * a.h, o, inv, a.h, g, live);
 }
 
+// Adds up the parts of a row in their order: a row to 16, 32 or 64 lanes (`lanes`), four dims to a lane.
+template <class T>
+__global__ __launch_bounds__(TPB) void rows_join_kernel(WindowArgs a, int parts, int lanes) {
+  const int lane = threadIdx.x & 63, G = a.Hq / a.Hkv;
+  const long long rows = (long long)a.max_new * G, all = (long long)a.S * a.Hkv * rows, first = ((long long)blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 / lanes);
+  const long long at = first + lane / lanes;
+  if (first >= all) return;
+  const int unit = (int)(min(at, all - 1) / rows), m = (int)(min(at, all - 1) - unit * rows), s = unit / a.Hkv, kvh = unit - s * a.Hkv;
+  const Seq q = load_seq(a, s, true);
+  const bool live = at < all && m < q.n * G;
+  const RowParts from = row_parts(a, parts);
+  const float2* stats = from.stats + ((long long)unit * rows + m) * parts;
+  const float* out = from.out + ((long long)unit * rows + m) * parts * a.h;
+  const int d = lane % lanes * 4, tok = m / G, head = kvh * G + m - tok * G;
+  float mx = -INFINITY, sum = 0.f;
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  if (live) {
+    for (int p = 0; p < parts; ++p) mx = fmaxf(mx, stats[p].x);
+    const float base = mx == -INFINITY ? 0.f : mx;
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p) {
+      const float2 part = stats[p];
+      const float f = __builtin_amdgcn_exp2f(part.x - base);
+      sum = fmaf(part.y, f, sum);
+      if (d < a.h) y += *(const f32x4*)(out + (long long)p * a.h + d) * f;
+    }
+    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+    const long long row = q.row0 + tok;
+    if (d < a.h) *(u32x2*)((uint16_t*)a.out + row * a.out_stride + (long long)head * a.h + d) = u32x2{T::pack(y[0] * inv, y[1] * inv), T::pack(y[2] * inv, y[3] * inv)};
+    if (a.lse && d == 0) a.lse[row * a.Hq + head] = sum == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  }
+  for (int i = 0; i < 64; i += lanes) {
+    if (!__shfl(live && sum != sum ? 1 : 0, i, WAVE)) continue;
+    const int s1 = __shfl(s, i, WAVE), kvh1 = __shfl(kvh, i, WAVE), m1 = __shfl(m, i, WAVE);
+    rows_key_by_key<T, true>(a, load_seq(a, s1, true), s1, kvh1, m1, m1 + 1, lane);
+  }
+}
+
+// Parts of the keys of a call over pages: those whose walk, with what writing and reading the partial results adds, is estimated to be the
+// shortest, a part having at least eight tiles and partial results staying below 128 MB.  A tile of keys costs a block about 0.9 us alone on its CU and 0.45 us for each other block
+// there; partial results pass at 4 TB/s and the second launch costs 5 us.  Measured whole and parted: 8 new tokens on 12000, 32 heads over
+// 8 of 128, 338 us and 46; 500 on 8000, 234 and 118; 3 on each of seven of 1067 to 6375, 32 heads of 80, 189 and 59; but 200 on each of
+// four with a window of 1024, 38 and 53: those stay whole.
+int rows_parts(const WindowArgs& a) {
+  const int G = a.Hq / a.Hkv, at_once = a.h > 128 ? 1 : a.h > 96 ? 3 : 4;
+  const double blocks = (double)(((long long)a.max_new * G + BM - 1) / BM) * a.S * a.Hkv, row_us = (double)a.S * a.max_new * a.Hq * (a.h + 2) * 8 / 4e6;
+  long long seen = a.max_total;
+  if (a.window && (long long)a.window + BM / G + a.sinks < seen) seen = (long long)a.window + BM / G + a.sinks;
+  const double tiles = (double)((seen + 31) / 32);
+  int best = 1;
+  double best_us = 0;
+  for (int parts = 1; parts <= 64 && (parts == 1 || (parts * 8 <= tiles && parts * row_us < 64)); ++parts) {
+    const double on_cu = ceil(blocks * parts / 256), rounds = ceil(on_cu / at_once);
+    const double us = ceil(tiles / parts) * rounds * 0.45 * (1 + (on_cu < at_once ? on_cu : at_once)) + (parts > 1 ? 5 + parts * row_us : 0);
+    if (parts == 1 || us < best_us) {
+      best = parts;
+      best_us = us;
+    }
+  }
+  return best;
+}
+size_t parts_bytes(const WindowArgs& a, int parts) {
+  return parts > 1 ? ((size_t)a.S * a.max_new * a.Hq * parts + 1) / 2 * 2 * (sizeof(float2) + (size_t)a.h * sizeof(float)) : 0;
+}
+
 template <class T, int HD>
 hipError_t launch_rows(const WindowArgs& a, hipStream_t s) {
   const int tiles = (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
-  const dim3 grid(mapped_blocks(a.S * a.Hkv, tiles));
-  if (a.pages) hipLaunchKernelGGL((window_rows_kernel<T, HD, true>), grid, dim3(TPB), 0, s, a, tiles);
-  else hipLaunchKernelGGL((window_rows_kernel<T, HD, false>), grid, dim3(TPB), 0, s, a, tiles);
+  if (!a.pages) {
+    hipLaunchKernelGGL((window_rows_kernel<T, HD, false>), dim3(mapped_blocks(a.S * a.Hkv, tiles)), dim3(TPB), 0, s, a, tiles, 1);
+    return hipGetLastError();
+  }
+  int parts = rows_parts(a);
+  if (parts > 1 && (!a.ws || a.ws_bytes < parts_bytes(a, parts))) parts = 1;
+  hipLaunchKernelGGL((window_rows_kernel<T, HD, true>), dim3(mapped_blocks(a.S * a.Hkv, tiles * parts)), dim3(TPB), 0, s, a, tiles, parts);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || parts == 1) return e;
+  const int lanes = a.h <= 64 ? 16 : a.h <= 128 ? 32 : 64;
+  const long long waves = ((long long)a.S * a.max_new * a.Hq + 64 / lanes - 1) / (64 / lanes);
+  hipLaunchKernelGGL((rows_join_kernel<T>), dim3((unsigned)((waves + 3) / 4)), dim3(TPB), 0, s, a, parts, lanes);
   return hipGetLastError();
 }
 template <class T>
@@ -268,6 +367,7 @@ hipError_t by_head(const WindowArgs& a, hipStream_t s) {
 
 hipError_t rl_window_rows(WindowArgs a, hipStream_t s) {
   if (a.rows <= 0) return hipSuccess;
-  if (a.max_new > a.rows) a.max_new = a.rows;
+  if (!a.pages && a.max_new > a.rows) a.max_new = a.rows;
   return a.dtype == RLGEN_DTYPE_F16 ? by_head<TypeF16>(a, s) : by_head<TypeBf16>(a, s);
 }
+size_t rl_window_rows_bytes(const WindowArgs& a) { return parts_bytes(a, rows_parts(a)); }

@@ -131,7 +131,7 @@ __device__ __forceinline__ float ds_factor(const Backward& b) {
 // parts_sum_kernel; else the block of the first keys would run for as long as all others together.  The same where few kv heads with many
 // query heads, or a long sequence, would leave a few blocks the longest walks.
 // At 128 dims eight waves share a block's keys, the second four taking the second half of every tile of queries, and add up in LDS at the
-// end: a block's keys, whose queries are a long serial walk, then take half as long (three sequences of
+// end, since a block's queries are a long serial walk (three sequences of
 // 1500 to 4000, window 1024, 32 heads over 8: 357 us, 480 with four waves).
 template <int HD> constexpr int KEYS_HALVES = HD >= 128 ? 2 : 1;
 // At 256 dims both gradients of a wave's keys would need all 512 registers and more: the first four waves take dv, the second dk, and both
@@ -519,8 +519,15 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
   store_row<T, DT>((uint16_t*)a.dq + row * a.dq_stride + (long long)head * a.h, dq, a.scale / factor, a.h, g, live);
 }
 
-// Sinks are parted while their partial sums (two fp32 vectors a sink, kv head and part) stay below 64 MB, into parts of a window but at
-// least 1024 tokens, which cost a block about what a tile of keys costs.
+// A walk of a tile of keys over the tokens that see it is long or short beside an even share of all such walks (512 blocks, two to a CU;
+// one where h > 128), but no part has less than 512 rows.
+int even_walk(const WindowArgs& a, long long walk) {
+  const long long tiles = (long long)a.rows * a.Hkv / BM + (long long)a.S * a.Hkv / 2 + 1, blocks = a.h > 128 ? 256 : 512;
+  const int G = a.Hq / a.Hkv, least = (512 + G - 1) / G;
+  const long long even = (tiles * walk + blocks - 1) / blocks;
+  return (int)(even < least ? least : even < a.max_new ? even : a.max_new);
+}
+// Sinks are parted while their partial sums (two fp32 vectors a sink, kv head and part) stay below 64 MB: into even shares.
 void part_sinks(Backward& b) {
   const WindowArgs& a = b.a;
   b.sinks = b.chunks = 0;
@@ -528,7 +535,8 @@ void part_sinks(Backward& b) {
   const int sinks = a.sinks < a.max_new ? a.sinks : a.max_new;
   const long long beyond = (long long)a.max_new - (BM - 1 + (long long)a.window);
   if (!a.window || sinks < 1 || beyond < 1) return;
-  long long chunk = a.window > 1024 ? a.window : 1024, chunks = (beyond + chunk - 1) / chunk;
+  const int chunk = even_walk(a, (long long)a.window + BM - 1);
+  long long chunks = (beyond + chunk - 1) / chunk;
   const long long slot = (long long)a.S * a.Hkv * sinks * a.h * 2 * 4;
   if (chunks > 63) chunks = 63;
   if (slot * (chunks + 1) > (64ll << 20)) chunks = (64ll << 20) / slot - 1;
@@ -537,22 +545,18 @@ void part_sinks(Backward& b) {
   b.chunks = (int)chunks;
   b.chunk = (int)((beyond + chunks - 1) / chunks);
 }
-// The queries that see a tile of keys are parted where the longest such walk would take well over an even share of all (512 blocks, two to
-// a CU; one where h > 128): few kv heads with many query heads each, a long sequence.  A part has at least 512 rows; partial sums stay below 256 MB.
+// The queries that see a tile of keys are parted where the longest such walk would take well over an even share: few kv heads with many
+// query heads each, a long sequence.  Partial sums stay below 256 MB.
 // Measured on six sequences of 500 to 2000 tokens, 12 heads over 2 of 96: 476 us in one walk, 224 parted with 10 for the sums; 16 over 4 of
 // 64: 222 us, 97 with 6.
 void part_runs(Backward& b) {
   const WindowArgs& a = b.a;
   b.runs = 1;
   b.run = a.max_new;
-  const int G = a.Hq / a.Hkv;
   long long longest = a.max_new;
   const bool bounded = a.window > 0 && (b.sinks > 0 || a.sinks == 0) && (long long)a.window + BM - 1 < longest;
   if (bounded) longest = (long long)a.window + BM - 1;
-  const long long tiles = (long long)a.rows * a.Hkv / BM + (long long)a.S * a.Hkv / 2 + 1;
-  const int even = a.h > 128 ? 256 : 512;
-  long long run = (tiles * (bounded ? longest : longest / 2) + even - 1) / even;
-  if (run < (512 + G - 1) / G) run = (512 + G - 1) / G;
+  const long long run = even_walk(a, bounded ? longest : longest / 2);
   if (2 * longest <= 3 * run) return;
   long long runs = (longest + run - 1) / run;
   if (runs > 8) runs = 8;

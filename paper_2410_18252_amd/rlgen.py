@@ -31,7 +31,7 @@ EXPORTS = ["rlgen_workspace_bytes", "rlgen_create", "rlgen_update_weights", "rlg
            "rlgen_status_bits", "rlgen_strerror", "rlgen_destroy", "rlgen_plan_pages", "rlgen_rope_table", "rlgen_qk_norm_rope",
            "rlgen_qk_norm_rope_backward", "rlgen_qk_norm_rope_backward_workspace", "rlgen_window_attention",
            "rlgen_window_attention_backward", "rlgen_window_attention_backward_workspace", "rlgen_window_attention_paged",
-           "rlgen_window_attention_paged_workspace"]
+           "rlgen_window_attention_paged_workspace", "rlgen_window_attention_chunk_workspace"]
 FAULT_TOKEN, FAULT_UNIFORM, FAULT_GROUP, FAULT_RANGE = 1, 2, 4, 8
 PLAN_ROWS, PLAN_PAGES, PLAN_TABLE, PLAN_LENGTH = 1, 2, 4, 8
 
@@ -119,7 +119,8 @@ for _name, _types in {
         "rlgen_window_attention_paged": _ROWS + [_i32] * 5 + [_vp, _i32, _i32, _vp, _i32, _vp, _vp] + [_i32] * 5 + [_f32] + _ROWS + [_vp, _vp, _size, _vp]}.items():
     getattr(lib, _name).restype, getattr(lib, _name).argtypes = C.c_int, _types
 for _name, _count in {"rlgen_qk_norm_rope_backward_workspace": 2, "rlgen_window_attention_backward_workspace": 8,
-                      "rlgen_window_attention_paged_workspace": 8}.items():
+                      "rlgen_window_attention_paged_workspace": 8,
+                      "rlgen_window_attention_chunk_workspace": 8}.items():
     getattr(lib, _name).restype, getattr(lib, _name).argtypes = _size, [_i32] * _count
 lib.rlgen_destroy.restype = None
 lib.rlgen_destroy.argtypes = [_vp]
@@ -561,7 +562,8 @@ def rlgen_window_attention_paged(q, pages, page_table, row_starts, total_lens, m
     o, lse = out if out is not None else (torch.empty((rows, n_q, h), dtype=dt, device=q.device),
                                           torch.empty((rows, n_q), dtype=torch.float32, device=q.device))
     assert o.shape == q.shape and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (rows, n_q)
-    need = lib.rlgen_window_attention_paged_workspace(n_q, n_kv, h, S, max_new, max_total, window, sinks)
+    size = lib.rlgen_window_attention_paged_workspace if max_new == 1 else lib.rlgen_window_attention_chunk_workspace
+    need = size(n_q, n_kv, h, S, max_new, max_total, window, sinks)
     if workspace is None and need:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     _check(lib.rlgen_window_attention_paged(*_heads(q, dt), _DTYPES[dt], rows, n_q, n_kv, h, *_pages(pages, n_kv, h), _ints(page_table, S, stride), stride,
