@@ -13,7 +13,7 @@
 namespace {
 
 constexpr int TPB = 256, BM = 128;
-constexpr int DELTA_BLOCKS = 1024;
+constexpr int DELTA_BLOCKS = 1024;              // at most
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int FEW_KEYS = 16;
 
@@ -23,6 +23,7 @@ struct Backward {
   float *lse2, *delta, *peak, *part;    // [rows, Hq]: lse log2 e, delta; the largest |dout| and |v| of each block; the sinks' parts
   int sinks, chunk, chunks;             // sinks that are parted (0: none); tokens to a part; parts of the longest sequence
   float* run_part;                      // [runs, rows, Hkv, 2, h]
+  int delta_blocks;                     // that delta_kernel has
   int run, runs;                        // tokens to a part of what a tile of keys is seen by, most parts (1: not parted)
 };
 
@@ -115,7 +116,7 @@ __device__ __forceinline__ float ds_factor(const Backward& b) {
   float peak[2] = {0.f, 0.f};
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    for (int i = threadIdx.x & 63; i < DELTA_BLOCKS; i += 64) peak[k] = fmaxf(peak[k], b.peak[k * DELTA_BLOCKS + i]);
+    for (int i = threadIdx.x & 63; i < b.delta_blocks; i += 64) peak[k] = fmaxf(peak[k], b.peak[k * DELTA_BLOCKS + i]);
     peak[k] = wave_max(peak[k]);
   }
   const float most = 2.f * (float)b.a.h * peak[0] * peak[1];
@@ -570,6 +571,9 @@ Backward parted(const WindowArgs& a) {
   Backward b;
   b.a = a;
   if (b.a.max_new > a.rows) b.a.max_new = a.rows < 1 ? 1 : a.rows;
+  // a block has 64 (row, head) pairs at once; the keys' and queries' sides read a maximum of each block
+  const long long blocks = ((long long)a.rows * a.Hq + 63) / 64;
+  b.delta_blocks = blocks < 1 ? 1 : blocks < DELTA_BLOCKS ? (int)blocks : DELTA_BLOCKS;
   part_sinks(b);
   part_runs(b);
   return b;
@@ -598,7 +602,7 @@ hipError_t launch(const Backward& b, hipStream_t s) {
   const int units = a.S * a.Hkv;
   const int key_tiles = (a.max_new + BM - 1) / BM, sink_tiles = (b.sinks + BM - 1) / BM, jobs = key_tiles * b.runs + sink_tiles * b.chunks;
   if ((long long)(units + 7) * jobs * TPB * KEYS_HALVES<HD> > 0xffffffffll) return hipErrorInvalidConfiguration;      // (before the first launch)
-  hipLaunchKernelGGL((delta_kernel<T, (HD > 128 ? 2 : 1)>), dim3(DELTA_BLOCKS), dim3(TPB), 0, s, b);
+  hipLaunchKernelGGL((delta_kernel<T, (HD > 128 ? 2 : 1)>), dim3(b.delta_blocks), dim3(TPB), 0, s, b);
   const int tiles = (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
   if (a.window > 0 && a.window <= FEW_KEYS)
     hipLaunchKernelGGL((queries_backward_kernel<T, HD, true>), dim3(mapped_blocks(units, tiles)), dim3(TPB), 0, s, b, tiles);
