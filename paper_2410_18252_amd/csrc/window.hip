@@ -141,6 +141,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) 
       }
     }
   };
+  const lds_t tiles0 = lds_address(lds[0][0]);
   auto request = [&](int t, int buf) {
     const int base = tile_key(t);
     if constexpr (PAGED) {
@@ -155,14 +156,14 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) 
         const uint16_t* ks = (const uint16_t*)a.pages + at * a.h + dim;
         const uint16_t* vs = ks + ((long long)a.Hkv << a.page_shift) * a.h;
         if (dim >= a.h) ks = vs = (const uint16_t*)&zero_chunk;
-        const int to = (n * 4 + wave) * 512;
-        ::request(ks, lds[buf][0] + to);
-        ::request(vs, lds[buf][1] + to);
+        const lds_t to = tiles0 + buf * 4 * TILE + (n * 4 + wave) * 1024;
+        ::request(ks, to);
+        ::request(vs, to + 2 * TILE);
       }
     } else {
       const int rows = min(q.n - base, BN);
-      request_pieces(k_rows.tile(base, rows), k_off, lds[buf][0], wave);
-      request_pieces(v_rows.tile(base, rows), v_off, lds[buf][1], wave);
+      request_pieces(k_rows.tile(base, rows), k_off, tiles0 + buf * 4 * TILE, wave);
+      request_pieces(v_rows.tile(base, rows), v_off, tiles0 + buf * 4 * TILE + 2 * TILE, wave);
     }
   };
 
@@ -176,10 +177,10 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) 
   constexpr float RISE = 8.f;
   float mx = -INFINITY, sum = 0.f;
   const float scale2 = score_factor(a.scale);
-  const lds_t k_base = lds_address(lds[0][0]) + row_base<HD>(lane);
+  const lds_t k_base = tiles0 + row_base<HD>(lane);
   ColumnBase<HD> v_base = column_base<HD>(lane);
-  v_base.all += lds_address(lds[0][1]);
-  v_base.last += lds_address(lds[0][1]);
+  v_base.all += tiles0 + 2 * TILE;
+  v_base.last += tiles0 + 2 * TILE;
   const int t0 = PAGED ? (int)((long long)n_tiles * part / parts) : 0, t1 = PAGED ? (int)((long long)n_tiles * (part + 1) / parts) : n_tiles;
   if (t0 < t1) {
     fetch_pages(t0);
@@ -187,6 +188,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) 
     if (t0 + 1 < t1) fetch_pages(t0 + 1);
   }
   settle(qf);                                  // (behind the first request: one wait for both)
+  scalars_landed();
   for (int t = t0; t < t1; ++t) {
     // this tile has landed, and nobody reads the other buffer any more
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");

@@ -206,13 +206,14 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
     }
     if constexpr (V_IN_LDS)
       request_pieces(row_source(a.v, q.row0, a.v_stride, kvh, 1, a.h).tile(kt * BM, min(q.n - kt * BM, BM)),
-                             piece_offsets<HD, BM, WAVES>(wave, lane, a.v_stride, a.h), v_tile, wave);
+                             piece_offsets<HD, BM, WAVES>(wave, lane, a.v_stride, a.h), lds_address(v_tile), wave);
   }
   const float factor = ds_factor<T>(b);
   // where tiles begin with a group's first head they all have the same offsets
   const bool even = BQ % G == 0;
   P q_off = flat_offsets<HD, BQ, WAVES>(wave, lane, a.q_stride, a.h, G, 0), o_off = flat_offsets<HD, BQ, WAVES>(wave, lane, a.dout_stride, a.h, G, 0);
   const RowSource q_rows = row_source(a.q, q.row0, a.q_stride, kvh * G, G, a.h), o_rows = row_source(a.dout, q.row0, a.dout_stride, kvh * G, G, a.h);
+  const lds_t tiles0 = lds_address(lds[0][0]), stats0 = lds_address(stat[0][0]);
   auto request = [&](int t, int buf) {
     const int base = m0 + t * BQ, tok_base = even ? tok0 + t * (BQ / G) : base / G;
     if (!even) {
@@ -220,13 +221,13 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
       o_off = flat_offsets<HD, BQ, WAVES>(wave, lane, a.dout_stride, a.h, G, base - tok_base * G);
     }
     const int rows = min(q.n - tok_base, BQ);
-    request_pieces(q_rows.tile(tok_base, rows), q_off, lds[buf][0], wave);
-    request_pieces(o_rows.tile(tok_base, rows), o_off, lds[buf][1], wave);
+    request_pieces(q_rows.tile(tok_base, rows), q_off, tiles0 + buf * 4 * TILE, wave);
+    request_pieces(o_rows.tile(tok_base, rows), o_off, tiles0 + buf * 4 * TILE + 2 * TILE, wave);
     if (wave < 3) {
       const int m = min(base + lane, M - 1), tok = m / G, head = kvh * G + m - tok * G;
       const long long at = (long long)(q.row0 + tok) * a.Hq + head;
       if (wave == 2) stat[buf][2][lane] = __int_as_float(base + lane < m1 ? tok : -1);      // (a row past the job's sees nothing)
-      else request_word((wave ? b.delta : b.lse2) + at, stat[buf][wave]);
+      else request_word((wave ? b.delta : b.lse2) + at, stats0 + (buf * 3 + wave) * 256);
     }
   };
 
@@ -237,11 +238,12 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
     for (int i = 0; i < 16; ++i) dk[t][i] = dv[BY_GRADIENT ? 0 : t][i] = 0.f;
   const float scale2 = a.scale * LOG2E;
   const int sub0 = BY_GRADIENT ? 0 : half * SUB;
-  const lds_t tiles = lds_address(lds[0][0]) + sub0 * 32 * HD * 2, by_row = row_base<HD>(lane), v_row = lds_address(v_tile) + key_wave * 32 * HD * 2 + by_row;
+  const lds_t tiles = tiles0 + sub0 * 32 * HD * 2, by_row = row_base<HD>(lane), v_row = lds_address(v_tile) + key_wave * 32 * HD * 2 + by_row;
   const ColumnBase<HD> by_column = column_base<HD>(lane);
   if (n_tiles > 0) request(0, 0);
   settle(kf);                                  // (behind the first request: one wait for both)
   if constexpr (!V_IN_LDS) settle(vf);
+  scalars_landed();
   for (int t = 0; t < n_tiles; ++t) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
@@ -426,11 +428,12 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
   const float factor = ds_factor<T>(b);
   const Pieces<HD, BN> k_off = piece_offsets<HD, BN>(wave, lane, a.k_stride, a.h), v_off = piece_offsets<HD, BN>(wave, lane, a.v_stride, a.h);
   const RowSource k_rows = row_source(a.k, q.row0, a.k_stride, kvh, 1, a.h), v_rows = row_source(a.v, q.row0, a.v_stride, kvh, 1, a.h);
+  const lds_t tiles0 = lds_address(lds[0][0]);
   auto request = [&](int t, int buf) {
     const int base = tile_key(t);
     const int rows = min(q.n - base, BN);
-    request_pieces(k_rows.tile(base, rows), k_off, lds[buf][0], wave);
-    request_pieces(v_rows.tile(base, rows), v_off, lds[buf][1], wave);
+    request_pieces(k_rows.tile(base, rows), k_off, tiles0 + buf * 4 * TILE, wave);
+    request_pieces(v_rows.tile(base, rows), v_off, tiles0 + buf * 4 * TILE + 2 * TILE, wave);
   };
   f32x16 dq[DT];
 #pragma unroll
@@ -438,12 +441,13 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
 #pragma unroll
     for (int i = 0; i < 16; ++i) dq[t][i] = 0.f;
   const float scale2 = a.scale * LOG2E;
-  const lds_t tiles0 = lds_address(lds[0][0]), by_row = row_base<HD>(lane);
+  const lds_t by_row = row_base<HD>(lane);
   const ColumnBase<HD> by_column = column_base<HD>(lane);
   if (n_tiles > 0) request(0, 0);
   settle(qf);
   settle(of);
   settle_words(of_row);
+  scalars_landed();
   const float lse2 = of_row[0];
   float delta = of_row[1];
   // This lane's row against 32 keys of the tile in buffer `buf`: scores (of the products' scale) and dP

@@ -115,25 +115,25 @@ __device__ __forceinline__ Pieces<HD, ROWS, WAVES> flat_offsets(int wave, int la
 // of every LDS read the compiler waits for all requests that it knows to write LDS, those of the next tile among them; the barrier
 // that a tile begins with waits for them instead.  They have no output register, so none can be overwritten by a late answer, and m0 is
 // used by nothing else in these kernels.
-__device__ __forceinline__ void request(Buffer from, uint32_t offset, const void* to) {
+__device__ __forceinline__ void request(Buffer from, uint32_t offset, lds_t to) {
   u32x4 d;
   d[0] = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)from.base);
   d[1] = __builtin_amdgcn_readfirstlane((uint32_t)((uintptr_t)from.base >> 32) & 0xffffu);
   d[2] = __builtin_amdgcn_readfirstlane(from.bytes);
   d[3] = 0x00027000;
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(d), "s"(__builtin_amdgcn_readfirstlane(lds_address(to))) : "memory");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(d), "s"(__builtin_amdgcn_readfirstlane(to)) : "memory");
 }
-__device__ __forceinline__ void request(const void* from, const void* to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(__builtin_amdgcn_readfirstlane(lds_address(to))) : "memory");
+__device__ __forceinline__ void request(const void* from, lds_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(__builtin_amdgcn_readfirstlane(to)) : "memory");
 }
-__device__ __forceinline__ void request_word(const float* from, const float* to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(__builtin_amdgcn_readfirstlane(lds_address(to))) : "memory");
+__device__ __forceinline__ void request_word(const float* from, lds_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(__builtin_amdgcn_readfirstlane(to)) : "memory");
 }
 template <int HD, int ROWS, int WAVES>
-__device__ __forceinline__ void request_pieces(Buffer from, const Pieces<HD, ROWS, WAVES>& p, const uint16_t* tile, int wave) {
+__device__ __forceinline__ void request_pieces(Buffer from, const Pieces<HD, ROWS, WAVES>& p, lds_t tile, int wave) {
 #pragma unroll
   for (int n = 0; n < p.PER; ++n)
-    if (p.ALL % WAVES == 0 || n * WAVES + wave < p.ALL) request(from, p.off[n], tile + (n * WAVES + wave) * 512);
+    if (p.ALL % WAVES == 0 || n * WAVES + wave < p.ALL) request(from, p.off[n], tile + (n * WAVES + wave) * 1024);
 }
 
 // Has the wave wait for fragments that it loaded itself: in front of a loop, or the compiler waits inside it, where requests of the next
@@ -151,6 +151,10 @@ template <class W, int N> __device__ __forceinline__ void settle_words(W (&v)[N]
 #pragma unroll
   for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
 }
+
+// In front of a loop: scalar loads of what went before have landed.  They count with the LDS reads but come back in any order, so while the
+// compiler takes one to be on its way it waits for all reads in front of the first product instead of for that product's own.
+__device__ __forceinline__ void scalars_landed() { __builtin_amdgcn_s_waitcnt(0xc07f); }      // lgkmcnt(0) alone
 
 // Row of register i of a 32x32 result in lane group g (its column is lane % 32)
 __device__ __forceinline__ constexpr int acc_row(int i, int g) { return (i >> 2) * 8 + 4 * g + (i & 3); }
