@@ -447,7 +447,6 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
   settle(qf);
   settle(of);
   settle_words(of_row);
-  scalars_landed();
   const float lse2 = of_row[0];
   float delta = of_row[1];
   // This lane's row against 32 keys of the tile in buffer `buf`: scores (of the products' scale) and dP
@@ -492,6 +491,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
       if (live && g == 0 && pos < 32) b.delta[row * a.Hq + head] = sum;
     }
   }
+  scalars_landed();
   for (int t = 0; t < n_tiles; ++t) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
@@ -519,6 +519,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
 #pragma unroll
         for (int d = 0; d < DT; ++d) dq[d] = T::mfma32(column_frag<HD, vec8>(kc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, w), dq[d]);
       }
+      order_products<2, 3, 2 * DT>();
     }
   }
   store_row<T, DT>((uint16_t*)a.dq + row * a.dq_stride + (long long)head * a.h, dq, a.scale / factor, a.h, g, live);
