@@ -7,15 +7,24 @@
 // not change from run to run.  P and dS are rounded to the inputs' type for their second products, errors of the order of the
 // gradients' own rounding; fp16, whose smallest normal number a dS easily falls below, multiplies dS by a power of two taken from the
 // largest |dout| and |v|.
+//
+// The queries' side goes first, since it corrects delta for the rows that see few keys; its walk is the forward pass's.  Both sides are bound
+// by their chains of products, exponentials and barriers with two or three waves to a SIMD (matrix unit 43 and 33 % busy at 128 dims),
+// not by memory.  Measured: 8250 rows, 32 heads over 8 of 128, window 1024: delta 25 us, queries' side 203, keys' side 346, sums of the
+// sinks' parts 5 (0.30 TFLOP without the products that are computed twice); 9985 rows, 32 heads of 80 in fp16: 32, 112 and 164 us.
 #include "../../include/rlgen.h"
 #include "window_tiles.h"
+#include <type_traits>
 
 namespace {
 
 constexpr int TPB = 256, BM = 128;
 constexpr int DELTA_BLOCKS = 1024;              // at most
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr int FEW_KEYS = 16;
+constexpr int FEW_KEYS = 32, FEW_ROWS = 64;
+
+// What a pair loses when it is rounded to the word that it was packed into, as such a word
+template <class T> __device__ __forceinline__ uint32_t rest_of(float lo, float hi, uint32_t word) { return T::pack(lo - T::low(word), hi - T::high(word)); }
 
 // Everything below in the caller's workspace, and how the queries that see the sinks from beyond the window are parted.
 struct Backward {
@@ -144,7 +153,7 @@ __device__ __forceinline__ int last_seer(const Backward& b, int kt, int n) {
   return a.window && (b.sinks > 0 || kt * BM >= a.sinks) ? (int)min((long long)n, (long long)kt * BM + BM - 1 + a.window) : n;
 }
 
-template <class T, int HD>
+template <class T, int HD, bool FEW>
 __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel(Backward b, int key_tiles, int jobs) {
   typedef typename T::vec8 vec8;
   const WindowArgs& a = b.a;
@@ -290,8 +299,23 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
           pw[j >> 1][2 * (j & 1) + e] = T::pack(p[2 * e], p[2 * e + 1]);
           sw[j >> 1][2 * (j & 1) + e] = T::pack(ds[2 * e], ds[2 * e + 1]);
         }
+        if constexpr (FEW) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dp[4 * j + e] = ds[e];
+        }
       }
       const ColumnBase<HD> oc = {ot + by_column.all, ot + by_column.last}, qc = {qt + by_column.all, qt + by_column.last};
+      if (FEW && (!BY_GRADIENT || half)) {
+        // (as on the queries' side: with what the rounding of dS loses)
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          u32x4 rest;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) rest[e] = rest_of<T>(dp[8 * v + 2 * e], dp[8 * v + 2 * e + 1], sw[v][e]);
+#pragma unroll
+          for (int d = 0; d < DT; ++d) dk[d] = T::mfma32(column_frag<HD, vec8>(qc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, rest), dk[d]);
+        }
+      }
 #pragma unroll
       for (int v = 0; v < 2; ++v) {
         if constexpr (BY_GRADIENT) {
@@ -462,7 +486,10 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
   };
   // out was rounded, and where a row sees few keys its delta is nearly as large as its dP: there the rounding shows in dS.  Such rows
   // take delta from the sum over their keys of P dP and leave it for the keys' side: a sequence's first 32 rows from the 32 keys that they
-  // see at most, which begin the first tile; with a window of up to FEW_KEYS (FEW) all rows, in a pass of its own.
+  // see at most, which begin the first tile; all rows, in a pass of its own, where every row sees few (FEW: a window of up to FEW_KEYS, or
+  // sequences of up to FEW_ROWS).  There dS also takes part with what its rounding loses, on both sides: over few keys, whose dS add up to
+  // nothing, such errors do not average out (against the formulas in 64 bits up to 2.1 times the error of gradients that are rounded
+  // once, 1.44 with it).  Long sequences come to 1.45 without, and would pay 15 % of the keys' side for it.
   auto own_delta = [&](int buf, int u, int kb) {
     f32x16 sc, dp;
     products(buf, u, sc, dp);
@@ -483,12 +510,12 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
     if (live && g == 0) b.delta[row * a.Hq + head] = delta;
     __syncthreads();                           // (the tiles are filled again)
     if (n_tiles > 0) request(0, 0);
-  } else if (p_lo < 32) {
+  } else if (p_lo < FEW_KEYS) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (wp_lo < 32) {
+    if (wp_lo < FEW_KEYS) {
       const float sum = sum_halves(own_delta(0, 0, tile_key(0)));
-      delta = pos < 32 ? sum : delta;
-      if (live && g == 0 && pos < 32) b.delta[row * a.Hq + head] = sum;
+      delta = pos < FEW_KEYS ? sum : delta;
+      if (live && g == 0 && pos < FEW_KEYS) b.delta[row * a.Hq + head] = sum;
     }
   }
   scalars_landed();
@@ -516,6 +543,13 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
         u32x4 w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = T::pack(dp[8 * v + 2 * e], dp[8 * v + 2 * e + 1]);
+        if constexpr (FEW) {
+          u32x4 rest;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) rest[e] = rest_of<T>(dp[8 * v + 2 * e], dp[8 * v + 2 * e + 1], w[e]);
+#pragma unroll
+          for (int d = 0; d < DT; ++d) dq[d] = T::mfma32(column_frag<HD, vec8>(kc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, rest), dq[d]);
+        }
 #pragma unroll
         for (int d = 0; d < DT; ++d) dq[d] = T::mfma32(column_frag<HD, vec8>(kc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, w), dq[d]);
       }
@@ -609,11 +643,12 @@ hipError_t launch(const Backward& b, hipStream_t s) {
   if ((long long)(units + 7) * jobs * TPB * KEYS_HALVES<HD> > 0xffffffffll) return hipErrorInvalidConfiguration;      // (before the first launch)
   hipLaunchKernelGGL((delta_kernel<T, (HD > 128 ? 2 : 1)>), dim3(b.delta_blocks), dim3(TPB), 0, s, b);
   const int tiles = (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
-  if (a.window > 0 && a.window <= FEW_KEYS)
-    hipLaunchKernelGGL((queries_backward_kernel<T, HD, true>), dim3(mapped_blocks(units, tiles)), dim3(TPB), 0, s, b, tiles);
-  else
-    hipLaunchKernelGGL((queries_backward_kernel<T, HD, false>), dim3(mapped_blocks(units, tiles)), dim3(TPB), 0, s, b, tiles);
-  hipLaunchKernelGGL((keys_backward_kernel<T, HD>), dim3(mapped_blocks(units, jobs)), dim3(TPB * KEYS_HALVES<HD>), 0, s, b, key_tiles, jobs);
+  auto sides = [&](auto few) {
+    hipLaunchKernelGGL((queries_backward_kernel<T, HD, few>), dim3(mapped_blocks(units, tiles)), dim3(TPB), 0, s, b, tiles);
+    hipLaunchKernelGGL((keys_backward_kernel<T, HD, few>), dim3(mapped_blocks(units, jobs)), dim3(TPB * KEYS_HALVES<HD>), 0, s, b, key_tiles, jobs);
+  };
+  if ((a.window > 0 && a.window <= FEW_KEYS) || a.max_new <= FEW_ROWS) sides(std::true_type{});
+  else sides(std::false_type{});
   if (b.sinks > 0 || b.runs > 1) hipLaunchKernelGGL((parts_sum_kernel<T>), dim3((unsigned)units, b.runs > 1 ? key_tiles : sink_tiles, BM / SUM_KEYS), dim3(TPB), 0, s, b);
   return hipGetLastError();
 }
