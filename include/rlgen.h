@@ -317,10 +317,10 @@ int rlgen_status_bits(rlgen_ctx *ctx, void *hip_stream, uint32_t *faults);
  *    sees nothing has output 0 and log-sum-exp -infinity.
  *  - Sizes: rows, S * heads and n_pages * page_size below 2^31.  Offsets are 64-bit.
  * Entries of row_starts, page_table and slots that lie outside their arrays are clamped or skipped, never followed. */
-#define RLGEN_PLAN_ROWS    1   /* counts[3]: more rows than max_rows (those beyond are not written)            */
+#define RLGEN_PLAN_ROWS    1   /* counts[3]: more rows than max_rows or 2^31 - 2 (those beyond are not written) */
 #define RLGEN_PLAN_PAGES   2   /* the free list ran out (pages and slots that lack one are -1)                 */
 #define RLGEN_PLAN_TABLE   4   /* a sequence needs more pages than a table row has (its slots beyond are -1)   */
-#define RLGEN_PLAN_LENGTH  8   /* a negative length (taken as 0)                                               */
+#define RLGEN_PLAN_LENGTH  8   /* a negative length (taken as 0), or one that passes 2^31 - 1 (cut there)      */
 
 /* The plan of one pass over the cache, from the requests' lengths alone: sequence s holds ctx_lens[s] tokens and gets new_lens[s] more.
  * Pages that it needs for them are taken from free_pages [n_free] in the order of the sequences, from entry *free_head on (DEVICE, null:
@@ -329,6 +329,7 @@ int rlgen_status_bits(rlgen_ctx *ctx, void *hip_stream, uint32_t *faults);
  *  slots, positions [max_rows]          out: where row i's key and value go, and its position; rows that no sequence has: -1 and 0
  *  counts [4]                           out: rows; the free list's next head (min(head + pages taken, n_free)); longest length after the
  *                                       pass; RLGEN_PLAN_* bits
+ * Sums stop at 2^31 - 1 (row_starts and counts[0] with RLGEN_PLAN_ROWS), so no length or head leads outside the arrays.
  * free_head must not be counts + 1 itself; two counts arrays in turn chain passes without the host.
  * Errors: NULL, BAD_ARG (S < 1, max_rows < 0, n_free < 0, table_stride < 1, page_size), DEVICE. */
 int rlgen_plan_pages(const int32_t *ctx_lens, const int32_t *new_lens, int32_t S, int32_t page_size, const int32_t *free_pages,

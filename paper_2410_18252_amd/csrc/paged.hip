@@ -9,13 +9,17 @@ namespace {
 
 constexpr int TPB = 256;
 
+// The plan's counts are of lengths that only the device knows: sums of numbers that are not negative, which stay at the largest int instead of
+// passing it.
+constexpr int MOST = 0x7fffffff;
+__device__ __forceinline__ int add_counts(int a, int b) { return (int)min((unsigned)a + (unsigned)b, (unsigned)MOST); }
 __device__ __forceinline__ int block_sum(int v, int* red) {          // of a block of 256 threads; red: 4 ints
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, WAVE);
+  for (int o = 32; o > 0; o >>= 1) v = add_counts(v, __shfl_xor(v, o, WAVE));
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  return red[0] + red[1] + red[2] + red[3];
+  return add_counts(add_counts(red[0], red[1]), add_counts(red[2], red[3]));
 }
 __device__ __forceinline__ int block_max(int v, int* red) {
 #pragma unroll
@@ -30,24 +34,27 @@ __device__ __forceinline__ int block_exclusive(int v, int* red) {    // exclusiv
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int y = __shfl_up(x, o, WAVE);
-    if ((threadIdx.x & 63) >= (unsigned)o) x += y;
+    if ((threadIdx.x & 63) >= (unsigned)o) x = add_counts(x, y);
   }
   __syncthreads();
   if ((threadIdx.x & 63) == 63) red[threadIdx.x >> 6] = x;
   __syncthreads();
-  int before = 0;
-  for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) before += red[w];
-  return before + x - v;
+  const int up = __shfl_up(x, 1, WAVE);
+  int before = (threadIdx.x & 63) ? up : 0;
+  for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) before = add_counts(before, red[w]);
+  return before;
 }
 
 constexpr int PLAN_GROUP = 4 * TPB;          // most requests to a block
 
-// How far a request's lengths go.  A negative length counts as zero.
-struct Lens { int ctx, add, had, need; };
+// How far a request's lengths go.  A negative length counts as zero, a length after the pass that an int does not hold is cut.
+struct Lens { int ctx, add, had, need; bool odd; };
 __device__ __forceinline__ Lens plan_lens(const PlanArgs& a, int s) {
   Lens l;
-  l.ctx = max(a.ctx_lens[s], 0);
-  l.add = max(a.new_lens[s], 0);
+  const int ctx = a.ctx_lens[s], add = a.new_lens[s];
+  l.ctx = max(ctx, 0);
+  l.add = min(max(add, 0), MOST - l.ctx);
+  l.odd = (ctx < 0) | (add < 0) | (add > l.add);
   const int round = (1 << a.page_shift) - 1;
   l.had = (int)(((unsigned)l.ctx + round) >> a.page_shift);
   l.need = (int)(((unsigned)l.ctx + (unsigned)l.add + round) >> a.page_shift);
@@ -63,40 +70,40 @@ __global__ __launch_bounds__(TPB) void plan_pages_kernel(PlanArgs a) {
   __shared__ int row_end[PLAN_GROUP], page_end[PLAN_GROUP], lens_ctx[PLAN_GROUP], lens_had[PLAN_GROUP];
   const int s0 = blockIdx.x * a.group, n = min(a.group, a.S - s0);
   const bool last = s0 + n == a.S, writer = blockIdx.y == 0;
-  const int head = a.free_head ? max(*a.free_head, 0) : 0;
+  const int asked = a.free_head ? max(*a.free_head, 0) : 0, head = min(asked, a.n_free);      // (beyond the list there is no page)
   int rows = 0, pages = 0, longest = 0, faults = 0;
   for (int s = threadIdx.x; s < s0; s += TPB) {
     const Lens l = plan_lens(a, s);
-    rows += l.add;
-    pages += l.need - l.had;
+    rows = add_counts(rows, l.add);
+    pages = add_counts(pages, l.need - l.had);
     if (last) {
       longest = max(longest, l.ctx + l.add);
       if (l.need > a.table_stride) faults |= RLGEN_PLAN_TABLE;
-      if (a.ctx_lens[s] < 0 || a.new_lens[s] < 0) faults |= RLGEN_PLAN_LENGTH;
+      if (l.odd) faults |= RLGEN_PLAN_LENGTH;
     }
   }
-  const int rows0 = block_sum(rows, red), pages0 = head + block_sum(pages, red);
+  const int rows0 = block_sum(rows, red), pages0 = add_counts(head, block_sum(pages, red));
   // this block's own requests: consecutive ones to a thread, so that the scan is one over threads
   const int per = (n + TPB - 1) / TPB, own0 = threadIdx.x * per, own1 = min(own0 + per, n);
   rows = pages = 0;
   for (int i = own0; i < own1; ++i) {
     const Lens l = plan_lens(a, s0 + i);
-    rows += l.add;
-    pages += l.need - l.had;
+    rows = add_counts(rows, l.add);
+    pages = add_counts(pages, l.need - l.had);
     row_end[i] = rows;
     page_end[i] = pages;
     lens_ctx[i] = l.ctx;
     lens_had[i] = l.had;
     longest = max(longest, l.ctx + l.add);
     if (l.need > a.table_stride) faults |= RLGEN_PLAN_TABLE;
-    if (a.ctx_lens[s0 + i] < 0 || a.new_lens[s0 + i] < 0) faults |= RLGEN_PLAN_LENGTH;
+    if (l.odd) faults |= RLGEN_PLAN_LENGTH;
     if (writer) a.total_lens[s0 + i] = l.ctx + l.add;
   }
-  const int rows_before = rows0 + block_exclusive(rows, red), pages_before = pages0 + block_exclusive(pages, red);
+  const int rows_before = add_counts(rows0, block_exclusive(rows, red)), pages_before = add_counts(pages0, block_exclusive(pages, red));
   for (int i = own0; i < own1; ++i) {
     if (writer) a.row_starts[s0 + i] = i > own0 ? row_end[i - 1] : rows_before;
-    row_end[i] += rows_before;
-    page_end[i] += pages_before;
+    row_end[i] = add_counts(row_end[i], rows_before);
+    page_end[i] = add_counts(page_end[i], pages_before);
   }
   __syncthreads();
   const int rows1 = row_end[n - 1], pages1 = page_end[n - 1];
@@ -105,8 +112,8 @@ __global__ __launch_bounds__(TPB) void plan_pages_kernel(PlanArgs a) {
     if (block_sum(faults & RLGEN_PLAN_TABLE, red)) faults |= RLGEN_PLAN_TABLE;
     if (block_sum((faults & RLGEN_PLAN_LENGTH) ? 1 : 0, red)) faults |= RLGEN_PLAN_LENGTH;
     if (threadIdx.x == 0) {
-      if (pages1 > a.n_free) faults |= RLGEN_PLAN_PAGES;
-      if (rows1 > a.max_rows) faults |= RLGEN_PLAN_ROWS;
+      if (pages1 > a.n_free || asked > a.n_free) faults |= RLGEN_PLAN_PAGES;
+      if (rows1 > a.max_rows || rows1 == MOST) faults |= RLGEN_PLAN_ROWS;
       a.row_starts[a.S] = rows1;
       a.counts[0] = rows1;
       a.counts[1] = min(pages1, a.n_free);
@@ -115,22 +122,31 @@ __global__ __launch_bounds__(TPB) void plan_pages_kernel(PlanArgs a) {
     }
   }
   // (a page that the free list no longer has is -1, and so are the slots in it)
-  auto fresh = [&](int at) { return at < a.n_free ? a.free_pages[at] : -1; };
-  if (writer) {
-    for (int at = pages0 + threadIdx.x; at < pages1; at += TPB) {
+  auto fresh = [&](unsigned at) { return at < (unsigned)a.n_free ? a.free_pages[at] : -1; };
+  if (writer && pages1 < MOST) {
+    for (unsigned at = pages0 + threadIdx.x; at < (unsigned)pages1; at += TPB) {
       int lo = 0, hi = n - 1;
       while (lo < hi) {
         const int mid = (lo + hi) >> 1;
-        if (page_end[mid] > at) hi = mid; else lo = mid + 1;
+        if ((unsigned)page_end[mid] > at) hi = mid; else lo = mid + 1;
       }
-      const int entry = lens_had[lo] + at - (lo ? page_end[lo - 1] : pages0);
+      const int entry = lens_had[lo] + (int)(at - (lo ? page_end[lo - 1] : pages0));
       if (entry < a.table_stride) a.page_table[(size_t)(s0 + lo) * a.table_stride + entry] = fresh(at);
+      else at += (page_end[lo] - 1 - at) / TPB * TPB;      // (to the last of this request that would be this thread's: none has a place)
+    }
+  } else if (writer) {
+    // more pages than can be counted: the places in the table are, and those past the free list get none
+    for (int i = 0; i < n; ++i) {
+      const Lens l = plan_lens(a, s0 + i);
+      const unsigned first = i ? page_end[i - 1] : pages0;
+      for (int entry = l.had + threadIdx.x; entry < min(l.need, a.table_stride); entry += TPB)
+        a.page_table[(size_t)(s0 + i) * a.table_stride + entry] = fresh(first + (entry - l.had));
     }
   }
   const int round = (1 << a.page_shift) - 1;
   const int row_stop = last ? a.max_rows : min(rows1, a.max_rows);
-  for (int r = rows0 + blockIdx.y * TPB + threadIdx.x; r < row_stop; r += gridDim.y * TPB) {
-    if (r >= rows1) {
+  for (unsigned r = rows0 + blockIdx.y * TPB + threadIdx.x; r < (unsigned)row_stop; r += gridDim.y * TPB) {
+    if (r >= (unsigned)rows1) {
       a.slots[r] = -1;
       a.positions[r] = 0;
       continue;
@@ -138,14 +154,14 @@ __global__ __launch_bounds__(TPB) void plan_pages_kernel(PlanArgs a) {
     int lo = 0, hi = n - 1;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
-      if (row_end[mid] > r) hi = mid; else lo = mid + 1;
+      if ((unsigned)row_end[mid] > r) hi = mid; else lo = mid + 1;
     }
-    const int pos = lens_ctx[lo] + r - (lo ? row_end[lo - 1] : rows0);
+    const int pos = lens_ctx[lo] + (int)(r - (lo ? row_end[lo - 1] : rows0));
     const int entry = pos >> a.page_shift;
     int page = -1;
     if (entry < a.table_stride)
       page = entry < lens_had[lo] ? a.page_table[(size_t)(s0 + lo) * a.table_stride + entry]
-                                  : fresh((lo ? page_end[lo - 1] : pages0) + entry - lens_had[lo]);
+                                  : fresh((unsigned)(lo ? page_end[lo - 1] : pages0) + (entry - lens_had[lo]));
     a.slots[r] = page < 0 ? -1 : (int)((unsigned)page << a.page_shift) + (pos & round);
     a.positions[r] = pos;
   }
