@@ -162,7 +162,8 @@ __global__ __launch_bounds__(TPB) void plan_pages_kernel(PlanArgs a) {
     if (entry < a.table_stride)
       page = entry < lens_had[lo] ? a.page_table[(size_t)(s0 + lo) * a.table_stride + entry]
                                   : fresh((unsigned)(lo ? page_end[lo - 1] : pages0) + (entry - lens_had[lo]));
-    a.slots[r] = page < 0 ? -1 : (int)((unsigned)page << a.page_shift) + (pos & round);
+    // (of a page whose slots an int does not hold, one outside any cache, there is none)
+    a.slots[r] = page < 0 || page > (MOST >> a.page_shift) ? -1 : (page << a.page_shift) + (pos & round);
     a.positions[r] = pos;
   }
 }

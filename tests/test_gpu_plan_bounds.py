@@ -81,3 +81,15 @@ def test_a_head_past_the_free_list(head):
     check([0, 3, 8], [6, 9, 20], 8, [4, 5, 6, 9], head, 3, 40)
     check([0, 3, 8], [0, 0, 0], 8, [4, 5, 6, 9], head, 3, 2)
     check([0] * 600, [30] * 600, 8, list(range(9)), head, 3, 600)
+
+
+@pytest.mark.parametrize("page_size, page", [(16, 2 ** 28 + 5), (16, 2 ** 27 + 3), (16, 2 ** 31 - 1), (8, 2 ** 29 + 2), (1024, 2 ** 22), (1024, 2 ** 21)])
+def test_a_page_whose_slots_pass_32_bits_has_none(page_size, page):
+    """Both from the table (a page already begun) and from the free list; pages next to them keep their slots."""
+    table = i32([[page, -7], [4, -7]])
+    plan = R.rlgen_plan_pages(i32([3, page_size]), i32([2, 2]), page_size, i32([page]), table, 4)
+    assert plan.slots.tolist() == [-1] * 4 and plan.positions.tolist() == [3, 4, page_size, page_size + 1]
+    assert table.tolist() == [[page, -7], [4, page]]
+    last = (2 ** 31 - 1) // page_size - 1                  # (the last page that has slots in 32 bits, all of it)
+    table = i32([[last, -7]])
+    assert R.rlgen_plan_pages(i32([3]), i32([1]), page_size, i32([0]), table, 1).slots.tolist() == [last * page_size + 3]
