@@ -397,7 +397,7 @@ def rlgen_debug_set_gemm(p: Policy, mode: int, which: int, variant: int):
 _DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
 
 
-_I32 = torch.int32
+_I32, _F32 = torch.int32, torch.float32
 
 
 def _heads(t: torch.Tensor, dtype: torch.dtype):
@@ -412,6 +412,19 @@ def _heads(t: torch.Tensor, dtype: torch.dtype):
 def _ints(t: torch.Tensor, *shape):
     assert t.dtype is _I32 and t.is_cuda and t.shape == shape and t.is_contiguous()
     return t.data_ptr()
+
+
+def _floats(t: torch.Tensor, n: int):
+    assert t.dtype is _F32 and t.is_cuda and t.numel() == n and t.is_contiguous()
+    return t.data_ptr()
+
+
+def _space(t: Optional[torch.Tensor]):
+    """A workspace's address and bytes."""
+    if t is None:
+        return None, 0
+    assert t.is_cuda and t.is_contiguous()
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 class PagePlan(NamedTuple):
@@ -444,7 +457,7 @@ def rlgen_plan_pages(ctx_lens: torch.Tensor, new_lens: torch.Tensor, page_size: 
 def rlgen_rope_table(max_pos: int, rotary_dim: int, theta: float, device="cuda") -> torch.Tensor:
     """[max_pos, rotary_dim / 2, 2] fp32: cos and sin."""
     table = torch.empty((max_pos, rotary_dim // 2, 2), dtype=torch.float32, device=device)
-    _check(lib.rlgen_rope_table(_ptr(table), max_pos, rotary_dim, theta, _stream()), "rlgen_rope_table")
+    _check(lib.rlgen_rope_table(_floats(table, table.numel()), max_pos, rotary_dim, theta, _stream()), "rlgen_rope_table")
     return table
 
 
@@ -453,11 +466,12 @@ def _norm_rope_args(qkv, q_gain, k_gain, eps, rope, positions, n_q, n_kv, dtype)
     row, dim = qkv.stride()
     h = q_gain.numel()
     assert qkv.is_cuda and dim == 1 and width == (n_q + 2 * n_kv) * h
-    assert q_gain.dtype is torch.float32 and q_gain.is_contiguous() and k_gain.dtype is torch.float32 and k_gain.is_contiguous() and k_gain.numel() == h
+    assert q_gain.dtype is _F32 and q_gain.is_cuda and q_gain.is_contiguous()
+    assert k_gain.dtype is _F32 and k_gain.is_cuda and k_gain.is_contiguous() and k_gain.numel() == h
     max_pos, half = 1, 0
     if rope is not None:
         max_pos, half, two = rope.shape
-        assert rope.dtype is torch.float32 and rope.is_contiguous() and two == 2
+        assert rope.dtype is _F32 and rope.is_cuda and rope.is_contiguous() and two == 2
     return (qkv.data_ptr(), row if rows > 1 else width, _DTYPES[qkv.dtype], rows, n_q, n_kv, h, q_gain.data_ptr(), k_gain.data_ptr(), eps,
             None if rope is None else rope.data_ptr(), max_pos, 2 * half, _ints(positions, rows), _DTYPES[dtype])
 
@@ -503,15 +517,13 @@ def rlgen_qk_norm_rope_backward(qkv, q_gain, k_gain, eps: float, rope, positions
     if out is None:
         out = (torch.empty((rows, qkv.shape[1]), dtype=qkv.dtype, device=qkv.device), torch.empty_like(q_gain), torch.empty_like(k_gain))
     dqkv, dqg, dkg = out
-    assert dqkv.dtype == qkv.dtype and dqkv.shape == qkv.shape and dqkv.stride(1) == 1
-    for t in (dqg, dkg):
-        assert t.dtype == torch.float32 and t.is_contiguous() and t.numel() == h
+    assert dqkv.dtype == qkv.dtype and dqkv.is_cuda and dqkv.shape == qkv.shape and dqkv.stride(1) == 1
     need = lib.rlgen_qk_norm_rope_backward_workspace(rows, h)
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=qkv.device)
     _check(lib.rlgen_qk_norm_rope_backward(*_norm_rope_args(qkv, q_gain, k_gain, eps, rope, positions, n_q, n_kv, dq.dtype), *_heads(dq, dq.dtype),
                                            *_heads(dk, dq.dtype), *_heads(dv, dq.dtype), dqkv.data_ptr(), dqkv.stride(0) if rows > 1 else dqkv.shape[1],
-                                           dqg.data_ptr(), dkg.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()),
+                                           _floats(dqg, h), _floats(dkg, h), *_space(workspace), _stream()),
            "rlgen_qk_norm_rope_backward")
     return dqkv, dqg, dkg
 
@@ -524,10 +536,10 @@ def rlgen_window_attention(q, k, v, row_starts, max_len: int, window: int, sinks
     assert k.shape == v.shape == (rows, n_kv, h)
     o, lse = out if out is not None else (torch.empty((rows, n_q, h), dtype=dt, device=q.device),
                                           torch.empty((rows, n_q), dtype=torch.float32, device=q.device))
-    assert o.shape == q.shape and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (rows, n_q)
+    assert o.shape == q.shape and lse.shape == (rows, n_q)
     S = row_starts.numel() - 1
     _check(lib.rlgen_window_attention(*_heads(q, dt), *_heads(k, dt), *_heads(v, dt), _DTYPES[dt], rows, n_q, n_kv, h, _ints(row_starts, S + 1), S,
-                                      max_len, window, sinks, scale, *_heads(o, dt), lse.data_ptr(), _stream()), "rlgen_window_attention")
+                                      max_len, window, sinks, scale, *_heads(o, dt), _floats(lse, rows * n_q), _stream()), "rlgen_window_attention")
     return o, lse
 
 
@@ -536,18 +548,17 @@ def rlgen_window_attention_backward(q, k, v, out, lse, dout, row_starts, max_len
     """From rlgen_window_attention's inputs, its (out, lse) and dout: (dq, dk, dv).  `grads`: the three to write into."""
     rows, n_q, h = q.shape
     n_kv, dt = k.shape[1], q.dtype
-    assert k.shape == v.shape == (rows, n_kv, h) and out.shape == dout.shape == q.shape
-    assert lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (rows, n_q)
+    assert k.shape == v.shape == (rows, n_kv, h) and out.shape == dout.shape == q.shape and lse.shape == (rows, n_q)
     dq, dk, dv = grads if grads is not None else (torch.empty((rows, n, h), dtype=dt, device=q.device) for n in (n_q, n_kv, n_kv))
     assert dq.shape == q.shape and dk.shape == dv.shape == k.shape
     S = row_starts.numel() - 1
     need = lib.rlgen_window_attention_backward_workspace(rows, n_q, n_kv, h, S, max_len, window, sinks)
     if workspace is None:
         workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
-    _check(lib.rlgen_window_attention_backward(*_heads(q, dt), *_heads(k, dt), *_heads(v, dt), *_heads(out, dt), lse.data_ptr(), *_heads(dout, dt),
-                                               _DTYPES[dt], rows, n_q, n_kv, h, _ints(row_starts, S + 1), S, max_len, window, sinks, scale,
-                                               *_heads(dq, dt), *_heads(dk, dt), *_heads(dv, dt), workspace.data_ptr(),
-                                               workspace.numel() * workspace.element_size(), _stream()), "rlgen_window_attention_backward")
+    _check(lib.rlgen_window_attention_backward(*_heads(q, dt), *_heads(k, dt), *_heads(v, dt), *_heads(out, dt), _floats(lse, rows * n_q),
+                                               *_heads(dout, dt), _DTYPES[dt], rows, n_q, n_kv, h, _ints(row_starts, S + 1), S, max_len, window, sinks, scale,
+                                               *_heads(dq, dt), *_heads(dk, dt), *_heads(dv, dt), *_space(workspace), _stream()),
+           "rlgen_window_attention_backward")
     return dq, dk, dv
 
 
@@ -561,14 +572,13 @@ def rlgen_window_attention_paged(q, pages, page_table, row_starts, total_lens, m
     S, stride = page_table.shape
     o, lse = out if out is not None else (torch.empty((rows, n_q, h), dtype=dt, device=q.device),
                                           torch.empty((rows, n_q), dtype=torch.float32, device=q.device))
-    assert o.shape == q.shape and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (rows, n_q)
+    assert o.shape == q.shape and lse.shape == (rows, n_q)
     size = lib.rlgen_window_attention_paged_workspace if max_new == 1 else lib.rlgen_window_attention_chunk_workspace
     need = size(n_q, n_kv, h, S, max_new, max_total, window, sinks)
     if workspace is None and need:
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     _check(lib.rlgen_window_attention_paged(*_heads(q, dt), _DTYPES[dt], rows, n_q, n_kv, h, *_pages(pages, n_kv, h), _ints(page_table, S, stride), stride,
                                             _ints(row_starts, S + 1), _ints(total_lens, S), S, max_new, max_total, window, sinks, scale,
-                                            *_heads(o, dt), lse.data_ptr(), _ptr(workspace),
-                                            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()),
+                                            *_heads(o, dt), _floats(lse, rows * n_q), *_space(workspace), _stream()),
            "rlgen_window_attention_paged")
     return o, lse
