@@ -316,7 +316,8 @@ int rlgen_status_bits(rlgen_ctx *ctx, void *hip_stream, uint32_t *faults);
  *  - Visibility: a query at position p sees key j if j <= p and (j > p - window, or j < sinks, or window == 0: no window).  A query that
  *    sees nothing has output 0 and log-sum-exp -infinity.
  *  - Sizes: rows, S * heads and n_pages * page_size below 2^31.  Offsets are 64-bit.
- * Entries of row_starts, page_table and slots that lie outside their arrays are clamped or skipped, never followed. */
+ * Entries of row_starts, page_table and slots that lie outside their arrays are clamped or skipped, never followed: a token whose page lies
+ * outside the cache is seen by no query. */
 #define RLGEN_PLAN_ROWS    1   /* counts[3]: more rows than max_rows or 2^31 - 2 (those beyond are not written) */
 #define RLGEN_PLAN_PAGES   2   /* the free list ran out (pages and slots that lack one are -1)                 */
 #define RLGEN_PLAN_TABLE   4   /* a sequence needs more pages than a table row has (its slots beyond are -1)   */

@@ -31,9 +31,10 @@ constexpr int TPB = 256, BM = 128;
 template <class T, bool PAGED>
 __device__ void rows_key_by_key(const WindowArgs& a, const Seq& q, int s, int kvh, int m_first, int m_end, int lane) {
   const int G = a.Hq / a.Hkv;
-  auto key_row = [&](int key, bool value) {
+  auto key_row = [&](int key, bool value) -> const uint16_t* {     // (null: the key's page lies outside the cache)
     if constexpr (PAGED) {
-      const unsigned entry = a.page_table[(size_t)s * a.table_stride + (key >> a.page_shift)], page = entry < (unsigned)a.n_pages ? entry : 0;
+      const unsigned page = a.page_table[(size_t)s * a.table_stride + (key >> a.page_shift)];
+      if (page >= (unsigned)a.n_pages) return nullptr;
       const long long row = ((((long long)page * 2 + (value ? 1 : 0)) * a.Hkv + kvh) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
       return (const uint16_t*)a.pages + row * a.h;
     } else {
@@ -49,8 +50,8 @@ __device__ void rows_key_by_key(const WindowArgs& a, const Seq& q, int s, int kv
     for (int i0 = 0; i0 < seen; i0 += 64) {
       const int i = i0 + lane;
       float sc = -INFINITY;
-      if (i < seen) {
-        const uint16_t* kp = key_row(i < sinks ? i : w_lo + i - sinks, false);
+      const uint16_t* kp = i < seen ? key_row(i < sinks ? i : w_lo + i - sinks, false) : nullptr;
+      if (kp) {
         sc = 0.f;
         for (int d = 0; d < a.h; d += 2) {
           const uint32_t kw = *(const uint32_t*)(kp + d), qw = *(const uint32_t*)(qp + d);
@@ -68,6 +69,7 @@ __device__ void rows_key_by_key(const WindowArgs& a, const Seq& q, int s, int kv
       for (int j = 0; j < min(64, seen - i0); ++j) {
         const float pj = __shfl(p, j, WAVE);
         const uint16_t* vp = key_row(i0 + j < sinks ? i0 + j : w_lo + i0 + j - sinks, true);
+        if (!vp) continue;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (lane + 64 * e < a.h) y[e] = fmaf(pj, T::low(vp[lane + 64 * e]), y[e]);
@@ -114,6 +116,23 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) 
   const int w_base = max(w_lo, sink_tiles * BN);
   const int n_tiles = sink_tiles + (key_end > w_base ? (key_end - w_base + BN - 1) / BN : 0);
   auto tile_key = [&](int t) { return t < sink_tiles ? t * BN : w_base + (t - sink_tiles) * BN; };
+  const int t0 = PAGED ? (int)((long long)n_tiles * part / parts) : 0, t1 = PAGED ? (int)((long long)n_tiles * (part + 1) / parts) : n_tiles;
+  // Pages outside the cache, which nobody sees, are looked for once in front of the walk: where there are none, as a rule, no tile asks.
+  // Of the table's entries that the walk reads, first the sinks', then the window's; a thread's first is under way while tiles are requested.
+  const int* table = PAGED ? a.page_table + (size_t)s * a.table_stride : nullptr;
+  auto entries_of = [&](int ta, int tb) {      // first, and how many
+    const int e = tile_key(ta) >> a.page_shift;
+    return int2{e, ta < tb ? ((min(tile_key(tb - 1) + BN, q.total) - 1) >> a.page_shift) - e + 1 : 0};
+  };
+  [[maybe_unused]] int2 near, far;
+  [[maybe_unused]] int page_seen = 0;
+  auto entry = [&](int i) { return table[i < far.y ? far.x + i : near.x + i - far.y]; };
+  if constexpr (PAGED) {
+    const int mid = min(max(sink_tiles, t0), max(t0, t1));
+    far = entries_of(t0, mid);
+    near = entries_of(mid, t1);
+    if ((int)threadIdx.x < far.y + near.y) page_seen = entry(threadIdx.x);
+  }
 
   // this lane's row
   const int m = m0 + wave * 32 + c;
@@ -144,7 +163,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) 
       for (int n = 0; n < P::PER; ++n) {
         int row, dim;
         P::place(n, wave, lane, row, dim);
-        page_of[n] = a.page_table[(size_t)s * a.table_stride + (min(tile_key(t) + row, key_max) >> a.page_shift)];
+        page_of[n] = table[min(tile_key(t) + row, key_max) >> a.page_shift];
       }
     }
   };
@@ -158,7 +177,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) 
         int row, dim;
         P::place(n, wave, lane, row, dim);
         const int key = min(base + row, key_max);                  // (rows past the last are masked)
-        const unsigned page = (unsigned)page_of[n] < (unsigned)a.n_pages ? page_of[n] : 0;      // (an entry outside is not followed)
+        const unsigned page = (unsigned)page_of[n] < (unsigned)a.n_pages ? page_of[n] : 0;      // (an entry outside is not followed, its keys are masked)
         const long long at = (((long long)page * 2 * a.Hkv + kvh) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
         const uint16_t* ks = (const uint16_t*)a.pages + at * a.h + dim;
         const uint16_t* vs = ks + ((long long)a.Hkv << a.page_shift) * a.h;
@@ -188,11 +207,16 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) 
   ColumnBase<HD> v_base = column_base<HD>(lane);
   v_base.all += tiles0 + 2 * TILE;
   v_base.last += tiles0 + 2 * TILE;
-  const int t0 = PAGED ? (int)((long long)n_tiles * part / parts) : 0, t1 = PAGED ? (int)((long long)n_tiles * (part + 1) / parts) : n_tiles;
   if (t0 < t1) {
     fetch_pages(t0);
     request(t0, t0 & 1);
     if (t0 + 1 < t1) fetch_pages(t0 + 1);
+  }
+  bool holes = false;
+  if constexpr (PAGED) {
+    holes = (unsigned)page_seen >= (unsigned)a.n_pages;
+    for (int i = threadIdx.x + TPB; i < far.y + near.y; i += TPB) holes |= (unsigned)entry(i) >= (unsigned)a.n_pages;
+    holes = __syncthreads_or(holes);
   }
   settle(qf);                                  // (behind the first request: one wait for both)
   scalars_landed();
@@ -212,10 +236,17 @@ __global__ __launch_bounds__(TPB, HD > 128 ? (PAGED ? 1 : 2) : HD > 96 ? 3 : 4) 
 #pragma unroll
     for (int i = 0; i < KS; ++i) sc = T::mfma32(row_frag<HD, vec8>(k_base + buffer, 0, i), qf[i], sc);
     order_products<1, AHEAD, KS>();
-    const bool whole = kb + BN - 1 <= wp_lo && (a.window == 0 || kb > wp_hi - a.window || kb + BN - 1 < a.sinks);
+    const bool whole = kb + BN - 1 <= wp_lo && (a.window == 0 || kb > wp_hi - a.window || kb + BN - 1 < a.sinks) && !holes;
     float top = -INFINITY;
     if (!whole) {
-      const uint32_t bits = group_bits(seen_keys(pos, kb, a.window, a.sinks), g);
+      uint32_t seen = seen_keys(pos, kb, a.window, a.sinks);
+      if constexpr (PAGED) {
+        if (holes) {
+          const unsigned page = table[min(kb + c, key_max) >> a.page_shift];
+          seen &= (uint32_t)__ballot(page < (unsigned)a.n_pages);
+        }
+      }
+      const uint32_t bits = group_bits(seen, g);
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[i] = or_else(sc[i], element_mask(bits, i), 0xff800000u);      // -infinity
     }

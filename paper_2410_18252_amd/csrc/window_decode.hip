@@ -7,7 +7,8 @@
 // The scores leave the first product where the second wants its probabilities (key 8 g + 4 t + j in lane group g).  Visible keys are two
 // runs, sinks and window, so a step's cost follows the window.  Eight keys in a row share a page, so a lane looks up two pages for
 // 32 keys, one iteration before it needs them; the next 32 keys are requested before the present ones are used.
-// Values that are not seen are zeroed, not multiplied by zero.
+// Values that are not seen are zeroed, not multiplied by zero; a page outside the cache is not seen (a lane's scores and values are those of the
+// eight keys that it looked up together).
 //
 // Bound by HBM: 4 h bytes a visible key and kv head.  Measured: 512 sequences of 257 to 576 tokens, 32 heads of 80 in fp16: 443 us, 4.9 TB/s;
 // one of 32001, 32 heads over 8 of 128: 25 us and 4 for the join, 5.2 TB/s without it; 64 of up to 9000, window 1024: 46 us, 5.5 TB/s (in
@@ -65,8 +66,9 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void window_decode_kernel(Wi
     pk = table[key8(i, c >> 2) >> a.page_shift];
     pv = table[key8(i, g) >> a.page_shift];
   };
-  auto page_row = [&](int page, int key) {            // (an entry outside the cache is not followed)
-    const unsigned p = (unsigned)page < (unsigned)a.n_pages ? page : 0;
+  auto inside = [&](int page) { return (unsigned)page < (unsigned)a.n_pages; };
+  auto page_row = [&](int page, int key) {            // (an entry outside the cache is not followed, its keys are masked)
+    const unsigned p = inside(page) ? page : 0;
     return (const uint16_t*)a.pages + ((((long long)p * 2 * a.Hkv + kvh) << a.page_shift) + (key & in_page)) * a.h;
   };
   typedef uint32_t vraw_t __attribute__((ext_vector_type(VW / 2)));
@@ -100,14 +102,17 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void window_decode_kernel(Wi
   u32x4 k[2][KS], k_next[2][KS];
   vraw_t v[CH][8], v_next[CH][8];
   int pk, pv;
+  bool there = true, there_next = true;
   if (i0 < i1) {
     lookup(i0, pk, pv);
     load(i0, pk, pv, k, v);
+    there = inside(pv);
     lookup(min(i0 + JW, i1 - 1), pk, pv);
   }
   for (int i = i0; i < i1; i += JW) {
     if (i + JW < i1) {
       load(i + JW, pk, pv, k_next, v_next);
+      there_next = inside(pv);
       lookup(min(i + 2 * JW, i1 - 1), pk, pv);
     }
     const int kb = group_key(i);
@@ -119,12 +124,12 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void window_decode_kernel(Wi
       for (int j = 0; j < KS; ++j) sc[t] = T::mfma16(__builtin_bit_cast(vec8, k[t][j]), qf[j], sc[t]);
     }
     const int key0 = kb + 8 * g;
-    if (kb + 31 >= key_end || (kb < w_lo && kb + 31 >= a.sinks)) {
+    if (kb + 31 >= key_end || (kb < w_lo && kb + 31 >= a.sinks) || __any(!there)) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int key = key0 + e;
         // (selections, not a branch: of a branch that writes single elements of these vectors the compiler lost one)
-        const bool seen = (key < key_end) & ((key >= w_lo) | (key < a.sinks));
+        const bool seen = (key < key_end) & ((key >= w_lo) | (key < a.sinks)) & there;
         const uint32_t keep = seen ? 0xffffffffu : 0u;
         sc[e >> 2][e & 3] = seen ? sc[e >> 2][e & 3] : -INFINITY;
 #pragma unroll
@@ -175,6 +180,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void window_decode_kernel(Wi
     for (int x = 0; x < CH; ++x)
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[x][e] = v_next[x][e];
+    there = there_next;
   }
   sum += __shfl_xor(sum, 16, WAVE);
   sum += __shfl_xor(sum, 32, WAVE);
