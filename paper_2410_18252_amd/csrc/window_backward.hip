@@ -6,7 +6,7 @@
 // seven matrix products instead of the five that one kernel with atomic sums would need, but every sum has one order, so that results do
 // not change from run to run.  P and dS are rounded to the inputs' type for their second products, errors of the order of the
 // gradients' own rounding; fp16, whose smallest normal number a dS easily falls below, multiplies dS by a power of two taken from the
-// largest |dout| and |v|.
+// largest |dout| and |v| that enter the sum: of the row and of the keys in its sight for dq, of the queries walked and of the block's keys for dk.
 //
 // The queries' side goes first, since it corrects delta for the rows that see few keys; its walk is the forward pass's.  Both sides are bound
 // by their chains of products, exponentials and barriers with two or three waves to a SIMD (matrix unit 43 and 33 % busy at 128 dims),
@@ -19,7 +19,6 @@
 namespace {
 
 constexpr int TPB = 256, BM = 128;
-constexpr int DELTA_BLOCKS = 1024;              // at most
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int FEW_KEYS = 32, FEW_ROWS = 64;
 
@@ -29,32 +28,40 @@ template <class T> __device__ __forceinline__ uint32_t rest_of(float lo, float h
 // Everything below in the caller's workspace, and how the queries that see the sinks from beyond the window are parted.
 struct Backward {
   WindowArgs a;
-  float *lse2, *delta, *peak, *part;    // [rows, Hq]: lse log2 e, delta; the largest |dout| and |v| of each block; the sinks' parts
+  float *lse2, *delta, *part;           // [rows, Hq]: lse log2 e, delta; the sinks' parts
+  float *dout_peak, *v_peak;            // [S, delta_chunks]: the largest finite |dout| and |v| of delta_tokens tokens (fp16)
   int sinks, chunk, chunks;             // sinks that are parted (0: none); tokens to a part; parts of the longest sequence
   float* run_part;                      // [runs, rows, Hkv, 2, h]
-  int delta_blocks;                     // that delta_kernel has
+  int delta_tokens, delta_chunks;       // tokens to a block of delta_kernel, blocks to the longest sequence
   int run, runs;                        // tokens to a part of what a tile of keys is seen by, most parts (1: not parted)
 };
 
-// delta and lse log2 e, and in fp16 for each block the largest |dout| and |v|.  Bound by HBM: out and dout (and
-// v) once.
+// delta and lse log2 e of a sequence's tokens, delta_tokens of them to a block, and in fp16 the largest finite |dout| and |v| among them.
+// Bound by HBM: out and dout (and v) once.
 template <class T, int CH>
 __global__ __launch_bounds__(TPB) void delta_kernel(Backward b) {
   __shared__ float red[2][4];
   const WindowArgs& a = b.a;
-  constexpr int AHEAD = 4 / CH;                // (row, head) pairs requested before the first is used
-  const int li = threadIdx.x & 15;
-  const long long items = (long long)a.rows * a.Hq, step = (long long)gridDim.x * 16;
+  constexpr int AHEAD = 4 / CH;                // (token, head) pairs requested before the first is used
+  const int s = blockIdx.x / b.delta_chunks, tok0 = (blockIdx.x - s * b.delta_chunks) * b.delta_tokens, li = threadIdx.x & 15;
+  const Seq q = load_seq(a, s, false);
+  const int tokens = min(b.delta_tokens, q.n - tok0);
+  if (tokens <= 0) return;
+  const int items = tokens * a.Hq;
+  const long long row0 = q.row0 + tok0;
   float peak[2] = {0.f, 0.f};
-  for (long long it0 = (long long)blockIdx.x * 16 + (threadIdx.x >> 4); it0 < items; it0 += step * AHEAD) {
+  auto finite_peak = [&](float& p, uint32_t w) {
+    const float lo = fabsf(T::low(w)), hi = fabsf(T::high(w));
+    p = fmaxf(p, fmaxf(lo < INFINITY ? lo : 0.f, hi < INFINITY ? hi : 0.f));
+  };
+  for (int it0 = threadIdx.x >> 4; it0 < items; it0 += 16 * AHEAD) {
     u32x4 o[AHEAD][CH], g[AHEAD][CH];
     float lse[AHEAD];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-      const long long it = it0 + u * step < items ? it0 + u * step : it0;
-      const long long row = it / a.Hq;
-      const long long head = (it - row * a.Hq) * a.h;
-      lse[u] = a.lse[it];
+      const int it = it0 + 16 * u < items ? it0 + 16 * u : it0, tok = it / a.Hq;
+      const long long row = row0 + tok, head = (long long)(it - tok * a.Hq) * a.h;
+      lse[u] = a.lse[row0 * a.Hq + it];
 #pragma unroll
       for (int x = 0; x < CH; ++x) {
         const int d = 128 * x + 8 * li;
@@ -69,28 +76,27 @@ __global__ __launch_bounds__(TPB) void delta_kernel(Backward b) {
       for (int x = 0; x < CH; ++x)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float lo = T::low(g[u][x][e]), hi = T::high(g[u][x][e]);
-          v = fmaf(T::low(o[u][x][e]), lo, v);
-          v = fmaf(T::high(o[u][x][e]), hi, v);
-          if constexpr (__is_same(T, TypeF16)) peak[0] = fmaxf(peak[0], fmaxf(fabsf(lo), fabsf(hi)));
+          v = fmaf(T::low(o[u][x][e]), T::low(g[u][x][e]), v);
+          v = fmaf(T::high(o[u][x][e]), T::high(g[u][x][e]), v);
+          if constexpr (__is_same(T, TypeF16)) finite_peak(peak[0], g[u][x][e]);
         }
 #pragma unroll
-      for (int s = 8; s > 0; s >>= 1) v += __shfl_xor(v, s, WAVE);
-      const long long it = it0 + u * step;
+      for (int o = 8; o > 0; o >>= 1) v += __shfl_xor(v, o, WAVE);
+      const int it = it0 + 16 * u;
       if (li == 0 && it < items) {
-        b.delta[it] = v;
-        b.lse2[it] = lse[u] * LOG2E;
+        b.delta[row0 * a.Hq + it] = v;
+        b.lse2[row0 * a.Hq + it] = lse[u] * LOG2E;
       }
     }
   }
   if constexpr (__is_same(T, TypeF16)) {
-    const long long values = (long long)a.rows * a.Hkv;
-    for (long long it0 = (long long)blockIdx.x * 16 + (threadIdx.x >> 4); it0 < values; it0 += step * AHEAD) {
+    const int values = tokens * a.Hkv;
+    for (int it0 = threadIdx.x >> 4; it0 < values; it0 += 16 * AHEAD) {
       u32x4 w[AHEAD][CH];
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
-        const long long it = it0 + u * step < values ? it0 + u * step : it0, row = it / a.Hkv;
-        const uint16_t* p = (const uint16_t*)a.v + row * a.v_stride + (it - row * a.Hkv) * a.h;
+        const int it = it0 + 16 * u < values ? it0 + 16 * u : it0, tok = it / a.Hkv;
+        const uint16_t* p = (const uint16_t*)a.v + (row0 + tok) * a.v_stride + (long long)(it - tok * a.Hkv) * a.h;
 #pragma unroll
         for (int x = 0; x < CH; ++x) {
           const int d = 128 * x + 8 * li;
@@ -102,7 +108,7 @@ __global__ __launch_bounds__(TPB) void delta_kernel(Backward b) {
 #pragma unroll
         for (int x = 0; x < CH; ++x)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) peak[1] = fmaxf(peak[1], fmaxf(fabsf(T::low(w[u][x][e])), fabsf(T::high(w[u][x][e]))));
+          for (int e = 0; e < 4; ++e) finite_peak(peak[1], w[u][x][e]);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -112,26 +118,25 @@ __global__ __launch_bounds__(TPB) void delta_kernel(Backward b) {
     __syncthreads();
     if (threadIdx.x < 2) {
       const float* r = red[threadIdx.x];
-      b.peak[threadIdx.x * DELTA_BLOCKS + blockIdx.x] = fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3]));
+      (threadIdx.x ? b.v_peak : b.dout_peak)[blockIdx.x] = fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3]));
     }
   }
 }
 
 // What fp16 multiplies dS by: a power of two with which none leaves the type's range.  |dP| is at most h max|dout| max|v| and so is
-// |delta|, and P is at most 1.  (Infinite or NaN inputs: 1.)
-template <class T>
-__device__ __forceinline__ float ds_factor(const Backward& b) {
-  if constexpr (__is_same(T, TypeBf16)) return 1.f;
-  float peak[2] = {0.f, 0.f};
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    for (int i = threadIdx.x & 63; i < b.delta_blocks; i += 64) peak[k] = fmaxf(peak[k], b.peak[k * DELTA_BLOCKS + i]);
-    peak[k] = wave_max(peak[k]);
-  }
-  const float most = 2.f * (float)b.a.h * peak[0] * peak[1];
-  if (!(most > 1e-30f) || most > 1e30f) return 1.f;
+// |delta|, and P is at most 1.  Only finite values count: what an infinity makes of a dS no factor changes.  Only values that the sum
+// is of count, so no other sequence, row or key takes bits from it.
+__device__ __forceinline__ float ds_factor(int h, float dout_peak, float v_peak) {
+  const float most = 2.f * (float)h * dout_peak * v_peak;
+  if (!(most > 1e-30f)) return 1.f;
   // 2^14 over the power of two at or below `most`: dS is below 2^15
   return __uint_as_float((uint32_t)(254 + 14 - (int)(__float_as_uint(most) >> 23)) << 23);
+}
+// The largest of a sequence's peaks over the blocks that hold its tokens tok0 .. tok1 - 1, by a wave
+__device__ __forceinline__ float peak_of(const Backward& b, const float* peaks, int s, int tok0, int tok1) {
+  float peak = 0.f;
+  for (int i = tok0 / b.delta_tokens + (threadIdx.x & 63); i * (long long)b.delta_tokens < tok1; i += 64) peak = fmaxf(peak, peaks[(long long)s * b.delta_chunks + i]);
+  return wave_max(peak);
 }
 
 // ------------------------------------------------------------------ keys' side
@@ -217,7 +222,8 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
       request_pieces(row_source(a.v, q.row0, a.v_stride, kvh, 1, a.h).tile(kt * BM, min(q.n - kt * BM, BM)),
                              piece_offsets<HD, BM, WAVES>(wave, lane, a.v_stride, a.h), lds_address(v_tile), wave);
   }
-  const float factor = ds_factor<T>(b);
+  float factor = 1.f;
+  if constexpr (__is_same(T, TypeF16)) factor = ds_factor(a.h, peak_of(b, b.dout_peak, s, tok0, tok1), peak_of(b, b.v_peak, s, kt * BM, min(kt * BM + BM, q.n)));
   // where tiles begin with a group's first head they all have the same offsets
   const bool even = BQ % G == 0;
   P q_off = flat_offsets<HD, BQ, WAVES>(wave, lane, a.q_stride, a.h, G, 0), o_off = flat_offsets<HD, BQ, WAVES>(wave, lane, a.dout_stride, a.h, G, 0);
@@ -449,7 +455,8 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
     of[i] = d < a.h ? *(const vec8*)((const uint16_t*)a.dout + row * a.dout_stride + (long long)head * a.h + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
   }
   float of_row[2] = {b.lse2[row * a.Hq + head], b.delta[row * a.Hq + head]};
-  const float factor = ds_factor<T>(b);
+  float v_peak = 0.f;
+  if constexpr (__is_same(T, TypeF16)) v_peak = fmaxf(peak_of(b, b.v_peak, s, w_lo, key_end), peak_of(b, b.v_peak, s, 0, min(min(a.sinks, w_lo), key_end)));
   const Pieces<HD, BN> k_off = piece_offsets<HD, BN>(wave, lane, a.k_stride, a.h), v_off = piece_offsets<HD, BN>(wave, lane, a.v_stride, a.h);
   const RowSource k_rows = row_source(a.k, q.row0, a.k_stride, kvh, 1, a.h), v_rows = row_source(a.v, q.row0, a.v_stride, kvh, 1, a.h);
   const lds_t tiles0 = lds_address(lds[0][0]);
@@ -471,6 +478,19 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
   settle(qf);
   settle(of);
   settle_words(of_row);
+  float factor = 1.f;
+  if constexpr (__is_same(T, TypeF16)) {
+    float dout_peak = 0.f;
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t w = __builtin_bit_cast(u32x4, of[i])[e];
+        const float lo = fabsf(T::low(w)), hi = fabsf(T::high(w));
+        dout_peak = fmaxf(dout_peak, fmaxf(lo < INFINITY ? lo : 0.f, hi < INFINITY ? hi : 0.f));
+      }
+    factor = ds_factor(a.h, max_halves(dout_peak), v_peak);
+  }
   const float lse2 = of_row[0];
   float delta = of_row[1];
   // This lane's row against 32 keys of the tile in buffer `buf`: scores (of the products' scale) and dP
@@ -610,9 +630,11 @@ Backward parted(const WindowArgs& a) {
   Backward b;
   b.a = a;
   if (b.a.max_new > a.rows) b.a.max_new = a.rows < 1 ? 1 : a.rows;
-  // a block has 64 (row, head) pairs at once; the keys' and queries' sides read a maximum of each block
-  const long long blocks = ((long long)a.rows * a.Hq + 63) / 64;
-  b.delta_blocks = blocks < 1 ? 1 : blocks < DELTA_BLOCKS ? (int)blocks : DELTA_BLOCKS;
+  // A block has 64 (token, head) pairs at once and two such steps (8250 tokens of 32 heads of 128 in bf16 23 us, 24 with four steps; 9985 of 80 in
+  // fp16 36 and 42), or as many as keep the blocks, of which those past a short sequence's end do nothing, to 8192 and one a sequence.
+  const long long even = ((long long)a.S * b.a.max_new + 8191) / 8192, steps = (128 + a.Hq - 1) / a.Hq;
+  b.delta_tokens = (int)(even > steps ? even : steps);
+  b.delta_chunks = (int)(((long long)b.a.max_new + b.delta_tokens - 1) / b.delta_tokens);
   part_sinks(b);
   part_runs(b);
   return b;
@@ -626,8 +648,9 @@ size_t place(Backward& b, char* ws) {
   at += round_up((size_t)a.rows * a.Hq * sizeof(float));
   b.delta = (float*)(ws + at);
   at += round_up((size_t)a.rows * a.Hq * sizeof(float));
-  b.peak = (float*)(ws + at);
-  at += round_up(2 * DELTA_BLOCKS * sizeof(float));
+  b.dout_peak = (float*)(ws + at);
+  b.v_peak = b.dout_peak + (size_t)a.S * b.delta_chunks;
+  at += round_up(2 * (size_t)a.S * b.delta_chunks * sizeof(float));
   b.part = (float*)(ws + at);
   at += round_up((size_t)a.S * a.Hkv * (b.chunks + 1) * 2 * b.sinks * a.h * sizeof(float));
   b.run_part = (float*)(ws + at);
@@ -641,7 +664,7 @@ hipError_t launch(const Backward& b, hipStream_t s) {
   const int units = a.S * a.Hkv;
   const int key_tiles = (a.max_new + BM - 1) / BM, sink_tiles = (b.sinks + BM - 1) / BM, jobs = key_tiles * b.runs + sink_tiles * b.chunks;
   if ((long long)(units + 7) * jobs * TPB * KEYS_HALVES<HD> > 0xffffffffll) return hipErrorInvalidConfiguration;      // (before the first launch)
-  hipLaunchKernelGGL((delta_kernel<T, (HD > 128 ? 2 : 1)>), dim3(b.delta_blocks), dim3(TPB), 0, s, b);
+  hipLaunchKernelGGL((delta_kernel<T, (HD > 128 ? 2 : 1)>), dim3((unsigned)(a.S * b.delta_chunks)), dim3(TPB), 0, s, b);
   const int tiles = (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
   auto sides = [&](auto few) {
     hipLaunchKernelGGL((queries_backward_kernel<T, HD, few>), dim3(mapped_blocks(units, tiles)), dim3(TPB), 0, s, b, tiles);
