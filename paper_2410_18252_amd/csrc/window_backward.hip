@@ -21,6 +21,10 @@ namespace {
 constexpr int TPB = 256, BM = 128;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int FEW_KEYS = 32, FEW_ROWS = 64;
+// fp16 takes every P times 2^15 (P is at most 1 but for roundings, so that stays in its range): a P down to 2^-29 is then a normal number, where
+// beside one dominant key or among tens of thousands of keys it would lose its bits below 2^-14.  The shift is part of the exponent.
+template <class T> constexpr float P_SHIFT = __is_same(T, TypeF16) ? 15.f : 0.f;
+template <class T> constexpr float P_SIZE = __is_same(T, TypeF16) ? 32768.f : 1.f;
 
 // What a pair loses when it is rounded to the word that it was packed into, as such a word
 template <class T> __device__ __forceinline__ uint32_t rest_of(float lo, float hi, uint32_t word) { return T::pack(lo - T::low(word), hi - T::high(word)); }
@@ -28,7 +32,7 @@ template <class T> __device__ __forceinline__ uint32_t rest_of(float lo, float h
 // Everything below in the caller's workspace, and how the queries that see the sinks from beyond the window are parted.
 struct Backward {
   WindowArgs a;
-  float *lse2, *delta, *part;           // [rows, Hq]: lse log2 e, delta; the sinks' parts
+  float *lse2, *delta, *part;           // [rows, Hq]: lse log2 e less P's shift, delta; the sinks' parts
   float *dout_peak, *v_peak;            // [S, delta_chunks]: the largest finite |dout| and |v| of delta_tokens tokens (fp16)
   int sinks, chunk, chunks;             // sinks that are parted (0: none); tokens to a part; parts of the longest sequence
   float* run_part;                      // [runs, rows, Hkv, 2, h]
@@ -36,7 +40,7 @@ struct Backward {
   int run, runs;                        // tokens to a part of what a tile of keys is seen by, most parts (1: not parted)
 };
 
-// delta and lse log2 e of a sequence's tokens, delta_tokens of them to a block, and in fp16 the largest finite |dout| and |v| among them.
+// delta and lse log2 e (less P's shift) of a sequence's tokens, delta_tokens of them to a block, and in fp16 the largest finite |dout| and |v| among them.
 // Bound by HBM: out and dout (and v) once.
 template <class T, int CH>
 __global__ __launch_bounds__(TPB) void delta_kernel(Backward b) {
@@ -85,7 +89,7 @@ __global__ __launch_bounds__(TPB) void delta_kernel(Backward b) {
       const int it = it0 + 16 * u;
       if (li == 0 && it < items) {
         b.delta[row0 * a.Hq + it] = v;
-        b.lse2[row0 * a.Hq + it] = lse[u] * LOG2E;
+        b.lse2[row0 * a.Hq + it] = fmaf(lse[u], LOG2E, -P_SHIFT<T>);
       }
     }
   }
@@ -170,7 +174,7 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
   typedef Pieces<HD, BQ, WAVES> P;
   __shared__ __attribute__((aligned(256))) uint16_t lds[2][2][TILE];
   __shared__ __attribute__((aligned(256))) uint16_t v_tile[V_IN_LDS ? BM * HD : 128];
-  __shared__ __attribute__((aligned(16))) float stat[2][3][64];            // of a tile's rows: lse log2 e, delta, position (bits)
+  __shared__ __attribute__((aligned(16))) float stat[2][3][64];            // of a tile's rows: lse log2 e less P's shift, delta, position (bits)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int key_wave = HALVES > 1 ? wave & 3 : wave, half = HALVES > 1 ? wave >> 2 : 0;
   const int c = lane & 31, g = lane >> 5;
@@ -224,6 +228,7 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
   }
   float factor = 1.f;
   if constexpr (__is_same(T, TypeF16)) factor = ds_factor(a.h, peak_of(b, b.dout_peak, s, tok0, tok1), peak_of(b, b.v_peak, s, kt * BM, min(kt * BM + BM, q.n)));
+  const float p_factor = factor * (1.f / P_SIZE<T>);
   // where tiles begin with a group's first head they all have the same offsets
   const bool even = BQ % G == 0;
   P q_off = flat_offsets<HD, BQ, WAVES>(wave, lane, a.q_stride, a.h, G, 0), o_off = flat_offsets<HD, BQ, WAVES>(wave, lane, a.dout_stride, a.h, G, 0);
@@ -299,7 +304,7 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
           for (int e = 0; e < 4; ++e) p[e] = (uint32_t)(__float_as_int(where[e]) - key) <= seen_by ? p[e] : 0.f;
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) ds[e] = p[e] * (dp[4 * j + e] - delta[e]) * factor;
+        for (int e = 0; e < 4; ++e) ds[e] = p[e] * (dp[4 * j + e] - delta[e]) * p_factor;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           pw[j >> 1][2 * (j & 1) + e] = T::pack(p[2 * e], p[2 * e + 1]);
@@ -376,19 +381,19 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
         const int d = 32 * t + 8 * j + 4 * g;
         if (d >= a.h) continue;
         if constexpr (BY_GRADIENT) {
-          *(f32x4*)(to + (half ? 0 : to_values) + d) = f32x4{dk[t][4 * j], dk[t][4 * j + 1], dk[t][4 * j + 2], dk[t][4 * j + 3]} * (half ? back : 1.f);
+          *(f32x4*)(to + (half ? 0 : to_values) + d) = f32x4{dk[t][4 * j], dk[t][4 * j + 1], dk[t][4 * j + 2], dk[t][4 * j + 3]} * (half ? back : 1.f / P_SIZE<T>);
         } else {
           *(f32x4*)(to + d) = f32x4{dk[t][4 * j], dk[t][4 * j + 1], dk[t][4 * j + 2], dk[t][4 * j + 3]} * back;
-          *(f32x4*)(to + to_values + d) = f32x4{dv[t][4 * j], dv[t][4 * j + 1], dv[t][4 * j + 2], dv[t][4 * j + 3]};
+          *(f32x4*)(to + to_values + d) = f32x4{dv[t][4 * j], dv[t][4 * j + 1], dv[t][4 * j + 2], dv[t][4 * j + 3]} * (1.f / P_SIZE<T>);
         }
       }
   }
   const bool whole_sum = key < q.n && slot <= 0 && !parted && !in_runs;
   if constexpr (BY_GRADIENT) {
-    store_row<T, DT>((uint16_t*)(half ? a.dk : a.dv) + row * (half ? a.dk_stride : a.dv_stride) + (long long)kvh * a.h, dk, half ? back : 1.f, a.h, g, whole_sum);
+    store_row<T, DT>((uint16_t*)(half ? a.dk : a.dv) + row * (half ? a.dk_stride : a.dv_stride) + (long long)kvh * a.h, dk, half ? back : 1.f / P_SIZE<T>, a.h, g, whole_sum);
   } else {
     store_row<T, DT>((uint16_t*)a.dk + row * a.dk_stride + (long long)kvh * a.h, dk, back, a.h, g, whole_sum);
-    store_row<T, DT>((uint16_t*)a.dv + row * a.dv_stride + (long long)kvh * a.h, dv, 1.f, a.h, g, whole_sum);
+    store_row<T, DT>((uint16_t*)a.dv + row * a.dv_stride + (long long)kvh * a.h, dv, 1.f / P_SIZE<T>, a.h, g, whole_sum);
   }
 }
 
@@ -517,8 +522,9 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) sum += or_else(__builtin_amdgcn_exp2f(fmaf(sc[i], scale2, -lse2)) * dp[i], element_mask(bits, i), 0u);
-    return sum;
+    return sum * (1.f / P_SIZE<T>);
   };
+  const float p_factor = factor * (1.f / P_SIZE<T>);
   if constexpr (FEW) {
     float sum = 0.f;
     for (int t = 0; t < n_tiles; ++t) {
@@ -555,7 +561,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
       products(t & 1, u, sc, dp);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float ds = __builtin_amdgcn_exp2f(fmaf(sc[i], scale2, -lse2)) * (dp[i] - delta) * factor;
+        const float ds = __builtin_amdgcn_exp2f(fmaf(sc[i], scale2, -lse2)) * (dp[i] - delta) * p_factor;
         dp[i] = or_else(ds, element_mask(bits, i), 0u);
       }
 #pragma unroll
