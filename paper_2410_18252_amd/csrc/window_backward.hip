@@ -26,6 +26,9 @@ constexpr int FEW_KEYS = 32, FEW_ROWS = 64;
 template <class T> constexpr float P_SHIFT = __is_same(T, TypeF16) ? 15.f : 0.f;
 template <class T> constexpr float P_SIZE = __is_same(T, TypeF16) ? 32768.f : 1.f;
 
+// Whether all rows of a sequence of n see few keys: a rule on the sequence alone, so that its gradients' precision is its own in any call
+__device__ __forceinline__ bool sees_few(const WindowArgs& a, int n) { return (a.window > 0 && a.window <= FEW_KEYS) || n <= FEW_ROWS; }
+
 // What a pair loses when it is rounded to the word that it was packed into, as such a word
 template <class T> __device__ __forceinline__ uint32_t rest_of(float lo, float hi, uint32_t word) { return T::pack(lo - T::low(word), hi - T::high(word)); }
 
@@ -162,7 +165,7 @@ __device__ __forceinline__ int last_seer(const Backward& b, int kt, int n) {
   return a.window && (b.sinks > 0 || kt * BM >= a.sinks) ? (int)min((long long)n, (long long)kt * BM + BM - 1 + a.window) : n;
 }
 
-template <class T, int HD, bool FEW>
+template <class T, int HD>
 __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel(Backward b, int key_tiles, int jobs) {
   typedef typename T::vec8 vec8;
   const WindowArgs& a = b.a;
@@ -264,85 +267,92 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
   settle(kf);                                  // (behind the first request: one wait for both)
   if constexpr (!V_IN_LDS) settle(vf);
   scalars_landed();
-  for (int t = 0; t < n_tiles; ++t) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
-    if (idle) continue;
-    const lds_t qt = tiles + (t & 1) * 4 * TILE, ot = qt + 2 * TILE;
+  const bool few_keys = sees_few(a, q.n);
+  auto walk = [&](auto few) {
+    constexpr bool FEW = decltype(few)::value;
+    for (int t = 0; t < n_tiles; ++t) {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
+      if (idle) continue;
+      const lds_t qt = tiles + (t & 1) * 4 * TILE, ot = qt + 2 * TILE;
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) {
-      const int base = m0 + t * BQ + 32 * (sub0 + u);
-      if (base >= m1) break;
-      const int p_lo = base / G, p_hi = min(base + 31, M - 1) / G;
-      if (p_hi < kw || (a.window && kw + 31 <= p_lo - a.window && kw >= a.sinks)) continue;
-      const bool whole = base + 31 < m1 && kw + 31 <= p_lo && (a.window == 0 || kw > p_hi - a.window || kw + 31 < a.sinks);
-      f32x16 sc, dp;
+      for (int u = 0; u < SUB; ++u) {
+        const int base = m0 + t * BQ + 32 * (sub0 + u);
+        if (base >= m1) break;
+        const int p_lo = base / G, p_hi = min(base + 31, M - 1) / G;
+        if (p_hi < kw || (a.window && kw + 31 <= p_lo - a.window && kw >= a.sinks)) continue;
+        const bool whole = base + 31 < m1 && kw + 31 <= p_lo && (a.window == 0 || kw > p_hi - a.window || kw + 31 < a.sinks);
+        f32x16 sc, dp;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
+        for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < KS; ++i) sc = T::mfma32(row_frag<HD, vec8>(qt + by_row, 32 * u, i), kf[i], sc);
-      if (!BY_GRADIENT || half)
+        for (int i = 0; i < KS; ++i) sc = T::mfma32(row_frag<HD, vec8>(qt + by_row, 32 * u, i), kf[i], sc);
+        if (!BY_GRADIENT || half)
 #pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        if constexpr (V_IN_LDS) dp = T::mfma32(row_frag<HD, vec8>(ot + by_row, 32 * u, i), row_frag<HD, vec8>(v_row, 0, i), dp);
-        else dp = T::mfma32(row_frag<HD, vec8>(ot + by_row, 32 * u, i), vf[i], dp);
-      }
-      if constexpr (!V_IN_LDS) order_products<1, 6, 2 * KS>();
-      u32x4 pw[2], sw[2];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int r = 32 * (sub0 + u) + 8 * j + 4 * g;
-        const f32x4 lse2 = *(const f32x4*)&stat[t & 1][0][r], delta = *(const f32x4*)&stat[t & 1][1][r];
-        float p[4], ds[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(fmaf(sc[4 * j + e], scale2, -lse2[e]));
+        for (int i = 0; i < KS; ++i) {
+          if constexpr (V_IN_LDS) dp = T::mfma32(row_frag<HD, vec8>(ot + by_row, 32 * u, i), row_frag<HD, vec8>(v_row, 0, i), dp);
+          else dp = T::mfma32(row_frag<HD, vec8>(ot + by_row, 32 * u, i), vf[i], dp);
         }
-        if (!whole) {
-          const f32x4 where = *(const f32x4*)&stat[t & 1][2][r];
+        if constexpr (!V_IN_LDS) order_products<1, 6, 2 * KS>();
+        u32x4 pw[2], sw[2];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) p[e] = (uint32_t)(__float_as_int(where[e]) - key) <= seen_by ? p[e] : 0.f;
+        for (int j = 0; j < 4; ++j) {
+          const int r = 32 * (sub0 + u) + 8 * j + 4 * g;
+          const f32x4 lse2 = *(const f32x4*)&stat[t & 1][0][r], delta = *(const f32x4*)&stat[t & 1][1][r];
+          float p[4], ds[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(fmaf(sc[4 * j + e], scale2, -lse2[e]));
+          }
+          if (!whole) {
+            const f32x4 where = *(const f32x4*)&stat[t & 1][2][r];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = (uint32_t)(__float_as_int(where[e]) - key) <= seen_by ? p[e] : 0.f;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) ds[e] = p[e] * (dp[4 * j + e] - delta[e]) * p_factor;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            pw[j >> 1][2 * (j & 1) + e] = T::pack(p[2 * e], p[2 * e + 1]);
+            sw[j >> 1][2 * (j & 1) + e] = T::pack(ds[2 * e], ds[2 * e + 1]);
+          }
+          if constexpr (FEW) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) dp[4 * j + e] = ds[e];
+          }
         }
+        const ColumnBase<HD> oc = {ot + by_column.all, ot + by_column.last}, qc = {qt + by_column.all, qt + by_column.last};
+        if (FEW && (!BY_GRADIENT || (half && few_keys))) {
+          // (as on the queries' side: with what the rounding of dS loses)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) ds[e] = p[e] * (dp[4 * j + e] - delta[e]) * p_factor;
+          for (int v = 0; v < 2; ++v) {
+            u32x4 rest;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          pw[j >> 1][2 * (j & 1) + e] = T::pack(p[2 * e], p[2 * e + 1]);
-          sw[j >> 1][2 * (j & 1) + e] = T::pack(ds[2 * e], ds[2 * e + 1]);
+            for (int e = 0; e < 4; ++e) rest[e] = rest_of<T>(dp[8 * v + 2 * e], dp[8 * v + 2 * e + 1], sw[v][e]);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) dk[d] = T::mfma32(column_frag<HD, vec8>(qc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, rest), dk[d]);
+          }
         }
-        if constexpr (FEW) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) dp[4 * j + e] = ds[e];
-        }
-      }
-      const ColumnBase<HD> oc = {ot + by_column.all, ot + by_column.last}, qc = {qt + by_column.all, qt + by_column.last};
-      if (FEW && (!BY_GRADIENT || half)) {
-        // (as on the queries' side: with what the rounding of dS loses)
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
-          u32x4 rest;
+          if constexpr (BY_GRADIENT) {
+            const ColumnBase<HD> mine = {half ? qc.all : oc.all, half ? qc.last : oc.last};
+            const u32x4 w = half ? sw[v] : pw[v];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) rest[e] = rest_of<T>(dp[8 * v + 2 * e], dp[8 * v + 2 * e + 1], sw[v][e]);
+            for (int d = 0; d < DT; ++d) dk[d] = T::mfma32(column_frag<HD, vec8>(mine, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, w), dk[d]);
+          } else {
 #pragma unroll
-          for (int d = 0; d < DT; ++d) dk[d] = T::mfma32(column_frag<HD, vec8>(qc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, rest), dk[d]);
-        }
-      }
+            for (int d = 0; d < DT; ++d) dv[d] = T::mfma32(column_frag<HD, vec8>(oc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, pw[v]), dv[d]);
 #pragma unroll
-      for (int v = 0; v < 2; ++v) {
-        if constexpr (BY_GRADIENT) {
-          const ColumnBase<HD> mine = {half ? qc.all : oc.all, half ? qc.last : oc.last};
-          const u32x4 w = half ? sw[v] : pw[v];
-#pragma unroll
-          for (int d = 0; d < DT; ++d) dk[d] = T::mfma32(column_frag<HD, vec8>(mine, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, w), dk[d]);
-        } else {
-#pragma unroll
-          for (int d = 0; d < DT; ++d) dv[d] = T::mfma32(column_frag<HD, vec8>(oc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, pw[v]), dv[d]);
-#pragma unroll
-          for (int d = 0; d < DT; ++d) dk[d] = T::mfma32(column_frag<HD, vec8>(qc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, sw[v]), dk[d]);
+            for (int d = 0; d < DT; ++d) dk[d] = T::mfma32(column_frag<HD, vec8>(qc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, sw[v]), dk[d]);
+          }
         }
       }
     }
-  }
+  };
+  // (by gradient one walk asks at every tile: a wave's registers do not hold two)
+  if (BY_GRADIENT || few_keys) walk(std::true_type{});
+  else walk(std::false_type{});
   if constexpr (HALVES > 1 && !BY_GRADIENT) {
     // the second half's sums through LDS, first those of dv, then those of dk: a register of 64 lanes a 256-byte row
     static_assert(sizeof(lds) >= 4 * DT * 16 * 64 * sizeof(float), "the tiles' place holds one gradient of four waves");
@@ -425,8 +435,8 @@ __global__ __launch_bounds__(TPB) void parts_sum_kernel(Backward b) {
 // ------------------------------------------------------------------ queries' side
 // The forward pass's walk: a block owns 128 rows of a group's queries, a wave 32 of them with q and dout in registers; keys and values pass
 // through LDS (K by rows and transposed, V by rows).
-template <class T, int HD, bool FEW>
-__global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void queries_backward_kernel(Backward b, int tiles) {
+template <class T, int HD>
+__global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 ? 2 : 3) void queries_backward_kernel(Backward b, int tiles) {
   typedef typename T::vec8 vec8;
   const WindowArgs& a = b.a;
   constexpr int BN = HD > 128 ? 32 : 64, SUB = BN / 32, KS = HD / 16, DT = (HD + 31) / 32, TILE = BN * HD;
@@ -512,7 +522,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
   // out was rounded, and where a row sees few keys its delta is nearly as large as its dP: there the rounding shows in dS.  Such rows
   // take delta from the sum over their keys of P dP and leave it for the keys' side: a sequence's first 32 rows from the 32 keys that they
   // see at most, which begin the first tile; all rows, in a pass of its own, where every row sees few (FEW: a window of up to FEW_KEYS, or
-  // sequences of up to FEW_ROWS).  There dS also takes part with what its rounding loses, on both sides: over few keys, whose dS add up to
+  // a sequence of up to FEW_ROWS).  There dS also takes part with what its rounding loses, on both sides: over few keys, whose dS add up to
   // nothing, such errors do not average out (against the formulas in 64 bits up to 2.1 times the error of gradients that are rounded
   // once, 1.44 with it).  Long sequences come to 1.45 without, and would pay 15 % of the keys' side for it.
   auto own_delta = [&](int buf, int u, int kb) {
@@ -525,63 +535,68 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 || FEW ? 2 : 3) void qu
     return sum * (1.f / P_SIZE<T>);
   };
   const float p_factor = factor * (1.f / P_SIZE<T>);
-  if constexpr (FEW) {
-    float sum = 0.f;
+  auto walk = [&](auto few) {
+    constexpr bool FEW = decltype(few)::value;
+    if constexpr (FEW) {
+      float sum = 0.f;
+      for (int t = 0; t < n_tiles; ++t) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
+        for (int u = 0; u < SUB; ++u) sum += own_delta(t & 1, u, tile_key(t) + 32 * u);
+      }
+      delta = sum_halves(sum);
+      if (live && g == 0) b.delta[row * a.Hq + head] = delta;
+      __syncthreads();                           // (the tiles are filled again)
+      if (n_tiles > 0) request(0, 0);
+    } else if (p_lo < FEW_KEYS) {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      if (wp_lo < FEW_KEYS) {
+        const float sum = sum_halves(own_delta(0, 0, tile_key(0)));
+        delta = pos < FEW_KEYS ? sum : delta;
+        if (live && g == 0 && pos < FEW_KEYS) b.delta[row * a.Hq + head] = sum;
+      }
+    }
+    scalars_landed();
     for (int t = 0; t < n_tiles; ++t) {
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
-      for (int u = 0; u < SUB; ++u) sum += own_delta(t & 1, u, tile_key(t) + 32 * u);
-    }
-    delta = sum_halves(sum);
-    if (live && g == 0) b.delta[row * a.Hq + head] = delta;
-    __syncthreads();                           // (the tiles are filled again)
-    if (n_tiles > 0) request(0, 0);
-  } else if (p_lo < FEW_KEYS) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (wp_lo < FEW_KEYS) {
-      const float sum = sum_halves(own_delta(0, 0, tile_key(0)));
-      delta = pos < FEW_KEYS ? sum : delta;
-      if (live && g == 0 && pos < FEW_KEYS) b.delta[row * a.Hq + head] = sum;
-    }
-  }
-  scalars_landed();
-  for (int t = 0; t < n_tiles; ++t) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (t + 1 < n_tiles) request(t + 1, (t + 1) & 1);
-    const lds_t kt = tiles0 + (t & 1) * 4 * TILE;
-    const ColumnBase<HD> kc = {kt + by_column.all, kt + by_column.last};
+      const lds_t kt = tiles0 + (t & 1) * 4 * TILE;
+      const ColumnBase<HD> kc = {kt + by_column.all, kt + by_column.last};
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) {
-      const int kb = tile_key(t) + 32 * u;
-      if (kb > wp_hi || (a.window && kb + 31 <= wp_lo - a.window && kb >= a.sinks)) continue;
-      const bool whole = kb + 31 <= wp_lo && (a.window == 0 || kb > wp_hi - a.window || kb + 31 < a.sinks);
-      uint32_t bits = ~0u;
-      if (!whole) bits = group_bits(seen_keys(pos, kb, a.window, a.sinks), g);
-      f32x16 sc, dp;
-      products(t & 1, u, sc, dp);
+      for (int u = 0; u < SUB; ++u) {
+        const int kb = tile_key(t) + 32 * u;
+        if (kb > wp_hi || (a.window && kb + 31 <= wp_lo - a.window && kb >= a.sinks)) continue;
+        const bool whole = kb + 31 <= wp_lo && (a.window == 0 || kb > wp_hi - a.window || kb + 31 < a.sinks);
+        uint32_t bits = ~0u;
+        if (!whole) bits = group_bits(seen_keys(pos, kb, a.window, a.sinks), g);
+        f32x16 sc, dp;
+        products(t & 1, u, sc, dp);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float ds = __builtin_amdgcn_exp2f(fmaf(sc[i], scale2, -lse2)) * (dp[i] - delta) * p_factor;
-        dp[i] = or_else(ds, element_mask(bits, i), 0u);
-      }
-#pragma unroll
-      for (int v = 0; v < 2; ++v) {
-        u32x4 w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = T::pack(dp[8 * v + 2 * e], dp[8 * v + 2 * e + 1]);
-        if constexpr (FEW) {
-          u32x4 rest;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) rest[e] = rest_of<T>(dp[8 * v + 2 * e], dp[8 * v + 2 * e + 1], w[e]);
-#pragma unroll
-          for (int d = 0; d < DT; ++d) dq[d] = T::mfma32(column_frag<HD, vec8>(kc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, rest), dq[d]);
+        for (int i = 0; i < 16; ++i) {
+          const float ds = __builtin_amdgcn_exp2f(fmaf(sc[i], scale2, -lse2)) * (dp[i] - delta) * p_factor;
+          dp[i] = or_else(ds, element_mask(bits, i), 0u);
         }
 #pragma unroll
-        for (int d = 0; d < DT; ++d) dq[d] = T::mfma32(column_frag<HD, vec8>(kc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, w), dq[d]);
+        for (int v = 0; v < 2; ++v) {
+          u32x4 w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = T::pack(dp[8 * v + 2 * e], dp[8 * v + 2 * e + 1]);
+          if constexpr (FEW) {
+            u32x4 rest;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) rest[e] = rest_of<T>(dp[8 * v + 2 * e], dp[8 * v + 2 * e + 1], w[e]);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) dq[d] = T::mfma32(column_frag<HD, vec8>(kc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, rest), dq[d]);
+          }
+#pragma unroll
+          for (int d = 0; d < DT; ++d) dq[d] = T::mfma32(column_frag<HD, vec8>(kc, 32 * u + 16 * v, d), __builtin_bit_cast(vec8, w), dq[d]);
+        }
+        order_products<2, 3, 2 * DT>();
       }
-      order_products<2, 3, 2 * DT>();
     }
-  }
+  };
+  if (sees_few(a, q.n)) walk(std::true_type{});
+  else walk(std::false_type{});
   store_row<T, DT>((uint16_t*)a.dq + row * a.dq_stride + (long long)head * a.h, dq, a.scale / factor, a.h, g, live);
 }
 
@@ -672,12 +687,8 @@ hipError_t launch(const Backward& b, hipStream_t s) {
   if ((long long)(units + 7) * jobs * TPB * KEYS_HALVES<HD> > 0xffffffffll) return hipErrorInvalidConfiguration;      // (before the first launch)
   hipLaunchKernelGGL((delta_kernel<T, (HD > 128 ? 2 : 1)>), dim3((unsigned)(a.S * b.delta_chunks)), dim3(TPB), 0, s, b);
   const int tiles = (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
-  auto sides = [&](auto few) {
-    hipLaunchKernelGGL((queries_backward_kernel<T, HD, few>), dim3(mapped_blocks(units, tiles)), dim3(TPB), 0, s, b, tiles);
-    hipLaunchKernelGGL((keys_backward_kernel<T, HD, few>), dim3(mapped_blocks(units, jobs)), dim3(TPB * KEYS_HALVES<HD>), 0, s, b, key_tiles, jobs);
-  };
-  if ((a.window > 0 && a.window <= FEW_KEYS) || a.max_new <= FEW_ROWS) sides(std::true_type{});
-  else sides(std::false_type{});
+  hipLaunchKernelGGL((queries_backward_kernel<T, HD>), dim3(mapped_blocks(units, tiles)), dim3(TPB), 0, s, b, tiles);
+  hipLaunchKernelGGL((keys_backward_kernel<T, HD>), dim3(mapped_blocks(units, jobs)), dim3(TPB * KEYS_HALVES<HD>), 0, s, b, key_tiles, jobs);
   if (b.sinks > 0 || b.runs > 1) hipLaunchKernelGGL((parts_sum_kernel<T>), dim3((unsigned)units, b.runs > 1 ? key_tiles : sink_tiles, BM / SUM_KEYS), dim3(TPB), 0, s, b);
   return hipGetLastError();
 }
