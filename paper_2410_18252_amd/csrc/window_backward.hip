@@ -139,10 +139,18 @@ __device__ __forceinline__ float ds_factor(int h, float dout_peak, float v_peak)
   // 2^14 over the power of two at or below `most`: dS is below 2^15
   return __uint_as_float((uint32_t)(254 + 14 - (int)(__float_as_uint(most) >> 23)) << 23);
 }
-// The largest of a sequence's peaks over the blocks that hold its tokens tok0 .. tok1 - 1, by a wave
-__device__ __forceinline__ float peak_of(const Backward& b, const float* peaks, int s, int tok0, int tok1) {
-  float peak = 0.f;
-  for (int i = tok0 / b.delta_tokens + (threadIdx.x & 63); i * (long long)b.delta_tokens < tok1; i += 64) peak = fmaxf(peak, peaks[(long long)s * b.delta_chunks + i]);
+// A sequence's peaks over the blocks that hold its tokens tok0 .. tok1 - 1.  A lane's first is on its way from where this is made on, the largest is
+// found once other loads are waited for too.
+struct Peaks { const float* from; int n; float first; };
+__device__ __forceinline__ Peaks peaks_of(const Backward& b, const float* peaks, int s, int tok0, int tok1) {
+  const int lane = threadIdx.x & 63, i0 = tok0 / b.delta_tokens;
+  Peaks p{peaks + (long long)s * b.delta_chunks + i0, tok1 > tok0 ? (tok1 - 1) / b.delta_tokens - i0 + 1 : 0, 0.f};
+  if (lane < p.n) p.first = p.from[lane];
+  return p;
+}
+__device__ __forceinline__ float largest(const Peaks& p) {
+  float peak = p.first;
+  for (int i = (threadIdx.x & 63) + 64; i < p.n; i += 64) peak = fmaxf(peak, p.from[i]);
   return wave_max(peak);
 }
 
@@ -214,6 +222,11 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
   // parts beyond the window concern the sinks alone
   const bool idle = kw >= q.n || (slot > 0 && kw >= b.sinks);
 
+  [[maybe_unused]] Peaks dout_peaks, v_peaks;
+  if constexpr (__is_same(T, TypeF16)) {
+    dout_peaks = peaks_of(b, b.dout_peak, s, tok0, tok1);
+    v_peaks = peaks_of(b, b.v_peak, s, kt * BM, min(kt * BM + BM, q.n));
+  }
   vec8 kf[KS], vf[V_IN_LDS ? 1 : KS];
   {
     const long long row = q.row0 + min(key, q.n - 1);
@@ -229,9 +242,6 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
       request_pieces(row_source(a.v, q.row0, a.v_stride, kvh, 1, a.h).tile(kt * BM, min(q.n - kt * BM, BM)),
                              piece_offsets<HD, BM, WAVES>(wave, lane, a.v_stride, a.h), lds_address(v_tile), wave);
   }
-  float factor = 1.f;
-  if constexpr (__is_same(T, TypeF16)) factor = ds_factor(a.h, peak_of(b, b.dout_peak, s, tok0, tok1), peak_of(b, b.v_peak, s, kt * BM, min(kt * BM + BM, q.n)));
-  const float p_factor = factor * (1.f / P_SIZE<T>);
   // where tiles begin with a group's first head they all have the same offsets
   const bool even = BQ % G == 0;
   P q_off = flat_offsets<HD, BQ, WAVES>(wave, lane, a.q_stride, a.h, G, 0), o_off = flat_offsets<HD, BQ, WAVES>(wave, lane, a.dout_stride, a.h, G, 0);
@@ -266,6 +276,9 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
   if (n_tiles > 0) request(0, 0);
   settle(kf);                                  // (behind the first request: one wait for both)
   if constexpr (!V_IN_LDS) settle(vf);
+  float factor = 1.f;
+  if constexpr (__is_same(T, TypeF16)) factor = ds_factor(a.h, largest(dout_peaks), largest(v_peaks));
+  const float p_factor = factor * (1.f / P_SIZE<T>);
   scalars_landed();
   const bool few_keys = sees_few(a, q.n);
   auto walk = [&](auto few) {
@@ -462,6 +475,11 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 ? 2 : 3) void queries_b
   const int tok = min(m, M - 1) / G, head = kvh * G + min(m, M - 1) % G, pos = tok;
   const int wp_lo = min(m0 + wave * 32, M - 1) / G, wp_hi = min(m0 + wave * 32 + 31, M - 1) / G;
   const long long row = q.row0 + tok;
+  [[maybe_unused]] Peaks near, far;            // of the values in the window, of those of the sinks
+  if constexpr (__is_same(T, TypeF16)) {
+    near = peaks_of(b, b.v_peak, s, w_lo, key_end);
+    far = peaks_of(b, b.v_peak, s, 0, min(a.sinks, w_lo));
+  }
   vec8 qf[KS], of[KS];
 #pragma unroll
   for (int i = 0; i < KS; ++i) {
@@ -470,8 +488,6 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 ? 2 : 3) void queries_b
     of[i] = d < a.h ? *(const vec8*)((const uint16_t*)a.dout + row * a.dout_stride + (long long)head * a.h + d) : __builtin_bit_cast(vec8, u32x4{0, 0, 0, 0});
   }
   float of_row[2] = {b.lse2[row * a.Hq + head], b.delta[row * a.Hq + head]};
-  float v_peak = 0.f;
-  if constexpr (__is_same(T, TypeF16)) v_peak = fmaxf(peak_of(b, b.v_peak, s, w_lo, key_end), peak_of(b, b.v_peak, s, 0, min(min(a.sinks, w_lo), key_end)));
   const Pieces<HD, BN> k_off = piece_offsets<HD, BN>(wave, lane, a.k_stride, a.h), v_off = piece_offsets<HD, BN>(wave, lane, a.v_stride, a.h);
   const RowSource k_rows = row_source(a.k, q.row0, a.k_stride, kvh, 1, a.h), v_rows = row_source(a.v, q.row0, a.v_stride, kvh, 1, a.h);
   const lds_t tiles0 = lds_address(lds[0][0]);
@@ -504,7 +520,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 ? 2 : 3) void queries_b
         const float lo = fabsf(T::low(w)), hi = fabsf(T::high(w));
         dout_peak = fmaxf(dout_peak, fmaxf(lo < INFINITY ? lo : 0.f, hi < INFINITY ? hi : 0.f));
       }
-    factor = ds_factor(a.h, max_halves(dout_peak), v_peak);
+    factor = ds_factor(a.h, max_halves(dout_peak), fmaxf(largest(near), largest(far)));
   }
   const float lse2 = of_row[0];
   float delta = of_row[1];
@@ -651,9 +667,9 @@ Backward parted(const WindowArgs& a) {
   Backward b;
   b.a = a;
   if (b.a.max_new > a.rows) b.a.max_new = a.rows < 1 ? 1 : a.rows;
-  // A block has 64 (token, head) pairs at once and two such steps (8250 tokens of 32 heads of 128 in bf16 23 us, 24 with four steps; 9985 of 80 in
-  // fp16 36 and 42), or as many as keep the blocks, of which those past a short sequence's end do nothing, to 8192 and one a sequence.
-  const long long even = ((long long)a.S * b.a.max_new + 8191) / 8192, steps = (128 + a.Hq - 1) / a.Hq;
+  // A block has 64 (token, head) pairs at once, or as many times that as keep the blocks, of which those past a short sequence's end do nothing,
+  // to 8192 and one a sequence (8250 tokens of 32 heads of 128 in bf16 in one step 22 us, 23 in two, 24 in four).
+  const long long even = ((long long)a.S * b.a.max_new + 8191) / 8192, steps = (64 + a.Hq - 1) / a.Hq;
   b.delta_tokens = (int)(even > steps ? even : steps);
   b.delta_chunks = (int)(((long long)b.a.max_new + b.delta_tokens - 1) / b.delta_tokens);
   part_sinks(b);
