@@ -45,11 +45,6 @@ bool window_ok(const WindowArgs& a) {
   return heads_ok(a.rows, a.Hq, a.Hkv, a.h) && type16(a.dtype) && a.S >= 1 && (int64_t)a.S * a.Hq <= INT32_MAX && a.max_new >= 1 &&
          a.window >= 0 && a.sinks >= 0 && std::isfinite(a.scale) && (int64_t)a.max_new * (a.Hq / a.Hkv) <= INT32_MAX - 256;
 }
-// every tile of the longest sequence for every sequence and kv head, and what the order of blocks adds: a launch's blocks
-bool grid_ok(const WindowArgs& a) {
-  const int64_t tiles = ((int64_t)a.max_new * (a.Hq / a.Hkv) + 127) / 128 + 128;
-  return tiles * ((int64_t)a.S * a.Hkv + 1024) <= INT32_MAX / 128;                // (a launch has at most 2^32 threads)
-}
 WindowArgs window_shape(int dtype, int rows, int Hq, int Hkv, int h, int S, int max_new, int window, int sinks, float scale) {
   WindowArgs a{};
   a.dtype = dtype; a.rows = rows; a.Hq = Hq; a.Hkv = Hkv; a.h = h; a.S = S; a.max_new = max_new;
@@ -135,8 +130,8 @@ int rlgen_window_attention(const void* q, int64_t q_stride, const void* k, int64
                            void* hip_stream) {
   if (!q || !k || !v || !row_starts || !out) return RLGEN_ERR_NULL;
   WindowArgs a = window_shape(dtype, rows, n_q_heads, n_kv_heads, head_dim, S, max_len, window, sinks, scale);
-  if (!window_ok(a) || !grid_ok(a) || !rows_ok(q, q_stride, n_q_heads, head_dim) || !rows_ok(k, k_stride, n_kv_heads, head_dim) ||
-      !rows_ok(v, v_stride, n_kv_heads, head_dim) || !rows_ok(out, out_stride, n_q_heads, head_dim))
+  if (!window_ok(a) || rl_window_rows_blocks(a) >= MOST_BLOCKS || !rows_ok(q, q_stride, n_q_heads, head_dim) ||
+      !rows_ok(k, k_stride, n_kv_heads, head_dim) || !rows_ok(v, v_stride, n_kv_heads, head_dim) || !rows_ok(out, out_stride, n_q_heads, head_dim))
     return RLGEN_ERR_BAD_ARG;
   a.row_starts = row_starts;
   a.q = q; a.q_stride = q_stride; a.k = k; a.k_stride = k_stride; a.v = v; a.v_stride = v_stride;
@@ -158,8 +153,8 @@ int rlgen_window_attention_backward(const void* q, int64_t q_stride, const void*
                                     size_t workspace_bytes, void* hip_stream) {
   if (!q || !k || !v || !out || !lse || !dout || !row_starts || !dq || !dk || !dv || !workspace) return RLGEN_ERR_NULL;
   WindowArgs a = window_shape(dtype, rows, n_q_heads, n_kv_heads, head_dim, S, max_len, window, sinks, scale);
-  if (!window_ok(a) || !grid_ok(a) || !rows_ok(q, q_stride, n_q_heads, head_dim) || !rows_ok(k, k_stride, n_kv_heads, head_dim) ||
-      !rows_ok(v, v_stride, n_kv_heads, head_dim) || !rows_ok(out, out_stride, n_q_heads, head_dim) ||
+  if (!window_ok(a) || rl_window_backward_blocks(a) >= MOST_BLOCKS || !rows_ok(q, q_stride, n_q_heads, head_dim) ||
+      !rows_ok(k, k_stride, n_kv_heads, head_dim) || !rows_ok(v, v_stride, n_kv_heads, head_dim) || !rows_ok(out, out_stride, n_q_heads, head_dim) ||
       !rows_ok(dout, dout_stride, n_q_heads, head_dim) || !rows_ok(dq, dq_stride, n_q_heads, head_dim) ||
       !rows_ok(dk, dk_stride, n_kv_heads, head_dim) || !rows_ok(dv, dv_stride, n_kv_heads, head_dim))
     return RLGEN_ERR_BAD_ARG;
@@ -193,13 +188,14 @@ int rlgen_window_attention_paged(const void* q, int64_t q_stride, int32_t dtype,
   if (!q || !pages || !page_table || !row_starts || !total_lens || !out) return RLGEN_ERR_NULL;
   WindowArgs a = window_shape(dtype, rows, n_q_heads, n_kv_heads, head_dim, S, max_new, window, sinks, scale);
   const int shift = page_shift(page_size);
-  if (!window_ok(a) || !grid_ok(a) || max_total < 1 || table_stride < 1 || !pages_ok(pages, n_pages, shift, n_kv_heads, head_dim) ||
+  if (!window_ok(a) || max_total < 1 || table_stride < 1 || !pages_ok(pages, n_pages, shift, n_kv_heads, head_dim) ||
       !rows_ok(q, q_stride, n_q_heads, head_dim) || !rows_ok(out, out_stride, n_q_heads, head_dim))
     return RLGEN_ERR_BAD_ARG;
   a.row_starts = row_starts; a.total_lens = total_lens; a.max_total = max_total;
   a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride; a.lse = lse;
   a.pages = pages; a.n_pages = n_pages; a.page_shift = shift; a.page_table = page_table; a.table_stride = table_stride;
   a.ws = workspace; a.ws_bytes = workspace_bytes;
+  if ((max_new == 1 ? rl_window_decode_blocks(a) : rl_window_rows_blocks(a)) >= MOST_BLOCKS) return RLGEN_ERR_BAD_ARG;
   if (max_new == 1) {
     const size_t need = rl_window_decode_bytes(a);
     if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return RLGEN_ERR_WORKSPACE;

@@ -47,7 +47,12 @@ struct WindowArgs {
   void *dq, *dk, *dv; long long dq_stride, dk_stride, dv_stride;
   void* ws; size_t ws_bytes;
 };
-hipError_t rl_window_rows(WindowArgs a, hipStream_t s);
+// What a launch of each would have in blocks of 256 threads, which have to stay below MOST_BLOCKS (a launch has fewer than 2^32 threads)
+constexpr long long MOST_BLOCKS = 1 << 24;
+long long rl_window_rows_blocks(const WindowArgs& a);
+long long rl_window_decode_blocks(const WindowArgs& a);
+long long rl_window_backward_blocks(const WindowArgs& a);
+hipError_t rl_window_rows(const WindowArgs& a, hipStream_t s);
 size_t rl_window_rows_bytes(const WindowArgs& a);
 size_t rl_window_decode_bytes(const WindowArgs& a);
 hipError_t rl_window_decode(const WindowArgs& a, hipStream_t s);

@@ -375,16 +375,28 @@ size_t parts_bytes(const WindowArgs& a, int parts) {
   return parts > 1 ? ((size_t)a.S * a.max_new * a.Hq * parts + 1) / 2 * 2 * (sizeof(float2) + (size_t)a.h * sizeof(float)) : 0;
 }
 
+struct Rows { int max_new, tiles, parts; };
+Rows rows_launch(const WindowArgs& a) {
+  Rows r{a.pages || a.max_new < a.rows ? a.max_new : a.rows, 0, 1};          // (packed sequences have no more rows than there are)
+  r.tiles = (int)(((long long)r.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
+  if (a.pages) {
+    r.parts = rows_parts(a);
+    if (r.parts > 1 && (!a.ws || a.ws_bytes < parts_bytes(a, r.parts))) r.parts = 1;
+  }
+  return r;
+}
+
 template <class T, int HD>
-hipError_t launch_rows(const WindowArgs& a, hipStream_t s) {
-  const int tiles = (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
+hipError_t launch_rows(WindowArgs a, hipStream_t s) {
+  const Rows r = rows_launch(a);
+  const int tiles = r.tiles, parts = r.parts;
+  a.max_new = r.max_new;
+  const dim3 grid((unsigned)mapped_blocks((long long)a.S * a.Hkv, (long long)tiles * parts));
   if (!a.pages) {
-    hipLaunchKernelGGL((window_rows_kernel<T, HD, false>), dim3(mapped_blocks(a.S * a.Hkv, tiles)), dim3(TPB), 0, s, a, tiles, 1);
+    hipLaunchKernelGGL((window_rows_kernel<T, HD, false>), grid, dim3(TPB), 0, s, a, tiles, 1);
     return hipGetLastError();
   }
-  int parts = rows_parts(a);
-  if (parts > 1 && (!a.ws || a.ws_bytes < parts_bytes(a, parts))) parts = 1;
-  hipLaunchKernelGGL((window_rows_kernel<T, HD, true>), dim3(mapped_blocks(a.S * a.Hkv, tiles * parts)), dim3(TPB), 0, s, a, tiles, parts);
+  hipLaunchKernelGGL((window_rows_kernel<T, HD, true>), grid, dim3(TPB), 0, s, a, tiles, parts);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || parts == 1) return e;
   const int lanes = a.h <= 64 ? 16 : a.h <= 128 ? 32 : 64;
@@ -405,9 +417,12 @@ hipError_t by_head(const WindowArgs& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t rl_window_rows(WindowArgs a, hipStream_t s) {
+long long rl_window_rows_blocks(const WindowArgs& a) {
+  const Rows r = rows_launch(a);
+  return mapped_blocks((long long)a.S * a.Hkv, (long long)r.tiles * r.parts);
+}
+hipError_t rl_window_rows(const WindowArgs& a, hipStream_t s) {
   if (a.rows <= 0) return hipSuccess;
-  if (!a.pages && a.max_new > a.rows) a.max_new = a.rows;
   return a.dtype == RLGEN_DTYPE_F16 ? by_head<TypeF16>(a, s) : by_head<TypeBf16>(a, s);
 }
 size_t rl_window_rows_bytes(const WindowArgs& a) { return parts_bytes(a, rows_parts(a)); }

@@ -695,17 +695,22 @@ size_t place(Backward& b, char* ws) {
   return at;
 }
 
+struct Tiles { int keys, sinks, jobs, queries; };
+Tiles tiles_of(const Backward& b) {
+  const WindowArgs& a = b.a;
+  Tiles t{(int)(((long long)a.max_new + BM - 1) / BM), (b.sinks + BM - 1) / BM, 0, (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM)};
+  t.jobs = t.keys * b.runs + t.sinks * b.chunks;
+  return t;
+}
 template <class T, int HD>
 hipError_t launch(const Backward& b, hipStream_t s) {
   const WindowArgs& a = b.a;
   const int units = a.S * a.Hkv;
-  const int key_tiles = (a.max_new + BM - 1) / BM, sink_tiles = (b.sinks + BM - 1) / BM, jobs = key_tiles * b.runs + sink_tiles * b.chunks;
-  if ((long long)(units + 7) * jobs * TPB * KEYS_HALVES<HD> > 0xffffffffll) return hipErrorInvalidConfiguration;      // (before the first launch)
+  const Tiles t = tiles_of(b);
   hipLaunchKernelGGL((delta_kernel<T, (HD > 128 ? 2 : 1)>), dim3((unsigned)(a.S * b.delta_chunks)), dim3(TPB), 0, s, b);
-  const int tiles = (int)(((long long)a.max_new * (a.Hq / a.Hkv) + BM - 1) / BM);
-  hipLaunchKernelGGL((queries_backward_kernel<T, HD>), dim3(mapped_blocks(units, tiles)), dim3(TPB), 0, s, b, tiles);
-  hipLaunchKernelGGL((keys_backward_kernel<T, HD>), dim3(mapped_blocks(units, jobs)), dim3(TPB * KEYS_HALVES<HD>), 0, s, b, key_tiles, jobs);
-  if (b.sinks > 0 || b.runs > 1) hipLaunchKernelGGL((parts_sum_kernel<T>), dim3((unsigned)units, b.runs > 1 ? key_tiles : sink_tiles, BM / SUM_KEYS), dim3(TPB), 0, s, b);
+  hipLaunchKernelGGL((queries_backward_kernel<T, HD>), dim3((unsigned)mapped_blocks(units, t.queries)), dim3(TPB), 0, s, b, t.queries);
+  hipLaunchKernelGGL((keys_backward_kernel<T, HD>), dim3((unsigned)mapped_blocks(units, t.jobs)), dim3(TPB * KEYS_HALVES<HD>), 0, s, b, t.keys, t.jobs);
+  if (b.sinks > 0 || b.runs > 1) hipLaunchKernelGGL((parts_sum_kernel<T>), dim3((unsigned)units, b.runs > 1 ? t.keys : t.sinks, BM / SUM_KEYS), dim3(TPB), 0, s, b);
   return hipGetLastError();
 }
 template <class T>
@@ -724,6 +729,12 @@ hipError_t by_head(const Backward& b, hipStream_t s) {
 size_t rl_window_backward_bytes(const WindowArgs& a) {
   Backward b = parted(a);
   return place(b, nullptr);
+}
+long long rl_window_backward_blocks(const WindowArgs& a) {
+  const Backward b = parted(a);
+  const Tiles t = tiles_of(b);
+  const long long keys = (long long)t.jobs * (a.h > 96 ? KEYS_HALVES<128> : 1);          // (heads of more than 96 dims run as 128 or 256)
+  return mapped_blocks((long long)a.S * a.Hkv, keys > t.queries ? keys : t.queries);
 }
 hipError_t rl_window_backward(const WindowArgs& a, hipStream_t s) {
   if (a.rows <= 0) return hipSuccess;

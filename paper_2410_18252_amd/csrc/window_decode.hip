@@ -312,16 +312,21 @@ Split decode_split(const WindowArgs& a) {
   return r;
 }
 
+long long blocks(const WindowArgs& a, const Split& r) {
+  const long long jobs = (long long)a.S * a.Hkv * r.col_blocks * r.parts;
+  return r.waves == 1 ? (jobs + 3) / 4 : jobs;
+}
+
 template <class T, int HD>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
   const Split r = decode_split(a);
-  const long long jobs = (long long)a.S * a.Hkv * r.col_blocks * r.parts;
+  const dim3 grid((unsigned)blocks(a, r));
   const int G = a.Hq / a.Hkv, cb = HD > 128 ? 8 : 16;
   if (r.waves == 1) {
-    hipLaunchKernelGGL((window_decode_kernel<T, HD, 1>), dim3((unsigned)((jobs + 3) / 4)), dim3(TPB), 0, s, a, r.parts, r.col_blocks);
+    hipLaunchKernelGGL((window_decode_kernel<T, HD, 1>), grid, dim3(TPB), 0, s, a, r.parts, r.col_blocks);
   } else {
     const size_t lds = (size_t)4 * (G < cb ? G : cb) * a.h * sizeof(float);
-    hipLaunchKernelGGL((window_decode_kernel<T, HD, 4>), dim3((unsigned)jobs), dim3(TPB), lds, s, a, r.parts, r.col_blocks);
+    hipLaunchKernelGGL((window_decode_kernel<T, HD, 4>), grid, dim3(TPB), lds, s, a, r.parts, r.col_blocks);
     if (r.parts > 1) {
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
@@ -344,6 +349,7 @@ size_t rl_window_decode_bytes(const WindowArgs& a) {
   const Split r = decode_split(a);
   return r.parts > 1 ? (size_t)a.S * a.Hq * r.parts * ((size_t)a.h * sizeof(float) + sizeof(Part)) : 0;
 }
+long long rl_window_decode_blocks(const WindowArgs& a) { return blocks(a, decode_split(a)); }
 hipError_t rl_window_decode(const WindowArgs& a, hipStream_t s) {
   if (a.rows <= 0) return hipSuccess;
   return a.dtype == RLGEN_DTYPE_F16 ? by_head<TypeF16>(a, s) : by_head<TypeBf16>(a, s);

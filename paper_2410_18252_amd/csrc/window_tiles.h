@@ -240,7 +240,7 @@ __device__ __forceinline__ bool map_block(int id, int units, int jobs, int& unit
   unit = (group * at_once + r - job * at_once) * 8 + x;
   return unit < units;
 }
-inline unsigned mapped_blocks(int units, int jobs) { return (unsigned)((units + 7) / 8 * 8) * jobs; }      // (at_once is all or one)
+inline long long mapped_blocks(long long units, long long jobs) { return (units + 7) / 8 * 8 * jobs; }      // (at_once is all or one)
 
 // The sign of a scale goes to the queries (their sign bits, exactly), so that the largest product has the largest score; a scale of zero
 // becomes one that every score vanishes under, since -infinity stands for masked scores.
