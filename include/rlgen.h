@@ -315,6 +315,7 @@ int rlgen_status_bits(rlgen_ctx *ctx, void *hip_stream, uint32_t *faults);
  *  - head_dim is a multiple of 16, at most 256; n_kv_heads divides n_q_heads.
  *  - Visibility: a query at position p sees key j if j <= p and (j > p - window, or j < sinks, or window == 0: no window).  A query that
  *    sees nothing has output 0 and log-sum-exp -infinity.
+ *  - Without rows (0) an operator returns at once, gradients of gains are zeroed, and pointers to tensors of rows may be null.
  *  - Sizes: rows * heads, S * heads and n_pages * page_size below 2^31.  Offsets are 64-bit.  A launch has fewer than 2^24 blocks: of the attention
  *    over rows S * n_kv_heads (rounded up to 8) times the tiles, of 128 pairs of a row and a query head of the group, that max_len (at most rows)
  *    or max_new makes, and in the backward pass the tiles of 128 keys, two blocks each beyond 96 dims; of single tokens S * n_kv_heads / 4.

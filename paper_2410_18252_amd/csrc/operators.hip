@@ -1,4 +1,5 @@
 // C entry points of the operators over a cache in pages and packed rows: what the host can check is checked here, then launched.
+// A pass without rows has no tensors of rows, so their pointers may be null.
 #include "../../include/rlgen.h"
 #include "kernels.h"
 #include "window.h"
@@ -31,7 +32,7 @@ bool pages_ok(const void* pages, int n_pages, int shift, int Hkv, int h) {
 
 int norm_rope_args(NormRopeArgs& a, const void* qkv, int64_t qkv_stride, int src_dtype, int rows, int Hq, int Hkv, int h, const float* q_gain,
                    const float* k_gain, float eps, const float* rope, int max_pos, int r, const int* positions, int dtype) {
-  if (!qkv || !q_gain || !k_gain || !positions || (r > 0 && !rope)) return RLGEN_ERR_NULL;
+  if (!q_gain || !k_gain || (rows > 0 && (!qkv || !positions)) || (r > 0 && !rope)) return RLGEN_ERR_NULL;
   if (!heads_ok(rows, Hq, Hkv, h) || !type16(dtype) || src_dtype < RLGEN_DTYPE_F32 || src_dtype > RLGEN_DTYPE_F16 || !std::isfinite(eps) || eps < 0.f ||
       r < 0 || r > h || r % 2 != 0 || max_pos < 1 || !rows_ok(qkv, qkv_stride, Hq + 2 * Hkv, h, src_dtype == RLGEN_DTYPE_F32 ? 4 : 8))
     return RLGEN_ERR_BAD_ARG;
@@ -90,7 +91,7 @@ int rlgen_qk_norm_rope(const void* qkv, int64_t qkv_stride, int32_t src_dtype, i
   const int rc = norm_rope_args(a, qkv, qkv_stride, src_dtype, rows, n_q_heads, n_kv_heads, head_dim, q_gain, k_gain, eps, rope, max_pos,
                                 rotary_dim, positions, dtype);
   if (rc != RLGEN_OK) return rc;
-  if (!q || (!pages && !k) || (pages && !slots)) return RLGEN_ERR_NULL;
+  if (rows > 0 && (!q || (!pages && !k) || (pages && !slots))) return RLGEN_ERR_NULL;
   const int shift = pages ? page_shift(page_size) : 0;
   if (!rows_ok(q, q_stride, n_q_heads, head_dim) || (k && !rows_ok(k, k_stride, n_kv_heads, head_dim)) ||
       (v && !rows_ok(v, v_stride, n_kv_heads, head_dim)) || (pages && !pages_ok(pages, n_pages, shift, n_kv_heads, head_dim)))
@@ -113,7 +114,7 @@ int rlgen_qk_norm_rope_backward(const void* qkv, int64_t qkv_stride, int32_t src
   const int rc = norm_rope_args(a, qkv, qkv_stride, src_dtype, rows, n_q_heads, n_kv_heads, head_dim, q_gain, k_gain, eps, rope, max_pos,
                                 rotary_dim, positions, dtype);
   if (rc != RLGEN_OK) return rc;
-  if (!dq || !dk || !dv || !dqkv || !dq_gain || !dk_gain || !workspace) return RLGEN_ERR_NULL;
+  if ((rows > 0 && (!dq || !dk || !dv || !dqkv)) || !dq_gain || !dk_gain || !workspace) return RLGEN_ERR_NULL;
   if (!rows_ok(dq, dq_stride, n_q_heads, head_dim) || !rows_ok(dk, dk_stride, n_kv_heads, head_dim) || !rows_ok(dv, dv_stride, n_kv_heads, head_dim) ||
       !rows_ok(dqkv, dqkv_stride, n_q_heads + 2 * n_kv_heads, head_dim, src_dtype == RLGEN_DTYPE_F32 ? 4 : 8))
     return RLGEN_ERR_BAD_ARG;
@@ -128,7 +129,7 @@ int rlgen_window_attention(const void* q, int64_t q_stride, const void* k, int64
                            int32_t rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const int32_t* row_starts, int32_t S,
                            int32_t max_len, int32_t window, int32_t sinks, float scale, void* out, int64_t out_stride, float* lse,
                            void* hip_stream) {
-  if (!q || !k || !v || !row_starts || !out) return RLGEN_ERR_NULL;
+  if ((rows > 0 && (!q || !k || !v || !out)) || !row_starts) return RLGEN_ERR_NULL;
   WindowArgs a = window_shape(dtype, rows, n_q_heads, n_kv_heads, head_dim, S, max_len, window, sinks, scale);
   if (!window_ok(a) || rl_window_rows_blocks(a) >= MOST_BLOCKS || !rows_ok(q, q_stride, n_q_heads, head_dim) ||
       !rows_ok(k, k_stride, n_kv_heads, head_dim) || !rows_ok(v, v_stride, n_kv_heads, head_dim) || !rows_ok(out, out_stride, n_q_heads, head_dim))
@@ -151,7 +152,7 @@ int rlgen_window_attention_backward(const void* q, int64_t q_stride, const void*
                                     const int32_t* row_starts, int32_t S, int32_t max_len, int32_t window, int32_t sinks, float scale,
                                     void* dq, int64_t dq_stride, void* dk, int64_t dk_stride, void* dv, int64_t dv_stride, void* workspace,
                                     size_t workspace_bytes, void* hip_stream) {
-  if (!q || !k || !v || !out || !lse || !dout || !row_starts || !dq || !dk || !dv || !workspace) return RLGEN_ERR_NULL;
+  if ((rows > 0 && (!q || !k || !v || !out || !lse || !dout || !dq || !dk || !dv)) || !row_starts || !workspace) return RLGEN_ERR_NULL;
   WindowArgs a = window_shape(dtype, rows, n_q_heads, n_kv_heads, head_dim, S, max_len, window, sinks, scale);
   if (!window_ok(a) || rl_window_backward_blocks(a) >= MOST_BLOCKS || !rows_ok(q, q_stride, n_q_heads, head_dim) ||
       !rows_ok(k, k_stride, n_kv_heads, head_dim) || !rows_ok(v, v_stride, n_kv_heads, head_dim) || !rows_ok(out, out_stride, n_q_heads, head_dim) ||
@@ -185,7 +186,7 @@ int rlgen_window_attention_paged(const void* q, int64_t q_stride, int32_t dtype,
                                  int32_t table_stride, const int32_t* row_starts, const int32_t* total_lens, int32_t S, int32_t max_new,
                                  int32_t max_total, int32_t window, int32_t sinks, float scale, void* out, int64_t out_stride, float* lse,
                                  void* workspace, size_t workspace_bytes, void* hip_stream) {
-  if (!q || !pages || !page_table || !row_starts || !total_lens || !out) return RLGEN_ERR_NULL;
+  if ((rows > 0 && (!q || !out)) || !pages || !page_table || !row_starts || !total_lens) return RLGEN_ERR_NULL;
   WindowArgs a = window_shape(dtype, rows, n_q_heads, n_kv_heads, head_dim, S, max_new, window, sinks, scale);
   const int shift = page_shift(page_size);
   if (!window_ok(a) || max_total < 1 || table_stride < 1 || !pages_ok(pages, n_pages, shift, n_kv_heads, head_dim) ||
