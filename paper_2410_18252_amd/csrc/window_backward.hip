@@ -6,7 +6,7 @@
 // seven matrix products instead of the five that one kernel with atomic sums would need, but every sum has one order, so that results do
 // not change from run to run.  P and dS are rounded to the inputs' type for their second products, errors of the order of the
 // gradients' own rounding; fp16, whose smallest normal number a dS easily falls below, multiplies dS by a power of two taken from the
-// largest |dout| and |v| that enter the sum: of the row and of the keys in its sight for dq, of the queries walked and of the block's keys for dk.
+// largest |dout| and |v| that enter the sum: of the row and of the keys in its sight for dq, of the queries walked and of the keys in theirs for dk.
 //
 // The queries' side goes first, since it corrects delta for the rows that see few keys; its walk is the forward pass's.  Both sides are bound
 // by their chains of products, exponentials and barriers with two or three waves to a SIMD (matrix unit 43 and 33 % busy at 128 dims),
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(TPB) void delta_kernel(Backward b) {
 }
 
 // What fp16 multiplies dS by: a power of two with which none leaves the type's range.  |dP| is at most h max|dout| max|v| and so is
-// |delta|, and P is at most 1.  Only finite values count: what an infinity makes of a dS no factor changes.  Only values that the sum
+// |delta|, v of all keys that the query sees, and P is at most 1.  Only finite values count: what an infinity makes of a dS no factor changes.  Only values that the sum
 // is of count, so no other sequence, row or key takes bits from it.
 __device__ __forceinline__ float ds_factor(int h, float dout_peak, float v_peak) {
   const float most = 2.f * (float)h * dout_peak * v_peak;
@@ -222,10 +222,12 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
   // parts beyond the window concern the sinks alone
   const bool idle = kw >= q.n || (slot > 0 && kw >= b.sinks);
 
-  [[maybe_unused]] Peaks dout_peaks, v_peaks;
+  [[maybe_unused]] Peaks dout_peaks, near, far;      // of the queries walked; of the values in their sight, which delta is made of
   if constexpr (__is_same(T, TypeF16)) {
+    const int lo = a.window ? max(tok0 - a.window + 1, 0) : 0;
     dout_peaks = peaks_of(b, b.dout_peak, s, tok0, tok1);
-    v_peaks = peaks_of(b, b.v_peak, s, kt * BM, min(kt * BM + BM, q.n));
+    near = peaks_of(b, b.v_peak, s, lo, tok1);
+    far = peaks_of(b, b.v_peak, s, 0, min(a.sinks, lo));
   }
   vec8 kf[KS], vf[V_IN_LDS ? 1 : KS];
   {
@@ -277,7 +279,7 @@ __global__ __launch_bounds__(TPB * KEYS_HALVES<HD>, 2) void keys_backward_kernel
   settle(kf);                                  // (behind the first request: one wait for both)
   if constexpr (!V_IN_LDS) settle(vf);
   float factor = 1.f;
-  if constexpr (__is_same(T, TypeF16)) factor = ds_factor(a.h, largest(dout_peaks), largest(v_peaks));
+  if constexpr (__is_same(T, TypeF16)) factor = ds_factor(a.h, largest(dout_peaks), fmaxf(largest(near), largest(far)));
   const float p_factor = factor * (1.f / P_SIZE<T>);
   scalars_landed();
   const bool few_keys = sees_few(a, q.n);

@@ -77,3 +77,17 @@ def test_a_row_keeps_its_precision_beside_larger_ones(Hq, Hkv, h, window, sinks,
     dq = gradients(x, i32([0, n]), n, window, sinks, scale)[2][0]
     keep = [i for i in range(n) if i != row]
     W.check("dq", dq[keep], want[0][keep], want[1][keep])
+
+
+@pytest.mark.parametrize("Hq, Hkv, h, window, sinks", [(2, 1, 64, 0, 0), (4, 4, 80, 250, 3), (4, 2, 128, 0, 0), (2, 2, 256, 200, 130), (8, 1, 32, 0, 0)])
+@pytest.mark.parametrize("first", [True, False])
+def test_small_values_beside_large_ones(Hq, Hkv, h, window, sinks, first):
+    """What is subtracted in dS comes from all keys in sight: where they are of very different sizes, dS of the small ones stays in the type's range."""
+    n, scale = 420, 1 / math.sqrt(h)
+    x = inputs(n, Hq, Hkv, h, 1.0, 60 + h)
+    size = torch.where((torch.arange(n) < 150) == first, 2.0 ** -10, 2.0 ** 8)[:, None, None].cuda()
+    x[2] = (x[2].float() * size).half()
+    want = W.attention(*x[:3], 0, window, sinks, scale, HF, x[3])
+    out, lse, got = gradients(x, i32([0, n]), n, window, sinks, scale)
+    for name, g in zip(("dq", "dk", "dv"), got):
+        W.check(name, g, *want[name])
