@@ -359,7 +359,7 @@ int rlgen_qk_norm_rope(const void *qkv, int64_t qkv_stride, int32_t src_dtype, i
                        const int32_t *slots, void *hip_stream);
 
 /* Its gradients: dq, dk, dv (type dtype, of q, k and v as rlgen_qk_norm_rope returns them) to dqkv (type src_dtype, all of it written)
- * and dq_gain, dk_gain [head_dim] fp32 (sums over rows and heads in a fixed order).  workspace: 16-byte aligned,
+ * and dq_gain, dk_gain [head_dim] fp32 (sums over all rows and heads in a fixed order, padding rows among them).  workspace: 16-byte aligned,
  * rlgen_qk_norm_rope_backward_workspace(rows, head_dim) bytes.  Errors: NULL, BAD_ARG, WORKSPACE, DEVICE. */
 size_t rlgen_qk_norm_rope_backward_workspace(int32_t rows, int32_t head_dim);
 int rlgen_qk_norm_rope_backward(const void *qkv, int64_t qkv_stride, int32_t src_dtype, int32_t rows, int32_t n_q_heads,
@@ -378,8 +378,10 @@ int rlgen_window_attention(const void *q, int64_t q_stride, const void *k, int64
                            const int32_t *row_starts, int32_t S, int32_t max_len, int32_t window, int32_t sinks, float scale, void *out,
                            int64_t out_stride, float *lse, void *hip_stream);
 
-/* Its gradients, from its own inputs and outputs and dout (all of dq, dk and dv is written; a query that sees nothing and a key that
- * nobody sees have zeros).  Within a sequence infinities and NaN go where the products carry them; no other sequence is touched.
+/* Its gradients, from its own inputs and outputs and dout.  Written are the rows of dq, dk and dv that a sequence has within max_len (zeros for a
+ * query that sees nothing and a key that nobody sees); the others, and lse and out of the forward pass there, are left as they are: zero
+ * them where a later sum goes over all rows.  Within a sequence infinities and NaN go where the products carry them; no other sequence's
+ * values change a bit of its gradients.
  * workspace: 16-byte aligned, rlgen_window_attention_backward_workspace(...) bytes.  Errors: NULL, BAD_ARG, WORKSPACE, DEVICE. */
 size_t rlgen_window_attention_backward_workspace(int32_t rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t S,
                                                  int32_t max_len, int32_t window, int32_t sinks);

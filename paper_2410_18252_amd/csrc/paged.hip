@@ -64,7 +64,7 @@ __device__ __forceinline__ Lens plan_lens(const PlanArgs& a, int s) {
 // A pass's plan in one launch without scratch memory: a block owns the `group` requests from blockIdx.x * group on and adds up the
 // lengths of all requests before them itself (8 bytes a request out of L2: 1000 requests are four loads a thread), then scans its own in
 // LDS and writes their rows and pages.  Where a group has many rows, blockIdx.y parts them.  Bound by a launch and three or four
-// dependent memory latencies, not by its bytes (1000 requests of a token each: 5.4 us).
+// dependent memory latencies, not by its bytes (1000 requests of a token each: 5.6 us).
 __global__ __launch_bounds__(TPB) void plan_pages_kernel(PlanArgs a) {
   __shared__ int red[4];
   __shared__ int row_end[PLAN_GROUP], page_end[PLAN_GROUP], lens_ctx[PLAN_GROUP], lens_had[PLAN_GROUP];
@@ -566,8 +566,8 @@ hipError_t by_type(const NormRopeArgs& a, bool backward, Launch l, hipStream_t s
 }  // namespace
 
 hipError_t rl_plan_pages(PlanArgs a, hipStream_t s) {
-  // 256 blocks of requests at most while a block's requests fit its LDS (1000 requests of one token: 5.5 us, 6.6 in 16 blocks; 512 prompts of
-  // 256 to 512 tokens: 6.3 us, 9.0); rows of a group are parted until a part has 1024 of them or the launch 1024 blocks (4
+  // 256 blocks of requests at most while a block's requests fit its LDS (1000 requests of one token: 5.6 us, 6.6 in 16 blocks; 512 prompts of
+  // 256 to 512 tokens: 6.5 us, 9.0); rows of a group are parted until a part has 1024 of them or the launch 1024 blocks (4
   // requests of 50000 tokens: 8.5 us, 22 with parts of 16384)
   a.group = (a.S + 255) / 256;
   if (a.group > PLAN_GROUP) a.group = PLAN_GROUP;

@@ -10,14 +10,14 @@
 //   S^T[key, m] = K q^T             32x32x16 matrix instructions, K fragments from LDS, q in registers
 //   O^T[d, m]  += V^T[d, key] P^T   the probabilities leave the first product in the layout the second wants; V is read transposed
 // The probabilities are rounded to the inputs' type for the second product (the sum that they are divided by is of the unrounded ones):
-// an error of the order of the output's own rounding.
+// an error of the order of the output's own rounding.  (fp16 loses bits of those below 2^-14 of the largest, 2^-25 of it at most.)
 //
 // Tiles: 128 rows to a block and 32 of them to a wave, so that q stays in registers and a wave's sums are four (eight at 256 dims)
 // accumulators; 32 keys to a tile, so that K and V of two tiles take 32 KB at 128 dims and three blocks share a CU (tiles of 64 keys: 33 us
 // where these take 27, 48 sequences of up to 512 tokens, window 128).  Bound by neither memory nor the matrix unit alone: at 128 dims the
 // exponentials, masks and conversions of a tile take as many cycles as its products, 46 and 39 % of the launch, and three waves to a SIMD
-// overlap them only in part.  Measured: 8250 rows, 32 heads over 8 of 128, window 1024: 145 us for 0.11 TFLOP; 9985 rows, 32 heads of
-// 80 in fp16: 77 us; a chunk of 500 rows on each of six contexts over pages: 74 us.
+// overlap them only in part.  Measured: 8250 rows, 32 heads over 8 of 128, window 1024: 137 us for 0.11 TFLOP; 9985 rows, 32 heads of
+// 80 in fp16: 77 us; a chunk of 500 rows on each of six contexts over pages: 71 us (on other cards 133 to 149, 76 to 84, 70 to 79).
 #include "../../include/rlgen.h"
 #include "window_tiles.h"
 

@@ -9,9 +9,10 @@
 // largest |dout| and |v| that enter the sum: of the row and of the keys in its sight for dq, of the queries walked and of the keys in theirs for dk.
 //
 // The queries' side goes first, since it corrects delta for the rows that see few keys; its walk is the forward pass's.  Both sides are bound
-// by their chains of products, exponentials and barriers with two or three waves to a SIMD (matrix unit 43 and 33 % busy at 128 dims),
-// not by memory.  Measured: 8250 rows, 32 heads over 8 of 128, window 1024: delta 25 us, queries' side 203, keys' side 346, sums of the
-// sinks' parts 5 (0.30 TFLOP without the products that are computed twice); 9985 rows, 32 heads of 80 in fp16: 32, 112 and 164 us.
+// by their chains of products, exponentials and barriers with two or three waves to a SIMD (matrix unit 43 and 31 % busy at 128 dims),
+// not by memory.  Measured: 8250 rows, 32 heads over 8 of 128, window 1024: delta 22 us, queries' side 187, keys' side 311, sums of the
+// sinks' parts 5 (0.30 TFLOP without the products that are computed twice; 182 to 209 and 302 to 368 us on other cards); 9985 rows, 32 heads of
+// 80 in fp16: 32, 104 and 150 us.
 #include "../../include/rlgen.h"
 #include "window_tiles.h"
 #include <type_traits>
@@ -165,7 +166,7 @@ __device__ __forceinline__ float largest(const Peaks& p) {
 // 1500 to 4000, window 1024, 32 heads over 8: 357 us, 480 with four waves).
 template <int HD> constexpr int KEYS_HALVES = HD >= 128 ? 2 : 1;
 // At 256 dims both gradients of a wave's keys would need all 512 registers and more: the first four waves take dv, the second dk, and both
-// take S: five products for four, but two waves to a SIMD (six sequences of 500 to 2000, eight heads: 547 us as one wave to a SIMD, 247).
+// take S: five products for four, but two waves to a SIMD (six sequences of 500 to 2000, eight heads: 547 us as one wave to a SIMD, 244).
 
 // The token behind the last that a tile of keys is seen by, its parted sinks apart
 __device__ __forceinline__ int last_seer(const Backward& b, int kt, int n) {
@@ -541,8 +542,9 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : HD > 96 ? 2 : 3) void queries_b
   // take delta from the sum over their keys of P dP and leave it for the keys' side: a sequence's first 32 rows from the 32 keys that they
   // see at most, which begin the first tile; all rows, in a pass of its own, where every row sees few (FEW: a window of up to FEW_KEYS, or
   // a sequence of up to FEW_ROWS).  There dS also takes part with what its rounding loses, on both sides: over few keys, whose dS add up to
-  // nothing, such errors do not average out (against the formulas in 64 bits up to 2.1 times the error of gradients that are rounded
-  // once, 1.44 with it).  Long sequences come to 1.45 without, and would pay 15 % of the keys' side for it.
+  // nothing, such errors do not average out (28 calls of 1 to 64 tokens or windows up to 25, against the formulas in 64 bits: 1.22 to 1.47
+  // times the error of gradients that are rounded once, 1.00 with it).  Long sequences come to 1.45 without, and would pay 15 % of the keys'
+  // side for it.
   auto own_delta = [&](int buf, int u, int kb) {
     f32x16 sc, dp;
     products(buf, u, sc, dp);
@@ -646,8 +648,8 @@ void part_sinks(Backward& b) {
 }
 // The queries that see a tile of keys are parted where the longest such walk would take well over an even share: few kv heads with many
 // query heads each, a long sequence.  Partial sums stay below 256 MB.
-// Measured on six sequences of 500 to 2000 tokens, 12 heads over 2 of 96: 476 us in one walk, 224 parted with 10 for the sums; 16 over 4 of
-// 64: 222 us, 97 with 6.
+// Measured on six sequences of 500 to 2000 tokens, 12 heads over 2 of 96: 476 us in one walk, 220 parted with 11 for the sums; 16 over 4 of
+// 64: 222 us, 118 with 11.
 void part_runs(Backward& b) {
   const WindowArgs& a = b.a;
   b.runs = 1;

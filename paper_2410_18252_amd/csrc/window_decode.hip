@@ -291,9 +291,11 @@ __global__ __launch_bounds__(TPB) void window_join_kernel(WindowArgs a, int part
 
 // Waves to a job and blocks to a job.  Where jobs alone fill the card a wave takes one, which spares the join in LDS (512 sequences of up to
 // 576 tokens, 32 kv heads of 80, 16384 jobs: 447 us, 506 with four waves to a job); else four waves share it (64 sequences, 8 kv heads of
-// 128, window 1024, 512 jobs: 46 us, 77 with one).  Few jobs are parted over blocks until there are 512 of these, each with eight groups of keys
-// or more (one sequence of 32000 tokens, 8 jobs: 24 us and 4 for the join with 256, 512 or 1024 blocks, 1250 unparted by single waves; the
-// 512 jobs above in 1024 blocks: 50 us and 8).
+// 128, window 1024, 512 jobs: 46 us, 77 with one).  At the border, sequences of 257 to 576 tokens, one wave and four: 1024 jobs 40 and 36 us (80
+// dims), 46.1 and 45.6 (128), 33 and 24 (64); 2048 jobs 63 and 68, 82 and 83, 46 and 44; 4096 jobs 120 and 127, 156 and 158, 86 and 82.  Longer
+// contexts gain from four beyond it too (1000 to 4000 tokens, 2048 jobs: 371 and 353 us, 504 and 436, 269 and 239).
+// Few jobs are parted over blocks until there are 512 of these, each with eight groups of keys or more (one sequence of 32000 tokens, 8 jobs:
+// 24 us and 4 for the join with 256, 512 or 1024 blocks, 1250 unparted by single waves; the 512 jobs above in 1024 blocks: 50 us and 8).
 constexpr int MAX_PARTS = 64;                 // (window_join_kernel's lanes)
 struct Split { int waves, parts, col_blocks; };
 Split decode_split(const WindowArgs& a) {

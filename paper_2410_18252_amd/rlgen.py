@@ -394,6 +394,7 @@ def rlgen_debug_set_gemm(p: Policy, mode: int, which: int, variant: int):
 
 
 # ------------------------------------------------------------------ operators over a cache in pages and packed rows
+# They stand outside autograd: outputs carry no history whatever their inputs ask for, gradients come from the *_backward functions.
 _DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
 
 
@@ -530,7 +531,7 @@ def rlgen_qk_norm_rope_backward(qkv, q_gain, k_gain, eps: float, rope, positions
 
 def rlgen_window_attention(q, k, v, row_starts, max_len: int, window: int, sinks: int, scale: float, out=None):
     """Packed rows: q [rows, n_q, h], k and v [rows, n_kv, h] (any row stride), row_starts [S + 1] int32.  Returns (out [rows, n_q, h],
-    lse [rows, n_q] fp32); `out`: the two to write into."""
+    lse [rows, n_q] fp32); `out`: the two to write into.  Rows that no sequence has within max_len are not written."""
     rows, n_q, h = q.shape
     n_kv, dt = k.shape[1], q.dtype
     assert k.shape == v.shape == (rows, n_kv, h)
@@ -545,7 +546,8 @@ def rlgen_window_attention(q, k, v, row_starts, max_len: int, window: int, sinks
 
 def rlgen_window_attention_backward(q, k, v, out, lse, dout, row_starts, max_len: int, window: int, sinks: int, scale: float, grads=None,
                                     workspace=None):
-    """From rlgen_window_attention's inputs, its (out, lse) and dout: (dq, dk, dv).  `grads`: the three to write into."""
+    """From rlgen_window_attention's inputs, its (out, lse) and dout: (dq, dk, dv).  `grads`: the three to write into.  Rows that no sequence has
+    within max_len are not written."""
     rows, n_q, h = q.shape
     n_kv, dt = k.shape[1], q.dtype
     assert k.shape == v.shape == (rows, n_kv, h) and out.shape == dout.shape == q.shape and lse.shape == (rows, n_q)
