@@ -318,7 +318,8 @@ int rlgen_status_bits(rlgen_ctx *ctx, void *hip_stream, uint32_t *faults);
  *  - Without rows (0) an operator returns at once, gradients of gains are zeroed, and pointers to tensors of rows may be null.
  *  - Sizes: rows * heads, S * heads and n_pages * page_size below 2^31.  Offsets are 64-bit.  A launch has fewer than 2^24 blocks: of the attention
  *    over rows S * n_kv_heads (rounded up to 8) times the tiles, of 128 pairs of a row and a query head of the group, that max_len (at most rows)
- *    or max_new makes, and in the backward pass the tiles of 128 keys, two blocks each beyond 96 dims; of single tokens S * n_kv_heads / 4.
+ *    or max_new makes, and in the backward pass the tiles of 128 keys, two blocks each beyond 96 dims; of single tokens S * n_kv_heads / 4
+ *    times the query heads of a group over 16 (over 8 beyond 128 dims), rounded up.
  * Entries of row_starts, page_table and slots that lie outside their arrays are clamped or skipped, never followed: a token whose page lies
  * outside the cache is seen by no query. */
 #define RLGEN_PLAN_ROWS    1   /* counts[3]: more rows than max_rows or 2^31 - 2 (those beyond are not written) */
