@@ -7,6 +7,7 @@
 // The scores leave the first product where the second wants its probabilities (key 8 g + 4 t + j in lane group g).  Visible keys are two
 // runs, sinks and window, so a step's cost follows the window.  Eight keys in a row share a page, so a lane looks up two pages for
 // 32 keys, one iteration before it needs them; the next 32 keys are requested before the present ones are used.
+// In fp16 the probabilities are taken 2^15 times as large, which keeps those down to 2^-29 of the largest normal numbers.
 // Values that are not seen are zeroed, not multiplied by zero; a page outside the cache is not seen (a lane's scores and values are those of the
 // eight keys that it looked up together).
 //
@@ -97,6 +98,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void window_decode_kernel(Wi
   for (int x = 0; x < CH; ++x)
 #pragma unroll
     for (int e = 0; e < VW; ++e) o[x][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  constexpr float UP = __is_same(T, TypeF16) ? 15.f : 0.f;
   float mx = -INFINITY, sum = 0.f;
   const float scale2 = score_factor(a.scale);
   u32x4 k[2][KS], k_next[2][KS];
@@ -143,9 +145,9 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void window_decode_kernel(Wi
     for (int e = 0; e < 8; ++e) top = fmaxf(top, sc[e >> 2][e & 3]);
     top = fmaxf(top, __shfl_xor(top, 16, WAVE));
     top = fmaxf(top, __shfl_xor(top, 32, WAVE)) * scale2;
-    const float now = fmaxf(mx, top), base = now == -INFINITY ? 0.f : now;
+    const float now = fmaxf(mx, top), base = (now == -INFINITY ? 0.f : now) - UP;
     if (__any(now > mx)) {
-      const float shrink = __builtin_amdgcn_exp2f(mx - base);
+      const float shrink = __builtin_amdgcn_exp2f(mx - UP - base);
       sum *= shrink;
 #pragma unroll
       for (int x = 0; x < CH; ++x)
@@ -184,6 +186,7 @@ __global__ __launch_bounds__(TPB, HD > 128 ? 1 : 2) void window_decode_kernel(Wi
   }
   sum += __shfl_xor(sum, 16, WAVE);
   sum += __shfl_xor(sum, 32, WAVE);
+  mx -= UP;                                        // (what the sums refer to)
   // lane (c, g) holds of column c the dims VW (4 g + j) + e, j = 0..3
   const long long row = q.row0;
   if constexpr (JW == 1) {

@@ -41,3 +41,62 @@ def test_values_gradients_beside_a_dominant_key(Hq, Hkv, h, n, window, sinks, ga
     past = want.to(HF).isinf()                            # (the dominant key's sum passes the type's largest number: its cast is an infinity)
     want[past] = want[past].sign() * math.inf
     W.check("dv", dv, want, bound)
+
+
+def dominated(n, Hq, Hkv, h, gap, seed):
+    """Queries, keys and values of n tokens: key 0 lies `gap` above the others for every query and has next to no value."""
+    q, k, v = (rand(seed + i, n, m, h, dt=torch.float32) * s for i, (m, s) in enumerate(((Hq, 0.3), (Hkv, 0.3), (Hkv, 100.0))))
+    q[:, :, 3] = 4.0
+    k[:, :, 3] = 0.0
+    k[0, :, 3] = gap * math.sqrt(h) / 4.0
+    v[0] *= 2.0 ** -19
+    return q.half(), k.half(), v.half()
+
+
+def check_out(q, k, v, ctx, window, sinks, out):
+    """out = P v: P is rounded once to 11 bits, its exponent is off by the score's 32-bit sum, the sum that it is divided by likewise, and the
+    result is rounded once."""
+    u, eps, (n, Hq, h), T = W.U[HF], W.EPS, q.shape, k.shape[0]
+    q, k, v = q.double().cpu(), k.double().cpu(), v.double().cpu()
+    mask = W.seen(torch.arange(ctx, ctx + n), T, window, sinks)
+    want, bound = torch.zeros_like(q), torch.zeros_like(q)
+    for a in range(Hq):
+        b = a // (Hq // k.shape[1])
+        z = q[:, a] @ k[:, b].T / math.sqrt(h)
+        p = torch.softmax(z.masked_fill(~mask, -math.inf), 1)
+        assert float(p[mask].min()) > 2.0 ** -24 and (n < 100 or float(p[mask].median()) < 2.0 ** -19)
+        e_s = ((h + 8) * 2.0 ** -24 / math.sqrt(h) * (q[:, a].abs() @ k[:, b].abs().T)).masked_fill(~mask, 0.0).amax(1)
+        want[:, a] = p @ v[:, b]
+        bound[:, a] = (p * (u + 2 * e_s + 2 * eps)[:, None]) @ v[:, b].abs()
+    W.check("out", out, want, bound + u * (want.abs() + bound) + 2.0 ** -25)
+
+
+@pytest.mark.parametrize("Hq, Hkv, h", [(2, 1, 64), (4, 4, 80), (4, 1, 128), (2, 2, 256), (8, 1, 32), (6, 2, 96)])
+@pytest.mark.parametrize("window, sinks", [(0, 0), (100, 1)])
+def test_outputs_beside_a_dominant_key(Hq, Hkv, h, window, sinks):
+    n, scale = 600, 1 / math.sqrt(h)
+    q, k, v = dominated(n, Hq, Hkv, h, 15.0, h)
+    out, _ = R.rlgen_window_attention(q, k, v, i32([0, n]), n, window, sinks, scale)
+    check_out(q, k, v, 0, window, sinks, out)
+
+
+@pytest.mark.parametrize("Hq, Hkv, h", [(8, 2, 64), (4, 4, 80), (4, 1, 128), (2, 2, 256)])
+@pytest.mark.parametrize("window, sinks", [(0, 0), (300, 1)])
+@pytest.mark.parametrize("new", [1, 5, 200])
+def test_outputs_over_pages_beside_a_dominant_key(Hq, Hkv, h, window, sinks, new):
+    """Single tokens by the waves of several blocks and by one wave each, chunks whole and with their keys parted."""
+    n, P, scale = 900, 16, 1 / math.sqrt(h)
+    q, k, v = dominated(n, Hq, Hkv, h, 15.0, 100 + h)
+    need = -(-n // P)
+    ids = torch.randperm(need, generator=torch.Generator().manual_seed(h))
+    pages = torch.zeros(need, 2, Hkv, P, h, dtype=HF, device="cuda")
+    for e in range(need):
+        part = torch.stack([k[e * P:(e + 1) * P], v[e * P:(e + 1) * P]]).transpose(1, 2)
+        pages[int(ids[e]), :, :, :part.shape[2]] = part
+    for S in (1, 2048 // Hkv) if new == 1 else (1,):
+        table = ids.int().cuda().view(1, need).expand(S, need).contiguous()
+        qs = q[n - new:].repeat(S, 1, 1)
+        starts = torch.arange(S + 1, dtype=torch.int32, device="cuda") * new
+        for ws in (None, torch.empty(16, dtype=torch.uint8, device="cuda")) if new > 1 else (None,):
+            out, _ = R.rlgen_window_attention_paged(qs, pages, table, starts, i32([n] * S), new, n, window, sinks, scale, workspace=ws)
+            check_out(q[n - new:], k, v, n - new, window, sinks, out[-new:])
