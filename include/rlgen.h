@@ -49,7 +49,8 @@ extern "C" {
 
 #define RLGEN_DTYPE_F32   0  /* tensors supplied as fp32; rounded to bf16 (nearest even) on load */
 #define RLGEN_DTYPE_BF16  1  /* tensors supplied as bf16                                          */
-#define RLGEN_DTYPE_F16   2  /* tensors supplied as fp16 (the operators over pages and packed rows only) */
+#define RLGEN_DTYPE_F16   2  /* tensors supplied as fp16 (the operators over pages and packed rows, and the learner's, only) */
+#define RLGEN_DTYPE_E4M3  3  /* rlgen_add_rms_norm's output in 8 bits only: 4 exponent and 3 mantissa bits, largest value 448 */
 
 /* Threads: calls on one context must not overlap; different contexts may be used from different
  * threads.  The library reads no environment variables. */
@@ -409,6 +410,81 @@ int rlgen_window_attention_paged(const void *q, int64_t q_stride, int32_t dtype,
                                  int32_t table_stride, const int32_t *row_starts, const int32_t *total_lens, int32_t S,
                                  int32_t max_new, int32_t max_total, int32_t window, int32_t sinks, float scale, void *out,
                                  int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ------------------------------------------------------------------ the learner's rows: norm, log-probs, loss
+ *
+ * What a policy's learner runs between its matrix products, from the branch of a block to the gradient of the loss; the norm and the log-probs
+ * serve single tokens as well.  They need no context, keep nothing between calls, and have no sums whose order changes: the same call
+ * returns the same bits.  Statistics, sums, log-probs, losses and gains are fp32 or wider.
+ *
+ * Layouts
+ *  - Rows of the norm: width elements, a multiple of 8 up to 16384, any row stride (in elements) that is a multiple of 8 (fp32: 4), bases 16-byte
+ *    aligned.  fewer than 2^24 rows.
+ *  - Rows of logits: vocab elements, at most 2^24, any row stride and any base that suits the element type.
+ *  - Without rows (0) an operator returns at once, the gain's gradient is zeroed, and pointers to tensors of rows may be null. */
+
+/* h = residual + dropout(x) and y = RMS norm of h times the gain, in one pass.
+ *  x [rows, width] of type dtype (RLGEN_DTYPE_F32, _BF16 or _F16); residual nullable (h is then dropout(x)) and h nullable out, both of type
+ *  residual_dtype, F32 or dtype: the residual stream.
+ *  y nullable out (gain is then not read): of type dtype, or any of the three where dtype is F32, or RLGEN_DTYPE_E4M3 with scales [rows, groups] fp32: y's value is
+ *  scales[row, c / scale_group] times the element; scale_group 32, 64 or 128 columns to a scale (the last group may be shorter), or 0: one
+ *  for the row.  A scale is the group's largest magnitude / 448; a group below 2^-100 has scale 0 and zeros; NaN is kept and counts for no scale.
+ *  The norm is that of h before it is rounded to residual_dtype; mean square and eps as in sqrt(mean h^2 + eps).
+ * Dropout: an element is dropped with probability drop_p in [0, 1], rounded to a multiple of 2^-16, else multiplied by the inverse of the rest.
+ *  The mask is a function of rng, row and column alone and never stored: rng [2] int64 DEVICE holds a seed and an offset (read when the
+ *  launch runs, so that a captured call draws anew when the caller advances the offset); Philox4x32 of ten rounds with key = the seed's
+ *  words and counter = (column / 8, row, the offset's words) gives 16 bits for each of eight columns, the low half of a word first,
+ *  and an element is dropped if its bits are below 65536 drop_p.  rng may be null if drop_p is 0.
+ * h may be residual or x itself, y may be x itself (same type and stride); other overlaps are not allowed.
+ * Errors: NULL, BAD_ARG, DEVICE. */
+int rlgen_add_rms_norm(const void *x, int64_t x_stride, int32_t dtype, const void *residual, int64_t residual_stride,
+                       int32_t residual_dtype, int32_t rows, int32_t width, float drop_p, const int64_t *rng, const float *gain, float eps,
+                       void *h, int64_t h_stride, void *y, int64_t y_stride, int32_t y_dtype, float *scales, int32_t scale_group,
+                       void *hip_stream);
+
+/* Its gradients, from h as rlgen_add_rms_norm returned it, dy (type dtype) and dh (nullable, type residual_dtype: the gradient that reaches h past
+ * the norm): dresidual (nullable, residual_dtype) = the gradient of h, dx (nullable, dtype) = the same through the dropout (drop_p and rng as
+ * they were), dgain [width] fp32.  gain null: no norm was taken, dy and dgain are null too and h is not read.  dresidual may be dh itself, dx may be dy
+ * itself.  workspace: 16-byte aligned, rlgen_add_rms_norm_backward_workspace(rows, width) bytes (null without a gain).
+ * Errors: NULL, BAD_ARG, WORKSPACE, DEVICE. */
+size_t rlgen_add_rms_norm_backward_workspace(int32_t rows, int32_t width);
+int rlgen_add_rms_norm_backward(const void *h, int64_t h_stride, int32_t residual_dtype, const void *dy, int64_t dy_stride, int32_t dtype,
+                                const void *dh, int64_t dh_stride, int32_t rows, int32_t width, float drop_p, const int64_t *rng,
+                                const float *gain, float eps, void *dresidual, int64_t dresidual_stride, void *dx, int64_t dx_stride,
+                                float *dgain, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Of each row of logits [rows, vocab] (type dtype: RLGEN_DTYPE_F32, _BF16 or _F16), under softmax(z / temperature):
+ *  logprobs [rows]       log-prob of tokens[row]; tokens and logprobs are given both or neither
+ *  entropy [rows]        nullable: -sum p log p
+ *  stats [rows, 2]       the largest logit m, and log sum exp((z - m) / temperature): what the backward pass needs
+ *  top_tokens, top_logprobs [rows, n_top]   the n_top (0 to 64, at most vocab) likeliest tokens in descending order, of equal ones the lowest index first
+ * A row whose token lies outside [0, vocab) (padding, a prompt's rows) is not read: its log-prob, entropy and stats are 0, its alternatives -1 and
+ * -infinity.  Logits of -infinity or of the type's lowest value are masked: they count 0.  A row of -infinity alone has log-prob -infinity,
+ * entropy 0, stats (-infinity, -infinity), and alternatives at -infinity.  A NaN or +infinity makes the row's numbers NaN; among the
+ * alternatives NaN counts as the largest.  temperature is finite and at least 1e-6.  Errors: NULL, BAD_ARG, DEVICE. */
+int rlgen_token_logprobs(const void *logits, int64_t stride, int32_t dtype, int32_t rows, int32_t vocab, const int32_t *tokens,
+                         float temperature, float *logprobs, float *stats, float *entropy, int32_t n_top, int32_t *top_tokens,
+                         float *top_logprobs, void *hip_stream);
+
+/* The gradient of logprobs and entropy to the logits: dlogits [rows, vocab] of type dtype, every element written, zeros in rows that were not read
+ * or are masked as a whole.  dlogprobs, dentropy [rows]: at least one of them; with dlogprobs tokens, with dentropy the forward pass's entropy.
+ * tokens null: no row is left out.  dlogits may be logits itself (same stride); other overlaps are not allowed.
+ * A launch has fewer than 2^24 blocks: rows times vocab / 8192 (fp32: 4096), rounded up.  Errors: NULL, BAD_ARG, DEVICE. */
+int rlgen_token_logprobs_backward(const void *logits, int64_t stride, int32_t dtype, int32_t rows, int32_t vocab, const int32_t *tokens,
+                                  float temperature, const float *stats, const float *entropy, const float *dlogprobs, const float *dentropy,
+                                  void *dlogits, int64_t dlogits_stride, void *hip_stream);
+
+/* The DPO loss of packed sequences, and its gradient, in one launch: prompt b has the k sequences b k to b k + k - 1 of row_starts [B k + 1], and
+ * idx_pos, idx_neg [B] (rlgen_select_pairs's) say which of them are y+ and y-.  token_logprobs, ref_logprobs [rows] fp32: per row, 0 where it does not
+ * count (as rlgen_token_logprobs leaves rows without a token).
+ *  loss [B]          -log sigmoid(beta ((sum pol - sum ref over y+) - (sum pol - sum ref over y-)))
+ *  dlogprobs [rows]  the gradient of weight * sum of the losses to token_logprobs: one value on y+'s rows, its negative on y-'s, 0 on the other
+ *                    sequences'; rows that no sequence has are left as they are
+ * idx_pos[b] == idx_neg[b] is a pair without a difference: log 2 and zeros.  Indices and row starts outside their ranges are clamped.  Sums
+ * and the loss are formed in fp64.  All DEVICE.  Errors: NULL, BAD_ARG (B or k < 1, B >= 2^22, beta or weight not finite), DEVICE. */
+int rlgen_dpo_pairs(const float *token_logprobs, const float *ref_logprobs, int32_t rows, const int32_t *row_starts, int32_t B, int32_t k,
+                    const int32_t *idx_pos, const int32_t *idx_neg, float beta, float weight, float *loss, float *dlogprobs,
+                    void *hip_stream);
 
 const char *rlgen_strerror(int code);
 void rlgen_destroy(rlgen_ctx *ctx);

@@ -13,7 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librlgen.so")
 SOURCES = ["rlgen.hip", "gemm.hip", "attention.hip", "elementwise.hip", "sampler.hip", "operators.hip", "paged.hip", "window.hip",
-           "window_decode.hip", "window_backward.hip"]
+           "window_decode.hip", "window_backward.hip", "add_norm.hip", "token_logprobs.hip", "learner.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed-fp32 instruction selection is switched off on the test machines

@@ -1,0 +1,323 @@
+// Residual addition with dropout and a root-mean-square norm over rows, and its gradients.
+//   h = residual + m x,  y = h / sqrt(mean h^2 + eps) gain
+//   d = dh + r (t - h r^2 mean(t h)),  r = 1 / sqrt(mean h^2 + eps),  t = dy gain;   dresidual = d,  dx = m d,  dgain = sum over rows of dy h r
+// with m = 0 for a dropped element, else 65536 / (65536 - drop).
+#include "learner.h"
+#include "../../include/rlgen.h"
+
+namespace {
+
+// The dropout mask is never stored: both passes make it from (seed, offset, row, column) with Philox4x32 of ten rounds (Salmon, Moraes, Dror
+// and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011).  One call gives 128 bits, 16 for each of eight columns: key = the
+// seed's two words, counter = (column / 8, row, the offset's two words).  16 bits an element quantise the drop probability to 2^-16, and
+// the factor is the quantised one's, so the expectation is exact; 32 bits would take twice the multiplications.
+struct Bits { uint32_t w[4]; };
+__device__ __forceinline__ Bits philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1) {
+#pragma unroll
+  for (int i = 0; i < 10; ++i) {
+    const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+    c1 = (uint32_t)b;
+    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    c3 = (uint32_t)a;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return {{c0, c1, c2, c3}};
+}
+struct Generator {
+  uint32_t k0, k1, o0, o1;
+  __device__ __forceinline__ void begin(const unsigned long long* rng) {
+    k0 = (uint32_t)rng[0]; k1 = (uint32_t)(rng[0] >> 32);
+    o0 = (uint32_t)rng[1]; o1 = (uint32_t)(rng[1] >> 32);
+  }
+  // the eight elements' factors, applied
+  __device__ __forceinline__ void apply(float* x, int vec, int row, unsigned drop, float scale) const {
+    const Bits r = philox((uint32_t)vec, (uint32_t)row, o0, o1, k0, k1);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t bits = e & 1 ? r.w[e >> 1] >> 16 : r.w[e >> 1] & 0xffffu;
+      x[e] = bits >= drop ? x[e] * scale : 0.f;
+    }
+  }
+};
+
+// Sum or maximum over a row's waves: `slot` is the row's own part of LDS
+template <bool MAX> __device__ __forceinline__ float over_row(float v, float* slot, int wave, int waves) {
+  v = MAX ? wave_max(v) : wave_sum(v);
+  if (waves == 1) return v;
+  if ((threadIdx.x & 63) == 0) slot[wave] = v;
+  __syncthreads();
+  float t = slot[0];
+  for (int w = 1; w < waves; ++w) t = MAX ? fmaxf(t, slot[w]) : t + slot[w];
+  return t;
+}
+
+constexpr int MOST_WAVES = 8;
+
+// A row lies in the registers of `waves` waves: thread t of them holds its 16-byte pieces t, t + 64 waves, ...
+// LAST: what y is stored as.
+__device__ __forceinline__ uint32_t pack_e4m3x4(const float* y) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+}
+constexpr float E4M3_MAX = 448.f;
+// A scale below this has no reciprocal in 32 bits: such values count as zeros
+constexpr float E4M3_LEAST = 7.8886090522101181e-31f;       // 2^-100
+
+template <class TX, class TR, int NV>
+__global__ __launch_bounds__(512) void add_norm_kernel(AddNormArgs a, int waves) {
+  __shared__ float red[2][MOST_WAVES];
+  const int wave_all = threadIdx.x >> 6, wave = wave_all % waves, sub = wave_all / waves;
+  const int t = wave * 64 + (threadIdx.x & 63), step = waves * 64;
+  const int rows_here = blockDim.x / step;
+  const int row = blockIdx.x * rows_here + sub;
+  if (row >= a.rows) return;                   // only where a row has one wave: no barrier follows
+  const int n8 = a.width >> 3;
+  float h[NV][8];
+  {
+    Vec8<TX> x[NV];
+    Vec8<TR> r[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int v = t + i * step;
+      x[i] = v < n8 ? Vec8<TX>::load(a.x, row * a.x_stride + 8ll * v) : Vec8<TX>::zero();
+      r[i] = a.residual && v < n8 ? Vec8<TR>::load(a.residual, row * a.residual_stride + 8ll * v) : Vec8<TR>::zero();
+    }
+    Generator rng{};
+    if (a.drop) rng.begin(a.rng);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float y[8];
+      x[i].to(y);
+      r[i].to(h[i]);
+      if (a.drop) rng.apply(y, t + i * step, row, a.drop, a.keep_scale);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[i][e] += y[e];
+    }
+  }
+  if (a.h) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (t + i * step < n8) Vec8<TR>::store(a.h, row * a.h_stride + 8ll * (t + i * step), h[i]);
+  }
+  if (!a.gain) return;
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss = fmaf(h[i][e], h[i][e], ss);
+  ss = over_row<false>(ss, red[0] + sub * waves, wave, waves);
+  const float inv = 1.0f / sqrtf(ss / (float)a.width + a.eps);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int v = t + i * step;
+    if (v >= n8) continue;
+    const Vec8<TypeF32> g8 = Vec8<TypeF32>::load(a.gain, 8ll * v);
+    float g[8];
+    g8.to(g);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[i][e] = h[i][e] * inv * g[e];
+  }
+  if (a.y_dtype != RLGEN_DTYPE_E4M3) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int v = t + i * step;
+      if (v >= n8) continue;
+      const long long at = row * a.y_stride + 8ll * v;
+      if (a.y_dtype == RLGEN_DTYPE_BF16) Vec8<TypeBf16>::store(a.y, at, h[i]);
+      else if (a.y_dtype == RLGEN_DTYPE_F16) Vec8<TypeF16>::store(a.y, at, h[i]);
+      else Vec8<TypeF32>::store(a.y, at, h[i]);
+    }
+    return;
+  }
+  // 8 bits: scale = largest magnitude / 448, of the row or of scale_group columns (4, 8 or 16 lanes next to each other)
+  float most[NV], row_most = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    most[i] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most[i] = fmaxf(most[i], fabsf(h[i][e]));
+    row_most = fmaxf(row_most, most[i]);
+  }
+  if (a.scale_group == 0) {
+    row_most = over_row<true>(row_most, red[1] + sub * waves, wave, waves);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) most[i] = row_most;
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      for (int o = 1; o < a.scale_group / 8; o <<= 1) most[i] = fmaxf(most[i], __shfl_xor(most[i], o, WAVE));
+  }
+  const int groups = a.scale_group ? (a.width + a.scale_group - 1) / a.scale_group : 1;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int v = t + i * step;
+    if (v >= n8) continue;
+    const bool some = most[i] >= E4M3_LEAST;
+    const float f = some ? E4M3_MAX / most[i] : 0.f;
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = h[i][e] * f;
+    u32x2 w;
+    w[0] = pack_e4m3x4(y);
+    w[1] = pack_e4m3x4(y + 4);
+    *(u32x2*)((uint8_t*)a.y + row * a.y_stride + 8ll * v) = w;
+    const float scale = some ? most[i] / E4M3_MAX : 0.f;
+    if (a.scale_group == 0) {
+      if (v == 0) a.scales[row] = scale;
+    } else if (v % (a.scale_group / 8) == 0) {
+      a.scales[(long long)row * groups + v / (a.scale_group / 8)] = scale;
+    }
+  }
+}
+
+// The backward pass: a block walks rows in turn, its threads on the same columns throughout, so that the gain's gradient is summed in registers;
+// a second launch adds up the blocks in their order.
+template <class TX, class TR, int NV>
+__global__ __launch_bounds__(512) void add_norm_backward_kernel(AddNormArgs a, int waves) {
+  __shared__ float red[2][2][MOST_WAVES];
+  const int wave_all = threadIdx.x >> 6, wave = wave_all % waves, sub = wave_all / waves;
+  const int t = wave * 64 + (threadIdx.x & 63), step = waves * 64;
+  const int rows_here = blockDim.x / step;
+  const int n8 = a.width >> 3;
+  const float inv_width = 1.0f / (float)a.width;
+  Generator rng{};
+  if (a.drop) rng.begin(a.rng);
+  float gain[NV][8], sum[NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int v = t + i * step;
+    if (a.gain && v < n8) Vec8<TypeF32>::load(a.gain, 8ll * v).to(gain[i]);
+    else
+#pragma unroll
+      for (int e = 0; e < 8; ++e) gain[i][e] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[i][e] = 0.f;
+  }
+  int turn = 0;
+  for (int row = blockIdx.x * rows_here + sub; row < a.rows; row += gridDim.x * rows_here, turn ^= 1) {
+    float h[NV][8], dy[NV][8], d[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int v = t + i * step;
+      const bool on = v < n8;
+      (on && a.gain ? Vec8<TR>::load(a.h, row * a.h_stride + 8ll * v) : Vec8<TR>::zero()).to(h[i]);
+      (on && a.gain ? Vec8<TX>::load(a.dy, row * a.dy_stride + 8ll * v) : Vec8<TX>::zero()).to(dy[i]);
+      (on && a.dh ? Vec8<TR>::load(a.dh, row * a.dh_stride + 8ll * v) : Vec8<TR>::zero()).to(d[i]);
+    }
+    if (a.gain) {
+      float ss = 0.f, th = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          ss = fmaf(h[i][e], h[i][e], ss);
+          th = fmaf(dy[i][e] * gain[i][e], h[i][e], th);
+        }
+      ss = wave_sum(ss);
+      th = wave_sum(th);
+      if (waves > 1) {
+        if ((threadIdx.x & 63) == 0) { red[turn][0][wave] = ss; red[turn][1][wave] = th; }
+        __syncthreads();
+        ss = th = 0.f;
+        for (int w = 0; w < waves; ++w) { ss += red[turn][0][w]; th += red[turn][1][w]; }
+      }
+      const float inv = 1.0f / sqrtf(ss * inv_width + a.eps), back = inv * inv * (th * inv_width);
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          sum[i][e] = fmaf(dy[i][e], h[i][e] * inv, sum[i][e]);
+          d[i][e] = fmaf(inv, dy[i][e] * gain[i][e] - h[i][e] * back, d[i][e]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int v = t + i * step;
+      if (v >= n8) continue;
+      if (a.dres) Vec8<TR>::store(a.dres, row * a.dres_stride + 8ll * v, d[i]);
+      if (a.dx) {
+        if (a.drop) rng.apply(d[i], v, row, a.drop, a.keep_scale);
+        Vec8<TX>::store(a.dx, row * a.dx_stride + 8ll * v, d[i]);
+      }
+    }
+  }
+  if (!a.dgain) return;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int v = t + i * step;
+    if (v < n8) Vec8<TypeF32>::store(a.partial, ((long long)blockIdx.x * rows_here + sub) * a.width + 8ll * v, sum[i]);
+  }
+}
+
+// dgain over the parts: 32 columns to a block, 32 runs of parts at once and then the runs, in one order
+__global__ __launch_bounds__(1024) void gain_sum_kernel(const float* partial, int parts, int width, float* dgain) {
+  __shared__ float red[32][33];
+  const int col = threadIdx.x & 31, run = threadIdx.x >> 5, d = blockIdx.x * 32 + col;
+  float v = 0.f;
+  if (d < width)
+#pragma unroll 8
+    for (int p = run; p < parts; p += 32) v += partial[(long long)p * width + d];
+  red[run][col] = v;
+  __syncthreads();
+  if (run == 0 && d < width) {
+    for (int p = 1; p < 32; ++p) v += red[p][col];
+    dgain[d] = v;
+  }
+}
+
+struct Shape { int nv, waves, rows_here; };
+// by the width alone, so that a row's sums do not depend on how many rows there are
+Shape shape_of(int width) {
+  const int n8 = (width + 7) / 8;
+  Shape s;
+  s.nv = n8 <= 64 ? 1 : n8 <= 1024 ? 2 : 4;
+  s.waves = (n8 + 64 * s.nv - 1) / (64 * s.nv);
+  s.rows_here = s.waves == 1 ? 4 : 1;
+  return s;
+}
+int backward_blocks(int rows, const Shape& s) {
+  const int blocks = (rows + s.rows_here - 1) / s.rows_here;
+  return blocks < 1024 ? blocks : 1024;
+}
+
+template <class TX, class TR>
+hipError_t launch(const AddNormArgs& a, bool backward, hipStream_t s) {
+  const Shape f = shape_of(a.width);
+  const dim3 block(64 * f.waves * f.rows_here), grid(backward ? backward_blocks(a.rows, f) : (a.rows + f.rows_here - 1) / f.rows_here);
+#define ADD_NORM(NV) do { \
+    if (backward) hipLaunchKernelGGL((add_norm_backward_kernel<TX, TR, NV>), grid, block, 0, s, a, f.waves); \
+    else hipLaunchKernelGGL((add_norm_kernel<TX, TR, NV>), grid, block, 0, s, a, f.waves); } while (0)
+  if (f.nv == 1) ADD_NORM(1);
+  else if (f.nv == 2) ADD_NORM(2);
+  else ADD_NORM(4);
+#undef ADD_NORM
+  return hipGetLastError();
+}
+hipError_t by_type(const AddNormArgs& a, bool backward, hipStream_t s) {
+  switch (a.dtype) {
+    case RLGEN_DTYPE_F32: return launch<TypeF32, TypeF32>(a, backward, s);
+    case RLGEN_DTYPE_BF16: return a.res_dtype == RLGEN_DTYPE_F32 ? launch<TypeBf16, TypeF32>(a, backward, s) : launch<TypeBf16, TypeBf16>(a, backward, s);
+    case RLGEN_DTYPE_F16: return a.res_dtype == RLGEN_DTYPE_F32 ? launch<TypeF16, TypeF32>(a, backward, s) : launch<TypeF16, TypeF16>(a, backward, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace
+
+hipError_t rl_add_norm(const AddNormArgs& a, hipStream_t s) { return a.rows <= 0 ? hipSuccess : by_type(a, false, s); }
+size_t rl_add_norm_backward_bytes(int rows, int width) {
+  const Shape f = shape_of(width);
+  return (size_t)backward_blocks(rows < 1 ? 1 : rows, f) * f.rows_here * width * sizeof(float);
+}
+hipError_t rl_add_norm_backward(const AddNormArgs& a, hipStream_t s) {
+  const Shape f = shape_of(a.width);
+  const int blocks = a.rows > 0 ? backward_blocks(a.rows, f) : 0;
+  if (blocks > 0) {
+    const hipError_t e = by_type(a, true, s);
+    if (e != hipSuccess) return e;
+  }
+  if (a.dgain) hipLaunchKernelGGL(gain_sum_kernel, dim3((a.width + 31) / 32), dim3(1024), 0, s, a.partial, blocks * f.rows_here, a.width, a.dgain);
+  return hipGetLastError();
+}

@@ -1,0 +1,83 @@
+// What the norm with residual and dropout, the token log-probs and the pairs' loss share.  Internal to librlgen.so.
+#pragma once
+#include "window.h"
+
+// ------------------------------------------------------------------ launchers
+struct AddNormArgs {
+  int dtype, res_dtype, y_dtype;        // of x, dy and dx; of residual, h and their gradients; of y
+  int rows, width;
+  unsigned drop; float keep_scale;      // an element is dropped if its 16 random bits are below `drop`
+  const unsigned long long* rng;        // seed, offset
+  const float* gain; float eps;         // gain null: no norm
+  const void *x, *residual; long long x_stride, residual_stride;
+  void *h, *y; long long h_stride, y_stride;
+  float* scales; int scale_group;       // columns to a scale, 0: the whole row
+  // backward (h is an input there)
+  const void *dy, *dh; long long dy_stride, dh_stride;
+  void *dres, *dx; long long dres_stride, dx_stride;
+  float *dgain, *partial;
+};
+hipError_t rl_add_norm(const AddNormArgs& a, hipStream_t s);
+size_t rl_add_norm_backward_bytes(int rows, int width);
+hipError_t rl_add_norm_backward(const AddNormArgs& a, hipStream_t s);
+constexpr int MOST_WIDTH = 16384;
+
+struct LogprobArgs {
+  int dtype, rows, vocab;
+  const void* logits; long long stride;
+  const int* tokens; float temperature;
+  float *logprobs, *stats, *entropy;
+  int n_top; int* top_tokens; float* top_logprobs;
+  // backward
+  const float *g, *g_entropy;
+  void* dlogits; long long d_stride;
+};
+hipError_t rl_token_logprobs(const LogprobArgs& a, hipStream_t s);
+long long rl_token_logprobs_backward_blocks(const LogprobArgs& a);
+hipError_t rl_token_logprobs_backward(const LogprobArgs& a, hipStream_t s);
+constexpr int MOST_TOP = 64;
+
+struct PairArgs {
+  const float *pol, *ref; int rows;
+  const int* row_starts; int B, k;
+  const int *pos, *neg;
+  float beta, weight;
+  float *loss, *grad;
+};
+hipError_t rl_dpo_pairs(const PairArgs& a, hipStream_t s);
+
+// ------------------------------------------------------------------ element types
+struct TypeF32 {};
+// Eight elements of a row in registers, 16-byte accesses
+template <class T> struct Vec8 {
+  u32x4 w;
+  static __device__ __forceinline__ Vec8 load(const void* p, long long at) { return {*(const u32x4*)((const uint16_t*)p + at)}; }
+  static __device__ __forceinline__ Vec8 zero() { return {u32x4{0, 0, 0, 0}}; }
+  __device__ __forceinline__ void to(float* y) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { y[2 * e] = T::low(w[e]); y[2 * e + 1] = T::high(w[e]); }
+  }
+  static __device__ __forceinline__ void store(void* p, long long at, const float* y) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = T::pack(y[2 * e], y[2 * e + 1]);
+    *(u32x4*)((uint16_t*)p + at) = w;
+  }
+};
+template <> struct Vec8<TypeF32> {
+  f32x4 a, b;
+  static __device__ __forceinline__ Vec8 load(const void* p, long long at) {
+    const float* x = (const float*)p + at;
+    return {*(const f32x4*)x, *(const f32x4*)(x + 4)};
+  }
+  static __device__ __forceinline__ Vec8 zero() { return {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}}; }
+  __device__ __forceinline__ void to(float* y) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { y[e] = a[e]; y[4 + e] = b[e]; }
+  }
+  static __device__ __forceinline__ void store(void* p, long long at, const float* y) {
+    float* x = (float*)p + at;
+    *(f32x4*)x = f32x4{y[0], y[1], y[2], y[3]};
+    *(f32x4*)(x + 4) = f32x4{y[4], y[5], y[6], y[7]};
+  }
+};

@@ -22,7 +22,7 @@ lib = C.CDLL(LIB_PATH)
 OK = 0
 ERR_NULL, ERR_BAD_CFG, ERR_BAD_ARG, ERR_CAPACITY, ERR_WORKSPACE, ERR_UNIMPLEMENTED, ERR_DEVICE = -1, -2, -3, -4, -5, -6, -7
 ARCH_NEOX, ARCH_LLAMA = 0, 1
-DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
+DTYPE_F32, DTYPE_BF16, DTYPE_F16, DTYPE_E4M3 = 0, 1, 2, 3
 
 EXPORTS = ["rlgen_workspace_bytes", "rlgen_create", "rlgen_update_weights", "rlgen_generate", "rlgen_score",
            "rlgen_debug_logits", "rlgen_debug_sample", "rlgen_sample_static", "rlgen_sequence_logprob", "rlgen_dpo_loss", "rlgen_select_pairs", "rlgen_proximal_rloo",
@@ -31,7 +31,9 @@ EXPORTS = ["rlgen_workspace_bytes", "rlgen_create", "rlgen_update_weights", "rlg
            "rlgen_status_bits", "rlgen_strerror", "rlgen_destroy", "rlgen_plan_pages", "rlgen_rope_table", "rlgen_qk_norm_rope",
            "rlgen_qk_norm_rope_backward", "rlgen_qk_norm_rope_backward_workspace", "rlgen_window_attention",
            "rlgen_window_attention_backward", "rlgen_window_attention_backward_workspace", "rlgen_window_attention_paged",
-           "rlgen_window_attention_paged_workspace", "rlgen_window_attention_chunk_workspace"]
+           "rlgen_window_attention_paged_workspace", "rlgen_window_attention_chunk_workspace", "rlgen_add_rms_norm",
+           "rlgen_add_rms_norm_backward", "rlgen_add_rms_norm_backward_workspace", "rlgen_token_logprobs", "rlgen_token_logprobs_backward",
+           "rlgen_dpo_pairs"]
 FAULT_TOKEN, FAULT_UNIFORM, FAULT_GROUP, FAULT_RANGE = 1, 2, 4, 8
 PLAN_ROWS, PLAN_PAGES, PLAN_TABLE, PLAN_LENGTH = 1, 2, 4, 8
 
@@ -116,11 +118,16 @@ for _name, _types in {
         "rlgen_qk_norm_rope_backward": _NORM_ROPE + 4 * _ROWS + [_vp, _vp, _vp, _size, _vp],
         "rlgen_window_attention": 3 * _ROWS + [_i32] * 5 + [_vp] + [_i32] * 4 + [_f32] + _ROWS + [_vp, _vp],
         "rlgen_window_attention_backward": 4 * _ROWS + [_vp] + _ROWS + [_i32] * 5 + [_vp] + [_i32] * 4 + [_f32] + 3 * _ROWS + [_vp, _size, _vp],
-        "rlgen_window_attention_paged": _ROWS + [_i32] * 5 + [_vp, _i32, _i32, _vp, _i32, _vp, _vp] + [_i32] * 5 + [_f32] + _ROWS + [_vp, _vp, _size, _vp]}.items():
+        "rlgen_window_attention_paged": _ROWS + [_i32] * 5 + [_vp, _i32, _i32, _vp, _i32, _vp, _vp] + [_i32] * 5 + [_f32] + _ROWS + [_vp, _vp, _size, _vp],
+        "rlgen_add_rms_norm": _ROWS + [_i32] + _ROWS + [_i32] * 3 + [_f32, _vp, _vp, _f32] + 2 * _ROWS + [_i32, _vp, _i32, _vp],
+        "rlgen_add_rms_norm_backward": _ROWS + [_i32] + _ROWS + [_i32] + _ROWS + [_i32] * 2 + [_f32, _vp, _vp, _f32] + 2 * _ROWS + [_vp, _vp, _size, _vp],
+        "rlgen_token_logprobs": _ROWS + [_i32] * 3 + [_vp, _f32, _vp, _vp, _vp, _i32, _vp, _vp, _vp],
+        "rlgen_token_logprobs_backward": _ROWS + [_i32] * 3 + [_vp, _f32, _vp, _vp, _vp, _vp] + _ROWS + [_vp],
+        "rlgen_dpo_pairs": [_vp, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _f32, _f32, _vp, _vp, _vp]}.items():
     getattr(lib, _name).restype, getattr(lib, _name).argtypes = C.c_int, _types
 for _name, _count in {"rlgen_qk_norm_rope_backward_workspace": 2, "rlgen_window_attention_backward_workspace": 8,
                       "rlgen_window_attention_paged_workspace": 8,
-                      "rlgen_window_attention_chunk_workspace": 8}.items():
+                      "rlgen_window_attention_chunk_workspace": 8, "rlgen_add_rms_norm_backward_workspace": 2}.items():
     getattr(lib, _name).restype, getattr(lib, _name).argtypes = _size, [_i32] * _count
 lib.rlgen_destroy.restype = None
 lib.rlgen_destroy.argtypes = [_vp]
@@ -584,3 +591,142 @@ def rlgen_window_attention_paged(q, pages, page_table, row_starts, total_lens, m
                                             *_heads(o, dt), _floats(lse, rows * n_q), *_space(workspace), _stream()),
            "rlgen_window_attention_paged")
     return o, lse
+
+
+# ------------------------------------------------------------------ the learner's rows: norm, log-probs, loss
+# They stand outside autograd too.
+_E4M3 = torch.float8_e4m3fn
+_NORM_DTYPES = {**_DTYPES, _E4M3: DTYPE_E4M3}
+
+
+def _rows(t: Optional[torch.Tensor], dtype: torch.dtype, shape):
+    """[rows, width] with contiguous rows: (address, row stride)."""
+    if t is None:
+        return None, shape[1]
+    assert t.dtype is dtype and t.is_cuda and t.shape == shape and (t.stride(1) == 1 or shape[1] == 1)
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def _rng(t: Optional[torch.Tensor]):
+    if t is None:
+        return None
+    assert t.dtype is torch.int64 and t.is_cuda and t.shape == (2,) and t.is_contiguous()
+    return t.data_ptr()
+
+
+def rlgen_add_rms_norm(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float, residual: Optional[torch.Tensor] = None, drop_p: float = 0.0,
+                       rng: Optional[torch.Tensor] = None, h_dtype: Optional[torch.dtype] = None, y_dtype: Optional[torch.dtype] = None,
+                       scale_group: int = 0, out=None):
+    """h = residual + dropout(x) [rows, width] (residual's type; without a residual h_dtype, default x's) and y = its RMS norm times gain (fp32 [width]) of
+    y_dtype (default x's; torch.float8_e4m3fn: with scales, one for scale_group columns, 0: for the row).  Returns (h, y), or (h, y, scales) for 8
+    bits; gain None: y is None.  rng [2] int64: seed and offset.  `out`: what to write into, h or y None where it is not wanted.  Without
+    `out`, and with nothing to add, drop or round, h is x itself."""
+    shape = rows, width = x.shape
+    res = residual.dtype if residual is not None else x.dtype if h_dtype is None else h_dtype
+    if out is None:
+        same = residual is None and drop_p == 0 and res is x.dtype
+        h = None if same else torch.empty(shape, dtype=res, device=x.device)
+        y = None if gain is None else torch.empty(shape, dtype=x.dtype if y_dtype is None else y_dtype, device=x.device)
+        if same and y is None:
+            return x, None
+        out = (x if same else h, y)
+        if y is not None and y.dtype is _E4M3:
+            out += (torch.empty((rows, -(-width // scale_group) if scale_group > 0 else 1), dtype=_F32, device=x.device),)
+    else:
+        h, y = out[0], out[1]
+        if h is not None and residual is None:
+            res = h.dtype
+    eight = y is not None and y.dtype is _E4M3
+    scales = None
+    if eight:
+        assert len(out) == 3 and out[2].shape == (rows, -(-width // scale_group) if scale_group > 0 else 1)
+        scales = _floats(out[2], out[2].numel())
+    ydt = x.dtype if y is None else y.dtype
+    _check(lib.rlgen_add_rms_norm(*_rows(x, x.dtype, shape), _DTYPES[x.dtype], *_rows(residual, res, shape), _DTYPES[res], rows, width, drop_p, _rng(rng),
+                                  None if gain is None else _floats(gain, width), eps, *_rows(h, res, shape), *_rows(y, ydt, shape),
+                                  _NORM_DTYPES[ydt], scales, scale_group, _stream()), "rlgen_add_rms_norm")
+    return out
+
+
+def rlgen_add_rms_norm_backward(h: Optional[torch.Tensor], gain: Optional[torch.Tensor], eps: float, dy: Optional[torch.Tensor],
+                                dh: Optional[torch.Tensor] = None, drop_p: float = 0.0, rng: Optional[torch.Tensor] = None,
+                                dtype: Optional[torch.dtype] = None, out=None, workspace=None):
+    """From rlgen_add_rms_norm's h, dy (gradient of y) and dh (of h, or None): (dresidual like h, dx of x's type, dgain fp32 [width]).  x's type is
+    dy's, or `dtype` where there was no norm (gain, h and dy None; dgain is None then).  `out`: the three to write into, dresidual or dx None
+    where it is not wanted; without it, and with nothing dropped or rounded, dx is dresidual itself."""
+    like = h if h is not None else dh
+    shape = rows, width = like.shape
+    res = like.dtype
+    dt = dy.dtype if dy is not None else res if dtype is None else dtype
+    if out is None:
+        dres = torch.empty(shape, dtype=res, device=like.device)
+        dx = None if drop_p == 0 and dt is res else torch.empty(shape, dtype=dt, device=like.device)
+        dgain = None if gain is None else torch.empty(width, dtype=_F32, device=like.device)
+        out = (dres, dres if dx is None else dx, dgain)
+    else:
+        dres, dx, dgain = out
+    if gain is not None and workspace is None:
+        workspace = torch.empty(max(lib.rlgen_add_rms_norm_backward_workspace(rows, width), 16), dtype=torch.uint8, device=like.device)
+    _check(lib.rlgen_add_rms_norm_backward(*_rows(h, res, shape), _DTYPES[res], *_rows(dy, dt, shape), _DTYPES[dt], *_rows(dh, res, shape), rows, width,
+                                           drop_p, _rng(rng), None if gain is None else _floats(gain, width), eps, *_rows(dres, res, shape),
+                                           *_rows(dx, dt, shape), None if dgain is None else _floats(dgain, width), *_space(workspace), _stream()),
+           "rlgen_add_rms_norm_backward")
+    return out
+
+
+class TokenLogprobs(NamedTuple):
+    """What rlgen_token_logprobs fills: logprobs [rows], entropy [rows], stats [rows, 2] fp32, top_tokens [rows, n] int32, top_logprobs
+    [rows, n] fp32; None where it was not asked for."""
+    logprobs: Optional[torch.Tensor]
+    entropy: Optional[torch.Tensor]
+    stats: torch.Tensor
+    top_tokens: Optional[torch.Tensor]
+    top_logprobs: Optional[torch.Tensor]
+
+
+def rlgen_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, temperature: float = 1.0, entropy: bool = True, n_top: int = 0,
+                         out=None) -> TokenLogprobs:
+    """logits [rows, vocab] (fp32, bf16 or fp16; any row stride), tokens [rows] int32 or None.  A row whose token lies outside the vocabulary is skipped.
+    `out`: a TokenLogprobs (or tuple) of tensors to fill; entropy and n_top are then what it holds."""
+    shape = rows, vocab = logits.shape
+    if out is None:
+        new = dict(dtype=_F32, device=logits.device)
+        out = TokenLogprobs(None if tokens is None else torch.empty(rows, **new), torch.empty(rows, **new) if entropy else None,
+                            torch.empty((rows, 2), **new), torch.empty((rows, n_top), dtype=_I32, device=logits.device) if n_top else None,
+                            torch.empty((rows, n_top), **new) if n_top else None)
+    lp, ent, stats, ids, top = out
+    n_top = 0 if ids is None else ids.shape[1]
+    assert stats.shape == (rows, 2) and (top is None) == (ids is None) and (top is None or top.shape == (rows, n_top))
+    _check(lib.rlgen_token_logprobs(*_rows(logits, logits.dtype, shape), _DTYPES[logits.dtype], rows, vocab, None if tokens is None else _ints(tokens, rows),
+                                    temperature, None if lp is None else _floats(lp, rows), _floats(stats, 2 * rows),
+                                    None if ent is None else _floats(ent, rows), n_top, None if ids is None else _ints(ids, rows, n_top),
+                                    None if top is None else _floats(top, rows * n_top), _stream()), "rlgen_token_logprobs")
+    return out if type(out) is TokenLogprobs else TokenLogprobs(lp, ent, stats, ids, top)
+
+
+def rlgen_token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.Tensor], temperature: float, stats: torch.Tensor,
+                                  dlogprobs: Optional[torch.Tensor], entropy: Optional[torch.Tensor] = None, dentropy: Optional[torch.Tensor] = None,
+                                  out=None):
+    """From rlgen_token_logprobs's inputs, its stats (and entropy, with dentropy) and the gradients [rows] of logprobs and entropy: dlogits like
+    logits.  `out` may be logits itself."""
+    shape = rows, vocab = logits.shape
+    if out is None:
+        out = torch.empty(shape, dtype=logits.dtype, device=logits.device)
+    assert stats.shape == (rows, 2)
+    _check(lib.rlgen_token_logprobs_backward(*_rows(logits, logits.dtype, shape), _DTYPES[logits.dtype], rows, vocab,
+                                             None if tokens is None else _ints(tokens, rows), temperature, _floats(stats, 2 * rows),
+                                             None if entropy is None else _floats(entropy, rows), None if dlogprobs is None else _floats(dlogprobs, rows),
+                                             None if dentropy is None else _floats(dentropy, rows), *_rows(out, logits.dtype, shape), _stream()),
+           "rlgen_token_logprobs_backward")
+    return out
+
+
+def rlgen_dpo_pairs(token_logprobs: torch.Tensor, ref_logprobs: torch.Tensor, row_starts: torch.Tensor, idx_pos: torch.Tensor, idx_neg: torch.Tensor,
+                    k: int, beta: float, weight: float = 1.0, out=None):
+    """token_logprobs, ref_logprobs [rows] fp32 of packed sequences, row_starts [B k + 1], idx_pos and idx_neg [B] int32.  Returns (loss [B], the gradient
+    of weight times the losses' sum to token_logprobs [rows]); `out`: the two to write into.  Rows that no sequence has are not written."""
+    rows, B = token_logprobs.numel(), idx_pos.numel()
+    loss, grad = out if out is not None else (token_logprobs.new_empty(B), torch.empty_like(token_logprobs))
+    _check(lib.rlgen_dpo_pairs(_floats(token_logprobs, rows), _floats(ref_logprobs, rows), rows, _ints(row_starts, B * k + 1), B, k, _ints(idx_pos, B),
+                               _ints(idx_neg, B), beta, weight, _floats(loss, B), _floats(grad, rows), _stream()), "rlgen_dpo_pairs")
+    return loss, grad

@@ -1,0 +1,280 @@
+"""Residual addition with dropout and the root-mean-square norm, and their gradients, against the 64-bit forms.  Bounds: one rounding to the
+output's type (half a step) and those of the 32-bit sums, of which a row of 16384 has at most 16384 / 512 + 6 + 8 behind each other, 60 with the
+few operations around them; U is half a step of 32 bits."""
+import pytest
+import torch
+
+import learner_reference as L
+
+R = pytest.importorskip("paper_2410_18252_amd.rlgen", reason="librlgen.so not built")
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+F32, BF, F16, E4M3 = torch.float32, torch.bfloat16, torch.float16, torch.float8_e4m3fn
+EPS = 1e-5
+
+
+def half(t):
+    """Half a step of a type, and half of its smallest number (where numbers are subnormal)."""
+    return torch.finfo(t).eps / 2, torch.finfo(t).smallest_normal * torch.finfo(t).eps / 2
+
+
+def rand(seed, *shape, scale=1.0, dtype=F32):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).to(dtype)
+
+
+def strided(t, pad):
+    """The same rows with `pad` elements between them, and what surrounds them."""
+    if t is None or pad == 0:
+        return t.cuda() if t is not None else None
+    big = torch.full((t.shape[0], t.shape[1] + pad), 7.0, dtype=torch.float32).to(t.dtype).cuda()
+    big[:, :t.shape[1]] = t.cuda()
+    return big[:, :t.shape[1]]
+
+
+def rng_of(seed, offset):
+    return torch.tensor([seed, offset], dtype=torch.int64, device="cuda")
+
+
+def close(got, want, bound, what):
+    got, want = got.double().cpu(), want.double()
+    off = (got - want).abs()
+    assert torch.isfinite(got).all() and bool((off <= bound).all()), (what, float((off / bound.clamp(min=1e-300)).max()))
+
+
+def check_forward(rows, width, dt, res, drop, with_residual=True, y_dtype=None, group=0, pad=0, seed=0, offset=3 << 33, scale=1.0):
+    x, r = rand(seed + 1, rows, width, dtype=dt, scale=scale), rand(seed + 2, rows, width, scale=2.0 * scale, dtype=res) if with_residual else None
+    gain = 1 + 0.2 * rand(seed + 3, width)
+    y_dtype = dt if y_dtype is None else y_dtype
+    h, y = strided(torch.zeros(rows, width, dtype=res), pad), strided(torch.zeros(rows, width).to(y_dtype), pad)
+    out = (h, y)
+    if y_dtype is E4M3:
+        out += (torch.zeros(rows, -(-width // group) if group else 1, device="cuda"),)
+    got = R.rlgen_add_rms_norm(strided(x, pad), gain.cuda(), EPS, residual=strided(r, pad), drop_p=drop, rng=rng_of(seed * 999 - 7, offset) if drop else None,
+                               scale_group=group, out=out)
+    f = L.keep_factors(rows, width, drop, seed * 999 - 7, offset) if drop else torch.ones(rows, width, dtype=torch.float64)
+    want_h, want_y, inv = L.add_norm(x, r, f, gain, EPS)
+    parts = (x.double() * f).abs() + (0 if r is None else r.double().abs())       # what h is added up from
+    e, tiny = half(res)
+    close(got[0], want_h, e * want_h.abs() + 3 * U * parts + tiny, "h")
+    slop = 60 * U * want_y.abs() + 3 * U * parts * inv * gain.double().abs()
+    if y_dtype is not E4M3:
+        e, tiny = half(y_dtype)
+        close(got[1], want_y, e * (1 + 60 * U) * want_y.abs() + slop + tiny, "y")
+        return
+    n = group or width
+    for a in range(0, width, n):
+        part, scale = want_y[:, a:a + n], got[2][:, a // n].double().cpu()[:, None]
+        want_scale = part.abs().max(-1, keepdim=True).values / 448
+        close(scale, want_scale, want_scale * 64 * U + slop[:, a:a + n].max(-1, keepdim=True).values / 448, "scale")
+        # steps of 2^-3 of a value, of 2^-9 below 2^-6, in units of the scale
+        q = got[1][:, a:a + n].double().cpu()
+        v = part / scale.clamp(min=1e-300)
+        close(q, v, 2.0 ** -4 * v.abs() * (1 + 64 * U) + 2.0 ** -10 + slop[:, a:a + n] / scale.clamp(min=1e-300), "e4m3")
+        assert (q.abs() <= 448).all()
+
+
+TYPES = [(BF, BF), (BF, F32), (F16, F16), (F16, F32), (F32, F32)]
+
+
+@pytest.mark.parametrize("dt, res", TYPES)
+@pytest.mark.parametrize("width", [8, 72, 512, 520, 2560, 4096, 8192, 8200, 16384])
+def test_forward(dt, res, width):
+    for rows, drop, with_residual, pad in ((1, 0.0, True, 0), (3, 0.3, True, 8), (6, 0.1, False, 0)):
+        check_forward(rows, width, dt, res, drop, with_residual, pad=pad, seed=width + rows)
+
+
+@pytest.mark.parametrize("dt, res", TYPES)
+@pytest.mark.parametrize("width, group", [(8, 0), (8, 32), (200, 0), (200, 64), (1024, 128), (2568, 32), (4096, 0), (4104, 128), (16384, 0), (16384, 64)])
+def test_eight_bits(dt, res, width, group):
+    check_forward(5, width, dt, res, 0.1 if group == 64 else 0.0, y_dtype=E4M3, group=group, pad=16 if group == 32 else 0, seed=width + group)
+
+
+@pytest.mark.parametrize("y", [BF, F16, F32])
+def test_output_types_of_32_bit_rows(y):
+    check_forward(4, 1000, F32, F32, 0.0, False, y_dtype=y)
+
+
+def test_many_rows():
+    check_forward(5001, 264, BF, BF, 0.25, seed=4)
+    check_forward(2000, 1288, F16, F32, 0.0, seed=5)
+
+
+def test_nothing_to_add_returns_the_rows_themselves():
+    x, gain = rand(1, 3, 64, dtype=BF).cuda(), torch.ones(64, device="cuda")
+    h, y = R.rlgen_add_rms_norm(x, gain, EPS)
+    assert h is x
+    h2, y2 = R.rlgen_add_rms_norm(x, gain, EPS, residual=torch.zeros_like(x))
+    assert torch.equal(y, y2) and torch.equal(h2, x)
+    assert R.rlgen_add_rms_norm(x, None, EPS) == (x, None)
+    h3, none = R.rlgen_add_rms_norm(x, None, EPS, residual=x)
+    assert none is None and torch.equal(h3, x + x)
+
+
+def test_in_place_is_the_same():
+    x, r, gain = rand(1, 33, 1032, dtype=BF).cuda(), rand(2, 33, 1032, dtype=BF).cuda(), 1 + rand(3, 1032).cuda() * 0.1
+    rng = rng_of(5, 6)
+    h, y = R.rlgen_add_rms_norm(x, gain, EPS, residual=r, drop_p=0.2, rng=rng)
+    x2, r2 = x.clone(), r.clone()
+    R.rlgen_add_rms_norm(x2, gain, EPS, residual=r2, drop_p=0.2, rng=rng, out=(r2, x2))
+    assert torch.equal(h, r2) and torch.equal(y, x2)
+    dy, dh = rand(4, 33, 1032, dtype=BF).cuda(), rand(5, 33, 1032, dtype=BF).cuda()
+    a = R.rlgen_add_rms_norm_backward(h, gain, EPS, dy, dh, 0.2, rng)
+    R.rlgen_add_rms_norm_backward(h, gain, EPS, dy, dh, 0.2, rng, out=(dh, dy, (g := torch.empty_like(gain))))
+    assert all(torch.equal(p, q) for p, q in zip(a, (dh, dy, g)))
+
+
+def check_backward(rows, width, dt, res, drop, with_dh=True, pad=0, seed=0, scale=1.0):
+    h, gain = rand(seed, rows, width, dtype=res, scale=scale), 1 + 0.2 * rand(seed + 1, width)
+    dy, dh = rand(seed + 2, rows, width, dtype=dt, scale=0.3), rand(seed + 3, rows, width, dtype=res, scale=0.3) if with_dh else None
+    out = (strided(torch.zeros(rows, width, dtype=res), pad), strided(torch.zeros(rows, width, dtype=dt), pad), torch.zeros(width, device="cuda"))
+    got = R.rlgen_add_rms_norm_backward(strided(h, pad), gain.cuda(), EPS, strided(dy, pad), strided(dh, pad), drop,
+                                        rng_of(seed + 11, -5) if drop else None, out=out)
+    f = L.keep_factors(rows, width, drop, seed + 11, -5) if drop else torch.ones(rows, width, dtype=torch.float64)
+    d, dx, dgain = L.add_norm_backward(h, gain, EPS, dy, dh, f)
+    inv = 1 / torch.sqrt((h.double() ** 2).mean(-1, keepdim=True) + EPS)
+    t = (dy.double() * gain.double()).abs()
+    # the terms of the sum, each with the errors of inv (30 U) and of the mean (60 U of the magnitudes it is made of)
+    parts = (0 if dh is None else dh.double().abs()) + inv * t + inv ** 3 * h.double().abs() * (t * h.double().abs()).mean(-1, keepdim=True)
+    for got_one, want, m, ty in ((got[0], d, 1.0, res), (got[1], dx, f, dt)):
+        e, tiny = half(ty)
+        close(got_one, want, e * (1 + 160 * U) * want.abs() + 160 * U * parts * m + tiny, "gradient")
+    # a column's sum: rows of one block behind each other, parts behind each other
+    terms = (dy.double() * h.double() * inv).abs().sum(0)
+    close(got[2], dgain, (40 + 60 + rows / 256 + 64) * U * terms, "gain")
+
+
+@pytest.mark.parametrize("dt, res", TYPES)
+@pytest.mark.parametrize("width", [8, 72, 512, 520, 2560, 4096, 8200, 16384])
+def test_backward(dt, res, width):
+    for rows, drop, with_dh, pad in ((1, 0.0, True, 0), (3, 0.3, True, 8), (7, 0.1, False, 0)):
+        check_backward(rows, width, dt, res, drop, with_dh, pad, seed=width + rows)
+
+
+def test_backward_of_many_rows():
+    check_backward(5003, 264, BF, BF, 0.25, seed=4)
+    check_backward(2049, 1288, F16, F32, 0.0, seed=5)
+    check_backward(1500, 4096, BF, BF, 0.1, seed=6)
+
+
+def test_without_a_norm():
+    rows, width = 37, 136
+    x, r = rand(1, rows, width, dtype=BF), rand(2, rows, width, dtype=F32)
+    rng, f = rng_of(77, 1), L.keep_factors(rows, width, 0.5, 77, 1)
+    h, y = R.rlgen_add_rms_norm(x.cuda(), None, 0.0, residual=r.cuda(), drop_p=0.5, rng=rng)
+    assert y is None and torch.equal(h.cpu(), (r.double() + x.double() * f).float())
+    d, dx, dgain = R.rlgen_add_rms_norm_backward(None, None, 0.0, None, dh=r.cuda(), drop_p=0.5, rng=rng, dtype=BF)
+    assert dgain is None and torch.equal(d.cpu(), r) and torch.equal(dx.cpu(), (r.double() * f).to(BF))
+
+
+def test_gradients_are_slopes():
+    """Central differences of the forward pass in 32 bits along random directions.  With steps of 2^-5 the cubic term stays below 1e-2 of
+    directions of unit size per element; the rounding of y, U |y|, enters over the step."""
+    rows, width, drop = 6, 256, 0.2
+    x, r, gain = rand(1, rows, width).cuda(), rand(2, rows, width).cuda(), 1 + 0.2 * rand(3, width).cuda()
+    wy, wh, rng = rand(4, rows, width).cuda(), rand(5, rows, width).cuda(), rng_of(1, 2)
+
+    def value(x, r, gain):
+        h, y = R.rlgen_add_rms_norm(x, gain, EPS, residual=r, drop_p=drop, rng=rng)
+        return float((h.double() * wh.double()).sum() + (y.double() * wy.double()).sum())
+
+    h, _ = R.rlgen_add_rms_norm(x, gain, EPS, residual=r, drop_p=drop, rng=rng)
+    dr, dx, dg = R.rlgen_add_rms_norm_backward(h, gain, EPS, wy, wh, drop, rng)
+    for i, grad in enumerate((dx, dr, dg)):
+        u = grad / grad.abs().max()
+        t = 2.0 ** -5
+        args = [x, r, gain]
+        up, down = list(args), list(args)
+        up[i], down[i] = args[i] + t * u, args[i] - t * u
+        slope, want = (value(*up) - value(*down)) / (2 * t), float((grad.double() * u.double()).sum())
+        assert abs(slope - want) <= 2e-3 * want, (i, slope, want)
+
+
+@pytest.mark.parametrize("drop", [0.0, 2.0 ** -17, 1.0 / 3, 0.9999, 1.0])
+def test_share_of_dropped_elements(drop):
+    rows, width = 4096, 512
+    x = torch.ones(rows, width, device="cuda")
+    h, _ = R.rlgen_add_rms_norm(x, None, 0.0, drop_p=drop, rng=rng_of(123456789123456789, 42))
+    t = int(drop * 65536 + 0.5)
+    n, p = rows * width, t / 65536
+    kept = int((h != 0).sum())
+    assert abs(kept - n * (1 - p)) <= 5 * (n * p * (1 - p)) ** 0.5
+    if kept:
+        assert float(h.max()) == float(torch.tensor(65536 / (65536 - t), dtype=F32)) and float(h[h != 0].min()) == float(h.max())
+    # neighbours in rows and columns are independent: pairs dropped together
+    z = (h == 0).double()
+    for a, b in ((z[1:], z[:-1]), (z[:, 1:], z[:, :-1])):
+        both, m = float((a * b).sum()), a.numel()
+        assert abs(both - m * p * p) <= 6 * (m * p * p * (1 - p * p)) ** 0.5 + 1e-9
+
+
+def test_the_mask_depends_on_seed_offset_row_and_column_alone():
+    x = torch.ones(40, 264, device="cuda")
+    h, _ = R.rlgen_add_rms_norm(x, None, 0.0, drop_p=0.5, rng=rng_of(1, 2))
+    few, _ = R.rlgen_add_rms_norm(x[:7], None, 0.0, drop_p=0.5, rng=rng_of(1, 2))
+    narrow, _ = R.rlgen_add_rms_norm(x[:, :128], torch.ones(128, device="cuda"), EPS, drop_p=0.5, rng=rng_of(1, 2))
+    assert torch.equal(h[:7], few) and torch.equal(h[:, :128], narrow)
+    for seed, offset in ((2, 2), (1, 3), (1 + (1 << 40), 2), (1, 2 + (1 << 40))):
+        other, _ = R.rlgen_add_rms_norm(x, None, 0.0, drop_p=0.5, rng=rng_of(seed, offset))
+        assert 0.4 < float((other != h).double().mean()) < 0.6
+
+
+def test_zeros_infinities_and_nan_stay_in_their_rows():
+    x = rand(1, 6, 512, dtype=BF).cuda()
+    clean = R.rlgen_add_rms_norm(x, torch.ones(512, device="cuda"), EPS)[1]
+    x[1], x[3, 5], x[4, 500] = 0, float("nan"), float("inf")
+    y = R.rlgen_add_rms_norm(x, torch.ones(512, device="cuda"), EPS)[1]
+    assert torch.equal(y[[0, 2, 5]], clean[[0, 2, 5]]) and (y[1] == 0).all()
+    assert torch.isnan(y[3]).all() and torch.isnan(y[4, 500]) and (y[4, :500] == 0).all()
+    _, q, s = R.rlgen_add_rms_norm(x, torch.ones(512, device="cuda"), EPS, y_dtype=E4M3, scale_group=128)
+    assert (q[1].float() == 0).all() and (s[1] == 0).all() and torch.isnan(q[3].float()).all() and torch.isfinite(s[[0, 2, 5]]).all()
+    # eps = 0 and a row of zeros: 0 / 0
+    assert torch.isnan(R.rlgen_add_rms_norm(torch.zeros(1, 8, device="cuda"), torch.ones(8, device="cuda"), 0.0)[1]).all()
+
+
+def test_values_around_rows_are_left_alone():
+    x, gain = rand(1, 9, 104, dtype=BF), torch.ones(104, device="cuda")
+    h, y = strided(torch.zeros(9, 104, dtype=BF), 24), strided(torch.zeros(9, 104, dtype=BF), 24)
+    R.rlgen_add_rms_norm(strided(x, 24), gain, EPS, residual=strided(x, 8), out=(h, y))
+    R.rlgen_add_rms_norm_backward(h, gain, EPS, y, out=(h, y, torch.empty_like(gain)))
+    for t in (h, y):
+        assert (t._base[:, 104:] == 7).all()
+
+
+def test_no_rows():
+    gain = torch.ones(64, device="cuda")
+    x = torch.empty(0, 64, device="cuda", dtype=BF)
+    h, y, s = R.rlgen_add_rms_norm(x, gain, EPS, residual=x, y_dtype=E4M3)
+    assert h.shape == y.shape == (0, 64) and s.shape == (0, 1)
+    assert (R.rlgen_add_rms_norm_backward(x, gain, EPS, x, out=(x, x, torch.full_like(gain, 5)))[2] == 0).all()
+
+
+def test_replays_of_a_graph_draw_anew_when_the_offset_moves():
+    x, gain, rng = rand(1, 70, 512, dtype=BF).cuda(), torch.ones(512, device="cuda"), rng_of(9, 0)
+    r = torch.zeros_like(x)
+    out = torch.empty_like(x), torch.empty_like(x)
+    grads = torch.empty_like(x), torch.empty_like(x), torch.empty_like(gain)
+    ws = torch.empty(R.lib.rlgen_add_rms_norm_backward_workspace(70, 512), dtype=torch.uint8, device="cuda")
+
+    def step():
+        R.rlgen_add_rms_norm(x, gain, EPS, residual=r, drop_p=0.3, rng=rng, out=out)
+        R.rlgen_add_rms_norm_backward(out[0], gain, EPS, out[1], drop_p=0.3, rng=rng, out=grads, workspace=ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    seen = []
+    for i in range(4):
+        rng[1] = i
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (*out, *grads)]
+        step()
+        assert all(torch.equal(a, b) for a, b in zip(got, (*out, *grads)))
+        seen.append(got[0])
+    assert not torch.equal(seen[0], seen[1]) and not torch.equal(seen[2], seen[3])

@@ -1,0 +1,293 @@
+"""Token log-probs, entropy, alternatives and their gradient against the 64-bit forms.  U is half a step of 32 bits; a lane adds V / 256 terms behind each
+other at most, 64 more with what follows, and a term's exponent is off by 4 U of its size."""
+import pytest
+import torch
+
+import learner_reference as L
+
+R = pytest.importorskip("paper_2410_18252_amd.rlgen", reason="librlgen.so not built")
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+F32, BF, F16 = torch.float32, torch.bfloat16, torch.float16
+INF = float("inf")
+
+
+def rand(seed, *shape, scale=2.0, dtype=F32):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).to(dtype)
+
+
+def placed(t, pad=0, shift=0):
+    """The same rows on the GPU, `pad` elements apart, from element `shift` of a buffer on."""
+    rows, V = t.shape
+    flat = torch.full((shift + rows * (V + pad) + 16,), 99.0).to(t.dtype).cuda()
+    out = flat.as_strided((rows, V), (V + pad, 1), shift)
+    out.copy_(t.cuda())
+    return out
+
+
+def tokens_of(seed, rows, V, skip=True):
+    g = torch.Generator().manual_seed(seed)
+    t = torch.randint(0, V, (rows,), generator=g)
+    if skip:
+        t[1::4] = torch.tensor([-1, V, -2 ** 31, 2 ** 31 - 1])[torch.arange(len(t[1::4])) % 4]
+    return t
+
+
+def check(z, tokens, T, n, pad=0, shift=0):
+    rows, V = z.shape
+    tok = None if tokens is None else tokens.to(torch.int32).cuda()
+    got = R.rlgen_token_logprobs(placed(z, pad, shift), tok, T, n_top=n)
+    lp, H, m, ls = L.logprobs(z, T)
+    live = torch.ones(rows, dtype=torch.bool) if tokens is None else (tokens >= 0) & (tokens < V)
+    x = torch.where(torch.isinf(lp), torch.zeros_like(lp), lp + ls[:, None]).abs()
+    p = torch.exp(lp)
+    mean = (p * x).sum(-1)                                       # mean size of an exponent
+    e = (V / 256 + 64) * U * (1 + 4 * mean)                       # of the log of the sum
+    for name, a, b in (("stats", got.stats[:, 1], ls), ("entropy", got.entropy, H)):
+        bound = e * (1 if name == "stats" else 4) + 4 * U * ls.abs()
+        off = torch.where(a.double().cpu() == b, torch.zeros_like(b), (a.double().cpu() - b).abs())       # (both may be -infinity)
+        assert bool((off <= bound)[live].all()), (name, float((off / bound)[live].max()))
+        assert (a.cpu()[~live] == 0).all()
+    assert torch.equal(got.stats[:, 0].cpu()[live], m.float()[live]) and (got.stats[:, 0].cpu()[~live] == 0).all()
+    if tokens is not None:
+        want = lp[torch.arange(rows), tokens.clamp(0, V - 1).long()].float().double()       # (what 32 bits do not hold is infinite)
+        off = (got.logprobs.double().cpu() - want).abs()
+        fine = live & torch.isfinite(want)
+        assert bool((off <= e + 8 * U * (want.abs() + ls.abs()))[fine].all())
+        assert (got.logprobs.cpu()[live & ~torch.isfinite(want)] == -INF).all() and (got.logprobs.cpu()[~live] == 0).all()
+    if n:
+        ids = L.top(z, n)
+        assert torch.equal(got.top_tokens.cpu().long()[live], ids[live])
+        want = lp.gather(1, ids).float().double()
+        off = (got.top_logprobs.double().cpu() - want).abs()
+        bound = (e + 4 * U * ls.abs())[:, None] + 4 * U * want.abs()
+        fine = live[:, None] & torch.isfinite(want)
+        assert bool((off <= bound)[fine].all())
+        assert (got.top_logprobs.cpu()[live[:, None] & ~torch.isfinite(want)] == -INF).all()
+        assert (got.top_tokens.cpu()[~live] == -1).all() and (got.top_logprobs.cpu()[~live] == -INF).all()
+    else:
+        assert got.top_tokens is None and got.top_logprobs is None
+    return got
+
+
+@pytest.mark.parametrize("dtype", [F32, BF, F16])
+@pytest.mark.parametrize("V", [1, 2, 5, 7, 8, 9, 63, 257, 1024, 8191, 8209, 50304])
+def test_forward(dtype, V):
+    rows = 9 if V < 50000 else 5
+    for T, pad, shift, n in ((0.7, 0, 0, min(V, 5)), (1.0, 3, 1, 0), (2.0, 1, 5, min(V, 64))):
+        check(rand(V, rows, V, dtype=dtype), tokens_of(V + 1, rows, V), T, n, pad, shift)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_many_rows(dtype):
+    """Over 256 rows a block has fewer threads."""
+    check(rand(1, 300, 9001, dtype=dtype), tokens_of(2, 300, 9001), 0.7, 20)
+    check(rand(3, 257, 130, dtype=dtype), None, 1.0, 64, 1, 3)
+
+
+def test_rows_and_blocks_of_both_sizes_agree():
+    z = rand(5, 300, 5000, dtype=BF).cuda()
+    a, b = R.rlgen_token_logprobs(z, n_top=8), R.rlgen_token_logprobs(z[:100], n_top=8)
+    assert torch.equal(a.top_tokens[:100], b.top_tokens)
+    assert (a.entropy[:100] - b.entropy).abs().max() <= 2 * (5000 / 256 + 64) * U * 4 * 40
+
+
+def test_alternatives_where_values_are_equal_or_crowded():
+    """Few different values, one value, a rising and a falling row, all large values at one thread's places."""
+    V = 40000
+    z = torch.zeros(8, V)
+    z[1] = torch.arange(V) % 7
+    z[2], z[3] = torch.arange(V) / 1000.0, -torch.arange(V) / 1000.0
+    z[4, ::1024] = 5
+    z[5, 8 * 1024 * 2:8 * 1024 * 2 + 8] = 3
+    z[6] = rand(1, V).round()
+    z[7, 11111] = -0.0
+    z[7, 5] = -0.0
+    for dtype in (F32, F16, BF):
+        for n in (1, 17, 64):
+            check(z.to(dtype), None, 1.0, n)
+    wide = torch.cat([z] * 40)
+    got = R.rlgen_token_logprobs(wide.bfloat16().cuda(), n_top=33)
+    assert torch.equal(got.top_tokens.cpu().long(), L.top(z.bfloat16(), 33).repeat(40, 1))
+
+
+@pytest.mark.parametrize("low", [-INF, None])
+@pytest.mark.parametrize("dtype", [F32, BF, F16])
+def test_masks(dtype, low):
+    """Few tokens allowed, one, none; masked with -infinity and with the type's lowest value."""
+    V, low = 30011, torch.finfo(dtype).min if low is None else low
+    z = rand(7, 6, V, dtype=dtype)
+    keep = torch.zeros(6, V, dtype=torch.bool)
+    keep[0, [5, 17, 29000]] = True
+    keep[1, 12345] = True
+    keep[2] = torch.rand(V, generator=torch.Generator().manual_seed(1)) < 0.5
+    keep[3, -1] = True
+    keep[5] = True
+    z = torch.where(keep, z, torch.full_like(z, low))
+    tok = torch.tensor([17, 3, 8, V - 1, 8, 8])
+    for n in (0, 5, 64):
+        got = check(z, tok, 0.7, n, pad=1)
+        assert float(got.entropy[1]) == 0 and float(got.logprobs[3]) == 0
+        if low == -INF:
+            assert float(got.entropy[4]) == 0 and float(got.logprobs[4]) == -INF and got.stats[4].tolist() == [-INF, -INF]
+            assert n == 0 or got.top_tokens[4].tolist() == list(range(n))
+    g, ge = rand(8, 6, scale=1.0), rand(9, 6, scale=1.0)
+    d = R.rlgen_token_logprobs_backward(placed(z, 1), tok.int().cuda(), 0.7, got.stats, g.cuda(), got.entropy, ge.cuda())
+    assert torch.isfinite(d).all() and (low != -INF or (d[4] == 0).all()) and (d.cpu()[:4][(~keep[:4]) & (torch.arange(V) != tok[:4, None])] == 0).all()
+
+
+def test_nan_and_infinity_stay_in_their_rows():
+    V = 3001
+    z = rand(1, 6, V)
+    clean = R.rlgen_token_logprobs(z.cuda(), torch.full((6,), 7, dtype=torch.int32, device="cuda"), n_top=4)
+    z[1, 100], z[3, 2], z[4, 3000] = float("nan"), INF, -float("nan")
+    got = R.rlgen_token_logprobs(z.cuda(), torch.full((6,), 7, dtype=torch.int32, device="cuda"), n_top=4)
+    keep = [0, 2, 5]
+    for a, b in zip(clean, got):
+        assert torch.equal(a[keep], b[keep])
+    assert torch.isnan(got.logprobs[[1, 4]]).all() and torch.isnan(got.entropy[[1, 3, 4]]).all()
+    assert torch.equal(got.top_tokens.cpu().long(), L.top(z, 4)) and got.top_tokens[[1, 3, 4], 0].tolist() == [100, 2, 3000]
+    d = R.rlgen_token_logprobs_backward(z.cuda(), torch.full((6,), 7, dtype=torch.int32, device="cuda"), 1.0, got.stats, torch.ones(6, device="cuda"))
+    assert torch.isfinite(d[keep]).all() and torch.isnan(d[[1, 3, 4]]).all()
+
+
+def test_temperatures():
+    z = rand(1, 4, 2000, scale=3.0)
+    for T in (1e-6, 1e-3, 50.0, 3e38):
+        check(z, tokens_of(2, 4, 2000, skip=False), T, 3)
+
+
+def test_values_far_from_zero():
+    """Logits near the type's ends: only their differences count."""
+    for dtype, at in ((F32, 3e4), (F32, -3e4), (F16, 6e4), (BF, 3e38), (BF, -3e38)):
+        z = (rand(1, 3, 500) + at).to(dtype)
+        check(z, tokens_of(2, 3, 500, skip=False), 1.0, 5)
+
+
+def check_backward(z, tokens, T, with_entropy, pad=0, shift=0, out_pad=0, out_shift=0, scale=1.0):
+    rows, V = z.shape
+    g, ge = rand(3, rows, scale=scale), rand(4, rows, scale=scale) if with_entropy else None
+    lp, H, m, ls = L.logprobs(z, T)
+    stats = torch.stack([m, ls], -1).float().cuda()
+    out = placed(torch.zeros(rows, V).to(z.dtype), out_pad, out_shift)
+    got = R.rlgen_token_logprobs_backward(placed(z, pad, shift), tokens.to(torch.int32).cuda(), T, stats, g.cuda(), H.float().cuda() if with_entropy else None,
+                                          ge.cuda() if with_entropy else None, out=out)
+    want = L.logprobs_backward(z, tokens, T, g, ge)
+    p, size = torch.exp(lp), g.double().abs()[:, None].expand(rows, V)
+    if with_entropy:
+        size = size + ge.double().abs()[:, None] * (lp.clamp(min=-1000).abs() + H[:, None])
+    x = (lp.clamp(min=-1000) + ls[:, None]).abs()
+    # p is off by the error of its exponent, the rest by a few roundings; the target's own g is added
+    off = p * size / T * U * (16 + 8 * (x + ls.abs()[:, None]))
+    at = torch.zeros(rows, V)
+    at[torch.arange(rows), tokens.clamp(0, V - 1).long()] = 1
+    off = off + at * 8 * U * g.double().abs()[:, None] / T
+    e, tiny = torch.finfo(z.dtype).eps / 2, torch.finfo(z.dtype).smallest_normal * torch.finfo(z.dtype).eps / 2
+    err = (got.double().cpu() - want).abs()
+    bound = e * (1 + 100 * U) * want.abs() + off + tiny
+    assert bool((err <= bound).all()), float((err / bound).max())
+    dead = (tokens < 0) | (tokens >= V)
+    assert (got.cpu()[dead] == 0).all()
+    flat = out.as_strided((out_shift + rows * (V + out_pad) + 16,), (1,), 0)
+    mask = torch.ones_like(flat, dtype=torch.bool)
+    mask.as_strided((rows, V), (V + out_pad, 1), out_shift).fill_(False)
+    assert (flat[mask].float() - torch.tensor(99.0).to(z.dtype).float().item()).abs().max() == 0
+    return got
+
+
+@pytest.mark.parametrize("dtype", [F32, BF, F16])
+@pytest.mark.parametrize("V", [1, 5, 8, 63, 1024, 8209, 50304])
+def test_backward(dtype, V):
+    z, tok = rand(V, 6, V, dtype=dtype), tokens_of(V + 1, 6, V)
+    check_backward(z, tok, 0.7, True)
+    check_backward(z, tok, 1.0, False, pad=3, shift=1, out_pad=3, out_shift=1)
+    check_backward(z, tok, 1.3, True, pad=2, shift=0, out_pad=1, out_shift=7)
+
+
+def test_backward_in_place():
+    z, tok = rand(1, 40, 5003, dtype=BF), tokens_of(2, 40, 5003)
+    got = check_backward(z, tok, 0.9, True)
+    _, H, m, ls = L.logprobs(z, 0.9)
+    here = z.cuda()
+    out = R.rlgen_token_logprobs_backward(here, tok.int().cuda(), 0.9, torch.stack([m, ls], -1).float().cuda(), rand(3, 40, scale=1.0).cuda(), H.float().cuda(),
+                                          rand(4, 40, scale=1.0).cuda(), out=here)
+    assert out is here and torch.equal(got, here)
+
+
+def test_entropys_gradient_alone():
+    z = rand(1, 5, 333)
+    _, H, m, ls = L.logprobs(z, 0.8)
+    ge = rand(2, 5, scale=1.0)
+    got = R.rlgen_token_logprobs_backward(z.cuda(), None, 0.8, torch.stack([m, ls], -1).float().cuda(), None, H.float().cuda(), ge.cuda())
+    want = L.logprobs_backward(z, None, 0.8, torch.zeros(5), ge)
+    assert float((got.double().cpu() - want).abs().max()) <= 400 * U
+
+
+def test_gradients_are_slopes():
+    """Central differences of the forward pass in 32 bits: steps of 2^-5 along the gradient leave a cubic term below 2e-3 and rounding of 64 U over
+    the step."""
+    z, tok = rand(1, 4, 200, scale=1.5).cuda(), tokens_of(2, 4, 200, skip=False).int().cuda()
+    g, ge, T = rand(3, 4, scale=1.0).cuda(), rand(4, 4, scale=1.0).cuda(), 0.7
+
+    def value(z):
+        r = R.rlgen_token_logprobs(z, tok, T)
+        return float((r.logprobs.double() * g.double()).sum() + (r.entropy.double() * ge.double()).sum())
+
+    r = R.rlgen_token_logprobs(z, tok, T)
+    d = R.rlgen_token_logprobs_backward(z, tok, T, r.stats, g, r.entropy, ge)
+    u, t = d / d.abs().max(), 2.0 ** -5
+    slope, want = (value(z + t * u) - value(z - t * u)) / (2 * t), float((d.double() * u.double()).sum())
+    assert abs(slope - want) <= 2e-3 * want + 64 * U * 40 / t, (slope, want)
+
+
+def test_large_offsets():
+    """Rows that lie beyond 2^31 elements of their buffer."""
+    V, far = 1000, (1 << 31) // 3 + 8
+    flat = torch.empty(4 * far, dtype=torch.bfloat16, device="cuda")
+    z = flat.as_strided((4, V), (far, 1))
+    rows = rand(1, 4, V, dtype=BF)
+    z.copy_(rows.cuda())
+    tok = tokens_of(2, 4, V, skip=False)
+    a, b = R.rlgen_token_logprobs(z, tok.int().cuda(), n_top=3), R.rlgen_token_logprobs(rows.cuda(), tok.int().cuda(), n_top=3)
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    g = torch.ones(4, device="cuda")
+    want = R.rlgen_token_logprobs_backward(rows.cuda(), tok.int().cuda(), 1.0, a.stats, g)
+    assert torch.equal(R.rlgen_token_logprobs_backward(z, tok.int().cuda(), 1.0, a.stats, g, out=z), want)
+
+
+def test_no_rows():
+    z = torch.empty(0, 50, device="cuda")
+    r = R.rlgen_token_logprobs(z, torch.empty(0, dtype=torch.int32, device="cuda"), n_top=3)
+    assert r.logprobs.shape == (0,) and r.top_tokens.shape == (0, 3)
+    e = torch.empty(0, device="cuda")
+    assert R.rlgen_token_logprobs_backward(z, torch.empty(0, dtype=torch.int32, device="cuda"), 1.0, r.stats, e).shape == (0, 50)
+
+
+def test_another_stream_and_replays_of_a_graph():
+    z, tok = rand(1, 30, 9000, dtype=BF).cuda(), tokens_of(2, 30, 9000).int().cuda()
+    g = rand(3, 30, scale=1.0).cuda()
+    want = R.rlgen_token_logprobs(z, tok, 0.7, n_top=6)
+    grad = R.rlgen_token_logprobs_backward(z, tok, 0.7, want.stats, g)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    out = R.TokenLogprobs(*[torch.zeros_like(t) for t in want])
+    d = torch.zeros_like(z)
+
+    def step():
+        R.rlgen_token_logprobs(z, tok, 0.7, out=out)
+        R.rlgen_token_logprobs_backward(z, tok, 0.7, out.stats, g, out=d)
+
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((*want, grad), (*out, d)))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        z.mul_(0.9)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = R.rlgen_token_logprobs(z, tok, 0.7, n_top=6)
+        assert all(torch.equal(a, b) for a, b in zip((*want, R.rlgen_token_logprobs_backward(z, tok, 0.7, want.stats, g)), (*out, d)))
