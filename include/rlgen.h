@@ -461,10 +461,13 @@ int rlgen_add_rms_norm_backward(const void *h, int64_t h_stride, int32_t residua
  * A row whose token lies outside [0, vocab) (padding, a prompt's rows) is not read: its log-prob, entropy and stats are 0, its alternatives -1 and
  * -infinity.  Logits of -infinity or of the type's lowest value are masked: they count 0.  A row of -infinity alone has log-prob -infinity,
  * entropy 0, stats (-infinity, -infinity), and alternatives at -infinity.  A NaN or +infinity makes the row's numbers NaN; among the
- * alternatives NaN counts as the largest.  temperature is finite and at least 1e-6.  Errors: NULL, BAD_ARG, DEVICE. */
+ * alternatives NaN counts as the largest.  temperature is finite and at least 1e-6.
+ * workspace: 16-byte aligned, rlgen_token_logprobs_workspace(...) bytes (0, and workspace may be null, unless few rows are parted over many
+ * blocks).  Errors: NULL, BAD_ARG, WORKSPACE, DEVICE. */
+size_t rlgen_token_logprobs_workspace(int32_t dtype, int32_t rows, int32_t vocab, int32_t n_top);
 int rlgen_token_logprobs(const void *logits, int64_t stride, int32_t dtype, int32_t rows, int32_t vocab, const int32_t *tokens,
                          float temperature, float *logprobs, float *stats, float *entropy, int32_t n_top, int32_t *top_tokens,
-                         float *top_logprobs, void *hip_stream);
+                         float *top_logprobs, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* The gradient of logprobs and entropy to the logits: dlogits [rows, vocab] of type dtype, every element written, zeros in rows that were not read
  * or are masked as a whole.  dlogprobs, dentropy [rows]: at least one of them; with dlogprobs tokens, with dentropy the forward pass's entropy.

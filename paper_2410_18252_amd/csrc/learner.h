@@ -28,11 +28,13 @@ struct LogprobArgs {
   const int* tokens; float temperature;
   float *logprobs, *stats, *entropy;
   int n_top; int* top_tokens; float* top_logprobs;
+  float4* partial; uint64_t* part_keys; // of rows that are parted: largest value and sums, and n_top keys, of each part
   // backward
   const float *g, *g_entropy;
   void* dlogits; long long d_stride;
 };
-hipError_t rl_token_logprobs(const LogprobArgs& a, hipStream_t s);
+size_t rl_token_logprobs_bytes(const LogprobArgs& a);
+hipError_t rl_token_logprobs(LogprobArgs a, void* workspace, hipStream_t s);
 long long rl_token_logprobs_backward_blocks(const LogprobArgs& a);
 hipError_t rl_token_logprobs_backward(const LogprobArgs& a, hipStream_t s);
 constexpr int MOST_TOP = 64;
@@ -45,6 +47,32 @@ struct PairArgs {
   float *loss, *grad;
 };
 hipError_t rl_dpo_pairs(const PairArgs& a, hipStream_t s);
+
+// ------------------------------------------------------------------ over a wave
+// Sum and largest value of a wave's lanes, in every lane: shifts within rows of 16 lanes, then from row to row, as operands of the additions
+// themselves (six shuffles through LDS take about ten times as long).  The order is fixed.  NaN passes through sums, not through maxima.
+template <int CTRL, int ROWS> __device__ __forceinline__ float moved(float v, float other) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, other), __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float last_lane(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63)); }
+__device__ __forceinline__ float lanes_sum(float v) {
+  v += moved<0x111, 0xf>(v, 0.f);       // from the lanes 1, 2, 4 and 8 before in a row
+  v += moved<0x112, 0xf>(v, 0.f);
+  v += moved<0x114, 0xf>(v, 0.f);
+  v += moved<0x118, 0xf>(v, 0.f);
+  v += moved<0x142, 0xa>(v, 0.f);       // a row's last lane to the next row, then the second row's to the last two
+  v += moved<0x143, 0xc>(v, 0.f);
+  return last_lane(v);
+}
+__device__ __forceinline__ float lanes_max(float v) {
+  v = fmaxf(v, moved<0x111, 0xf>(v, -INFINITY));
+  v = fmaxf(v, moved<0x112, 0xf>(v, -INFINITY));
+  v = fmaxf(v, moved<0x114, 0xf>(v, -INFINITY));
+  v = fmaxf(v, moved<0x118, 0xf>(v, -INFINITY));
+  v = fmaxf(v, moved<0x142, 0xa>(v, -INFINITY));
+  v = fmaxf(v, moved<0x143, 0xc>(v, -INFINITY));
+  return last_lane(v);
+}
 
 // ------------------------------------------------------------------ element types
 struct TypeF32 {};

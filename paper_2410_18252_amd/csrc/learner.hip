@@ -121,9 +121,15 @@ int rlgen_add_rms_norm_backward(const void* h, int64_t h_stride, int32_t residua
   return RLGEN_OK;
 }
 
+size_t rlgen_token_logprobs_workspace(int32_t dtype, int32_t rows, int32_t vocab, int32_t n_top) {
+  if (!type_ok(dtype) || rows < 0 || rows >= MOST_BLOCKS || vocab < 1 || vocab > MOST_VOCAB || n_top < 0 || n_top > MOST_TOP || n_top > vocab) return 0;
+  LogprobArgs a{};
+  a.dtype = dtype; a.rows = rows; a.vocab = vocab; a.n_top = n_top;
+  return rl_token_logprobs_bytes(a);
+}
 int rlgen_token_logprobs(const void* logits, int64_t stride, int32_t dtype, int32_t rows, int32_t vocab, const int32_t* tokens,
                          float temperature, float* logprobs, float* stats, float* entropy, int32_t n_top, int32_t* top_tokens,
-                         float* top_logprobs, void* hip_stream) {
+                         float* top_logprobs, void* workspace, size_t workspace_bytes, void* hip_stream) {
   if (rows > 0 && (!logits || !stats || (n_top > 0 && (!top_tokens || !top_logprobs)) || !tokens != !logprobs)) return RLGEN_ERR_NULL;
   if (rows < 0 || rows >= MOST_BLOCKS || vocab < 1 || vocab > MOST_VOCAB || n_top < 0 || n_top > MOST_TOP || n_top > vocab ||
       !logits_ok(logits, stride, vocab, dtype) || !temperature_ok(temperature))
@@ -131,7 +137,9 @@ int rlgen_token_logprobs(const void* logits, int64_t stride, int32_t dtype, int3
   LogprobArgs a{};
   a.dtype = dtype; a.rows = rows; a.vocab = vocab; a.logits = logits; a.stride = stride; a.tokens = tokens; a.temperature = temperature;
   a.logprobs = logprobs; a.stats = stats; a.entropy = entropy; a.n_top = n_top; a.top_tokens = top_tokens; a.top_logprobs = top_logprobs;
-  HIPCHK(rl_token_logprobs(a, (hipStream_t)hip_stream));
+  const size_t need = rl_token_logprobs_bytes(a);
+  if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return RLGEN_ERR_WORKSPACE;
+  HIPCHK(rl_token_logprobs(a, workspace, (hipStream_t)hip_stream));
   return RLGEN_OK;
 }
 

@@ -6,7 +6,7 @@
 
 namespace {
 
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LOWEST = -3.4028234663852886e38f;
 
 // 16 bytes of a row's logits
@@ -14,6 +14,11 @@ template <class E> struct Some {
   static constexpr int N = 8;
   u32x4 w;
   static __device__ __forceinline__ Some load(const void* row, long long at) { return {*(const u32x4*)((const uint16_t*)row + at)}; }
+  static __device__ __forceinline__ Some of(u32x4 w) { return {w}; }
+  static __device__ __forceinline__ Some masked() {
+    const uint32_t w = E::pack(-INFINITY, -INFINITY);
+    return {u32x4{w, w, w, w}};
+  }
   __device__ __forceinline__ float operator[](int e) const { return e & 1 ? E::high(w[e >> 1]) : E::low(w[e >> 1]); }
   static __device__ __forceinline__ float one(const void* row, long long at) { return E::low(((const uint16_t*)row)[at]); }
   static __device__ __forceinline__ void store(void* row, long long at, const float* y) {
@@ -28,6 +33,8 @@ template <> struct Some<TypeF32> {
   static constexpr int N = 4;
   f32x4 w;
   static __device__ __forceinline__ Some load(const void* row, long long at) { return {*(const f32x4*)((const float*)row + at)}; }
+  static __device__ __forceinline__ Some of(u32x4 w) { return {__builtin_bit_cast(f32x4, w)}; }
+  static __device__ __forceinline__ Some masked() { return {f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY}}; }
   __device__ __forceinline__ float operator[](int e) const { return w[e]; }
   static __device__ __forceinline__ float one(const void* row, long long at) { return ((const float*)row)[at]; }
   static __device__ __forceinline__ void store(void* row, long long at, const float* y) { *(f32x4*)((float*)row + at) = f32x4{y[0], y[1], y[2], y[3]}; }
@@ -35,22 +42,34 @@ template <> struct Some<TypeF32> {
 };
 template <class E> constexpr int SIZE = 16 / Some<E>::N;
 
-// A row may start anywhere: `head` elements up to the first 16-byte border, then `full` pieces of 16 bytes, then `tail` elements
-struct Cut { int head, full, tail; };
+// A row may start anywhere: `head` elements up to the first 16-byte border, then `full` pieces of 16 bytes (the first one at element `first`),
+// then `tail` elements.  Of a row that is parted the first part has the head and the tail beside its pieces.
+struct Cut { int head, first, full, tail; };
 template <class E> __device__ __forceinline__ Cut cut_row(const void* row, int vocab) {
   constexpr int N = Some<E>::N;
   const int lead = (int)((uintptr_t)row & 15) / SIZE<E>;
   Cut c;
-  c.head = lead ? min(N - lead, vocab) : 0;
+  c.head = c.first = lead ? min(N - lead, vocab) : 0;
   c.full = (vocab - c.head) / N;
   c.tail = vocab - c.head - c.full * N;
   return c;
+}
+template <class E> __device__ __forceinline__ Cut cut_part(Cut c, int part, int parts) {
+  const int per = (c.full + parts - 1) / parts, from = min(part * per, c.full);
+  c.full = min(per, c.full - from);
+  c.first += from * Some<E>::N;
+  if (part > 0) c.head = c.tail = 0;
+  return c;
+}
+// The pieces of a row through a bounded buffer: past the last one a load brings zeros and no traffic
+template <class E> __device__ __forceinline__ auto pieces_of(const void* row, const Cut& c) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)row + (long long)c.first * SIZE<E>), 0, c.full * 16, 0x00027000);
 }
 template <class E> __device__ __forceinline__ const void* row_at(const void* p, long long row, long long stride) {
   return (const char*)p + row * stride * SIZE<E>;
 }
 // the element of the head or the tail that this thread has, -1: none
-__device__ __forceinline__ int edge_of(const Cut& c, int n, int vocab) {
+__device__ __forceinline__ int edge_of(const Cut& c, int vocab) {
   const int t = threadIdx.x;
   return t < c.head ? t : t >= 8 && t - 8 < c.tail ? vocab - c.tail + t - 8 : -1;
 }
@@ -65,15 +84,6 @@ __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o
 // larger values first, of equal ones the lower index
 __device__ __forceinline__ uint64_t key_of(uint32_t order, int index) { return ((uint64_t)order << 32) | (0xffffffffu - (uint32_t)index); }
 
-template <int T> __device__ __forceinline__ float over_block(float v, float* slots, bool max) {
-  v = max ? wave_max(v) : wave_sum(v);
-  if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float t = slots[0];
-#pragma unroll
-  for (int w = 1; w < T / 64; ++w) t = max ? fmaxf(t, slots[w]) : t + slots[w];
-  return t;
-}
 template <int T> __device__ __forceinline__ int count_block(int v, int* slots) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, WAVE);
@@ -85,58 +95,39 @@ template <int T> __device__ __forceinline__ int count_block(int v, int* slots) {
   for (int w = 0; w < T / 64; ++w) t += slots[w];
   return t;
 }
-// the wave's values in descending order over its lanes
-__device__ __forceinline__ float sorted_wave(float v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int k = 2; k <= 64; k <<= 1)
-#pragma unroll
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      const float o = __shfl_xor(v, j, WAVE);
-      v = ((lane & j) == 0) == ((lane & k) == 0) ? fmaxf(v, o) : fminf(v, o);
-    }
-  return v;
+// The n-th largest of the lanes' values, n from 1 to 64
+__device__ __forceinline__ float nth_of_lanes(float v, int n) {
+  float most = lanes_max(v);
+  for (int i = 1; i < n; ++i) {
+    const unsigned long long at = __ballot(v == most);
+    if (__ffsll((long long)at) - 1 == (int)(threadIdx.x & 63)) v = -INFINITY;
+    most = lanes_max(v);
+  }
+  return most;
 }
 
-constexpr int CANDIDATES = 256;
+constexpr int CANDIDATES = 512, EQUALS = 256, HITS = 512;
 
 // What the likeliest tokens' search holds in LDS
 struct Found {
-  uint64_t key[CANDIDATES];
-  float slots[16];
+  uint64_t key[CANDIDATES], same[EQUALS];        // of values above the bound, and equal to it
+  uint32_t hit[HITS];                            // steps of threads that hold such values: step * T + thread
   int counts[16];
-  int n;
+  int hits, above, equal;
 };
 
-// The n largest of a row whose values do not thin out above any simple bound (many equal ones, NaN): the n-th largest order by
-// halving, every step counting over the row, then the values above it, and of those equal to it the first ones.
-template <class E, int T> __device__ void select_top(const void* row, const Cut& c, int vocab, int n, Found& f) {
-  constexpr int N = Some<E>::N;
-  const int edge = edge_of(c, N, vocab);
-  auto each = [&](auto&& use) {
-    for (int k = threadIdx.x; k < c.full; k += T) {
-      const Some<E> s = Some<E>::load(row, c.head + (long long)k * N);
-#pragma unroll
-      for (int e = 0; e < N; ++e) use(order_of(s[e]), c.head + k * N + e);
+template <class F> __device__ __forceinline__ void note_hits(const float* kept, int steps, int threads, F&& wanted, Found& f) {
+  for (int step = 0; step < steps; ++step)
+    if (wanted(kept[step * threads + threadIdx.x])) {
+      const int i = atomicAdd(&f.hits, 1);
+      if (i < HITS) f.hit[i] = step * threads + threadIdx.x;
     }
-    if (edge >= 0) use(order_of(Some<E>::one(row, edge)), edge);
-  };
-  uint32_t least = 0;                              // the n-th largest order
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t trial = least | (1u << bit);
-    int mine = 0;
-    each([&](uint32_t o, int) { mine += o >= trial; });
-    if (count_block<T>(mine, f.counts) >= n) least = trial;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) f.n = 0;
-  __syncthreads();
-  each([&](uint32_t o, int at) {
-    if (o > least) f.key[atomicAdd(&f.n, 1)] = key_of(o, at);     // (fewer than n of them)
-  });
-  __syncthreads();
-  int have = f.n;
-  // equal ones in the order of their indices: the head, the pieces, the tail
+}
+
+// Of the values equal to `least` (as orders) the first ones, in the order of their indices (the head, the pieces, the tail), behind the
+// `have` keys that there are, until there are n.
+template <class E, int T> __device__ void fill_equal(const void* row, const Cut& c, int vocab, int n, uint32_t least, int have, Found& f) {
+  constexpr int N = Some<E>::N;
   const int turns = 2 + (c.full + T - 1) / T;
   for (int turn = 0; turn < turns && have < n; ++turn) {
     uint32_t same = 0;
@@ -148,8 +139,8 @@ template <class E, int T> __device__ void select_top(const void* row, const Cut&
     } else {
       const int k = (turn - 1) * T + threadIdx.x;
       if (k < c.full) {
-        const Some<E> s = Some<E>::load(row, c.head + (long long)k * N);
-        first = c.head + k * N;
+        const Some<E> s = Some<E>::load(row, c.first + (long long)k * N);
+        first = c.first + k * N;
 #pragma unroll
         for (int e = 0; e < N; ++e) same |= (order_of(s[e]) == least ? 1u : 0u) << e;
       }
@@ -175,162 +166,326 @@ template <class E, int T> __device__ void select_top(const void* row, const Cut&
     have += all;
   }
   __syncthreads();
-  if (threadIdx.x == 0) f.n = n;
-  __syncthreads();
 }
 
-// One block to a row, one pass.  Every lane sums exp((z - m) / T) relative to the largest value m that its wave has met, which rises a few
-// times a row; the entropy's sum goes along.  The likeliest tokens cost the pass a maximum per thread and step, kept in LDS: n of the
-// lanes' maxima bound the n-th largest from below so closely that little more than n values lie above, and only the steps that hold one
-// are read again.  Bound by HBM.
-template <class E, int T, bool TOP>
-__global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int steps_kept) {
+// The n largest of a row where no simple bound leaves few values (crowded ones, NaN): the n-th largest order by halving, every step counting
+// over the row, then the values above it, and of those equal to it the first ones.
+template <class E, int T> __device__ void select_top(const void* row, const Cut& c, int vocab, int n, Found& f) {
+  constexpr int N = Some<E>::N;
+  const int edge = edge_of(c, vocab);
+  auto each = [&](auto&& use) {
+    for (int k = threadIdx.x; k < c.full; k += T) {
+      const Some<E> s = Some<E>::load(row, c.first + (long long)k * N);
+#pragma unroll
+      for (int e = 0; e < N; ++e) use(order_of(s[e]), c.first + k * N + e);
+    }
+    if (edge >= 0) use(order_of(Some<E>::one(row, edge)), edge);
+  };
+  uint32_t least = 0;                              // the n-th largest order, as far as its bits have been found
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t trial = least | (1u << bit);
+    int mine = 0;
+    each([&](uint32_t o, int) { mine += o >= trial; });
+    if (count_block<T>(mine, f.counts) >= n) least = trial;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) f.above = 0;
+  __syncthreads();
+  each([&](uint32_t o, int at) {
+    if (o > least) f.key[atomicAdd(&f.above, 1)] = key_of(o, at);     // (fewer than n of them)
+  });
+  __syncthreads();
+  fill_equal<E, T>(row, c, vocab, n, least, f.above, f);
+}
+
+// A row's numbers from the largest value and the sums relative to it: sum of 2^y, and of y 2^y
+__device__ __forceinline__ void finish(const LogprobArgs& a, long long row, float M, float sum, float along, float z_token) {
+  const bool empty = M == -INFINITY && sum == 0.f;
+  const float log_sum = logf(sum);               // (-infinity for a row that is masked as a whole)
+  if (a.logprobs) a.logprobs[row] = empty ? -INFINITY : (z_token - M) / a.temperature - log_sum;
+  a.stats[2 * row] = M;
+  a.stats[2 * row + 1] = log_sum;
+  if (a.entropy) a.entropy[row] = empty ? 0.f : log_sum - along / sum * LN2;
+}
+// An alternative's place in the result
+struct Likely {
+  float M, log_sum, temperature;
+  bool empty;
+  __device__ __forceinline__ void put(const LogprobArgs& a, long long row, int rank, uint64_t key) const {
+    const long long at = row * a.n_top + rank;
+    a.top_tokens[at] = (int)(0xffffffffu - (uint32_t)key);
+    a.top_logprobs[at] = empty ? -INFINITY : (value_of((uint32_t)(key >> 32)) - M) / temperature - log_sum;
+  }
+};
+__device__ __forceinline__ Likely likely_of(float M, float sum, float temperature) { return {M, logf(sum), temperature, M == -INFINITY && sum == 0.f}; }
+// Each key's place among them all, for those among the first n
+template <class F> __device__ __forceinline__ void rank_keys(const uint64_t* keys, int have, int n, int threads, F&& put) {
+  for (int i = threadIdx.x; i < have; i += threads) {
+    const uint64_t key = keys[i];
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < have; ++j) rank += keys[j] > key;
+    if (rank < n) put(key, rank);
+  }
+}
+// A row that was not asked for
+template <bool TOP> __device__ __forceinline__ void leave_out(const LogprobArgs& a, long long row) {
+  if (threadIdx.x == 0) {
+    if (a.logprobs) a.logprobs[row] = 0.f;
+    a.stats[2 * row] = a.stats[2 * row + 1] = 0.f;
+    if (a.entropy) a.entropy[row] = 0.f;
+  }
+  if (TOP && (int)threadIdx.x < a.n_top) {
+    a.top_tokens[row * a.n_top + threadIdx.x] = -1;
+    a.top_logprobs[row * a.n_top + threadIdx.x] = -INFINITY;
+  }
+}
+
+// One block to a row or to a part of one, one pass.  Every lane sums exp((z - m) / T) relative to the largest value m that its wave has met, which rises
+// a few times a row; the entropy's sum goes along.  The likeliest tokens cost the pass a maximum per thread and step, kept in LDS: a wave's share of
+// n among its lanes' maxima bounds the n-th largest from below so closely that little more than n values lie above, and only the steps
+// that hold one are read again, a value to a thread.  ONE: a row of a single step, whose values are still in registers then.
+// Bound by HBM where rows are many.
+template <class E, int T, bool TOP, bool ONE>
+__global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int steps_kept, int parts) {
   constexpr int N = Some<E>::N, U = 32 / N, WAVES = T / 64;
   extern __shared__ float kept[];                // [steps][T]: the largest value of a thread's step
   __shared__ float red[4][WAVES];
   __shared__ Found found;
-  const int row = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row = parts > 1 ? blockIdx.x / parts : blockIdx.x, part = parts > 1 ? blockIdx.x % parts : 0;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int token = a.tokens ? a.tokens[row] : 0;
   if (a.tokens && (token < 0 || token >= a.vocab)) {          // not asked for
-    if (threadIdx.x == 0) {
-      if (a.logprobs) a.logprobs[row] = 0.f;
-      a.stats[2ll * row] = a.stats[2ll * row + 1] = 0.f;
-      if (a.entropy) a.entropy[row] = 0.f;
-    }
-    if (TOP && (int)threadIdx.x < a.n_top) {
-      a.top_tokens[(long long)row * a.n_top + threadIdx.x] = -1;
-      a.top_logprobs[(long long)row * a.n_top + threadIdx.x] = -INFINITY;
-    }
+    if (parts == 1) leave_out<TOP>(a, row);
     return;
   }
   const void* z = row_at<E>(a.logits, row, a.stride);
-  const Cut c = cut_row<E>(z, a.vocab);
+  Cut c = cut_row<E>(z, a.vocab);
+  if (parts > 1) c = cut_part<E>(c, part, parts);
   const float scale = LOG2E / a.temperature;
-  const int steps = (c.full + T * U - 1) / (T * U);
-  float m = -INFINITY, own = -INFINITY, sum = 0.f, along = 0.f;   // m: of the wave, own: of this lane
+  const int steps = ONE ? 1 : (c.full + T * U - 1) / (T * U);
+  const auto pieces = pieces_of<E>(z, c);
+  auto load = [&](int step, Some<E> (&s)[U]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) s[u] = Some<E>::of(__builtin_amdgcn_raw_buffer_load_b128(pieces, ((step * U + u) * T + threadIdx.x) * 16, 0, 0));
+  };
+  // (requested first, so that waiting for these leaves the pieces on their way)
+  const int edge = edge_of(c, a.vocab);
+  const float some_edge = Some<E>::one(z, max(edge, 0)), z_token = Some<E>::one(z, token);
+  Some<E> s0[U], s1[U];
+  load(0, s0);
+  if (!ONE) load(1, s1);
+  const float at_edge = edge >= 0 ? some_edge : -INFINITY;
+  // In powers of two, relative to m: a term is 2^y with y = (v - m) scale, so that a likely token's own is exact
+  float m = -INFINITY, base = 0.f, own = at_edge, sum = 0.f, along = 0.f;     // m: of the wave (base: 0 in its place before there is one), own: of this lane
   auto rise = [&](float most) {                                   // m to the largest of the lanes'
     if (!__any(most > m)) return;
-    const float up = wave_max(fmaxf(most, m));
+    const float up = lanes_max(fmaxf(most, m));
     if (m == -INFINITY) {
-      // (nothing but NaN so far)
-      along = 0.f;
+      along = 0.f;                               // (nothing but NaN so far)
     } else {
-      const float by = m - up, f = __builtin_amdgcn_exp2f(by * scale);
-      along = f > 0.f ? fmaf(sum, by, along) * f : 0.f;         // (by may be the lowest value, the sum of it infinite)
+      const float by = (m - up) * scale, f = __builtin_amdgcn_exp2f(by);
+      along = f > 0.f ? fmaf(sum, by, along) * f : 0.f;         // (by may be infinite)
       sum *= f;
     }
-    m = up;
+    m = base = up;
   };
-  auto add = [&](float v, float base) {
-    const float x = v - base, e = __builtin_amdgcn_exp2f(x * scale);
+  auto add = [&](float v) {
+    const float y = (v - base) * scale, e = __builtin_amdgcn_exp2f(y);
     sum += e;
-    along = fmaf(e, fmaxf(x, LOWEST), along);    // (a masked value counts 0, not 0 times infinity)
+    along = fmaf(e, fmaxf(y, LOWEST), along);    // (a masked value counts 0, not 0 times infinity)
   };
-  const int edge = edge_of(c, N, a.vocab);
-  const float at_edge = edge >= 0 ? Some<E>::one(z, edge) : -INFINITY;
-  own = at_edge;
-  rise(at_edge);
-  add(at_edge, m == -INFINITY ? 0.f : m);
-  for (int step = 0; step < steps; ++step) {
-    Some<E> s[U];
-    float most = -INFINITY;
+  auto use = [&](int step, Some<E> (&s)[U]) {
+    if ((step + 1) * (T * U) > c.full) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = (step * U + u) * T + threadIdx.x;
-      if (k < c.full) s[u] = Some<E>::load(z, c.head + (long long)k * N);
+      for (int u = 0; u < U; ++u)
+        if ((step * U + u) * T + (int)threadIdx.x >= c.full) s[u] = Some<E>::masked();
     }
+    float most = s[0][0];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if ((step * U + u) * T + (int)threadIdx.x < c.full)
 #pragma unroll
-        for (int e = 0; e < N; ++e) most = fmaxf(most, s[u][e]);
+      for (int e = 0; e < N; ++e) most = fmaxf(most, s[u][e]);
     rise(most);
     if (TOP) {
       own = fmaxf(own, most);
-      if (step < steps_kept) kept[step * T + threadIdx.x] = most;
+      if (!ONE && step < steps_kept) kept[step * T + threadIdx.x] = most;
     }
-    const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if ((step * U + u) * T + (int)threadIdx.x < c.full)
 #pragma unroll
-        for (int e = 0; e < N; ++e) add(s[u][e], base);
+      for (int e = 0; e < N; ++e) add(s[u][e]);
+  };
+  if (TOP && threadIdx.x == 0) found.hits = found.above = found.equal = 0;
+  if constexpr (ONE) {
+    use(0, s0);
+  } else {
+    for (int step = 0; step < steps; step += 2) {
+      use(step, s0);
+      load(step + 2, s0);
+      if (step + 1 >= steps) break;
+      use(step + 1, s1);
+      load(step + 3, s1);
+    }
+  }
+  if (c.head + c.tail > 0) {
+    rise(at_edge);
+    add(at_edge);
   }
   // over the block
   if (lane == 0) red[0][wave] = m;
+  const int n = TOP ? min(a.n_top, c.head + c.tail + c.full * N) : 0;
+  if constexpr (TOP) {
+    // the waves that have values: a short row fills the first ones
+    const int busy = max(1, min(WAVES, (c.full + 63) / 64));
+    const float bound = wave < busy ? nth_of_lanes(own, (n + busy - 1) / busy) : INFINITY;
+    if (lane == 0) red[3][wave] = bound;
+  }
   __syncthreads();
   float M = red[0][0];
 #pragma unroll
   for (int w = 1; w < WAVES; ++w) M = fmaxf(M, red[0][w]);
   {
-    const float by = m == M ? 0.f : m - M;       // (both -infinity: nothing to shift)
-    const float f = __builtin_amdgcn_exp2f(by * scale);
+    const float by = m == M ? 0.f : (m - M) * scale;      // (both -infinity: nothing to shift)
+    const float f = __builtin_amdgcn_exp2f(by);
     along = f > 0.f ? fmaf(sum, by, along) * f : 0.f;
     sum *= f;
   }
-  sum = wave_sum(sum);
-  along = wave_sum(along);
+  sum = lanes_sum(sum);
+  along = lanes_sum(along);
   if (lane == 0) { red[1][wave] = sum; red[2][wave] = along; }
+  float least = -INFINITY;
+  if constexpr (TOP) {
+    // every busy wave has its share of n values that are not below the smallest of their bounds
+    least = red[3][0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) least = fminf(least, red[3][w]);
+    if (!ONE && steps <= steps_kept && own >= least) note_hits(kept, steps, T, [&](float v) { return v >= least; }, found);
+  }
   __syncthreads();
   sum = along = 0.f;
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) { sum += red[1][w]; along += red[2][w]; }
-  const bool empty = M == -INFINITY && sum == 0.f;
-  const float log_sum = logf(sum);               // (-infinity for a row that is masked as a whole)
-  if (threadIdx.x == 0) {
-    if (a.logprobs) a.logprobs[row] = empty ? -INFINITY : (Some<E>::one(z, token) - M) / a.temperature - log_sum;
-    a.stats[2ll * row] = M;
-    a.stats[2ll * row + 1] = log_sum;
-    if (a.entropy) a.entropy[row] = empty ? 0.f : log_sum - along / sum / a.temperature;
+  if (parts > 1) {
+    if (threadIdx.x == 0) a.partial[(long long)row * parts + part] = make_float4(M, sum, along, z_token);
+  } else if (threadIdx.x == 0) {
+    finish(a, row, M, sum, along, z_token);
   }
   if constexpr (TOP) {
-    const int n = a.n_top, per = (n + WAVES - 1) / WAVES;
-    const float bound = __shfl(sorted_wave(own), per - 1, WAVE);
-    if (lane == 0) red[3][wave] = bound;
-    if (threadIdx.x == 0) found.n = 0;
-    __syncthreads();
-    float least = red[3][0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) least = fminf(least, red[3][w]);
-    // NaN (or an infinity, which makes one) in the sum: the maxima passed over it
-    bool plain = sum == sum && steps <= steps_kept;
-    if (plain) {
+    const bool known = sum == sum && steps <= steps_kept;          // (NaN, or an infinity, which makes one: the maxima passed over it)
+    int hits = found.hits;
+    const bool crowded = hits > HITS;
+    if (crowded && known) {
+      // many values equal to the bound, masked ones as a rule: the values above it alone
+      __syncthreads();
+      if (threadIdx.x == 0) found.hits = 0;
+      __syncthreads();
+      note_hits(kept, steps, T, [&](float v) { return v > least; }, found);
+      __syncthreads();
+      hits = found.hits;
+    }
+    const bool simple = known && hits <= HITS;
+    if (simple) {
       auto take = [&](float v, int at) {
-        if (v >= least) {
-          const int i = atomicAdd(&found.n, 1);
+        if (v > least) {
+          const int i = atomicAdd(&found.above, 1);
           if (i < CANDIDATES) found.key[i] = key_of(order_of(v), at);
+        } else if (v == least && !crowded && found.equal <= EQUALS) {
+          const int i = atomicAdd(&found.equal, 1);
+          if (i < EQUALS) found.same[i] = key_of(order_of(v), at);
         }
       };
-      if (least == -INFINITY && a.vocab > CANDIDATES) {
-        plain = false;
-      } else if (own >= least) {
-        if (edge >= 0) take(at_edge, edge);
-        for (int step = 0; step < steps; ++step) {
-          if (!(kept[step * T + threadIdx.x] >= least)) continue;
-          for (int u = 0; u < U; ++u) {
-            const int k = (step * U + u) * T + threadIdx.x;
-            if (k >= c.full) break;
-            const Some<E> s = Some<E>::load(z, c.head + (long long)k * N);
+      if (edge >= 0) take(at_edge, edge);
+      if constexpr (ONE) {
+        if (own >= least)
 #pragma unroll
-            for (int e = 0; e < N; ++e) take(s[e], c.head + k * N + e);
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+              if (s0[u][e] >= least && u * T + (int)threadIdx.x < c.full) take(s0[u][e], c.first + (u * T + (int)threadIdx.x) * N + e);
+      } else {
+        // a thread to every value of the steps noted, four of them requested at once
+        constexpr int B = 4;
+        const int all = hits * U * N;
+        for (int i0 = threadIdx.x; i0 < all; i0 += T * B) {
+          float v[B];
+          int at[B];
+#pragma unroll
+          for (int b = 0; b < B; ++b) {
+            const int i = min(i0 + b * T, all - 1);
+            const uint32_t hit = found.hit[i / (U * N)];
+            const int k = ((int)(hit / T) * U + i % (U * N) / N) * T + (int)(hit % T);
+            at[b] = i == i0 + b * T && k < c.full ? c.first + k * N + i % N : -1;
+            v[b] = Some<E>::one(z, at[b] >= 0 ? at[b] : 0);
           }
+#pragma unroll
+          for (int b = 0; b < B; ++b)
+            if (at[b] >= 0) take(v[b], at[b]);
         }
       }
       __syncthreads();
-      plain = plain && found.n <= CANDIDATES;
     }
-    if (!plain) select_top<E, T>(z, c, a.vocab, n, found);
-    const int have = found.n;
-    for (int i = threadIdx.x; i < have; i += T) {
-      const uint64_t key = found.key[i];
-      int rank = 0;
-      for (int j = 0; j < have; ++j) rank += found.key[j] > key;
-      if (rank >= n) continue;
-      const long long at = (long long)row * n + rank;
-      a.top_tokens[at] = (int)(0xffffffffu - (uint32_t)key);
-      a.top_logprobs[at] = empty ? -INFINITY : (value_of((uint32_t)(key >> 32)) - M) / a.temperature - log_sum;
+    const int above = found.above, equal = found.equal;
+    int have = n;
+    if (!simple || above > CANDIDATES) {
+      select_top<E, T>(z, c, a.vocab, n, found);
+    } else if (above >= n) {
+      have = above;
+    } else if (!crowded && equal <= EQUALS && above + equal <= CANDIDATES) {
+      have = above + equal;
+      for (int i = threadIdx.x; i < equal; i += T) found.key[above + i] = found.same[i];
+      __syncthreads();
+    } else {
+      fill_equal<E, T>(z, c, a.vocab, n, order_of(least), above, found);
+    }
+    if (parts > 1) {
+      uint64_t* keys = a.part_keys + ((long long)row * parts + part) * a.n_top;
+      rank_keys(found.key, have, n, T, [&](uint64_t key, int rank) { keys[rank] = key; });
+      for (int i = n + threadIdx.x; i < a.n_top; i += T) keys[i] = 0;        // (below every value's)
+    } else {
+      const Likely l = likely_of(M, sum, a.temperature);
+      rank_keys(found.key, have, n, T, [&](uint64_t key, int rank) { l.put(a, row, rank, key); });
     }
   }
+}
+
+// A parted row's numbers and likeliest tokens from those of its parts, in their order.  One block to a row.
+constexpr int MOST_PARTS = 8;
+__global__ __launch_bounds__(256) void token_logprobs_join_kernel(LogprobArgs a, int parts) {
+  __shared__ uint64_t keys[MOST_PARTS * MOST_TOP];
+  __shared__ int count;
+  const int row = blockIdx.x, lane = threadIdx.x & 63;
+  const int token = a.tokens ? a.tokens[row] : 0;
+  if (a.tokens && (token < 0 || token >= a.vocab)) {
+    leave_out<true>(a, row);
+    return;
+  }
+  if (threadIdx.x == 0) count = 0;
+  const bool on = lane < parts;
+  const float4 p = on ? a.partial[(long long)row * parts + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  const int share = (a.n_top + parts - 1) / parts;
+  const uint64_t* from = a.part_keys + (long long)row * parts * a.n_top;
+  // every part has `share` values that are not below the smallest of the parts' bounds
+  uint64_t bound = a.n_top > 0 && on ? from[lane * a.n_top + share - 1] : ~0ull;
+#pragma unroll
+  for (int o = 1; o < MOST_PARTS; o <<= 1) {
+    const uint64_t other = ((uint64_t)(uint32_t)__shfl_xor((int)(bound >> 32), o, WAVE) << 32) | (uint32_t)__shfl_xor((int)bound, o, WAVE);
+    bound = other < bound ? other : bound;
+  }
+  bound = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(bound >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)bound);
+  const float M = lanes_max(p.x), scale = LOG2E / a.temperature;
+  const float by = p.x == M ? 0.f : (p.x - M) * scale, f = __builtin_amdgcn_exp2f(by);
+  const float sum = lanes_sum(p.y * f), along = lanes_sum(f > 0.f ? fmaf(p.y, by, p.z) * f : 0.f);
+  if (threadIdx.x == 0) finish(a, row, M, sum, along, p.w);
+  if (a.n_top == 0) return;
+  __syncthreads();
+  for (int i = threadIdx.x; i < parts * a.n_top; i += 256) {
+    const uint64_t key = from[i];
+    if (key >= bound && key != 0) keys[atomicAdd(&count, 1)] = key;
+  }
+  __syncthreads();
+  const Likely l = likely_of(M, sum, a.temperature);
+  rank_keys(keys, count, a.n_top, 256, [&](uint64_t key, int rank) { l.put(a, row, rank, key); });
 }
 
 // Gradient: every value read once and written once, by the same thread, so that the gradient may take the logits' place.  Bound by HBM.
@@ -360,7 +515,7 @@ __global__ __launch_bounds__(GT) void token_logprobs_backward_kernel(LogprobArgs
     return;
   }
   if (part == 0) {
-    const int edge = edge_of(c, N, a.vocab);
+    const int edge = edge_of(c, a.vocab);
     if (edge >= 0) Some<E>::store_one(dz, edge, grad(Some<E>::one(z, edge), edge));
   }
   for (int k0 = part * GT * GU; k0 < c.full; k0 += parts * GT * GU) {
@@ -368,7 +523,7 @@ __global__ __launch_bounds__(GT) void token_logprobs_backward_kernel(LogprobArgs
 #pragma unroll
     for (int u = 0; u < GU; ++u) {
       const int k = k0 + u * GT + threadIdx.x;
-      if (k < c.full && !none) s[u] = Some<E>::load(z, c.head + (long long)k * N);
+      if (k < c.full && !none) s[u] = Some<E>::load(z, c.first + (long long)k * N);
     }
 #pragma unroll
     for (int u = 0; u < GU; ++u) {
@@ -376,26 +531,40 @@ __global__ __launch_bounds__(GT) void token_logprobs_backward_kernel(LogprobArgs
       if (k >= c.full) continue;
       float y[N];
 #pragma unroll
-      for (int e = 0; e < N; ++e) y[e] = none ? 0.f : grad(s[u][e], c.head + k * N + e);
-      Some<E>::store(dz, c.head + (long long)k * N, y);
+      for (int e = 0; e < N; ++e) y[e] = none ? 0.f : grad(s[u][e], c.first + k * N + e);
+      Some<E>::store(dz, c.first + (long long)k * N, y);
     }
   }
 }
 
-template <class E, int T> hipError_t launch_forward(const LogprobArgs& a, hipStream_t s) {
-  constexpr int U = 32 / Some<E>::N;
-  const dim3 grid(a.rows), block(T);
+// Threads to a block and blocks to a row.  Four waves to a row; one where that holds the whole row in a step and rows are many (8192 rows of 1000 values:
+// 7.8 us, 22 with four; five alternatives 16.2 and 31.4, but 64 of them 143 and 64).  Few long rows are parted (times without and with 20
+// alternatives, in us; 100000 fp16 values: 16 rows 6.7 and 12.5 in eight parts, 8.1 and 13.5 in four, 11.1 and 16.5 whole; 64 rows 8.3 and
+// 14.4, 8.5 and 14.2, 11.1 and 16.7; 128 rows in four 10.8 and 16.8, whole 12.0 and 17.4; 300 rows whole 19.9 and 25.4, in four 20.4 and 27.0; one row of
+// 50304 values and five alternatives 9.3 in eight, 9.7 whole).  More waves to a row gain nothing: 256 rows 12.8 with four, 13.2 with eight, 15.2 with
+// sixteen.
+struct Shape { int threads, parts; };
+Shape shape_of(const LogprobArgs& a) {
+  if (a.vocab <= 64 * 32 && a.rows > 256 && a.n_top <= 32) return {64, 1};
+  return {256, a.vocab < 65536 || a.rows > 64 ? 1 : a.rows > 16 ? 4 : 8};
+}
+template <class E, int T, bool ONE> hipError_t launch_forward(const LogprobArgs& a, int parts, hipStream_t s) {
+  constexpr int N = Some<E>::N, U = 32 / N;
+  const dim3 grid((unsigned)(a.rows * parts)), block(T);
   if (a.n_top == 0) {
-    hipLaunchKernelGGL((token_logprobs_kernel<E, T, false>), grid, block, 0, s, a, 0);
+    hipLaunchKernelGGL((token_logprobs_kernel<E, T, false, ONE>), grid, block, 0, s, a, 0, parts);
   } else {
-    // 48 KB of maxima at most: vocabularies up to 393216, beyond them the likeliest tokens are searched by counting
-    const int steps = (a.vocab / Some<E>::N + T * U - 1) / (T * U), kept = steps <= 12288 / T ? steps : 0;
-    hipLaunchKernelGGL((token_logprobs_kernel<E, T, true>), grid, block, kept * T * sizeof(float), s, a, kept);
+    // 48 KB of maxima at most: rows or parts up to 393216 values, beyond them the likeliest tokens are searched by counting
+    const int steps = ((a.vocab / N + parts - 1) / parts + T * U - 1) / (T * U), kept = ONE ? 1 : steps <= 12288 / T ? steps : 0;
+    hipLaunchKernelGGL((token_logprobs_kernel<E, T, true, ONE>), grid, block, ONE ? 0 : kept * T * sizeof(float), s, a, kept, parts);
   }
+  if (parts > 1) hipLaunchKernelGGL(token_logprobs_join_kernel, dim3(a.rows), dim3(256), 0, s, a, parts);
   return hipGetLastError();
 }
 template <class E> hipError_t by_rows(const LogprobArgs& a, hipStream_t s) {
-  return a.rows <= 256 ? launch_forward<E, 1024>(a, s) : launch_forward<E, 256>(a, s);
+  const Shape f = shape_of(a);
+  if (f.threads == 64) return launch_forward<E, 64, true>(a, f.parts, s);
+  return a.vocab <= 256 * 32 ? launch_forward<E, 256, true>(a, f.parts, s) : launch_forward<E, 256, false>(a, f.parts, s);
 }
 int parts_of(const LogprobArgs& a) {
   const int n = a.dtype == RLGEN_DTYPE_F32 ? 4 : 8;
@@ -409,8 +578,14 @@ template <class E> hipError_t launch_backward(const LogprobArgs& a, hipStream_t 
 
 }  // namespace
 
-hipError_t rl_token_logprobs(const LogprobArgs& a, hipStream_t s) {
+size_t rl_token_logprobs_bytes(const LogprobArgs& a) {
+  const Shape f = shape_of(a);
+  return f.parts == 1 ? 0 : (size_t)a.rows * f.parts * (sizeof(float4) + a.n_top * sizeof(uint64_t));
+}
+hipError_t rl_token_logprobs(LogprobArgs a, void* workspace, hipStream_t s) {
   if (a.rows <= 0) return hipSuccess;
+  a.partial = (float4*)workspace;
+  a.part_keys = (uint64_t*)(a.partial + (size_t)a.rows * shape_of(a).parts);
   switch (a.dtype) {
     case RLGEN_DTYPE_F32: return by_rows<TypeF32>(a, s);
     case RLGEN_DTYPE_BF16: return by_rows<TypeBf16>(a, s);

@@ -32,7 +32,7 @@ EXPORTS = ["rlgen_workspace_bytes", "rlgen_create", "rlgen_update_weights", "rlg
            "rlgen_qk_norm_rope_backward", "rlgen_qk_norm_rope_backward_workspace", "rlgen_window_attention",
            "rlgen_window_attention_backward", "rlgen_window_attention_backward_workspace", "rlgen_window_attention_paged",
            "rlgen_window_attention_paged_workspace", "rlgen_window_attention_chunk_workspace", "rlgen_add_rms_norm",
-           "rlgen_add_rms_norm_backward", "rlgen_add_rms_norm_backward_workspace", "rlgen_token_logprobs", "rlgen_token_logprobs_backward",
+           "rlgen_add_rms_norm_backward", "rlgen_add_rms_norm_backward_workspace", "rlgen_token_logprobs", "rlgen_token_logprobs_workspace", "rlgen_token_logprobs_backward",
            "rlgen_dpo_pairs"]
 FAULT_TOKEN, FAULT_UNIFORM, FAULT_GROUP, FAULT_RANGE = 1, 2, 4, 8
 PLAN_ROWS, PLAN_PAGES, PLAN_TABLE, PLAN_LENGTH = 1, 2, 4, 8
@@ -121,13 +121,14 @@ for _name, _types in {
         "rlgen_window_attention_paged": _ROWS + [_i32] * 5 + [_vp, _i32, _i32, _vp, _i32, _vp, _vp] + [_i32] * 5 + [_f32] + _ROWS + [_vp, _vp, _size, _vp],
         "rlgen_add_rms_norm": _ROWS + [_i32] + _ROWS + [_i32] * 3 + [_f32, _vp, _vp, _f32] + 2 * _ROWS + [_i32, _vp, _i32, _vp],
         "rlgen_add_rms_norm_backward": _ROWS + [_i32] + _ROWS + [_i32] + _ROWS + [_i32] * 2 + [_f32, _vp, _vp, _f32] + 2 * _ROWS + [_vp, _vp, _size, _vp],
-        "rlgen_token_logprobs": _ROWS + [_i32] * 3 + [_vp, _f32, _vp, _vp, _vp, _i32, _vp, _vp, _vp],
+        "rlgen_token_logprobs": _ROWS + [_i32] * 3 + [_vp, _f32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _size, _vp],
         "rlgen_token_logprobs_backward": _ROWS + [_i32] * 3 + [_vp, _f32, _vp, _vp, _vp, _vp] + _ROWS + [_vp],
         "rlgen_dpo_pairs": [_vp, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _f32, _f32, _vp, _vp, _vp]}.items():
     getattr(lib, _name).restype, getattr(lib, _name).argtypes = C.c_int, _types
 for _name, _count in {"rlgen_qk_norm_rope_backward_workspace": 2, "rlgen_window_attention_backward_workspace": 8,
                       "rlgen_window_attention_paged_workspace": 8,
-                      "rlgen_window_attention_chunk_workspace": 8, "rlgen_add_rms_norm_backward_workspace": 2}.items():
+                      "rlgen_window_attention_chunk_workspace": 8, "rlgen_add_rms_norm_backward_workspace": 2,
+                      "rlgen_token_logprobs_workspace": 4}.items():
     getattr(lib, _name).restype, getattr(lib, _name).argtypes = _size, [_i32] * _count
 lib.rlgen_destroy.restype = None
 lib.rlgen_destroy.argtypes = [_vp]
@@ -685,7 +686,7 @@ class TokenLogprobs(NamedTuple):
 
 
 def rlgen_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, temperature: float = 1.0, entropy: bool = True, n_top: int = 0,
-                         out=None) -> TokenLogprobs:
+                         out=None, workspace=None) -> TokenLogprobs:
     """logits [rows, vocab] (fp32, bf16 or fp16; any row stride), tokens [rows] int32 or None.  A row whose token lies outside the vocabulary is skipped.
     `out`: a TokenLogprobs (or tuple) of tensors to fill; entropy and n_top are then what it holds."""
     shape = rows, vocab = logits.shape
@@ -697,10 +698,13 @@ def rlgen_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = 
     lp, ent, stats, ids, top = out
     n_top = 0 if ids is None else ids.shape[1]
     assert stats.shape == (rows, 2) and (top is None) == (ids is None) and (top is None or top.shape == (rows, n_top))
-    _check(lib.rlgen_token_logprobs(*_rows(logits, logits.dtype, shape), _DTYPES[logits.dtype], rows, vocab, None if tokens is None else _ints(tokens, rows),
+    dt = _DTYPES[logits.dtype]
+    if workspace is None and (need := lib.rlgen_token_logprobs_workspace(dt, rows, vocab, n_top)):
+        workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
+    _check(lib.rlgen_token_logprobs(*_rows(logits, logits.dtype, shape), dt, rows, vocab, None if tokens is None else _ints(tokens, rows),
                                     temperature, None if lp is None else _floats(lp, rows), _floats(stats, 2 * rows),
                                     None if ent is None else _floats(ent, rows), n_top, None if ids is None else _ints(ids, rows, n_top),
-                                    None if top is None else _floats(top, rows * n_top), _stream()), "rlgen_token_logprobs")
+                                    None if top is None else _floats(top, rows * n_top), *_space(workspace), _stream()), "rlgen_token_logprobs")
     return out if type(out) is TokenLogprobs else TokenLogprobs(lp, ent, stats, ids, top)
 
 

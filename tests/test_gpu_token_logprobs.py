@@ -81,9 +81,11 @@ def test_forward(dtype, V):
 
 @pytest.mark.parametrize("dtype", [F32, BF])
 def test_many_rows(dtype):
-    """Over 256 rows a block has fewer threads."""
+    """Over 256 short rows a block has fewer threads."""
     check(rand(1, 300, 9001, dtype=dtype), tokens_of(2, 300, 9001), 0.7, 20)
     check(rand(3, 257, 130, dtype=dtype), None, 1.0, 64, 1, 3)
+    check(rand(4, 257, 1300, dtype=dtype), None, 1.0, 32, 1, 3)
+    check(rand(5, 400, 40, dtype=dtype), None, 1.0, 20)
 
 
 def test_rows_and_blocks_of_both_sizes_agree():
@@ -91,6 +93,41 @@ def test_rows_and_blocks_of_both_sizes_agree():
     a, b = R.rlgen_token_logprobs(z, n_top=8), R.rlgen_token_logprobs(z[:100], n_top=8)
     assert torch.equal(a.top_tokens[:100], b.top_tokens)
     assert (a.entropy[:100] - b.entropy).abs().max() <= 2 * (5000 / 256 + 64) * U * 4 * 40
+
+
+@pytest.mark.parametrize("dtype", [F32, BF, F16])
+@pytest.mark.parametrize("rows", [1, 20, 70])
+def test_long_rows_whole_and_parted(dtype, rows):
+    """70 rows are taken whole, 20 in four parts, one in eight."""
+    z = rand(rows, rows, 66001, dtype=dtype)
+    tok = tokens_of(2, rows, 66001, skip=rows > 1)
+    check(z[:4], tok[:4], 0.7, 20, pad=3, shift=1)
+    check(z, tok, 1.0, 0)
+    got = R.rlgen_token_logprobs(z.cuda(), tok.int().cuda(), 0.7, n_top=64)
+    live = (tok >= 0) & (tok < 66001)
+    assert torch.equal(got.top_tokens.cpu().long()[live][:6], L.top(z[live][:6], 64))
+
+
+def test_parted_rows_with_crowded_masked_and_unusual_values():
+    """Each in rows of eight parts: one value everywhere, few allowed tokens, all of them in one part, none, NaN, infinity, the last element."""
+    V = 70003
+    z = rand(3, 8, V, dtype=F16)
+    z[0] = 1.5
+    z[1, 40:], z[2, :69000], z[3] = -INF, -INF, -INF
+    z[4, 33333], z[5, 60000], z[6, -1], z[7, 0] = float("nan"), INF, 30, 30
+    got = R.rlgen_token_logprobs(z.cuda(), torch.arange(8, dtype=torch.int32, device="cuda"), 0.9, n_top=64)
+    assert torch.equal(got.top_tokens.cpu().long(), L.top(z, 64))
+    sane = [0, 1, 2, 3, 6, 7]
+    check(z[sane], torch.arange(6), 0.9, 64, pad=1, shift=3)
+    assert torch.isnan(got.entropy[[4, 5]]).all() and torch.isfinite(got.entropy[sane]).all()
+
+
+def test_more_values_than_maxima_are_kept_of():
+    """Rows of over 393216 values."""
+    check(rand(1, 70, 400003, dtype=BF)[:70], None, 1.0, 0)
+    z = rand(2, 70, 400003, dtype=F16).cuda()
+    got = R.rlgen_token_logprobs(z, n_top=7)
+    assert torch.equal(got.top_tokens[::23].cpu().long(), L.top(z[::23].cpu(), 7))
 
 
 def test_alternatives_where_values_are_equal_or_crowded():
@@ -250,7 +287,12 @@ def test_large_offsets():
     z.copy_(rows.cuda())
     tok = tokens_of(2, 4, V, skip=False)
     a, b = R.rlgen_token_logprobs(z, tok.int().cuda(), n_top=3), R.rlgen_token_logprobs(rows.cuda(), tok.int().cuda(), n_top=3)
-    assert all(torch.equal(p, q) for p, q in zip(a, b))
+    assert torch.equal(a.top_tokens, b.top_tokens) and torch.equal(a.stats[:, 0], b.stats[:, 0])
+    # (rows that start differently within 16 bytes are added up by other lanes: both are within the forward pass's bound of the same numbers)
+    lp, H, _, ls = L.logprobs(rows, 1.0)
+    bound = 2 * (4 * (V / 256 + 64) * U * (1 + 4 * (torch.exp(lp) * (lp + ls[:, None]).abs()).sum(-1)) + 16 * U * ls.abs())
+    for p, q in ((a.logprobs, b.logprobs), (a.entropy, b.entropy), (a.stats[:, 1], b.stats[:, 1])):
+        assert bool(((p - q).abs().double().cpu() <= bound).all())
     g = torch.ones(4, device="cuda")
     want = R.rlgen_token_logprobs_backward(rows.cuda(), tok.int().cuda(), 1.0, a.stats, g)
     assert torch.equal(R.rlgen_token_logprobs_backward(z, tok.int().cuda(), 1.0, a.stats, g, out=z), want)

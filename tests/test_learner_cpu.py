@@ -59,8 +59,13 @@ LOGITS_BAD = [dict(rows=-1), dict(rows=1 << 24), dict(V=0), dict(V=(1 << 24) + 1
 
 @host_only
 def test_token_logprobs_refuses():
-    args = "z zs dtype rows V tokens T lp stats entropy n ids top stream".split()
-    good = dict(z=D, zs=100, dtype=1, rows=3, V=100, tokens=D, T=0.7, lp=D, stats=D, entropy=D, n=5, ids=D, top=D, stream=None)
+    args = "z zs dtype rows V tokens T lp stats entropy n ids top ws bytes stream".split()
+    good = dict(z=D, zs=100, dtype=1, rows=3, V=100, tokens=D, T=0.7, lp=D, stats=D, entropy=D, n=5, ids=D, top=D, ws=None, bytes=0, stream=None)
+    size = R.lib.rlgen_token_logprobs_workspace
+    need = size(1, 3, 100000, 5)
+    assert need > 0 and size(1, 300, 100000, 5) == 0 and size(1, 3, 1000, 5) == 0 and size(3, 3, 100000, 5) == 0 and size(1, 3, 100000, 65) == 0
+    for kw in (dict(ws=None, bytes=need), dict(ws=D, bytes=need - 1), dict(ws=C.c_void_p(264), bytes=need)):
+        refuse("rlgen_token_logprobs", args, good, R.ERR_WORKSPACE, V=100000, zs=100000, **kw)
     for kw in (dict(z=None), dict(stats=None), dict(tokens=None), dict(lp=None), dict(ids=None), dict(top=None)):
         refuse("rlgen_token_logprobs", args, good, R.ERR_NULL, **kw)
     for kw in LOGITS_BAD + [dict(n=-1), dict(n=65), dict(n=11, V=10)]:
