@@ -81,6 +81,8 @@ template <class T> struct Vec8 {
   u32x4 w;
   static __device__ __forceinline__ Vec8 load(const void* p, long long at) { return {*(const u32x4*)((const uint16_t*)p + at)}; }
   static __device__ __forceinline__ Vec8 zero() { return {u32x4{0, 0, 0, 0}}; }
+  // what is known of the values ends here
+  __device__ __forceinline__ void opaque() { asm volatile("" : "+v"(w)); }
   __device__ __forceinline__ void to(float* y) const {
 #pragma unroll
     for (int e = 0; e < 4; ++e) { y[2 * e] = T::low(w[e]); y[2 * e + 1] = T::high(w[e]); }
@@ -99,6 +101,7 @@ template <> struct Vec8<TypeF32> {
     return {*(const f32x4*)x, *(const f32x4*)(x + 4)};
   }
   static __device__ __forceinline__ Vec8 zero() { return {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}}; }
+  __device__ __forceinline__ void opaque() {}
   __device__ __forceinline__ void to(float* y) const {
 #pragma unroll
     for (int e = 0; e < 4; ++e) { y[e] = a[e]; y[4 + e] = b[e]; }

@@ -602,10 +602,12 @@ _NORM_DTYPES = {**_DTYPES, _E4M3: DTYPE_E4M3}
 
 def _rows(t: Optional[torch.Tensor], dtype: torch.dtype, shape):
     """[rows, width] with contiguous rows: (address, row stride)."""
+    rows, width = shape
     if t is None:
-        return None, shape[1]
-    assert t.dtype is dtype and t.is_cuda and t.shape == shape and (t.stride(1) == 1 or shape[1] == 1)
-    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
+        return None, width
+    row, one = t.stride()
+    assert t.dtype is dtype and t.is_cuda and t.shape == shape and (one == 1 or width == 1)
+    return t.data_ptr(), row if rows > 1 else width
 
 
 def _rng(t: Optional[torch.Tensor]):
@@ -667,7 +669,7 @@ def rlgen_add_rms_norm_backward(h: Optional[torch.Tensor], gain: Optional[torch.
     else:
         dres, dx, dgain = out
     if gain is not None and workspace is None:
-        workspace = torch.empty(max(lib.rlgen_add_rms_norm_backward_workspace(rows, width), 16), dtype=torch.uint8, device=like.device)
+        workspace = like.new_empty(max(lib.rlgen_add_rms_norm_backward_workspace(rows, width), 16), dtype=torch.uint8)
     _check(lib.rlgen_add_rms_norm_backward(*_rows(h, res, shape), _DTYPES[res], *_rows(dy, dt, shape), _DTYPES[dt], *_rows(dh, res, shape), rows, width,
                                            drop_p, _rng(rng), None if gain is None else _floats(gain, width), eps, *_rows(dres, res, shape),
                                            *_rows(dx, dt, shape), None if dgain is None else _floats(dgain, width), *_space(workspace), _stream()),
@@ -691,16 +693,15 @@ def rlgen_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = 
     `out`: a TokenLogprobs (or tuple) of tensors to fill; entropy and n_top are then what it holds."""
     shape = rows, vocab = logits.shape
     if out is None:
-        new = dict(dtype=_F32, device=logits.device)
-        out = TokenLogprobs(None if tokens is None else torch.empty(rows, **new), torch.empty(rows, **new) if entropy else None,
-                            torch.empty((rows, 2), **new), torch.empty((rows, n_top), dtype=_I32, device=logits.device) if n_top else None,
-                            torch.empty((rows, n_top), **new) if n_top else None)
+        new = logits.new_empty
+        out = TokenLogprobs(None if tokens is None else new(rows, dtype=_F32), new(rows, dtype=_F32) if entropy else None, new((rows, 2), dtype=_F32),
+                            new((rows, n_top), dtype=_I32) if n_top else None, new((rows, n_top), dtype=_F32) if n_top else None)
     lp, ent, stats, ids, top = out
     n_top = 0 if ids is None else ids.shape[1]
     assert stats.shape == (rows, 2) and (top is None) == (ids is None) and (top is None or top.shape == (rows, n_top))
     dt = _DTYPES[logits.dtype]
     if workspace is None and (need := lib.rlgen_token_logprobs_workspace(dt, rows, vocab, n_top)):
-        workspace = torch.empty(need, dtype=torch.uint8, device=logits.device)
+        workspace = logits.new_empty(need, dtype=torch.uint8)
     _check(lib.rlgen_token_logprobs(*_rows(logits, logits.dtype, shape), dt, rows, vocab, None if tokens is None else _ints(tokens, rows),
                                     temperature, None if lp is None else _floats(lp, rows), _floats(stats, 2 * rows),
                                     None if ent is None else _floats(ent, rows), n_top, None if ids is None else _ints(ids, rows, n_top),
