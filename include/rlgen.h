@@ -418,9 +418,9 @@ int rlgen_window_attention_paged(const void *q, int64_t q_stride, int32_t dtype,
  * returns the same bits.  Statistics, sums, log-probs, losses and gains are fp32 or wider.
  *
  * Layouts
- *  - Rows of the norm: width elements, a multiple of 8 up to 16384, any row stride (in elements) that is a multiple of 8 (fp32: 4), bases 16-byte
- *    aligned.  fewer than 2^24 rows.
- *  - Rows of logits: vocab elements, at most 2^24, any row stride and any base that suits the element type.
+ *  - Rows of the norm: width elements, a multiple of 8 up to 16384, any row stride (in elements) that is a multiple of 8 (fp32: 4), bases and gains
+ *    16-byte aligned, fewer than 2^23 rows.
+ *  - Rows of logits: vocab elements, at most 2^24, any row stride from vocab on and any base that suits the element type, fewer than 2^24 rows.
  *  - Without rows (0) an operator returns at once, the gain's gradient is zeroed, and pointers to tensors of rows may be null. */
 
 /* h = residual + dropout(x) and y = RMS norm of h times the gain, in one pass.
@@ -429,12 +429,13 @@ int rlgen_window_attention_paged(const void *q, int64_t q_stride, int32_t dtype,
  *  y nullable out (gain is then not read): of type dtype, or any of the three where dtype is F32, or RLGEN_DTYPE_E4M3 with scales [rows, groups] fp32: y's value is
  *  scales[row, c / scale_group] times the element; scale_group 32, 64 or 128 columns to a scale (the last group may be shorter), or 0: one
  *  for the row.  A scale is the group's largest magnitude / 448; a group below 2^-100 has scale 0 and zeros; NaN is kept and counts for no scale.
- *  The norm is that of h before it is rounded to residual_dtype; mean square and eps as in sqrt(mean h^2 + eps).
+ *  The norm is that of h before it is rounded to residual_dtype; squares are summed in fp32.
  * Dropout: an element is dropped with probability drop_p in [0, 1], rounded to a multiple of 2^-16, else multiplied by the inverse of the rest.
  *  The mask is a function of rng, row and column alone and never stored: rng [2] int64 DEVICE holds a seed and an offset (read when the
  *  launch runs, so that a captured call draws anew when the caller advances the offset); Philox4x32 of ten rounds with key = the seed's
  *  words and counter = (column / 8, row, the offset's words) gives 16 bits for each of eight columns, the low half of a word first,
- *  and an element is dropped if its bits are below 65536 drop_p.  rng may be null if drop_p is 0.
+ *  and an element is dropped if its bits are below 65536 drop_p.  Calls that are to draw apart need offsets (or seeds) of their own.  rng
+ *  may be null if drop_p is 0.
  * h may be residual or x itself, y may be x itself (same type and stride); other overlaps are not allowed.
  * Errors: NULL, BAD_ARG, DEVICE. */
 int rlgen_add_rms_norm(const void *x, int64_t x_stride, int32_t dtype, const void *residual, int64_t residual_stride,

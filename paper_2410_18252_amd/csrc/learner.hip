@@ -51,10 +51,11 @@ bool type_ok(int dtype) { return dtype >= RLGEN_DTYPE_F32 && dtype <= RLGEN_DTYP
 bool rows_ok(const void* p, int64_t stride, int width, int dtype) {
   return aligned16(p) && stride >= width && stride % (dtype == RLGEN_DTYPE_F32 ? 4 : 8) == 0 && stride <= INT32_MAX;
 }
+constexpr int MOST_ROWS = 1 << 23;           // (of up to 512 threads, which have to stay below 2^32)
 int add_norm_args(AddNormArgs& a, int dtype, int res_dtype, int rows, int width, float drop_p, const int64_t* rng, const float* gain, float eps) {
   if (drop_p > 0.f && !rng) return RLGEN_ERR_NULL;
   if (!type_ok(dtype) || (res_dtype != RLGEN_DTYPE_F32 && res_dtype != dtype) || rows < 0 || width < 8 || width % 8 != 0 || width > MOST_WIDTH ||
-      !(drop_p >= 0.f && drop_p <= 1.f) || ((uintptr_t)rng & 7) != 0 || !aligned16(gain) || !std::isfinite(eps) || eps < 0.f || rows >= MOST_BLOCKS)
+      !(drop_p >= 0.f && drop_p <= 1.f) || ((uintptr_t)rng & 7) != 0 || !aligned16(gain) || !std::isfinite(eps) || eps < 0.f || rows >= MOST_ROWS)
     return RLGEN_ERR_BAD_ARG;
   a.dtype = dtype; a.res_dtype = res_dtype; a.rows = rows; a.width = width;
   a.drop = (unsigned)std::lround((double)drop_p * 65536.0);
@@ -98,7 +99,7 @@ int rlgen_add_rms_norm(const void* x, int64_t x_stride, int32_t dtype, const voi
 }
 
 size_t rlgen_add_rms_norm_backward_workspace(int32_t rows, int32_t width) {
-  return rows < 0 || rows >= MOST_BLOCKS || width < 8 || width % 8 != 0 || width > MOST_WIDTH ? 0 : rl_add_norm_backward_bytes(rows, width);
+  return rows < 0 || rows >= MOST_ROWS || width < 8 || width % 8 != 0 || width > MOST_WIDTH ? 0 : rl_add_norm_backward_bytes(rows, width);
 }
 int rlgen_add_rms_norm_backward(const void* h, int64_t h_stride, int32_t residual_dtype, const void* dy, int64_t dy_stride, int32_t dtype,
                                 const void* dh, int64_t dh_stride, int32_t rows, int32_t width, float drop_p, const int64_t* rng,

@@ -523,7 +523,7 @@ __global__ __launch_bounds__(GT) void token_logprobs_backward_kernel(LogprobArgs
   void* dz = const_cast<void*>(row_at<E>(a.dlogits, row, a.d_stride));
   const int token = a.tokens ? a.tokens[row] : -1;
   const float m = a.stats[2ll * row], log_sum = a.stats[2ll * row + 1];
-  const bool none = (a.tokens && (token < 0 || token >= a.vocab)) || m == -INFINITY;
+  const bool none = (a.tokens && (token < 0 || token >= a.vocab)) || (m == -INFINITY && log_sum == -INFINITY);
   const float g = a.g ? a.g[row] : 0.f, h = a.g_entropy ? a.g_entropy[row] : 0.f, H = h != 0.f ? a.entropy[row] : 0.f;
   const float inv_t = 1.0f / a.temperature;
   auto grad = [&](float v, int at) {

@@ -600,21 +600,35 @@ _E4M3 = torch.float8_e4m3fn
 _NORM_DTYPES = {**_DTYPES, _E4M3: DTYPE_E4M3}
 
 
-def _rows(t: Optional[torch.Tensor], dtype: torch.dtype, shape):
+def _here():
+    """The current device, on which every tensor has to be, and its current stream."""
+    device = torch.cuda.current_device()
+    return device, torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(device)
+
+
+def _rows(t: Optional[torch.Tensor], dtype: torch.dtype, shape, device: int):
     """[rows, width] with contiguous rows: (address, row stride)."""
     rows, width = shape
     if t is None:
         return None, width
     row, one = t.stride()
-    assert t.dtype is dtype and t.is_cuda and t.shape == shape and (one == 1 or width == 1)
+    assert t.dtype is dtype and t.get_device() == device and t.shape == shape and (one == 1 or width == 1)
     return t.data_ptr(), row if rows > 1 else width
 
 
-def _rng(t: Optional[torch.Tensor]):
+def _numbers(t: Optional[torch.Tensor], dtype: torch.dtype, shape, device: int):
+    """A contiguous tensor of a shape: its address."""
     if t is None:
         return None
-    assert t.dtype is torch.int64 and t.is_cuda and t.shape == (2,) and t.is_contiguous()
+    assert t.dtype is dtype and t.get_device() == device and t.shape == shape and t.is_contiguous()
     return t.data_ptr()
+
+
+def _scratch(t: Optional[torch.Tensor], device: int):
+    if t is None:
+        return None, 0
+    assert t.get_device() == device and t.is_contiguous()
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def rlgen_add_rms_norm(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float, residual: Optional[torch.Tensor] = None, drop_p: float = 0.0,
@@ -639,15 +653,12 @@ def rlgen_add_rms_norm(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float
         h, y = out[0], out[1]
         if h is not None and residual is None:
             res = h.dtype
-    eight = y is not None and y.dtype is _E4M3
-    scales = None
-    if eight:
-        assert len(out) == 3 and out[2].shape == (rows, -(-width // scale_group) if scale_group > 0 else 1)
-        scales = _floats(out[2], out[2].numel())
+    dev, stream = _here()
+    scales = _numbers(out[2], _F32, (rows, -(-width // scale_group) if scale_group > 0 else 1), dev) if y is not None and y.dtype is _E4M3 else None
     ydt = x.dtype if y is None else y.dtype
-    _check(lib.rlgen_add_rms_norm(*_rows(x, x.dtype, shape), _DTYPES[x.dtype], *_rows(residual, res, shape), _DTYPES[res], rows, width, drop_p, _rng(rng),
-                                  None if gain is None else _floats(gain, width), eps, *_rows(h, res, shape), *_rows(y, ydt, shape),
-                                  _NORM_DTYPES[ydt], scales, scale_group, _stream()), "rlgen_add_rms_norm")
+    _check(lib.rlgen_add_rms_norm(*_rows(x, x.dtype, shape, dev), _DTYPES[x.dtype], *_rows(residual, res, shape, dev), _DTYPES[res], rows, width, drop_p,
+                                  _numbers(rng, torch.int64, (2,), dev), _numbers(gain, _F32, (width,), dev), eps, *_rows(h, res, shape, dev),
+                                  *_rows(y, ydt, shape, dev), _NORM_DTYPES[ydt], scales, scale_group, stream), "rlgen_add_rms_norm")
     return out
 
 
@@ -670,10 +681,11 @@ def rlgen_add_rms_norm_backward(h: Optional[torch.Tensor], gain: Optional[torch.
         dres, dx, dgain = out
     if gain is not None and workspace is None:
         workspace = like.new_empty(max(lib.rlgen_add_rms_norm_backward_workspace(rows, width), 16), dtype=torch.uint8)
-    _check(lib.rlgen_add_rms_norm_backward(*_rows(h, res, shape), _DTYPES[res], *_rows(dy, dt, shape), _DTYPES[dt], *_rows(dh, res, shape), rows, width,
-                                           drop_p, _rng(rng), None if gain is None else _floats(gain, width), eps, *_rows(dres, res, shape),
-                                           *_rows(dx, dt, shape), None if dgain is None else _floats(dgain, width), *_space(workspace), _stream()),
-           "rlgen_add_rms_norm_backward")
+    dev, stream = _here()
+    _check(lib.rlgen_add_rms_norm_backward(*_rows(h, res, shape, dev), _DTYPES[res], *_rows(dy, dt, shape, dev), _DTYPES[dt], *_rows(dh, res, shape, dev),
+                                           rows, width, drop_p, _numbers(rng, torch.int64, (2,), dev), _numbers(gain, _F32, (width,), dev), eps,
+                                           *_rows(dres, res, shape, dev), *_rows(dx, dt, shape, dev), _numbers(dgain, _F32, (width,), dev),
+                                           *_scratch(workspace, dev), stream), "rlgen_add_rms_norm_backward")
     return out
 
 
@@ -698,14 +710,15 @@ def rlgen_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = 
                             new((rows, n_top), dtype=_I32) if n_top else None, new((rows, n_top), dtype=_F32) if n_top else None)
     lp, ent, stats, ids, top = out
     n_top = 0 if ids is None else ids.shape[1]
-    assert stats.shape == (rows, 2) and (top is None) == (ids is None) and (top is None or top.shape == (rows, n_top))
+    assert (top is None) == (ids is None)
     dt = _DTYPES[logits.dtype]
     if workspace is None and (need := lib.rlgen_token_logprobs_workspace(dt, rows, vocab, n_top)):
         workspace = logits.new_empty(need, dtype=torch.uint8)
-    _check(lib.rlgen_token_logprobs(*_rows(logits, logits.dtype, shape), dt, rows, vocab, None if tokens is None else _ints(tokens, rows),
-                                    temperature, None if lp is None else _floats(lp, rows), _floats(stats, 2 * rows),
-                                    None if ent is None else _floats(ent, rows), n_top, None if ids is None else _ints(ids, rows, n_top),
-                                    None if top is None else _floats(top, rows * n_top), *_space(workspace), _stream()), "rlgen_token_logprobs")
+    dev, stream = _here()
+    _check(lib.rlgen_token_logprobs(*_rows(logits, logits.dtype, shape, dev), dt, rows, vocab, _numbers(tokens, _I32, (rows,), dev), temperature,
+                                    _numbers(lp, _F32, (rows,), dev), _numbers(stats, _F32, (rows, 2), dev), _numbers(ent, _F32, (rows,), dev), n_top,
+                                    _numbers(ids, _I32, (rows, n_top), dev), _numbers(top, _F32, (rows, n_top), dev), *_scratch(workspace, dev), stream),
+           "rlgen_token_logprobs")
     return out if type(out) is TokenLogprobs else TokenLogprobs(lp, ent, stats, ids, top)
 
 
@@ -717,12 +730,11 @@ def rlgen_token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.T
     shape = rows, vocab = logits.shape
     if out is None:
         out = torch.empty(shape, dtype=logits.dtype, device=logits.device)
-    assert stats.shape == (rows, 2)
-    _check(lib.rlgen_token_logprobs_backward(*_rows(logits, logits.dtype, shape), _DTYPES[logits.dtype], rows, vocab,
-                                             None if tokens is None else _ints(tokens, rows), temperature, _floats(stats, 2 * rows),
-                                             None if entropy is None else _floats(entropy, rows), None if dlogprobs is None else _floats(dlogprobs, rows),
-                                             None if dentropy is None else _floats(dentropy, rows), *_rows(out, logits.dtype, shape), _stream()),
-           "rlgen_token_logprobs_backward")
+    dev, stream = _here()
+    _check(lib.rlgen_token_logprobs_backward(*_rows(logits, logits.dtype, shape, dev), _DTYPES[logits.dtype], rows, vocab, _numbers(tokens, _I32, (rows,), dev),
+                                             temperature, _numbers(stats, _F32, (rows, 2), dev), _numbers(entropy, _F32, (rows,), dev),
+                                             _numbers(dlogprobs, _F32, (rows,), dev), _numbers(dentropy, _F32, (rows,), dev),
+                                             *_rows(out, logits.dtype, shape, dev), stream), "rlgen_token_logprobs_backward")
     return out
 
 
@@ -732,6 +744,8 @@ def rlgen_dpo_pairs(token_logprobs: torch.Tensor, ref_logprobs: torch.Tensor, ro
     of weight times the losses' sum to token_logprobs [rows]); `out`: the two to write into.  Rows that no sequence has are not written."""
     rows, B = token_logprobs.numel(), idx_pos.numel()
     loss, grad = out if out is not None else (token_logprobs.new_empty(B), torch.empty_like(token_logprobs))
-    _check(lib.rlgen_dpo_pairs(_floats(token_logprobs, rows), _floats(ref_logprobs, rows), rows, _ints(row_starts, B * k + 1), B, k, _ints(idx_pos, B),
-                               _ints(idx_neg, B), beta, weight, _floats(loss, B), _floats(grad, rows), _stream()), "rlgen_dpo_pairs")
+    dev, stream = _here()
+    _check(lib.rlgen_dpo_pairs(_numbers(token_logprobs, _F32, (rows,), dev), _numbers(ref_logprobs, _F32, (rows,), dev), rows,
+                               _numbers(row_starts, _I32, (B * k + 1,), dev), B, k, _numbers(idx_pos, _I32, (B,), dev), _numbers(idx_neg, _I32, (B,), dev), beta,
+                               weight, _numbers(loss, _F32, (B,), dev), _numbers(grad, _F32, (rows,), dev), stream), "rlgen_dpo_pairs")
     return loss, grad

@@ -189,6 +189,16 @@ def test_nan_and_infinity_stay_in_their_rows():
     assert torch.isfinite(d[keep]).all() and torch.isnan(d[[1, 3, 4]]).all()
 
 
+def test_a_row_of_nan_has_nan_gradients():
+    z = torch.full((2, 700), float("nan"))
+    z[1] = -INF
+    tok = torch.zeros(2, dtype=torch.int32, device="cuda")
+    r = R.rlgen_token_logprobs(z.cuda(), tok, n_top=3)
+    assert r.top_tokens.tolist() == [[0, 1, 2]] * 2 and torch.isnan(r.logprobs[0]) and r.logprobs[1] == -INF
+    d = R.rlgen_token_logprobs_backward(z.cuda(), tok, 1.0, r.stats, torch.ones(2, device="cuda"))
+    assert torch.isnan(d[0]).all() and (d[1] == 0).all()
+
+
 def test_temperatures():
     z = rand(1, 4, 2000, scale=3.0)
     for T in (1e-6, 1e-3, 50.0, 3e38):
