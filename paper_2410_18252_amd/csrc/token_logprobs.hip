@@ -16,7 +16,7 @@ typedef f32x4 any4f __attribute__((aligned(4)));
 template <class E> struct Some {
   static constexpr int N = 8;
   u32x4 w;
-  static __device__ __forceinline__ Some load(const void* row, long long at) { return {*(const u32x4*)((const uint16_t*)row + at)}; }
+  template <bool ONCE = false> static __device__ __forceinline__ Some load(const void* row, long long at) { return {take<ONCE>((const u32x4*)((const uint16_t*)row + at))}; }
   static __device__ __forceinline__ Some of(u32x4 w) { return {w}; }
   __device__ __forceinline__ void opaque() { asm volatile("" : "+v"(w)); }     // what is known of the values ends here
   static __device__ __forceinline__ Some masked() {
@@ -25,24 +25,29 @@ template <class E> struct Some {
   }
   __device__ __forceinline__ float operator[](int e) const { return e & 1 ? E::high(w[e >> 1]) : E::low(w[e >> 1]); }
   static __device__ __forceinline__ float one(const void* row, long long at) { return E::low(((const uint16_t*)row)[at]); }
-  static __device__ __forceinline__ void store(void* row, long long at, const float* y) {
+  template <bool ONCE> static __device__ __forceinline__ void store(void* row, long long at, const float* y) {
     u32x4 w;
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[e] = E::pack(y[2 * e], y[2 * e + 1]);
-    *(any4*)((uint16_t*)row + at) = w;
+    if constexpr (ONCE) __builtin_nontemporal_store(w, (any4*)((uint16_t*)row + at));
+    else *(any4*)((uint16_t*)row + at) = w;
   }
   static __device__ __forceinline__ void store_one(void* row, long long at, float y) { ((uint16_t*)row)[at] = (uint16_t)E::pack(y, 0.f); }
 };
 template <> struct Some<TypeF32> {
   static constexpr int N = 4;
   f32x4 w;
-  static __device__ __forceinline__ Some load(const void* row, long long at) { return {*(const f32x4*)((const float*)row + at)}; }
+  template <bool ONCE = false> static __device__ __forceinline__ Some load(const void* row, long long at) { return {take<ONCE>((const f32x4*)((const float*)row + at))}; }
   static __device__ __forceinline__ Some of(u32x4 w) { return {__builtin_bit_cast(f32x4, w)}; }
   __device__ __forceinline__ void opaque() {}
   static __device__ __forceinline__ Some masked() { return {f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY}}; }
   __device__ __forceinline__ float operator[](int e) const { return w[e]; }
   static __device__ __forceinline__ float one(const void* row, long long at) { return ((const float*)row)[at]; }
-  static __device__ __forceinline__ void store(void* row, long long at, const float* y) { *(any4f*)((float*)row + at) = f32x4{y[0], y[1], y[2], y[3]}; }
+  template <bool ONCE> static __device__ __forceinline__ void store(void* row, long long at, const float* y) {
+    const f32x4 v = {y[0], y[1], y[2], y[3]};
+    if constexpr (ONCE) __builtin_nontemporal_store(v, (any4f*)((float*)row + at));
+    else *(any4f*)((float*)row + at) = v;
+  }
   static __device__ __forceinline__ void store_one(void* row, long long at, float y) { ((float*)row)[at] = y; }
 };
 template <class E> constexpr int SIZE = 16 / Some<E>::N;
@@ -251,7 +256,7 @@ template <bool TOP> __device__ __forceinline__ void leave_out(const LogprobArgs&
 // n among its lanes' maxima bounds the n-th largest from below so closely that little more than n values lie above, and only the steps
 // that hold one are read again, a value to a thread.  ONE: a row of a single step, whose values are still in registers then.
 // Bound by HBM where rows are many.
-template <class E, int T, bool TOP, bool ONE>
+template <class E, int T, bool TOP, bool ONE, bool ONCE>
 __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int steps_kept, int parts) {
   constexpr int N = Some<E>::N, U = 32 / N, WAVES = T / 64;
   extern __shared__ float kept[];                // [steps][T]: the largest value of a thread's step
@@ -272,7 +277,7 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
   const auto pieces = pieces_of<E>(z, c);
   auto load = [&](int step, Some<E> (&s)[U]) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) s[u] = Some<E>::of(__builtin_amdgcn_raw_buffer_load_b128(pieces, ((step * U + u) * T + threadIdx.x) * 16, 0, 0));
+    for (int u = 0; u < U; ++u) s[u] = Some<E>::of(__builtin_amdgcn_raw_buffer_load_b128(pieces, ((step * U + u) * T + threadIdx.x) * 16, 0, ONCE ? 2 : 0));
   };
   // (requested first, so that waiting for these leaves the pieces on their way)
   const int edge = edge_of(c, a.vocab);
@@ -281,27 +286,34 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
   load(0, s0);
   if (!ONE) load(1, s1);
   const float at_edge = edge >= 0 ? some_edge : -INFINITY;
-  // In powers of two, relative to m: a term is 2^y with y = (v - m) scale, so that a likely token's own is exact
-  float m = -INFINITY, base = 0.f, own = at_edge, sum = 0.f, along = 0.f;     // m: of the wave (base: 0 in its place before there is one), own: of this lane
+  // In powers of two, relative to m: a term is 2^y with y = v scale - shift, one fma, where shift is base scale rounded to a float; the largest value's own
+  // y is then `off`, known exactly and taken out at the end.  (Where base scale is so large that off would be: y = (v - base) scale.)
+  float m = -INFINITY, own = at_edge, sum = 0.f, along = 0.f;     // m: of the wave, own: of this lane
+  float base = 0.f, shift = 0.f, off = 0.f;                       // base: m, or 0 before there is one
+  bool near = true;
   auto rise = [&](float most) {                                   // m to the largest of the lanes'
     if (!__any(most > m)) return;
-    const float up = lanes_max(fmaxf(most, m));
+    const float up = lanes_max(fmaxf(most, m)), before = off;
+    shift = up * scale;
+    near = fabsf(shift) < 65536.f;
+    off = near ? fmaf(up, scale, -shift) : 0.f;
     if (m == -INFINITY) {
       along = 0.f;                               // (nothing but NaN so far)
     } else {
-      const float by = (m - up) * scale, f = __builtin_amdgcn_exp2f(by);
+      const float by = (m - up) * scale - before + off, f = __builtin_amdgcn_exp2f(by);
       along = f > 0.f ? fmaf(sum, by, along) * f : 0.f;         // (by may be infinite)
       sum *= f;
     }
     m = base = up;
   };
   auto add = [&](float v) {
-    const float y = (v - base) * scale, e = __builtin_amdgcn_exp2f(y);
+    const float y = fmaf(v - base, scale, off), e = __builtin_amdgcn_exp2f(y);
     sum += e;
     along = fmaf(e, fmaxf(y, LOWEST), along);    // (a masked value counts 0, not 0 times infinity)
   };
   auto use = [&](int step, Some<E> (&s)[U]) {
-    if ((step + 1) * (T * U) > c.full) {
+    const bool whole = (step + 1) * (T * U) <= c.full;
+    if (!whole) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if ((step * U + u) * T + (int)threadIdx.x >= c.full) s[u] = Some<E>::masked();
@@ -318,25 +330,29 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
     }
     // a step's own sums, so that a masked value (0 times minus infinity in the second) shows there, and is left out in a second go
     float step_sum = 0.f, step_along = 0.f;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float y = (s[u][e] - base) * scale, f = __builtin_amdgcn_exp2f(y);
-        step_sum += f;
-        step_along = fmaf(f, y, step_along);
-      }
-    if (__any(step_along != step_along)) {
-      step_along = 0.f;
-#pragma unroll
-      for (int u = 0; u < U; ++u) s[u].opaque();           // (widened again: kept, they would cost every step 30 registers)
+    if (near && whole) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-          const float y = (s[u][e] - base) * scale;
-          step_along = fmaf(__builtin_amdgcn_exp2f(y), fmaxf(y, LOWEST), step_along);
+          const float y = fmaf(s[u][e], scale, -shift), f = __builtin_amdgcn_exp2f(y);
+          step_sum += f;
+          step_along = fmaf(f, y, step_along);
         }
+    }
+    if (!near || !whole || __any(step_along != step_along)) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) s[u].opaque();           // (widened again: kept, they would cost every step 30 registers)
+      const float sum_before = sum, along_before = along;
+      sum = along = 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < N; ++e) add(s[u][e]);
+      step_sum = sum;
+      step_along = along;
+      sum = sum_before;
+      along = along_before;
     }
     sum += step_sum;
     along += step_along;
@@ -371,6 +387,10 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
 #pragma unroll
   for (int w = 1; w < WAVES; ++w) M = fmaxf(M, red[0][w]);
   {
+    // `off` out of both sums (by division, so that a row with a single token sums up to exactly 1; what the second one's rounding leaves is none of it)
+    const float one = __builtin_amdgcn_exp2f(off), rest = fmaf(-off, sum, along);
+    along = fabsf(rest) <= 0x1p-22f * fabsf(off) * sum ? 0.f : rest / one;
+    sum /= one;
     const float by = m == M ? 0.f : (m - M) * scale;      // (both -infinity: nothing to shift)
     const float f = __builtin_amdgcn_exp2f(by);
     along = f > 0.f ? fmaf(sum, by, along) * f : 0.f;
@@ -515,7 +535,7 @@ __global__ __launch_bounds__(256) void token_logprobs_join_kernel(LogprobArgs a,
 
 // Gradient: every value read once and written once, by the same thread, so that the gradient may take the logits' place.  Bound by HBM.
 constexpr int GU = 4;
-template <class E, int GT>
+template <class E, int GT, bool ONCE>
 __global__ __launch_bounds__(GT) void token_logprobs_backward_kernel(LogprobArgs a, int parts) {
   constexpr int N = Some<E>::N;
   const int row = blockIdx.x / parts, part = blockIdx.x % parts;
@@ -543,7 +563,7 @@ __global__ __launch_bounds__(GT) void token_logprobs_backward_kernel(LogprobArgs
 #pragma unroll
     for (int u = 0; u < GU; ++u) {
       const int k = k0 + u * GT + threadIdx.x;
-      if (k < c.full && !none) s[u] = Some<E>::load(z, c.first + (long long)k * N);
+      if (k < c.full && !none) s[u] = Some<E>::template load<ONCE>(z, c.first + (long long)k * N);
     }
 #pragma unroll
     for (int u = 0; u < GU; ++u) {
@@ -552,39 +572,42 @@ __global__ __launch_bounds__(GT) void token_logprobs_backward_kernel(LogprobArgs
       float y[N];
 #pragma unroll
       for (int e = 0; e < N; ++e) y[e] = none ? 0.f : grad(s[u][e], c.first + k * N + e);
-      Some<E>::store(dz, c.first + (long long)k * N, y);
+      Some<E>::template store<ONCE>(dz, c.first + (long long)k * N, y);
     }
   }
 }
 
-// Threads to a block and blocks to a row.  Four waves to a row; one where that holds the whole row in a step and rows are many (8192 rows of 1000 values:
-// 7.8 us, 22 with four; five alternatives 16.2 and 31.4, but 64 of them 143 and 64).  Few long rows are parted (times without and with 20
-// alternatives, in us; 100000 fp16 values: 16 rows 6.7 and 12.5 in eight parts, 8.1 and 13.5 in four, 11.1 and 16.5 whole; 64 rows 8.3 and
-// 14.4, 8.5 and 14.2, 11.1 and 16.7; 128 rows in four 10.8 and 16.8, whole 12.0 and 17.4; 300 rows whole 19.9 and 25.4, in four 20.4 and 27.0; one row of
-// 50304 values and five alternatives 9.3 in eight, 9.7 whole).  More waves to a row gain nothing: 256 rows 12.8 with four, 13.2 with eight, 15.2 with
-// sixteen.
+// Threads to a block and blocks to a row.  Four waves to a row; one where that holds the whole row in a step and rows are many (8192 rows of 1000 bf16 values,
+// us: 8.6 and 25 without alternatives, 17 and 35 with five, 33 and 48 with 32, but 145 and 69 with 64).  Few long rows are parted (100000 fp16
+// values without and with 20 alternatives, us: 16 rows 6.7 and 12.9 in eight parts, 7.8 and 14.7 in four, 10.3 and 16.2 whole; 64 rows 8.2 and 15.2,
+// 8.2 and 14.4, 10.4 and 16.5; 200 rows 15.3 and 23.9, 16.0 and 22.3, 12.2 and 18.4; of 66000 values 16 rows with 20 alternatives 12.0 in eight,
+// 12.9 whole; one row of 50304 with five 9.0 in eight, 9.4 whole and without a workspace).  More waves to a row gain nothing (256 rows of
+// 100000: 12.8 with four, 13.2 with eight, 15.2 with sixteen).
 struct Shape { int threads, parts; };
 Shape shape_of(const LogprobArgs& a) {
   if (a.vocab <= 64 * 32 && a.rows > 256 && a.n_top <= 32) return {64, 1};
   return {256, a.vocab < 65536 || a.rows > 64 ? 1 : a.rows > 16 ? 4 : 8};
 }
-template <class E, int T, bool ONE> hipError_t launch_forward(const LogprobArgs& a, int parts, hipStream_t s) {
+// Of rows past the caches (8192 of 128256 bf16 values, a quarter left out: 243 us, 279 without; backward 644 and 667)
+bool past_caches(const LogprobArgs& a, int times) { return (double)times * a.rows * a.vocab * (a.dtype == RLGEN_DTYPE_F32 ? 4 : 2) > CACHE_BYTES; }
+template <class E, int T, bool ONE, bool ONCE> hipError_t launch_forward(const LogprobArgs& a, int parts, hipStream_t s) {
   constexpr int N = Some<E>::N, U = 32 / N;
   const dim3 grid((unsigned)(a.rows * parts)), block(T);
   if (a.n_top == 0) {
-    hipLaunchKernelGGL((token_logprobs_kernel<E, T, false, ONE>), grid, block, 0, s, a, 0, parts);
+    hipLaunchKernelGGL((token_logprobs_kernel<E, T, false, ONE, ONCE>), grid, block, 0, s, a, 0, parts);
   } else {
     // 48 KB of maxima at most: rows or parts up to 393216 values, beyond them the likeliest tokens are searched by counting
     const int steps = ((a.vocab / N + parts - 1) / parts + T * U - 1) / (T * U), kept = ONE ? 1 : steps <= 12288 / T ? steps : 0;
-    hipLaunchKernelGGL((token_logprobs_kernel<E, T, true, ONE>), grid, block, ONE ? 0 : kept * T * sizeof(float), s, a, kept, parts);
+    hipLaunchKernelGGL((token_logprobs_kernel<E, T, true, ONE, ONCE>), grid, block, ONE ? 0 : kept * T * sizeof(float), s, a, kept, parts);
   }
   if (parts > 1) hipLaunchKernelGGL(token_logprobs_join_kernel, dim3(a.rows), dim3(256), 0, s, a, parts);
   return hipGetLastError();
 }
 template <class E> hipError_t by_rows(const LogprobArgs& a, hipStream_t s) {
   const Shape f = shape_of(a);
-  if (f.threads == 64) return launch_forward<E, 64, true>(a, f.parts, s);
-  return a.vocab <= 256 * 32 ? launch_forward<E, 256, true>(a, f.parts, s) : launch_forward<E, 256, false>(a, f.parts, s);
+  if (f.threads == 64) return launch_forward<E, 64, true, false>(a, f.parts, s);
+  if (a.vocab <= 256 * 32) return launch_forward<E, 256, true, false>(a, f.parts, s);
+  return past_caches(a, 1) ? launch_forward<E, 256, false, true>(a, f.parts, s) : launch_forward<E, 256, false, false>(a, f.parts, s);
 }
 // Backward: one wave to a row that it holds in a step (8192 rows of 1000 bf16 values: 9.5 us, 12.9 with four), else four to 1024 pieces
 bool short_row(const LogprobArgs& a) { return a.vocab <= 64 * GU * (a.dtype == RLGEN_DTYPE_F32 ? 4 : 8); }
@@ -594,8 +617,9 @@ int parts_of(const LogprobArgs& a) {
 }
 template <class E> hipError_t launch_backward(const LogprobArgs& a, hipStream_t s) {
   const int parts = parts_of(a);
-  if (short_row(a)) hipLaunchKernelGGL((token_logprobs_backward_kernel<E, 64>), dim3((unsigned)a.rows), dim3(64), 0, s, a, 1);
-  else hipLaunchKernelGGL((token_logprobs_backward_kernel<E, 256>), dim3((unsigned)(a.rows * parts)), dim3(256), 0, s, a, parts);
+  if (short_row(a)) hipLaunchKernelGGL((token_logprobs_backward_kernel<E, 64, false>), dim3((unsigned)a.rows), dim3(64), 0, s, a, 1);
+  else if (past_caches(a, 2)) hipLaunchKernelGGL((token_logprobs_backward_kernel<E, 256, true>), dim3((unsigned)(a.rows * parts)), dim3(256), 0, s, a, parts);
+  else hipLaunchKernelGGL((token_logprobs_backward_kernel<E, 256, false>), dim3((unsigned)(a.rows * parts)), dim3(256), 0, s, a, parts);
   return hipGetLastError();
 }
 
