@@ -429,7 +429,8 @@ int rlgen_window_attention_paged(const void *q, int64_t q_stride, int32_t dtype,
  *  y nullable out (gain is then not read): of type dtype, or any of the three where dtype is F32, or RLGEN_DTYPE_E4M3 with scales [rows, groups] fp32: y's value is
  *  scales[row, c / scale_group] times the element; scale_group 32, 64 or 128 columns to a scale (the last group may be shorter), or 0: one
  *  for the row.  A scale is the group's largest magnitude / 448; a group below 2^-100 has scale 0 and zeros; NaN is kept and counts for no scale.
- *  The norm is that of h before it is rounded to residual_dtype; squares are summed in fp32.
+ *  The norm is that of h before it is rounded to residual_dtype; squares are summed in fp32.  Values beyond a 16-bit type become infinite, as a
+ *  cast makes them.
  * Dropout: an element is dropped with probability drop_p in [0, 1], rounded to a multiple of 2^-16, else multiplied by the inverse of the rest.
  *  The mask is a function of rng, row and column alone and never stored: rng [2] int64 DEVICE holds a seed and an offset (read when the
  *  launch runs, so that a captured call draws anew when the caller advances the offset); Philox4x32 of ten rounds with key = the seed's
@@ -439,18 +440,18 @@ int rlgen_window_attention_paged(const void *q, int64_t q_stride, int32_t dtype,
  * h may be residual or x itself, y may be x itself (same type and stride); other overlaps are not allowed.
  * Errors: NULL, BAD_ARG, DEVICE. */
 int rlgen_add_rms_norm(const void *x, int64_t x_stride, int32_t dtype, const void *residual, int64_t residual_stride,
-                       int32_t residual_dtype, int32_t rows, int32_t width, float drop_p, const int64_t *rng, const float *gain, float eps,
+                       int32_t residual_dtype, int32_t rows, int32_t width, double drop_p, const int64_t *rng, const float *gain, float eps,
                        void *h, int64_t h_stride, void *y, int64_t y_stride, int32_t y_dtype, float *scales, int32_t scale_group,
                        void *hip_stream);
 
 /* Its gradients, from h as rlgen_add_rms_norm returned it, dy (type dtype) and dh (nullable, type residual_dtype: the gradient that reaches h past
  * the norm): dresidual (nullable, residual_dtype) = the gradient of h, dx (nullable, dtype) = the same through the dropout (drop_p and rng as
- * they were), dgain [width] fp32.  gain null: no norm was taken, dy and dgain are null too and h is not read.  dresidual may be dh itself, dx may be dy
+ * they were), dgain [width] fp32 (the sum over all rows, padding rows among them).  gain null: no norm was taken, dy and dgain are null too and h is not read.  dresidual may be dh itself, dx may be dy
  * itself.  workspace: 16-byte aligned, rlgen_add_rms_norm_backward_workspace(rows, width) bytes (null without a gain).
  * Errors: NULL, BAD_ARG, WORKSPACE, DEVICE. */
 size_t rlgen_add_rms_norm_backward_workspace(int32_t rows, int32_t width);
 int rlgen_add_rms_norm_backward(const void *h, int64_t h_stride, int32_t residual_dtype, const void *dy, int64_t dy_stride, int32_t dtype,
-                                const void *dh, int64_t dh_stride, int32_t rows, int32_t width, float drop_p, const int64_t *rng,
+                                const void *dh, int64_t dh_stride, int32_t rows, int32_t width, double drop_p, const int64_t *rng,
                                 const float *gain, float eps, void *dresidual, int64_t dresidual_stride, void *dx, int64_t dx_stride,
                                 float *dgain, void *workspace, size_t workspace_bytes, void *hip_stream);
 

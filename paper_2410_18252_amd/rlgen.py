@@ -119,8 +119,8 @@ for _name, _types in {
         "rlgen_window_attention": 3 * _ROWS + [_i32] * 5 + [_vp] + [_i32] * 4 + [_f32] + _ROWS + [_vp, _vp],
         "rlgen_window_attention_backward": 4 * _ROWS + [_vp] + _ROWS + [_i32] * 5 + [_vp] + [_i32] * 4 + [_f32] + 3 * _ROWS + [_vp, _size, _vp],
         "rlgen_window_attention_paged": _ROWS + [_i32] * 5 + [_vp, _i32, _i32, _vp, _i32, _vp, _vp] + [_i32] * 5 + [_f32] + _ROWS + [_vp, _vp, _size, _vp],
-        "rlgen_add_rms_norm": _ROWS + [_i32] + _ROWS + [_i32] * 3 + [_f32, _vp, _vp, _f32] + 2 * _ROWS + [_i32, _vp, _i32, _vp],
-        "rlgen_add_rms_norm_backward": _ROWS + [_i32] + _ROWS + [_i32] + _ROWS + [_i32] * 2 + [_f32, _vp, _vp, _f32] + 2 * _ROWS + [_vp, _vp, _size, _vp],
+        "rlgen_add_rms_norm": _ROWS + [_i32] + _ROWS + [_i32] * 3 + [C.c_double, _vp, _vp, _f32] + 2 * _ROWS + [_i32, _vp, _i32, _vp],
+        "rlgen_add_rms_norm_backward": _ROWS + [_i32] + _ROWS + [_i32] + _ROWS + [_i32] * 2 + [C.c_double, _vp, _vp, _f32] + 2 * _ROWS + [_vp, _vp, _size, _vp],
         "rlgen_token_logprobs": _ROWS + [_i32] * 3 + [_vp, _f32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _size, _vp],
         "rlgen_token_logprobs_backward": _ROWS + [_i32] * 3 + [_vp, _f32, _vp, _vp, _vp, _vp] + _ROWS + [_vp],
         "rlgen_dpo_pairs": [_vp, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _f32, _f32, _vp, _vp, _vp]}.items():
@@ -624,6 +624,11 @@ def _numbers(t: Optional[torch.Tensor], dtype: torch.dtype, shape, device: int):
     return t.data_ptr()
 
 
+def _made_here(t: Optional[torch.Tensor], *_):
+    """The same of a tensor that the binding has just made."""
+    return None if t is None else t.data_ptr()
+
+
 def _scratch(t: Optional[torch.Tensor], device: int):
     if t is None:
         return None, 0
@@ -704,6 +709,7 @@ def rlgen_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = 
     """logits [rows, vocab] (fp32, bf16 or fp16; any row stride), tokens [rows] int32 or None.  A row whose token lies outside the vocabulary is skipped.
     `out`: a TokenLogprobs (or tuple) of tensors to fill; entropy and n_top are then what it holds."""
     shape = rows, vocab = logits.shape
+    numbers = _numbers if out is not None else _made_here
     if out is None:
         new = logits.new_empty
         out = TokenLogprobs(None if tokens is None else new(rows, dtype=_F32), new(rows, dtype=_F32) if entropy else None, new((rows, 2), dtype=_F32),
@@ -716,8 +722,8 @@ def rlgen_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = 
         workspace = logits.new_empty(need, dtype=torch.uint8)
     dev, stream = _here()
     _check(lib.rlgen_token_logprobs(*_rows(logits, logits.dtype, shape, dev), dt, rows, vocab, _numbers(tokens, _I32, (rows,), dev), temperature,
-                                    _numbers(lp, _F32, (rows,), dev), _numbers(stats, _F32, (rows, 2), dev), _numbers(ent, _F32, (rows,), dev), n_top,
-                                    _numbers(ids, _I32, (rows, n_top), dev), _numbers(top, _F32, (rows, n_top), dev), *_scratch(workspace, dev), stream),
+                                    numbers(lp, _F32, (rows,), dev), numbers(stats, _F32, (rows, 2), dev), numbers(ent, _F32, (rows,), dev), n_top,
+                                    numbers(ids, _I32, (rows, n_top), dev), numbers(top, _F32, (rows, n_top), dev), *_scratch(workspace, dev), stream),
            "rlgen_token_logprobs")
     return out if type(out) is TokenLogprobs else TokenLogprobs(lp, ent, stats, ids, top)
 
@@ -743,7 +749,7 @@ def rlgen_dpo_pairs(token_logprobs: torch.Tensor, ref_logprobs: torch.Tensor, ro
     """token_logprobs, ref_logprobs [rows] fp32 of packed sequences, row_starts [B k + 1], idx_pos and idx_neg [B] int32.  Returns (loss [B], the gradient
     of weight times the losses' sum to token_logprobs [rows]); `out`: the two to write into.  Rows that no sequence has are not written."""
     rows, B = token_logprobs.numel(), idx_pos.numel()
-    loss, grad = out if out is not None else (token_logprobs.new_empty(B), torch.empty_like(token_logprobs))
+    loss, grad = out if out is not None else (token_logprobs.new_empty(B), token_logprobs.new_empty(rows))
     dev, stream = _here()
     _check(lib.rlgen_dpo_pairs(_numbers(token_logprobs, _F32, (rows,), dev), _numbers(ref_logprobs, _F32, (rows,), dev), rows,
                                _numbers(row_starts, _I32, (B * k + 1,), dev), B, k, _numbers(idx_pos, _I32, (B,), dev), _numbers(idx_neg, _I32, (B,), dev), beta,
