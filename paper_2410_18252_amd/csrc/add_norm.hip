@@ -270,6 +270,7 @@ __global__ __launch_bounds__(512) void add_norm_backward_kernel(AddNormArgs a, i
     now = next;
   }
   if (!a.dgain) return;
+  float* to = gridDim.x == 1 ? a.dgain : a.partial + (long long)blockIdx.x * a.width;
   if (NV == 1 && rows_here > 1) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) sums[threadIdx.x * 8 + e] = sum[0][e];
@@ -277,14 +278,14 @@ __global__ __launch_bounds__(512) void add_norm_backward_kernel(AddNormArgs a, i
     for (int d = threadIdx.x; d < a.width; d += blockDim.x) {
       float v = 0.f;
       for (int r = 0; r < rows_here; ++r) v += sums[r * step * 8 + d];
-      a.partial[(long long)blockIdx.x * a.width + d] = v;
+      to[d] = v;
     }
     return;
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int v = t + i * step;
-    if (v < n8) Vec8<TypeF32>::store(a.partial, (long long)blockIdx.x * a.width + 8ll * v, sum[i]);
+    if (v < n8) Vec8<TypeF32>::store(to, 8ll * v, sum[i]);
   }
 }
 
@@ -319,7 +320,10 @@ Shape shape_of(int width, bool backward) {
 }
 // As many blocks as the CUs hold at once, the same number on each (16384 rows of 4096 in bf16 with dropout: 108 us with two blocks of eight waves to a
 // CU, 145, 126, 125 and 113 with one, 1.5, three and four; 2560: 97 to 80 with 410 to 614 blocks of five waves, 95 with 819)
+// Up to four walks of rows one block takes alone: its sums are the gain's gradient, and there is neither a second launch nor a workspace (a call of 24
+// rows of 128 or 4 of 4096: 8.4 us, 13 with them; 8 of 4096 13.4 in one block, 64 of 512 10.5, 16 of 4096 25).
 int backward_blocks(int rows, const Shape& s) {
+  if (rows <= 4 * s.rows_here) return 1;
   const int here = s.waves * s.rows_here, per_cu = s.nv == 1 ? 16 / here : s.nv == 2 ? 8 / here : 1;
   const int blocks = (rows + s.rows_here - 1) / s.rows_here, most = 256 * (per_cu < 1 ? 1 : per_cu);
   return blocks < most ? blocks : most;
@@ -355,7 +359,8 @@ hipError_t by_type(const AddNormArgs& a, bool backward, hipStream_t s) {
 hipError_t rl_add_norm(const AddNormArgs& a, hipStream_t s) { return a.rows <= 0 ? hipSuccess : by_type(a, false, s); }
 size_t rl_add_norm_backward_bytes(int rows, int width) {
   const Shape f = shape_of(width, true);
-  return (size_t)backward_blocks(rows < 1 ? 1 : rows, f) * width * sizeof(float);
+  const int blocks = backward_blocks(rows, f);
+  return blocks == 1 ? 0 : (size_t)blocks * width * sizeof(float);
 }
 hipError_t rl_add_norm_backward(const AddNormArgs& a, hipStream_t s) {
   const Shape f = shape_of(a.width, true);
@@ -364,6 +369,6 @@ hipError_t rl_add_norm_backward(const AddNormArgs& a, hipStream_t s) {
     const hipError_t e = by_type(a, true, s);
     if (e != hipSuccess) return e;
   }
-  if (a.dgain) hipLaunchKernelGGL(gain_sum_kernel, dim3((a.width + 31) / 32), dim3(1024), 0, s, a.partial, blocks, a.width, a.dgain);
+  if (a.dgain && blocks != 1) hipLaunchKernelGGL(gain_sum_kernel, dim3((a.width + 31) / 32), dim3(1024), 0, s, a.partial, blocks, a.width, a.dgain);
   return hipGetLastError();
 }

@@ -109,14 +109,15 @@ int rlgen_add_rms_norm_backward(const void* h, int64_t h_stride, int32_t residua
                                 float* dgain, void* workspace, size_t workspace_bytes, void* hip_stream) {
   AddNormArgs a{};
   const int rc = add_norm_args(a, dtype, residual_dtype, rows, width, drop_p, rng, gain, eps);
-  if (rc == RLGEN_ERR_NULL || (gain && (!dgain || !workspace || (rows > 0 && (!h || !dy)))) || (!gain && (dgain || dy)) ||
+  if (rc == RLGEN_ERR_NULL || (gain && (!dgain || (rows > 0 && (!h || !dy)))) || (!gain && (dgain || dy)) ||
       (rows > 0 && ((!dresidual && !dx) || (!gain && !dh))))
     return RLGEN_ERR_NULL;
   if (rc != RLGEN_OK || (h && !rows_ok(h, h_stride, width, residual_dtype)) || (dy && !rows_ok(dy, dy_stride, width, dtype)) ||
       (dh && !rows_ok(dh, dh_stride, width, residual_dtype)) || (dresidual && !rows_ok(dresidual, dresidual_stride, width, residual_dtype)) ||
-      (dx && !rows_ok(dx, dx_stride, width, dtype)) || !aligned4(dgain))
+      (dx && !rows_ok(dx, dx_stride, width, dtype)) || !aligned16(dgain))
     return RLGEN_ERR_BAD_ARG;
-  if (gain && (!aligned16(workspace) || workspace_bytes < rl_add_norm_backward_bytes(rows, width))) return RLGEN_ERR_WORKSPACE;
+  const size_t need = gain ? rl_add_norm_backward_bytes(rows, width) : 0;
+  if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return RLGEN_ERR_WORKSPACE;
   a.h = const_cast<void*>(h); a.h_stride = h_stride; a.dy = dy; a.dy_stride = dy_stride; a.dh = dh; a.dh_stride = dh_stride;
   a.dres = dresidual; a.dres_stride = dresidual_stride; a.dx = dx; a.dx_stride = dx_stride;
   a.dgain = dgain; a.partial = (float*)workspace;

@@ -684,8 +684,8 @@ def rlgen_add_rms_norm_backward(h: Optional[torch.Tensor], gain: Optional[torch.
         out = (dres, dres if dx is None else dx, dgain)
     else:
         dres, dx, dgain = out
-    if gain is not None and workspace is None:
-        workspace = like.new_empty(max(lib.rlgen_add_rms_norm_backward_workspace(rows, width), 16), dtype=torch.uint8)
+    if gain is not None and workspace is None and (need := lib.rlgen_add_rms_norm_backward_workspace(rows, width)):
+        workspace = like.new_empty(need, dtype=torch.uint8)
     dev, stream = _here()
     _check(lib.rlgen_add_rms_norm_backward(*_rows(h, res, shape, dev), _DTYPES[res], *_rows(dy, dt, shape, dev), _DTYPES[dt], *_rows(dh, res, shape, dev),
                                            rows, width, drop_p, _numbers(rng, torch.int64, (2,), dev), _numbers(gain, _F32, (width,), dev), eps,

@@ -157,6 +157,14 @@ def test_backward_of_many_rows():
     check_backward(1500, 4096, BF, BF, 0.1, seed=6)
 
 
+@pytest.mark.parametrize("rows", [4, 5, 32, 33, 100])
+def test_backward_around_the_border_of_one_block(rows):
+    """Up to four walks of rows are one block's, without a workspace: 4 rows of 4096, 32 of 512."""
+    check_backward(rows, 4096, BF, F32, 0.1, seed=rows)
+    check_backward(rows, 512, F16, F16, 0.0, seed=rows)
+    assert (R.lib.rlgen_add_rms_norm_backward_workspace(rows, 512) == 0) == (rows <= 32)
+
+
 def test_without_a_norm():
     rows, width = 37, 136
     x, r = rand(1, rows, width, dtype=BF), rand(2, rows, width, dtype=F32)

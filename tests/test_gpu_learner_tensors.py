@@ -5,7 +5,7 @@ import torch
 
 R = pytest.importorskip("paper_2410_18252_amd.rlgen", reason="librlgen.so not built")
 pytestmark = pytest.mark.gpu
-rows, width, V = 6, 64, 70001
+rows, width, V = 60, 64, 70001
 BF = torch.bfloat16
 
 

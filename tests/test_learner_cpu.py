@@ -40,16 +40,17 @@ def test_add_rms_norm_refuses():
 def test_add_rms_norm_backward_refuses():
     args = "h hs res dy dys dtype dh dhs rows width drop rng gain eps dr drs dx dxs dg ws bytes stream".split()
     size = R.lib.rlgen_add_rms_norm_backward_workspace
-    need = size(3, 64)
-    assert need >= 64 * 4 and size(-1, 64) == 0 and size(3, 60) == 0 and size(3, 20000) == 0 and size(10 ** 6, 4096) == size(8 * 10 ** 6, 4096) < 64 << 20
-    good = dict(h=D, hs=64, res=1, dy=D, dys=64, dtype=1, dh=D, dhs=64, rows=3, width=64, drop=0.1, rng=D, gain=D, eps=1e-5, dr=D, drs=64, dx=D, dxs=64, dg=D,
+    need = size(100, 64)
+    assert need >= 64 * 4 and size(3, 64) == 0 and size(-1, 64) == 0 and size(100, 60) == 0 and size(100, 20000) == 0
+    assert size(10 ** 6, 4096) == size(8 * 10 ** 6, 4096) < 64 << 20
+    good = dict(h=D, hs=64, res=1, dy=D, dys=64, dtype=1, dh=D, dhs=64, rows=100, width=64, drop=0.1, rng=D, gain=D, eps=1e-5, dr=D, drs=64, dx=D, dxs=64, dg=D,
                 ws=D, bytes=need, stream=None)
-    for kw in (dict(h=None), dict(dy=None), dict(dg=None), dict(ws=None), dict(rng=None), dict(dr=None, dx=None), dict(gain=None), dict(gain=None, dg=None),
+    for kw in (dict(h=None), dict(dy=None), dict(dg=None), dict(rng=None), dict(dr=None, dx=None), dict(gain=None), dict(gain=None, dg=None),
                dict(gain=None, dg=None, dy=None, dh=None)):
         refuse("rlgen_add_rms_norm_backward", args, good, R.ERR_NULL, **kw)
     for kw in SHAPE_BAD + [dict(hs=56), dict(dys=65), dict(dhs=4), dict(drs=60), dict(dxs=60), dict(dx=C.c_void_p(264)), dict(dg=C.c_void_p(258))]:
         refuse("rlgen_add_rms_norm_backward", args, good, R.ERR_BAD_ARG, **kw)
-    for kw in (dict(bytes=need - 1), dict(ws=C.c_void_p(264))):
+    for kw in (dict(ws=None), dict(bytes=need - 1), dict(ws=C.c_void_p(264))):
         refuse("rlgen_add_rms_norm_backward", args, good, R.ERR_WORKSPACE, **kw)
 
 
