@@ -127,6 +127,7 @@ struct Found {
 };
 
 template <class F> __device__ __forceinline__ void note_hits(const float* kept, int steps, int threads, F&& wanted, Found& f) {
+#pragma unroll 4
   for (int step = 0; step < steps; ++step)
     if (wanted(kept[step * threads + threadIdx.x])) {
       const int i = atomicAdd(&f.hits, 1);
@@ -449,8 +450,8 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
             for (int e = 0; e < N; ++e)
               if (s0[u][e] >= least && u * T + (int)threadIdx.x < c.full) take(s0[u][e], c.first + (u * T + (int)threadIdx.x) * N + e);
       } else {
-        // a thread to every value of the steps noted, four of them requested at once
-        constexpr int B = 4;
+        // a thread to every value of the steps noted, eight of them requested at once
+        constexpr int B = 8;
         const int all = hits * U * N;
         for (int i0 = threadIdx.x; i0 < all; i0 += T * B) {
           float v[B];
