@@ -28,7 +28,7 @@ struct LogprobArgs {
   const int* tokens; float temperature;
   float *logprobs, *stats, *entropy;
   int n_top; int* top_tokens; float* top_logprobs;
-  float4* partial; uint64_t* part_keys; // of rows that are parted: largest value and sums, and n_top keys, of each part
+  float4* partial; uint64_t* part_keys; // of rows that are parted: two of numbers, and n_top keys, of each part
   // backward
   const float *g, *g_entropy;
   void* dlogits; long long d_stride;

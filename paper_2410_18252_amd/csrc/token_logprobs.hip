@@ -209,14 +209,22 @@ template <class E, int T> __device__ void select_top(const void* row, const Cut&
   fill_equal<E, T>(row, c, vocab, n, least, f.above, f);
 }
 
-// A row's numbers from the largest value and the sums relative to it: sum of 2^y, and of y 2^y
-__device__ __forceinline__ void finish(const LogprobArgs& a, long long row, float M, float sum, float along, float z_token) {
-  const bool empty = M == -INFINITY && sum == 0.f;
-  const float log_sum = logf(sum);               // (-infinity for a row that is masked as a whole)
-  if (a.logprobs) a.logprobs[row] = empty ? -INFINITY : (z_token - M) / a.temperature - log_sum;
-  a.stats[2 * row] = M;
+// What a row adds up to: its largest value, the sum of the terms 2^y, and that of y 2^y.  In a row that is all but decided the largest value's own term, 1,
+// is counted (once) and not among the sums: beside it the others would keep few of their bits.
+struct Sums { float M, count, sum, along; };
+__device__ __forceinline__ bool all_masked(const Sums& s) { return s.M == -INFINITY && s.sum == 0.f; }
+__device__ __forceinline__ float log_sum_of(const Sums& s) {
+  // (log(1 + x) as log(u) x / (u - 1) with u = 1 + x rounded, which makes up for the rounding; -infinity for a row that is masked as a whole)
+  const float u = s.count + s.sum, l = logf(u);
+  return s.count == 1.f && u < 2.f ? (u == 1.f ? s.sum : l * (s.sum / (u - 1.f))) : l;
+}
+__device__ __forceinline__ void finish(const LogprobArgs& a, long long row, const Sums& s, float z_token) {
+  const bool empty = all_masked(s);
+  const float log_sum = log_sum_of(s);
+  if (a.logprobs) a.logprobs[row] = empty ? -INFINITY : (z_token - s.M) / a.temperature - log_sum;
+  a.stats[2 * row] = s.M;
   a.stats[2 * row + 1] = log_sum;
-  if (a.entropy) a.entropy[row] = empty ? 0.f : log_sum - along / sum * LN2;
+  if (a.entropy) a.entropy[row] = empty ? 0.f : log_sum - s.along / (s.count + s.sum) * LN2;
 }
 // An alternative's place in the result
 struct Likely {
@@ -228,7 +236,7 @@ struct Likely {
     a.top_logprobs[at] = empty ? -INFINITY : (value_of((uint32_t)(key >> 32)) - M) / temperature - log_sum;
   }
 };
-__device__ __forceinline__ Likely likely_of(float M, float sum, float temperature) { return {M, logf(sum), temperature, M == -INFINITY && sum == 0.f}; }
+__device__ __forceinline__ Likely likely_of(const Sums& s, float temperature) { return {s.M, log_sum_of(s), temperature, all_masked(s)}; }
 // Each key's place among them all, for those among the first n
 template <class F> __device__ __forceinline__ void rank_keys(const uint64_t* keys, int have, int n, int threads, F&& put) {
   for (int i = threadIdx.x; i < have; i += threads) {
@@ -325,10 +333,8 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
 #pragma unroll
       for (int e = 0; e < N; ++e) most = fmaxf(most, s[u][e]);
     rise(most);
-    if (TOP) {
-      own = fmaxf(own, most);
-      if (!ONE && step < steps_kept) kept[step * T + threadIdx.x] = most;
-    }
+    own = fmaxf(own, most);
+    if (TOP && !ONE && step < steps_kept) kept[step * T + threadIdx.x] = most;
     // a step's own sums, so that a masked value (0 times minus infinity in the second) shows there, and is left out in a second go
     float step_sum = 0.f, step_along = 0.f;
     if (near && whole) {
@@ -388,18 +394,19 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
 #pragma unroll
   for (int w = 1; w < WAVES; ++w) M = fmaxf(M, red[0][w]);
   {
-    // `off` out of both sums (by division, so that a row with a single token sums up to exactly 1; what the second one's rounding leaves is none of it)
-    const float one = __builtin_amdgcn_exp2f(off), rest = fmaf(-off, sum, along);
-    along = fabsf(rest) <= 0x1p-22f * fabsf(off) * sum ? 0.f : rest / one;
+    // `off` out of both sums (by division, so that a term of 1 is exactly that)
+    const float one = __builtin_amdgcn_exp2f(off);
+    along = fmaf(-off, sum, along) / one;
     sum /= one;
     const float by = m == M ? 0.f : (m - M) * scale;      // (both -infinity: nothing to shift)
     const float f = __builtin_amdgcn_exp2f(by);
     along = f > 0.f ? fmaf(sum, by, along) * f : 0.f;
     sum *= f;
   }
-  sum = lanes_sum(sum);
-  along = lanes_sum(along);
-  if (lane == 0) { red[1][wave] = sum; red[2][wave] = along; }
+  {
+    const float wave_sum = lanes_sum(sum), wave_along = lanes_sum(along);
+    if (lane == 0) { red[1][wave] = wave_sum; red[2][wave] = wave_along; }
+  }
   float least = -INFINITY;
   if constexpr (TOP) {
     // every busy wave has its share of n values that are not below the smallest of their bounds
@@ -409,16 +416,50 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
     if (!ONE && steps <= steps_kept && own >= least) note_hits(kept, steps, T, [&](float v) { return v >= least; }, found);
   }
   __syncthreads();
-  sum = along = 0.f;
+  Sums all = {M, 0.f, 0.f, 0.f};
+  auto add_waves = [&]() {
+    all.sum = all.along = 0.f;
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) { sum += red[1][w]; along += red[2][w]; }
+    for (int w = 0; w < WAVES; ++w) { all.sum += red[1][w]; all.along += red[2][w]; }
+  };
+  add_waves();
+  if (all.sum < 1.0625f && all.sum >= 1.f) {
+    // All but decided: the one lane that has the largest value added up small terms beside 1.  Its wave goes over that lane's values again, a piece to a lane,
+    // without the largest (the block comes here as one, and so does the wave).
+    __syncthreads();
+    const unsigned long long which = __ballot(own == M);
+    if (which) {
+      const int from = __ffsll((long long)which) - 1, thread = wave * 64 + from;
+      if (lane == from) sum = along = 0.f;
+      auto again = [&](float v) {
+        const float y = (v - M) * scale, e = v == M ? 0.f : __builtin_amdgcn_exp2f(y);
+        sum += e;
+        along = fmaf(e, fmaxf(y, LOWEST), along);
+      };
+      for (int k = lane * T + thread; k < c.full; k += 64 * T) {
+        const Some<E> s = Some<E>::load(z, c.first + (long long)k * N);
+#pragma unroll
+        for (int e = 0; e < N; ++e) again(s[e]);
+      }
+      if (lane == from) again(at_edge);
+      const float wave_sum = lanes_sum(sum), wave_along = lanes_sum(along);
+      if (lane == 0) { red[1][wave] = wave_sum; red[2][wave] = wave_along; }
+    }
+    __syncthreads();
+    add_waves();
+    all.count = 1.f;
+  }
   if (parts > 1) {
-    if (threadIdx.x == 0) a.partial[(long long)row * parts + part] = make_float4(M, sum, along, z_token);
+    if (threadIdx.x == 0) {
+      float4* to = a.partial + 2 * ((long long)row * parts + part);
+      to[0] = make_float4(M, all.count, all.sum, all.along);
+      to[1] = make_float4(z_token, 0.f, 0.f, 0.f);
+    }
   } else if (threadIdx.x == 0) {
-    finish(a, row, M, sum, along, z_token);
+    finish(a, row, all, z_token);
   }
   if constexpr (TOP) {
-    const bool known = sum == sum && steps <= steps_kept;          // (NaN, or an infinity, which makes one: the maxima passed over it)
+    const bool known = all.sum == all.sum && steps <= steps_kept;          // (NaN, or an infinity, which makes one: the maxima passed over it)
     int hits = found.hits;
     const bool crowded = hits > HITS;
     if (crowded && known) {
@@ -452,13 +493,13 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
       } else {
         // a thread to every value of the steps noted, eight of them requested at once
         constexpr int B = 8;
-        const int all = hits * U * N;
-        for (int i0 = threadIdx.x; i0 < all; i0 += T * B) {
+        const int values = hits * U * N;
+        for (int i0 = threadIdx.x; i0 < values; i0 += T * B) {
           float v[B];
           int at[B];
 #pragma unroll
           for (int b = 0; b < B; ++b) {
-            const int i = min(i0 + b * T, all - 1);
+            const int i = min(i0 + b * T, values - 1);
             const uint32_t hit = found.hit[i / (U * N)];
             const int k = ((int)(hit / T) * U + i % (U * N) / N) * T + (int)(hit % T);
             at[b] = i == i0 + b * T && k < c.full ? c.first + k * N + i % N : -1;
@@ -489,7 +530,7 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
       rank_keys(found.key, have, n, T, [&](uint64_t key, int rank) { keys[rank] = key; });
       for (int i = n + threadIdx.x; i < a.n_top; i += T) keys[i] = 0;        // (below every value's)
     } else {
-      const Likely l = likely_of(M, sum, a.temperature);
+      const Likely l = likely_of(all, a.temperature);
       rank_keys(found.key, have, n, T, [&](uint64_t key, int rank) { l.put(a, row, rank, key); });
     }
   }
@@ -499,16 +540,18 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
 constexpr int MOST_PARTS = 8;
 __global__ __launch_bounds__(256) void token_logprobs_join_kernel(LogprobArgs a, int parts) {
   __shared__ uint64_t keys[MOST_PARTS * MOST_TOP];
-  __shared__ int count;
+  __shared__ int found;
   const int row = blockIdx.x, lane = threadIdx.x & 63;
   const int token = a.tokens ? a.tokens[row] : 0;
   if (a.tokens && (token < 0 || token >= a.vocab)) {
     leave_out<true>(a, row);
     return;
   }
-  if (threadIdx.x == 0) count = 0;
+  if (threadIdx.x == 0) found = 0;
   const bool on = lane < parts;
-  const float4 p = on ? a.partial[(long long)row * parts + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  const float4* of = a.partial + 2 * ((long long)row * parts + lane);
+  const float4 p = on ? of[0] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  const float z_token = on ? of[1].x : 0.f;
   const int share = (a.n_top + parts - 1) / parts;
   const uint64_t* from = a.part_keys + (long long)row * parts * a.n_top;
   // every part has `share` values that are not below the smallest of the parts' bounds
@@ -520,18 +563,25 @@ __global__ __launch_bounds__(256) void token_logprobs_join_kernel(LogprobArgs a,
   }
   bound = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(bound >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)bound);
   const float M = lanes_max(p.x), scale = LOG2E / a.temperature;
-  const float by = p.x == M ? 0.f : (p.x - M) * scale, f = __builtin_amdgcn_exp2f(by);
-  const float sum = lanes_sum(p.y * f), along = lanes_sum(f > 0.f ? fmaf(p.y, by, p.z) * f : 0.f);
-  if (threadIdx.x == 0) finish(a, row, M, sum, along, p.w);
+  float count = p.y, sum = p.z, along = p.w;
+  if (p.x != M) {
+    const float by = (p.x - M) * scale, f = __builtin_amdgcn_exp2f(by);
+    sum += count;
+    count = 0.f;
+    along = f > 0.f ? fmaf(sum, by, along) * f : 0.f;
+    sum *= f;
+  }
+  const Sums all = {M, lanes_sum(count), lanes_sum(sum), lanes_sum(along)};
+  if (threadIdx.x == 0) finish(a, row, all, z_token);
   if (a.n_top == 0) return;
   __syncthreads();
   for (int i = threadIdx.x; i < parts * a.n_top; i += 256) {
     const uint64_t key = from[i];
-    if (key >= bound && key != 0) keys[atomicAdd(&count, 1)] = key;
+    if (key >= bound && key != 0) keys[atomicAdd(&found, 1)] = key;
   }
   __syncthreads();
-  const Likely l = likely_of(M, sum, a.temperature);
-  rank_keys(keys, count, a.n_top, 256, [&](uint64_t key, int rank) { l.put(a, row, rank, key); });
+  const Likely l = likely_of(all, a.temperature);
+  rank_keys(keys, found, a.n_top, 256, [&](uint64_t key, int rank) { l.put(a, row, rank, key); });
 }
 
 // Gradient: every value read once and written once, by the same thread, so that the gradient may take the logits' place.  Bound by HBM.
@@ -547,18 +597,28 @@ __global__ __launch_bounds__(GT) void token_logprobs_backward_kernel(LogprobArgs
   const bool none = (a.tokens && (token < 0 || token >= a.vocab)) || (m == -INFINITY && log_sum == -INFINITY);
   const float g = a.g ? a.g[row] : 0.f, h = a.g_entropy ? a.g_entropy[row] : 0.f, H = h != 0.f ? a.entropy[row] : 0.f;
   const float inv_t = 1.0f / a.temperature;
-  auto grad = [&](float v, int at) {
+  auto grad = [&](float v) {
     const float lp = (v - m) * inv_t - log_sum, p = __builtin_amdgcn_exp2f(lp * LOG2E);
     // (masked: p is 0 and its logarithm infinite)
-    float d = -p * fmaf(h, fmaxf(lp, -1000.f) + H, g);
-    if (at == token) d += g;
-    return none ? 0.f : d * inv_t;
+    return -p * fmaf(h, fmaxf(lp, -1000.f) + H, g) * inv_t;
+  };
+  // the token's own: g (1 - p) from the logarithm, as the difference would keep few bits where p is near 1
+  auto grad_token = [&](float v) {
+    const float lp = (v - m) * inv_t - log_sum, p = __builtin_amdgcn_exp2f(lp * LOG2E);
+    return fmaf(g, -expm1f(lp), -p * h * (fmaxf(lp, -1000.f) + H)) * inv_t;
   };
   const Cut c = cut_row<E>(z, a.vocab);
   if (part == 0) {
     const int edge = edge_of(c, a.vocab);
-    if (edge >= 0) Some<E>::store_one(dz, edge, grad(Some<E>::one(z, edge), edge));
+    if (edge >= 0) {
+      const float v = Some<E>::one(z, edge);
+      Some<E>::store_one(dz, edge, none ? 0.f : edge == token ? grad_token(v) : grad(v));
+    }
   }
+  // the thread that has the token's piece reads its logit ahead and writes its gradient over the piece's
+  const int k_token = token >= c.first && token < c.first + c.full * N ? (token - c.first) / N : -1;
+  const bool own = !none && k_token >= 0 && k_token / (GT * GU) % parts == part && k_token % GT == (int)threadIdx.x;
+  const float at_token = own ? Some<E>::one(z, token) : 0.f;
   for (int k0 = part * GT * GU; k0 < c.full; k0 += parts * GT * GU) {
     Some<E> s[GU];
 #pragma unroll
@@ -572,10 +632,11 @@ __global__ __launch_bounds__(GT) void token_logprobs_backward_kernel(LogprobArgs
       if (k >= c.full) continue;
       float y[N];
 #pragma unroll
-      for (int e = 0; e < N; ++e) y[e] = none ? 0.f : grad(s[u][e], c.first + k * N + e);
+      for (int e = 0; e < N; ++e) y[e] = none ? 0.f : grad(s[u][e]);
       Some<E>::template store<ONCE>(dz, c.first + (long long)k * N, y);
     }
   }
+  if (own) Some<E>::store_one(dz, token, grad_token(at_token));
 }
 
 // Threads to a block and blocks to a row.  Four waves to a row; one where that holds the whole row in a step and rows are many (8192 rows of 1000 bf16 values,
@@ -628,12 +689,12 @@ template <class E> hipError_t launch_backward(const LogprobArgs& a, hipStream_t 
 
 size_t rl_token_logprobs_bytes(const LogprobArgs& a) {
   const Shape f = shape_of(a);
-  return f.parts == 1 ? 0 : (size_t)a.rows * f.parts * (sizeof(float4) + a.n_top * sizeof(uint64_t));
+  return f.parts == 1 ? 0 : (size_t)a.rows * f.parts * (2 * sizeof(float4) + a.n_top * sizeof(uint64_t));
 }
 hipError_t rl_token_logprobs(LogprobArgs a, void* workspace, hipStream_t s) {
   if (a.rows <= 0) return hipSuccess;
   a.partial = (float4*)workspace;
-  a.part_keys = (uint64_t*)(a.partial + (size_t)a.rows * shape_of(a).parts);
+  a.part_keys = (uint64_t*)(a.partial + 2 * (size_t)a.rows * shape_of(a).parts);
   switch (a.dtype) {
     case RLGEN_DTYPE_F32: return by_rows<TypeF32>(a, s);
     case RLGEN_DTYPE_BF16: return by_rows<TypeBf16>(a, s);

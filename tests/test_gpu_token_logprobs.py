@@ -205,6 +205,39 @@ def test_temperatures():
         check(z, tokens_of(2, 4, 2000, skip=False), T, 3)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF, F16])
+@pytest.mark.parametrize("rows, V", [(7, 40), (7, 5000), (300, 1000), (70, 50304), (3, 70001)])
+def test_rows_that_are_all_but_decided(dtype, rows, V):
+    """The likeliest token stands 8 to 40 above the others: its log-prob is as small as the others' share R, and has R's relative error: that of a sum of V
+    small terms, (V / 256 + 64) U, and of their exponents, 4 U of 60 / T; the entropy is R times a mean exponent.  The gradient at the token is
+    g times that share.  Twice and thrice it stands there, nothing is small, and the plain bounds hold."""
+    T, gap = 0.8, torch.linspace(8, 32, rows).round()
+    z = rand(V, rows, V, dtype=dtype, scale=0.5).clamp(-2, 2)
+    at = torch.randint(0, V, (rows,), generator=torch.Generator().manual_seed(V))
+    z[torch.arange(rows), at] = (2 + gap).to(dtype)
+    r = R.rlgen_token_logprobs(placed(z, 3, 1), at.int().cuda(), T)
+    lp, H, m, ls = L.logprobs(z, T)
+    x = (z.double() - m[:, None]) / T
+    others = torch.exp(x)
+    others[torch.arange(rows), at] = 0
+    share = torch.log1p(others.sum(-1))                          # (1 - p as the sum of the others, which is exact to 64 bits)
+    rel = (V / 256 + 64) * U + 4 * U * 60 / T
+    assert bool(((r.logprobs.double().cpu() + share).abs() <= rel * share + 1e-44).all())
+    H = share - (others * x).sum(-1) / (1 + others.sum(-1))
+    assert bool(((r.entropy.double().cpu() - H).abs() <= 2 * rel * H + 1e-44).all())
+    g = rand(3, rows, scale=1.0)
+    d = R.rlgen_token_logprobs_backward(z.cuda(), at.int().cuda(), T, r.stats, g.cuda())
+    want = g.double() * others.sum(-1) / (1 + others.sum(-1)) / T
+    e, tiny = torch.finfo(dtype).eps / 2, torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps / 2
+    got = d[torch.arange(rows), at.cuda()].double().cpu()
+    assert bool(((got - want).abs() <= (e + 2 * rel + 8 * U) * want.abs() + tiny).all())
+    if V > 100:
+        for n in (2, 3):
+            for i in range(1, n):
+                z[torch.arange(rows), (at + 37 * i) % V] = (2 + gap).to(dtype)
+            check(z, at, T, 3)
+
+
 def test_values_far_from_zero():
     """Logits near the type's ends: only their differences count."""
     for dtype, at in ((F32, 3e4), (F32, -3e4), (F16, 6e4), (BF, 3e38), (BF, -3e38)):
