@@ -446,9 +446,9 @@ int rlgen_add_rms_norm(const void *x, int64_t x_stride, int32_t dtype, const voi
 
 /* Its gradients, from h as rlgen_add_rms_norm returned it, dy (type dtype) and dh (nullable, type residual_dtype: the gradient that reaches h past
  * the norm): dresidual (nullable, residual_dtype) = the gradient of h, dx (nullable, dtype) = the same through the dropout (drop_p and rng as
- * they were), dgain [width] fp32 (the sum over all rows, padding rows among them).  gain null: no norm was taken, dy and dgain are null too and h is not read.  dresidual may be dh itself, dx may be dy
- * itself.  workspace: 16-byte aligned, rlgen_add_rms_norm_backward_workspace(rows, width) bytes (0, and it may be null, for few rows; null
- * without a gain).
+ * they were), dgain [width] fp32 (the sum over all rows, padding rows among them).  gain null: no norm was taken, dy and dgain are null too and h is
+ * not read.  dresidual may be dh itself, dx may be dy itself.  workspace: 16-byte aligned, rlgen_add_rms_norm_backward_workspace(rows, width)
+ * bytes (0, and it may be null, for few rows; null without a gain).
  * Errors: NULL, BAD_ARG, WORKSPACE, DEVICE. */
 size_t rlgen_add_rms_norm_backward_workspace(int32_t rows, int32_t width);
 int rlgen_add_rms_norm_backward(const void *h, int64_t h_stride, int32_t residual_dtype, const void *dy, int64_t dy_stride, int32_t dtype,
