@@ -421,6 +421,7 @@ int rlgen_window_attention_paged(const void *q, int64_t q_stride, int32_t dtype,
  *  - Rows of the norm: width elements, a multiple of 8 up to 16384, any row stride (in elements) that is a multiple of 8 (fp32: 4), bases and gains
  *    16-byte aligned, fewer than 2^23 rows.
  *  - Rows of logits: vocab elements, at most 2^24, any row stride from vocab on and any base that suits the element type, fewer than 2^24 rows.
+ *  - A workspace serves one call at a time: calls that may overlap (on two streams, in two captured graphs) need their own.
  *  - Without rows (0) an operator returns at once, the gain's gradient is zeroed, and pointers to tensors of rows may be null. */
 
 /* h = residual + dropout(x) and y = RMS norm of h times the gain, in one pass.

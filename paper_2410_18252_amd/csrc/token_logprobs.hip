@@ -299,7 +299,7 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
   // y is then `off`, known exactly and taken out at the end.  (Where base scale is so large that off would be: y = (v - base) scale.)
   float m = -INFINITY, own = at_edge, sum = 0.f, along = 0.f;     // m: of the wave, own: of this lane
   float base = 0.f, shift = 0.f, off = 0.f;                       // base: m, or 0 before there is one
-  bool near = true;
+  bool near = true, masks = false;                                // masks: this wave has met masked values
   auto rise = [&](float most) {                                   // m to the largest of the lanes'
     if (!__any(most > m)) return;
     const float up = lanes_max(fmaxf(most, m)), before = off;
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
     if (TOP && !ONE && step < steps_kept) kept[step * T + threadIdx.x] = most;
     // a step's own sums, so that a masked value (0 times minus infinity in the second) shows there, and is left out in a second go
     float step_sum = 0.f, step_along = 0.f;
-    if (near && whole) {
+    if (near && whole && !masks) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -347,7 +347,8 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
           step_along = fmaf(f, y, step_along);
         }
     }
-    if (!near || !whole || __any(step_along != step_along)) {
+    if (!near || !whole || masks || __any(step_along != step_along)) {
+      masks |= near && whole;                    // (where some are, there are more as a rule: the next steps take this way at once)
 #pragma unroll
       for (int u = 0; u < U; ++u) s[u].opaque();           // (widened again: kept, they would cost every step 30 registers)
       const float sum_before = sum, along_before = along;
