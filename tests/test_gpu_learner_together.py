@@ -56,6 +56,34 @@ def test_from_rows_to_gradients(drop, T):
         assert float((got.double().cpu() - w).norm()) <= 1000 * 32 * 2.0 ** -24 * float(w.norm()), name
 
 
+def test_calls_on_two_streams_at_once():
+    """Each stream's calls, parted rows and a two-launch gradient among them, give what they give alone."""
+    def work(seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        z, x = torch.randn(5, 90001, generator=g, device="cuda").bfloat16(), torch.randn(700, 1032, generator=g, device="cuda").bfloat16()
+        tok, gain = torch.arange(5, dtype=torch.int32, device="cuda"), torch.randn(1032, generator=g, device="cuda")
+        rng = torch.tensor([seed, 1], dtype=torch.int64, device="cuda")
+
+        def run():
+            r = R.rlgen_token_logprobs(z, tok, 0.7, n_top=9)
+            d = R.rlgen_token_logprobs_backward(z, tok, 0.7, r.stats, r.entropy)
+            h, y = R.rlgen_add_rms_norm(x, gain, 1e-5, drop_p=0.3, rng=rng)
+            return [*r, d, h, y, *R.rlgen_add_rms_norm_backward(h, gain, 1e-5, y, drop_p=0.3, rng=rng)]
+        return run
+
+    runs = [work(1), work(2)]
+    want = [run() for run in runs]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [[], []]
+    for _ in range(10):
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(runs[i]())
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        assert all(torch.equal(a, b) for result in got[i] for a, b in zip(result, want[i]))
+
+
 @pytest.fixture(scope="module")
 def example():
     spec = importlib.util.spec_from_file_location("dpo_step", os.path.join(ROOT, "examples", "dpo_step.py"))
