@@ -7,6 +7,7 @@ kernels.  There is no fallback: if the shared library is missing, importing this
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Dict, NamedTuple, Optional
 
@@ -600,9 +601,12 @@ _E4M3 = torch.float8_e4m3fn
 _NORM_DTYPES = {**_DTYPES, _E4M3: DTYPE_E4M3}
 
 
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)       # (the former without its check for a first use: there are tensors)
+
+
 def _here():
     """The current device, on which every tensor has to be, and its current stream."""
-    device = torch.cuda.current_device()
+    device = _device()
     return device, torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(device)
 
 
@@ -624,9 +628,9 @@ def _numbers(t: Optional[torch.Tensor], dtype: torch.dtype, shape, device: int):
     return t.data_ptr()
 
 
-def _made_here(t: Optional[torch.Tensor], *_):
-    """The same of a tensor that the binding has just made."""
-    return None if t is None else t.data_ptr()
+# bytes by sizes alone: a lookup instead of a call
+_norm_backward_bytes = functools.lru_cache(256)(lib.rlgen_add_rms_norm_backward_workspace)
+_logprobs_bytes = functools.lru_cache(256)(lib.rlgen_token_logprobs_workspace)
 
 
 def _scratch(t: Optional[torch.Tensor], device: int):
@@ -684,7 +688,7 @@ def rlgen_add_rms_norm_backward(h: Optional[torch.Tensor], gain: Optional[torch.
         out = (dres, dres if dx is None else dx, dgain)
     else:
         dres, dx, dgain = out
-    if gain is not None and workspace is None and (need := lib.rlgen_add_rms_norm_backward_workspace(rows, width)):
+    if gain is not None and workspace is None and (need := _norm_backward_bytes(rows, width)):
         workspace = like.new_empty(need, dtype=torch.uint8)
     dev, stream = _here()
     _check(lib.rlgen_add_rms_norm_backward(*_rows(h, res, shape, dev), _DTYPES[res], *_rows(dy, dt, shape, dev), _DTYPES[dt], *_rows(dh, res, shape, dev),
@@ -709,22 +713,25 @@ def rlgen_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = 
     """logits [rows, vocab] (fp32, bf16 or fp16; any row stride), tokens [rows] int32 or None.  A row whose token lies outside the vocabulary is skipped.
     `out`: a TokenLogprobs (or tuple) of tensors to fill; entropy and n_top are then what it holds."""
     shape = rows, vocab = logits.shape
-    numbers = _numbers if out is not None else _made_here
+    dev, stream = _here()
     if out is None:
         new = logits.new_empty
-        out = TokenLogprobs(None if tokens is None else new(rows, dtype=_F32), new(rows, dtype=_F32) if entropy else None, new((rows, 2), dtype=_F32),
-                            new((rows, n_top), dtype=_I32) if n_top else None, new((rows, n_top), dtype=_F32) if n_top else None)
-    lp, ent, stats, ids, top = out
-    n_top = 0 if ids is None else ids.shape[1]
-    assert (top is None) == (ids is None)
+        lp, ent, stats = None if tokens is None else new(rows, dtype=_F32), new(rows, dtype=_F32) if entropy else None, new((rows, 2), dtype=_F32)
+        ids, top = (new((rows, n_top), dtype=_I32), new((rows, n_top), dtype=_F32)) if n_top else (None, None)
+        out = TokenLogprobs(lp, ent, stats, ids, top)
+        where = (None if lp is None else lp.data_ptr(), stats.data_ptr(), None if ent is None else ent.data_ptr(), n_top,
+                 None if ids is None else ids.data_ptr(), None if top is None else top.data_ptr())
+    else:
+        lp, ent, stats, ids, top = out
+        n_top = 0 if ids is None else ids.shape[1]
+        assert (top is None) == (ids is None)
+        where = (_numbers(lp, _F32, (rows,), dev), _numbers(stats, _F32, (rows, 2), dev), _numbers(ent, _F32, (rows,), dev), n_top,
+                 _numbers(ids, _I32, (rows, n_top), dev), _numbers(top, _F32, (rows, n_top), dev))
     dt = _DTYPES[logits.dtype]
-    if workspace is None and (need := lib.rlgen_token_logprobs_workspace(dt, rows, vocab, n_top)):
+    if workspace is None and (need := _logprobs_bytes(dt, rows, vocab, n_top)):
         workspace = logits.new_empty(need, dtype=torch.uint8)
-    dev, stream = _here()
-    _check(lib.rlgen_token_logprobs(*_rows(logits, logits.dtype, shape, dev), dt, rows, vocab, _numbers(tokens, _I32, (rows,), dev), temperature,
-                                    numbers(lp, _F32, (rows,), dev), numbers(stats, _F32, (rows, 2), dev), numbers(ent, _F32, (rows,), dev), n_top,
-                                    numbers(ids, _I32, (rows, n_top), dev), numbers(top, _F32, (rows, n_top), dev), *_scratch(workspace, dev), stream),
-           "rlgen_token_logprobs")
+    _check(lib.rlgen_token_logprobs(*_rows(logits, logits.dtype, shape, dev), dt, rows, vocab, _numbers(tokens, _I32, (rows,), dev), temperature, *where,
+                                    *_scratch(workspace, dev), stream), "rlgen_token_logprobs")
     return out if type(out) is TokenLogprobs else TokenLogprobs(lp, ent, stats, ids, top)
 
 
