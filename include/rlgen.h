@@ -487,8 +487,10 @@ int rlgen_token_logprobs_backward(const void *logits, int64_t stride, int32_t dt
  *  loss [B]          -log sigmoid(beta ((sum pol - sum ref over y+) - (sum pol - sum ref over y-)))
  *  dlogprobs [rows]  the gradient of weight * sum of the losses to token_logprobs: one value on y+'s rows, its negative on y-'s, 0 on the other
  *                    sequences'; rows that no sequence has are left as they are
- * idx_pos[b] == idx_neg[b] is a pair without a difference: log 2 and zeros.  Indices and row starts outside their ranges are clamped.  Sums
- * and the loss are formed in fp64.  All DEVICE.  Errors: NULL, BAD_ARG (B or k < 1, B >= 2^22, beta or weight not finite), DEVICE. */
+ * idx_pos[b] == idx_neg[b] is a pair without a difference, whatever its log-probs: log 2 and zeros.  A sum that is infinite or NaN (a masked token's log-prob
+ * is -infinity) gives its own pair's loss and rows their limits, or NaN where there is none (-infinity in both models), and no other rows anything.
+ * Indices and row starts outside their ranges are clamped.  Sums and the loss are formed in fp64.  All DEVICE.
+ * Errors: NULL, BAD_ARG (B or k < 1, B >= 2^22, beta or weight not finite), DEVICE. */
 int rlgen_dpo_pairs(const float *token_logprobs, const float *ref_logprobs, int32_t rows, const int32_t *row_starts, int32_t B, int32_t k,
                     const int32_t *idx_pos, const int32_t *idx_neg, float beta, float weight, float *loss, float *dlogprobs,
                     void *hip_stream);

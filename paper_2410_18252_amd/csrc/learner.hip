@@ -36,11 +36,13 @@ template <int T> __global__ __launch_bounds__(T) void dpo_pairs_kernel(PairArgs 
     sums[0] += part[0][w];
     sums[1] += part[1][w];
   }
-  const double x = (double)a.beta * (sums[0] - sums[1]);
+  const bool same = which[0] == which[1];       // no difference, whatever the log-probs are
+  const double x = same ? 0.0 : (double)a.beta * (sums[0] - sums[1]);
   if (threadIdx.x == 0) a.loss[b] = (float)(fmax(-x, 0.0) + log1p(exp(-fabs(x))));
   const float step = (float)((double)a.weight * a.beta / (1.0 + exp(x)));
   for (int i = 0; i < a.k; ++i) {
-    const float g = step * (float)((i == which[1]) - (i == which[0]));
+    // (chosen, not multiplied: a step of NaN or infinity is the pair's alone)
+    const float g = same ? 0.f : i == which[0] ? -step : i == which[1] ? step : 0.f;
     const int end = from(i + 1);
     for (int r = from(i) + threadIdx.x; r < end; r += T) a.grad[r] = g;
   }
