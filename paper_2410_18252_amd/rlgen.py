@@ -754,9 +754,10 @@ def rlgen_token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.T
 def rlgen_dpo_pairs(token_logprobs: torch.Tensor, ref_logprobs: torch.Tensor, row_starts: torch.Tensor, idx_pos: torch.Tensor, idx_neg: torch.Tensor,
                     k: int, beta: float, weight: float = 1.0, out=None):
     """token_logprobs, ref_logprobs [rows] fp32 of packed sequences, row_starts [B k + 1], idx_pos and idx_neg [B] int32.  Returns (loss [B], the gradient
-    of weight times the losses' sum to token_logprobs [rows]); `out`: the two to write into.  Rows that no sequence has are not written."""
+    of weight times the losses' sum to token_logprobs [rows]).  Rows that no sequence has are 0; with `out`, the two to write into, they are left as they
+    are, and the launch that zeroes them falls away."""
     rows, B = token_logprobs.numel(), idx_pos.numel()
-    loss, grad = out if out is not None else (token_logprobs.new_empty(B), token_logprobs.new_empty(rows))
+    loss, grad = out if out is not None else (token_logprobs.new_empty(B), token_logprobs.new_zeros(rows))
     dev, stream = _here()
     _check(lib.rlgen_dpo_pairs(_numbers(token_logprobs, _F32, (rows,), dev), _numbers(ref_logprobs, _F32, (rows,), dev), rows,
                                _numbers(row_starts, _I32, (B * k + 1,), dev), B, k, _numbers(idx_pos, _I32, (B,), dev), _numbers(idx_neg, _I32, (B,), dev), beta,
