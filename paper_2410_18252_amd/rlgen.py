@@ -633,6 +633,9 @@ _norm_backward_bytes = functools.lru_cache(256)(lib.rlgen_add_rms_norm_backward_
 _logprobs_bytes = functools.lru_cache(256)(lib.rlgen_token_logprobs_workspace)
 
 
+_MOST_INT = 2 ** 31 - 1      # (ctypes keeps the low 32 bits of what is larger)
+
+
 def _scratch(t: Optional[torch.Tensor], device: int):
     if t is None:
         return None, 0
@@ -648,6 +651,7 @@ def rlgen_add_rms_norm(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float
     bits; gain None: y is None.  rng [2] int64: seed and offset.  `out`: what to write into, h or y None where it is not wanted.  Without
     `out`, and with nothing to add, drop or round, h is x itself."""
     shape = rows, width = x.shape
+    assert rows <= _MOST_INT and width <= _MOST_INT and abs(scale_group) <= _MOST_INT
     res = residual.dtype if residual is not None else x.dtype if h_dtype is None else h_dtype
     if out is None:
         same = residual is None and drop_p == 0 and res is x.dtype
@@ -679,6 +683,7 @@ def rlgen_add_rms_norm_backward(h: Optional[torch.Tensor], gain: Optional[torch.
     where it is not wanted; without it, and with nothing dropped or rounded, dx is dresidual itself."""
     like = h if h is not None else dh
     shape = rows, width = like.shape
+    assert rows <= _MOST_INT and width <= _MOST_INT
     res = like.dtype
     dt = dy.dtype if dy is not None else res if dtype is None else dtype
     if out is None:
@@ -713,6 +718,7 @@ def rlgen_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = 
     """logits [rows, vocab] (fp32, bf16 or fp16; any row stride), tokens [rows] int32 or None.  A row whose token lies outside the vocabulary is skipped.
     `out`: a TokenLogprobs (or tuple) of tensors to fill; entropy and n_top are then what it holds."""
     shape = rows, vocab = logits.shape
+    assert rows <= _MOST_INT and vocab <= _MOST_INT
     dev, stream = _here()
     if out is None:
         new = logits.new_empty
@@ -724,7 +730,7 @@ def rlgen_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = 
     else:
         lp, ent, stats, ids, top = out
         n_top = 0 if ids is None else ids.shape[1]
-        assert (top is None) == (ids is None)
+        assert (top is None) == (ids is None) and n_top <= _MOST_INT
         where = (_numbers(lp, _F32, (rows,), dev), _numbers(stats, _F32, (rows, 2), dev), _numbers(ent, _F32, (rows,), dev), n_top,
                  _numbers(ids, _I32, (rows, n_top), dev), _numbers(top, _F32, (rows, n_top), dev))
     dt = _DTYPES[logits.dtype]
@@ -741,6 +747,7 @@ def rlgen_token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.T
     """From rlgen_token_logprobs's inputs, its stats (and entropy, with dentropy) and the gradients [rows] of logprobs and entropy: dlogits like
     logits.  `out` may be logits itself."""
     shape = rows, vocab = logits.shape
+    assert rows <= _MOST_INT and vocab <= _MOST_INT
     if out is None:
         out = torch.empty(shape, dtype=logits.dtype, device=logits.device)
     dev, stream = _here()
@@ -757,6 +764,7 @@ def rlgen_dpo_pairs(token_logprobs: torch.Tensor, ref_logprobs: torch.Tensor, ro
     of weight times the losses' sum to token_logprobs [rows]).  Rows that no sequence has are 0; with `out`, the two to write into, they are left as they
     are, and the launch that zeroes them falls away."""
     rows, B = token_logprobs.numel(), idx_pos.numel()
+    assert rows <= _MOST_INT and B <= _MOST_INT and abs(k) <= _MOST_INT
     loss, grad = out if out is not None else (token_logprobs.new_empty(B), token_logprobs.new_zeros(rows))
     dev, stream = _here()
     _check(lib.rlgen_dpo_pairs(_numbers(token_logprobs, _F32, (rows,), dev), _numbers(ref_logprobs, _F32, (rows,), dev), rows,
