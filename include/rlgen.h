@@ -463,9 +463,10 @@ int rlgen_add_rms_norm_backward(const void *h, int64_t h_stride, int32_t residua
  *  stats [rows, 2]       the largest logit m, and log sum exp((z - m) / temperature): what the backward pass needs
  *  top_tokens, top_logprobs [rows, n_top]   the n_top (0 to 64, at most vocab) likeliest tokens in descending order, of equal ones the lowest index first
  * A row whose token lies outside [0, vocab) (padding, a prompt's rows) is not read: its log-prob, entropy and stats are 0, its alternatives -1 and
- * -infinity.  Logits of -infinity or of the type's lowest value are masked: they count 0.  A row of -infinity alone has log-prob -infinity,
- * entropy 0, stats (-infinity, -infinity), and alternatives at -infinity.  A NaN or +infinity makes the row's numbers NaN; among the
- * alternatives NaN counts as the largest.  temperature is finite and at least 1e-6.
+ * -infinity.  A logit of -infinity is masked: it counts 0.  The type's lowest value is a value like any other: beside an allowed logit m its term is 0 once
+ * (m - z) / temperature passes 104 (fp16's -65504: at temperatures up to 600), and a row of lowest values alone is uniform.  A row of -infinity alone has
+ * log-prob -infinity, entropy 0, stats (-infinity, -infinity), and alternatives at -infinity.  A NaN or +infinity makes the row's log-prob, entropy and
+ * log sum NaN (m passes over NaN); among the alternatives NaN counts as the largest.  temperature is finite and at least 1e-6.
  * workspace: 16-byte aligned, rlgen_token_logprobs_workspace(...) bytes (0, and workspace may be null, unless few rows are parted over many
  * blocks).  Errors: NULL, BAD_ARG, WORKSPACE, DEVICE. */
 size_t rlgen_token_logprobs_workspace(int32_t dtype, int32_t rows, int32_t vocab, int32_t n_top);
@@ -474,7 +475,7 @@ int rlgen_token_logprobs(const void *logits, int64_t stride, int32_t dtype, int3
                          float *top_logprobs, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* The gradient of logprobs and entropy to the logits: dlogits [rows, vocab] of type dtype, every element written, zeros in rows that were not read
- * or are masked as a whole.  dlogprobs, dentropy [rows]: at least one of them; with dlogprobs tokens, with dentropy the forward pass's entropy.
+ * or hold -infinity alone.  dlogprobs, dentropy [rows]: at least one of them; with dlogprobs tokens, with dentropy the forward pass's entropy.
  * tokens null: no row is left out.  dlogits may be logits itself (same stride); other overlaps are not allowed.
  * A launch has fewer than 2^24 blocks: rows times vocab / 8192 (fp32: 4096), rounded up.  Errors: NULL, BAD_ARG, DEVICE. */
 int rlgen_token_logprobs_backward(const void *logits, int64_t stride, int32_t dtype, int32_t rows, int32_t vocab, const int32_t *tokens,
