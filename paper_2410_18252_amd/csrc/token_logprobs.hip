@@ -209,12 +209,13 @@ template <class E, int T> __device__ void select_top(const void* row, const Cut&
   fill_equal<E, T>(row, c, vocab, n, least, f.above, f);
 }
 
-// What a row adds up to: its largest value, the sum of the terms 2^y, and that of y 2^y.  In a row that is all but decided the largest value's own term, 1,
-// is counted (once) and not among the sums: beside it the others would keep few of their bits.
+// What a row adds up to: its largest value, the sum of the terms 2^y, and that of y 2^y.  Where one value has more than half of the probability its own
+// term, 1, is counted (once) and not among the sums: beside it the others would keep few of their bits.
 struct Sums { float M, count, sum, along; };
 __device__ __forceinline__ bool all_masked(const Sums& s) { return s.M == -INFINITY && s.sum == 0.f; }
 __device__ __forceinline__ float log_sum_of(const Sums& s) {
-  // (log(1 + x) as log(u) x / (u - 1) with u = 1 + x rounded, which makes up for the rounding; -infinity for a row that is masked as a whole)
+  // (log(1 + x) as log(u) x / (u - 1) with u = 1 + x rounded, which makes up for the rounding: Goldberg, "What every computer scientist should know about
+  // floating-point arithmetic", 1991, theorem 4; -infinity for a row that is masked as a whole)
   const float u = s.count + s.sum, l = logf(u);
   return s.count == 1.f && u < 2.f ? (u == 1.f ? s.sum : l * (s.sum / (u - 1.f))) : l;
 }
@@ -424,9 +425,10 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(LogprobArgs a, int st
     for (int w = 0; w < WAVES; ++w) { all.sum += red[1][w]; all.along += red[2][w]; }
   };
   add_waves();
-  if (all.sum < 1.0625f && all.sum >= 1.f) {
-    // All but decided: the one lane that has the largest value added up small terms beside 1.  Its wave goes over that lane's values again, a piece to a lane,
-    // without the largest (the block comes here as one, and so does the wave).
+  if (all.sum < 2.f && all.sum >= 1.f) {
+    // One value has more than half of the probability: the lane that has it added up small terms beside 1, in a step 32 and then the steps, each off by 2^-24
+    // at most.  Some 40 of them are 2e-7 as a rule and 2.4e-6 at worst, of a log S that may be as small; from S = 2 on, log S is 0.69 and there may be two such
+    // values.  The wave goes over that lane's values again, a piece to a lane, without the largest (the block comes here as one, and so does the wave).
     __syncthreads();
     const unsigned long long which = __ballot(own == M);
     if (which) {
