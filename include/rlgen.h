@@ -415,7 +415,7 @@ int rlgen_window_attention_paged(const void *q, int64_t q_stride, int32_t dtype,
  *
  * What a policy's learner runs between its matrix products, from the branch of a block to the gradient of the loss; the norm and the log-probs
  * serve single tokens as well.  They need no context, keep nothing between calls, and have no sums whose order changes: the same call
- * returns the same bits.  Statistics, sums, log-probs, losses and gains are fp32 or wider.
+ * returns the same bits (log-probs of another number of rows may be added up in another order).  Statistics, sums, log-probs, losses and gains are fp32 or wider.
  *
  * Layouts
  *  - Rows of the norm: width elements, a multiple of 8 up to 16384, any row stride (in elements) that is a multiple of 8 (fp32: 4), bases and gains
@@ -490,7 +490,7 @@ int rlgen_token_logprobs_backward(const void *logits, int64_t stride, int32_t dt
  *                    sequences'; rows that no sequence has are left as they are
  * idx_pos[b] == idx_neg[b] is a pair without a difference, whatever its log-probs: log 2 and zeros.  A sum that is infinite or NaN (a masked token's log-prob
  * is -infinity) gives its own pair's loss and rows their limits, or NaN where there is none (-infinity in both models), and no other rows anything.
- * Indices and row starts outside their ranges are clamped.  Sums and the loss are formed in fp64.  All DEVICE.
+ * Indices and row starts outside their ranges are clamped.  Sums and the loss are formed in fp64, of beta and weight as fp32 holds them.  All DEVICE.
  * Errors: NULL, BAD_ARG (B or k < 1, B >= 2^22, beta or weight not finite), DEVICE. */
 int rlgen_dpo_pairs(const float *token_logprobs, const float *ref_logprobs, int32_t rows, const int32_t *row_starts, int32_t B, int32_t k,
                     const int32_t *idx_pos, const int32_t *idx_neg, float beta, float weight, float *loss, float *dlogprobs,

@@ -61,7 +61,8 @@ __device__ __forceinline__ uint32_t pack_e4m3x4(const float* y) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
 }
 constexpr float E4M3_MAX = 448.f;
-// A scale below this has no reciprocal in 32 bits: such values count as zeros
+// A group whose largest magnitude is below this counts as zeros: chosen, far below what a norm gives, so that its scale (from 2^-109 on) and 448 over the
+// magnitude (up to 2^109) are normal numbers with room to spare
 constexpr float E4M3_LEAST = 7.8886090522101181e-31f;       // 2^-100
 
 // Forward.  A row lies in the registers of `waves` waves, thread t of them holding its 16-byte pieces t, t + 64 waves, ...: read once, written once, the norm
@@ -307,7 +308,10 @@ __global__ __launch_bounds__(1024) void gain_sum_kernel(const float* partial, in
 
 // 16-byte pieces of a thread, waves to a row and rows to a block: by the width alone, so that a row's sums do not depend on how many rows there are.
 // Forward (16384 rows of 4096 in bf16 with dropout, us): one piece 97, two 95, four 98, eight 110.  Backward, whose sums and requests ahead take
-// 90 to 110 registers for each piece of a thread: one piece while eight waves hold a row.
+// 88 to 111 registers with one piece to a thread, 143 to 185 with two and all 256 with four (63 more in scratch where the residual stream is fp32, 113 where x
+// is too): one piece while eight waves hold a row.  4000 rows of bf16 over bf16 | bf16 over fp32 | fp32 with dh, us, and their bytes at 5.08 TB/s: 4096
+// columns 38 | 57 | 72 (32 | 52 | 65), 5120 50 | 74 | 90 (40 | 65 | 81), 8192 70 | 110 | 139 (65 | 103 | 129), 8200 76 | 181 | 222 (65 | 103 | 129),
+// 16384 126 | 253 | 337 (129 | 206 | 258).
 struct Shape { int nv, waves, rows_here; };
 Shape shape_of(int width, bool backward) {
   const int n8 = (width + 7) / 8;
@@ -318,7 +322,7 @@ Shape shape_of(int width, bool backward) {
   s.rows_here = backward ? (s.nv == 1 ? 8 / s.waves : 1) : s.waves == 1 ? 4 : 1;
   return s;
 }
-// As many blocks as the CUs hold at once, the same number on each (16384 rows of 4096 in bf16 with dropout: 108 us with two blocks of eight waves to a
+// The same number of blocks on every CU: as many as it holds at once with one piece to a thread, one with two or four pieces (16384 rows of 4096 in bf16 with dropout: 108 us with two blocks of eight waves to a
 // CU, 145, 126, 125 and 113 with one, 1.5, three and four; 2560: 97 to 80 with 410 to 614 blocks of five waves, 95 with 819)
 // Up to four walks of rows one block takes alone: its sums are the gain's gradient, and there is neither a second launch nor a workspace (a call of 24
 // rows of 128 or 4 of 4096: 8.4 us, 13 with them; 8 of 4096 13.4 in one block, 64 of 512 10.5, 16 of 4096 25).

@@ -92,7 +92,9 @@ struct TypeF32 {};
 // Eight elements of a row in registers, 16-byte accesses
 template <class T> struct Vec8 {
   u32x4 w;
-  template <bool ONCE = false> static __device__ __forceinline__ Vec8 load(const void* p, long long at) { return {take<ONCE>((const u32x4*)((const uint16_t*)p + at))}; }
+  template <bool ONCE = false> static __device__ __forceinline__ Vec8 load(const void* p, long long at) {
+    return {take<ONCE>((const u32x4*)((const uint16_t*)p + at))};
+  }
   static __device__ __forceinline__ Vec8 zero() { return {u32x4{0, 0, 0, 0}}; }
   // what is known of the values ends here
   __device__ __forceinline__ void opaque() { asm volatile("" : "+v"(w)); }

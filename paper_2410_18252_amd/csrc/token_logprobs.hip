@@ -16,7 +16,9 @@ typedef f32x4 any4f __attribute__((aligned(4)));
 template <class E> struct Some {
   static constexpr int N = 8;
   u32x4 w;
-  template <bool ONCE = false> static __device__ __forceinline__ Some load(const void* row, long long at) { return {take<ONCE>((const u32x4*)((const uint16_t*)row + at))}; }
+  template <bool ONCE = false> static __device__ __forceinline__ Some load(const void* row, long long at) {
+    return {take<ONCE>((const u32x4*)((const uint16_t*)row + at))};
+  }
   static __device__ __forceinline__ Some of(u32x4 w) { return {w}; }
   __device__ __forceinline__ void opaque() { asm volatile("" : "+v"(w)); }     // what is known of the values ends here
   static __device__ __forceinline__ Some masked() {
@@ -37,7 +39,9 @@ template <class E> struct Some {
 template <> struct Some<TypeF32> {
   static constexpr int N = 4;
   f32x4 w;
-  template <bool ONCE = false> static __device__ __forceinline__ Some load(const void* row, long long at) { return {take<ONCE>((const f32x4*)((const float*)row + at))}; }
+  template <bool ONCE = false> static __device__ __forceinline__ Some load(const void* row, long long at) {
+    return {take<ONCE>((const f32x4*)((const float*)row + at))};
+  }
   static __device__ __forceinline__ Some of(u32x4 w) { return {__builtin_bit_cast(f32x4, w)}; }
   __device__ __forceinline__ void opaque() {}
   static __device__ __forceinline__ Some masked() { return {f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY}}; }
@@ -180,7 +184,9 @@ template <class E, int T> __device__ void fill_equal(const void* row, const Cut&
 }
 
 // The n largest of a row where no simple bound leaves few values (crowded ones, NaN): the n-th largest order by halving, every step counting
-// over the row, then the values above it, and of those equal to it the first ones.
+// over the row, then the values above it, and of those equal to it the first ones.  33 passes over the row, which is what it costs: with a NaN in every row 64
+// rows of 128256 bf16 values 202 us (16 without), 300 of 100003 881 (22), 256 of 50304 338 (13), one of 50304 279 (12); 70 rows of 400003, more than maxima
+// are kept of, 3290 (40 for 390003).
 template <class E, int T> __device__ void select_top(const void* row, const Cut& c, int vocab, int n, Found& f) {
   constexpr int N = Some<E>::N;
   const int edge = edge_of(c, vocab);
